@@ -9,7 +9,7 @@
  *
  * Conventions shared by every entry point
  *   - Every array argument is DEVICE memory owned by the caller, contiguous,
- *     row-major. The library allocates nothing and keeps no per-call state
+ *     row-major unless it comes with strides. The library allocates nothing and keeps no per-call state
  *     outside the caller's workspace.
  *   - Calls are asynchronous and ordered on `stream` (a cudaStream_t; NULL is
  *     the legacy default stream). Nothing synchronises with the host.
@@ -57,8 +57,8 @@ typedef struct {
   uint32_t reserved;
 } asd_partial;
 
-/* Logit storage types. */
-enum { ASD_F32 = 0, ASD_BF16 = 1 };
+/* Storage types. Logits are ASD_F32 or ASD_BF16; the cache entry points also take ASD_F16. */
+enum { ASD_F32 = 0, ASD_BF16 = 1, ASD_F16 = 2 };
 
 /* Flag ORed into the dtype argument of the verify entry points: the logits and
  * draft tokens are resident, i.e. no kernel that is still running or queued
@@ -76,9 +76,10 @@ enum { ASD_F32 = 0, ASD_BF16 = 1 };
 enum {
   ASD_OK = 0,
   ASD_ERR_NULL = 1,      /* a required pointer is NULL */
-  ASD_ERR_SHAPE = 2,     /* B < 0, K < 0, K > 31, V < 1, or H invalid */
+  ASD_ERR_SHAPE = 2,     /* B < 0, K < 0, K > 31, V < 1, or H invalid; cache entry points: a size, head
+                          * count, stride or rotation out of its range */
   ASD_ERR_DTYPE = 3,     /* unknown dtype code */
-  ASD_ERR_CONTROL = 4,   /* gate < 0 or NaN, cap < 0 */
+  ASD_ERR_CONTROL = 4,   /* gate < 0 or NaN, cap < 0; eps < 0 or NaN, scale not finite */
   ASD_ERR_WORKSPACE = 5, /* workspace smaller than the size query returns */
   ASD_ERR_ALIGN = 6,     /* pointer not aligned as documented */
   ASD_ERR_CUDA = 7,      /* a CUDA call failed (launch or device query) */
@@ -96,6 +97,12 @@ enum {
                                    * selected (asd_workspace_error): a kernel gave up waiting on
                                    * its copy pipeline, so row results may be missing. Set for
                                    * every request of such a call until asd_workspace_init. */
+
+#define ASD_STATUS_LENGTH 32u     /* cache entry points: kv_len < 0, a token count outside its range, or
+                                   * more slots than the request's row of the page table covers */
+#define ASD_STATUS_PAGE 64u       /* cache entry points: a page id outside [0, pages) */
+#define ASD_STATUS_POSITION 128u  /* asd_kv_append: a position outside the rotation's table */
+#define ASD_STATUS_PATH 256u      /* asd_kv_compact: path[i] < i or not ascending */
 
 /* Largest draft length: one warp lane per target row of a block. */
 #define ASD_MAX_K 31
@@ -340,6 +347,137 @@ int asd_lmhead_partials(const void* hidden, const void* weight, int H, int B, in
 int asd_commit(int B, int K, const int32_t* accepted_len, const int32_t* committed, int pending,
                int32_t* kv_len, int32_t* tokens, int32_t* token_len, int max_tokens, int32_t* status,
                asd_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The cache side of a verified block. The target pass that precedes a verify
+ * call feeds every request's pending token and drafts (a chain, or a tree in
+ * which several drafts share a prefix) through the model; per layer their keys
+ * and values enter a paged cache (asd_kv_append) and each of those tokens
+ * attends to the request's context and to its own ancestors
+ * (asd_tree_attention). Once a path of the tree has been verified, its keys and
+ * values move next to the context (asd_kv_compact) and asd_commit advances
+ * kv_len over them. The paper leaves these to the serving engine (Sec. 3.3,
+ * cache semantics).
+ *
+ * A paged cache. Element (layer, page, i, head, d) of the keys lies at
+ * k[layer * layer_stride + page * page_stride + i * token_stride +
+ *   head * head_stride + d], the values likewise from v: any order of the
+ * page's tokens and heads. Strides count elements; all are >= 0 and offsets are
+ * formed in 64 bits. Slot s of request b (its token number s) is place
+ * s % page_size of page page_table[b * table_width + s / page_size]. No two
+ * requests may share a page that a call writes.
+ */
+typedef struct {
+  void* k;
+  void* v;
+  int dtype;     /* ASD_F32, ASD_BF16 or ASD_F16 */
+  int layers;    /* >= 1 */
+  int pages;     /* >= 0 */
+  int page_size; /* >= 1 tokens */
+  int heads;     /* >= 1 key/value heads */
+  int head_dim;  /* 1 .. ASD_MAX_HEAD_DIM */
+  int64_t layer_stride, page_stride, token_stride, head_stride;
+  const int32_t* page_table; /* [B, table_width] device memory */
+  int B;                     /* requests */
+  int table_width;           /* pages that a request's row has room for */
+} asd_kv_cache;
+#define ASD_MAX_HEAD_DIM 256
+#define ASD_MAX_PATH 256 /* longest path that asd_kv_compact moves */
+
+/*
+ * Appends T tokens' keys and values to one layer of the cache, with an optional
+ * norm per head and the position rotation on the way; the queries of the same
+ * tokens take the same norm and rotation to q_out in the same pass.
+ *
+ * cache, layer  where the tokens go: token t of request b to slot kv_len[b] + t.
+ *               kv_len is not changed (asd_commit advances it)
+ * T             tokens per request, >= 0
+ * k, v          [B, T, heads, head_dim] of the cache's dtype; strides in elements
+ *               of the batch, token and head dimension (any, as in the rows of
+ *               a fused projection); the last dimension is contiguous
+ * q, q_heads    [B, T, q_heads, head_dim] the same way, or NULL and 0
+ * q_out         [B, T, q_heads, head_dim] contiguous; may be q itself where q is
+ *               contiguous
+ * kv_len        [B] int32 tokens that each request has in the cache
+ * new_len       [B] int32 how many of the T tokens exist (0..T), or NULL: all.
+ *               Nothing is written for the others, q_out included
+ * positions     [B, T] int32 rotation positions (a tree's nodes take their
+ *               depth), or NULL: kv_len[b] + t
+ * cos, sin      [rot_positions, rot_dim / 2] fp32, or both NULL: no rotation
+ * rot_dim       even, 2 .. head_dim: the leading elements that turn; 0 without
+ *               tables
+ * interleaved   0: element i turns with i + rot_dim / 2; 1: 2i with 2i + 1
+ * q_norm, k_norm [head_dim] weights of the cache's dtype, or NULL: no norm
+ * eps           >= 0, of the norm
+ * status        [B] int32, or NULL: ASD_STATUS_* bits are ORed in (zero it to
+ *               start; one array can serve all layers of a pass). A request
+ *               flagged ASD_STATUS_LENGTH writes nothing, a token whose position
+ *               is out of range is left out, and one whose page is out of range
+ *               leaves its key and value out.
+ *
+ * Arithmetic: x is widened to fp32; with a norm x <- x / sqrt(mean(x^2) + eps)
+ * * w; then (a, b) <- (a cos - b sin, b cos + a sin); one rounding at the end.
+ * Values are copied bit for bit.
+ */
+int asd_kv_append(const asd_kv_cache* cache, int layer, int T, const void* k, int64_t k_batch, int64_t k_token,
+                  int64_t k_head, const void* v, int64_t v_batch, int64_t v_token, int64_t v_head, const void* q,
+                  int64_t q_batch, int64_t q_token, int64_t q_head, int q_heads, void* q_out, const int32_t* kv_len,
+                  const int32_t* new_len, const int32_t* positions, const float* cos, const float* sin, int rot_dim,
+                  int rot_positions, int interleaved, const void* q_norm, const void* k_norm, float eps,
+                  int32_t* status, asd_stream_t stream);
+
+/*
+ * Attention of each request's T newest tokens over its paged cache: the tokens
+ * of a draft chain or tree after asd_kv_append has put them there (T = 1: plain
+ * decoding).
+ *
+ * Token t of request b sees every slot s < kv_len[b], and of the slots
+ * kv_len[b] + u (u < new_len[b]) those with bit u % 32 of word u / 32 of its row
+ * of tree_mask set (a node's row holds itself and its ancestors).
+ *
+ * q             [B, T, q_heads, head_dim] of the cache's dtype, strides as above;
+ *               q_heads a multiple of the cache's heads: query head h reads
+ *               key/value head h / (q_heads / heads)
+ * kv_len        [B] int32: the context, without the T new tokens
+ * new_len       [B] int32 (0..T), or NULL: T
+ * tree_mask     [B, T, ceil(T / 32)] uint32, or NULL: a chain (u <= t)
+ * scale         finite; scores are scale * (q . k)
+ * out           [B, T, q_heads, head_dim] contiguous, of the cache's dtype
+ * lse           [B, T, q_heads] fp32 natural log of the sum of exp(score), or
+ *               NULL
+ * status        as for asd_kv_append; a request flagged ASD_STATUS_LENGTH counts
+ *               as one without tokens, a slot on a page out of range as zeros
+ * workspace     >= asd_attention_workspace_size bytes, 16-byte aligned, zeroed by
+ *               asd_workspace_init before first use; one of the larger size
+ *               serves any smaller shape. Its error word is read with
+ *               asd_workspace_error; while it is set calls write nothing and
+ *               flag their requests ASD_STATUS_INCOMPLETE
+ *
+ * A row that sees nothing (new_len[b] <= t, or an empty context and an empty
+ * mask row) is 0 with lse = -INFINITY. What a row does not see does not reach
+ * it, NaN and infinities included.
+ * Arithmetic: scores, softmax statistics and sums in fp32, one rounding at the
+ * end. The result does not depend on the order in which CTAs finish.
+ */
+int asd_attention_workspace_size(const asd_kv_cache* cache, int T, int q_heads, size_t* bytes);
+int asd_tree_attention(const asd_kv_cache* cache, int layer, int T, const void* q, int64_t q_batch, int64_t q_token,
+                       int64_t q_head, int q_heads, const int32_t* kv_len, const int32_t* new_len,
+                       const uint32_t* tree_mask, float scale, void* out, float* lse, int32_t* status,
+                       void* workspace, size_t workspace_bytes, asd_stream_t stream);
+
+/*
+ * Moves the keys and values of a verified path next to the context, in place
+ * and in every layer: slot kv_len[b] + path[b][i] goes to slot kv_len[b] + i for
+ * i < path_len[b]. Call it before asd_commit advances kv_len.
+ *
+ * path          [B, P] int32 tree nodes, ascending, path[i] >= i (a topological
+ *               numbering gives both); a node that stays where it is costs
+ *               nothing. P <= ASD_MAX_PATH
+ * path_len      [B] int32, 0..P
+ * status        as above; a flagged request moves nothing
+ */
+int asd_kv_compact(const asd_kv_cache* cache, int P, const int32_t* kv_len, const int32_t* path,
+                   const int32_t* path_len, int32_t* status, asd_stream_t stream);
 
 /* The device address through which kernels read page-locked (pinned) host
  * memory, e.g. logits that stay in host memory and stream to the GPU over the

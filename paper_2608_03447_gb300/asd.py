@@ -25,6 +25,7 @@ HEADER = os.path.join(os.path.dirname(PKG), "include", "asd.h")
 
 F32 = 0
 BF16 = 1
+F16 = 2
 
 OK = 0
 STATUS_DRAFT_RANGE = 1
@@ -32,7 +33,13 @@ STATUS_NAN_LOGIT = 2
 STATUS_BAD_LEDGER = 4
 STATUS_OVERFLOW = 8
 STATUS_INCOMPLETE = 16
+STATUS_LENGTH = 32
+STATUS_PAGE = 64
+STATUS_POSITION = 128
+STATUS_PATH = 256
 MAX_K = 31
+MAX_HEAD_DIM = 256
+MAX_PATH = 256
 RESIDENT_INPUTS = 0x100  # ASD_RESIDENT_INPUTS, ORed into the dtype code
 INT32_MAX = 2**31 - 1
 
@@ -91,6 +98,16 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.asd_lmhead_logits.restype = i32
     lib.asd_lmhead_partials.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, sz, vp]
     lib.asd_lmhead_partials.restype = i32
+    i64 = ctypes.c_int64
+    lib.asd_kv_append.argtypes = [vp, i32, i32, vp, i64, i64, i64, vp, i64, i64, i64, vp, i64, i64, i64, i32, vp, vp, vp,
+                                  vp, vp, vp, i32, i32, i32, vp, vp, f32, vp, vp]
+    lib.asd_kv_append.restype = i32
+    lib.asd_attention_workspace_size.argtypes = [vp, i32, i32, ctypes.POINTER(sz)]
+    lib.asd_attention_workspace_size.restype = i32
+    lib.asd_tree_attention.argtypes = [vp, i32, i32, vp, i64, i64, i64, i32, vp, vp, vp, f32, vp, vp, vp, vp, sz, vp]
+    lib.asd_tree_attention.restype = i32
+    lib.asd_kv_compact.argtypes = [vp, i32, vp, vp, vp, vp, vp]
+    lib.asd_kv_compact.restype = i32
     lib.asd_set_launch_options.argtypes = [vp]
     lib.asd_set_launch_options.restype = i32
     lib.asd_get_launch_options.argtypes = [vp]
@@ -546,3 +563,187 @@ def commit(accepted_len: torch.Tensor, committed: torch.Tensor, pending: int = 1
     rc = load().asd_commit(B, K1 - 1, _ptr(accepted_len), _ptr(committed), int(pending), _ptr(kv_len), _ptr(tokens),
                            _ptr(token_len), max_tokens, _ptr(status), _stream(stream))
     _check("asd_commit", rc)
+
+
+# ---------------------------------------------------------------- the cache side of a verified block
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int), ("layers", ctypes.c_int),
+                ("pages", ctypes.c_int), ("page_size", ctypes.c_int), ("heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("layer_stride", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("page_table", ctypes.c_void_p),
+                ("B", ctypes.c_int), ("table_width", ctypes.c_int)]
+
+
+_CACHE_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+class KVCache:
+    """A paged key/value cache (asd_kv_cache) over the caller's tensors.
+
+    k, v        [layers, pages, page_size, heads, head_dim], or without the first dimension for one layer; float32,
+                bfloat16 or float16, the last dimension contiguous, any strides otherwise (the same for both): a
+                [pages, heads, page_size, head_dim] cache is passed as its ``transpose(-3, -2)``.
+    page_table  int32 [B, table_width]: slot s of request b is place s % page_size of page page_table[b, s // page_size].
+    """
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor):
+        if k.dim() == 4 and v.dim() == 4:
+            k, v = k.unsqueeze(0), v.unsqueeze(0)
+        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+            raise ValueError("k and v must be [layers, pages, page_size, heads, head_dim] alike, strides included")
+        if k.dtype not in _CACHE_DTYPES:
+            raise TypeError(f"a cache holds float32, bfloat16 or float16, got {k.dtype}")
+        if k.stride(4) != 1 and k.shape[4] > 1:
+            raise ValueError("the cache's last dimension must be contiguous")
+        if page_table.dim() != 2 or page_table.dtype != torch.int32 or not page_table.is_contiguous():
+            raise ValueError("page_table must be a contiguous int32 tensor [B, table_width]")
+        if not (k.is_cuda and k.device == v.device == page_table.device):
+            raise ValueError("k, v and page_table must be on one CUDA device")
+        self.k, self.v, self.page_table = k, v, page_table
+        self.dtype, self.device = k.dtype, k.device
+        self.layers, self.pages, self.page_size, self.heads, self.head_dim = k.shape
+        self.B, self.table_width = page_table.shape
+        s = k.stride()
+        self._c = _Cache(k.data_ptr(), v.data_ptr(), _CACHE_DTYPES[k.dtype], self.layers, self.pages, self.page_size,
+                         self.heads, self.head_dim, s[0], s[1], s[2], s[3], page_table.data_ptr(), self.B,
+                         self.table_width)
+        self._ref = ctypes.addressof(self._c)
+
+
+def _heads(name: str, t: torch.Tensor, cache: KVCache, T: int | None = None, heads: int | None = None):
+    """The strides of a [B, T, heads, head_dim] tensor of the cache's type."""
+    shape, st = t.shape, t.stride()
+    if len(shape) != 4 or t.dtype != cache.dtype or t.device != cache.device or shape[0] != cache.B or \
+            shape[3] != cache.head_dim or (st[3] != 1 and shape[3] > 1) or (T is not None and shape[1] != T) or \
+            (heads is not None and shape[2] != heads):
+        raise ValueError(f"{name} must be a [B, T, heads, head_dim] tensor of the cache's type and device, its last "
+                         "dimension contiguous")
+    return st
+
+
+def _int32(name: str, t: torch.Tensor | None, cache: KVCache, shape: tuple) -> int | None:
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.shape != shape or t.device != cache.device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 CUDA tensor {list(shape)}")
+    return t.data_ptr()
+
+
+def kv_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, kv_len: torch.Tensor, layer: int = 0,
+              q: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
+              positions: torch.Tensor | None = None, new_len: torch.Tensor | None = None,
+              cos: torch.Tensor | None = None, sin: torch.Tensor | None = None, interleaved: bool = False,
+              q_norm: torch.Tensor | None = None, k_norm: torch.Tensor | None = None, eps: float = 1e-6,
+              status: torch.Tensor | None = None, stream=None) -> torch.Tensor | None:
+    """asd_kv_append: norm and rotate the new tokens' keys (and queries), append keys and values to one layer.
+
+    k, v [B, T, heads, D] and q [B, T, q_heads, D] may be strided views of a fused projection's rows. cos, sin
+    [positions, rot_dim / 2] float32. Returns ``q_out`` (allocated if not given), or None without queries.
+    """
+    ks = _heads("k", k, cache, heads=cache.heads)
+    B, T = cache.B, k.shape[1]
+    vs = _heads("v", v, cache, T, cache.heads)
+    qs, q_heads = (0, 0, 0, 0), 0
+    if q is not None:
+        qs, q_heads = _heads("q", q, cache, T), q.shape[2]
+        if q_out is None:
+            q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+        elif q_out.shape != q.shape or q_out.dtype != q.dtype or q_out.device != q.device or not q_out.is_contiguous():
+            raise ValueError("q_out must be a contiguous tensor of q's shape, type and device")
+    rot, table = 0, 0
+    if cos is not None or sin is not None:
+        if cos is None or sin is None or cos.dim() != 2 or cos.shape != sin.shape or cos.dtype != torch.float32 or \
+                sin.dtype != torch.float32 or not cos.is_contiguous() or not sin.is_contiguous() or \
+                cos.device != cache.device or sin.device != cache.device:
+            raise ValueError("cos and sin must be contiguous float32 CUDA tensors [positions, rot_dim / 2] alike")
+        table, rot = cos.shape[0], 2 * cos.shape[1]
+    for w in (q_norm, k_norm):
+        if w is not None and (w.shape != (cache.head_dim,) or w.dtype != cache.dtype or w.device != cache.device or
+                              not w.is_contiguous()):
+            raise ValueError("q_norm and k_norm must be contiguous tensors [head_dim] of the cache's type")
+    rc = load().asd_kv_append(cache._ref, layer, T, k.data_ptr(), ks[0], ks[1], ks[2], v.data_ptr(), vs[0], vs[1],
+                              vs[2], _ptr(q), qs[0], qs[1], qs[2], q_heads, None if q is None else q_out.data_ptr(),
+                              _int32("kv_len", kv_len, cache, (B,)), _int32("new_len", new_len, cache, (B,)),
+                              _int32("positions", positions, cache, (B, T)), _ptr(cos), _ptr(sin), rot, table,
+                              int(interleaved), _ptr(q_norm), _ptr(k_norm), eps,
+                              _int32("status", status, cache, (B,)), _stream(stream))
+    _check("asd_kv_append", rc)
+    return None if q is None else q_out
+
+
+def attention_workspace(cache: KVCache, T: int, q_heads: int, stream=None) -> Workspace:
+    """A workspace for tree_attention with up to T tokens per request (asd_attention_workspace_size)."""
+    n = ctypes.c_size_t(0)
+    _check("asd_attention_workspace_size",
+           load().asd_attention_workspace_size(cache._ref, T, q_heads, ctypes.byref(n)))
+    ws = Workspace.__new__(Workspace)
+    ws.nbytes = n.value
+    ws.buffer = torch.empty(ws.nbytes, dtype=torch.uint8, device=cache.device)
+    _check("asd_workspace_init", load().asd_workspace_init(ws.buffer.data_ptr(), ws.nbytes, _stream(stream)))
+    return ws
+
+
+def tree_mask(parents: torch.Tensor) -> torch.Tensor:
+    """Trees as tree_attention takes them: parents int [B, T] (node t's parent, < t, or -1 for a root) -> int32
+    [B, T, ceil(T / 32)], bit u of row t set where u is t itself or one of its ancestors."""
+    B, T = parents.shape
+    at = torch.arange(T, device=parents.device)
+    if bool((parents >= at).any()) or bool((parents < -1).any()):
+        raise ValueError("a node's parent must come before it (or be -1)")
+    sees = torch.eye(T, dtype=torch.bool, device=parents.device).expand(B, T, T).clone()
+    rows = torch.arange(B, device=parents.device)
+    for t in range(1, T):
+        p = parents[:, t].long()
+        sees[:, t] |= sees[rows, p.clamp(min=0)] & (p >= 0)[:, None]
+    words = (T + 31) // 32
+    bits = torch.zeros(B, T, words * 32, dtype=torch.int64, device=parents.device)
+    bits[:, :, :T] = sees.long()
+    w = (bits.view(B, T, words, 32) << torch.arange(32, device=parents.device)).sum(-1)
+    return (w - ((w >> 31) << 32)).to(torch.int32).contiguous()
+
+
+def tree_attention(q: torch.Tensor, cache: KVCache, kv_len: torch.Tensor, layer: int = 0,
+                   tree_mask: torch.Tensor | None = None, new_len: torch.Tensor | None = None,
+                   scale: float | None = None, workspace: Workspace | None = None, out: dict | None = None,
+                   status: torch.Tensor | None = None, stream=None) -> dict:
+    """asd_tree_attention: the newest T tokens of every request against its context and their own ancestors.
+
+    q [B, T, q_heads, D] (any strides, last dimension contiguous); ``tree_mask`` int32 [B, T, ceil(T / 32)] or None
+    for a chain; ``scale`` defaults to 1 / sqrt(D). Returns {"out": [B, T, q_heads, D], "lse": float32 [B, T, q_heads]};
+    an ``out`` dict without "lse" leaves it out.
+    """
+    qs = _heads("q", q, cache)
+    B, T, q_heads, D = q.shape
+    if out is None:
+        out = {"out": torch.empty(q.shape, dtype=q.dtype, device=q.device),
+               "lse": torch.empty(B, T, q_heads, dtype=torch.float32, device=q.device)}
+    o, lse = out["out"], out.get("lse")
+    if o.shape != q.shape or o.dtype != q.dtype or o.device != q.device or not o.is_contiguous():
+        raise ValueError("out must be a contiguous tensor of q's shape, type and device")
+    if lse is not None and (lse.shape != (B, T, q_heads) or lse.dtype != torch.float32 or lse.device != q.device or
+                            not lse.is_contiguous()):
+        raise ValueError("lse must be a contiguous float32 tensor [B, T, q_heads]")
+    ws = workspace or attention_workspace(cache, T, q_heads, stream)
+    rc = load().asd_tree_attention(cache._ref, layer, T, q.data_ptr(), qs[0], qs[1], qs[2], q_heads,
+                                   _int32("kv_len", kv_len, cache, (B,)), _int32("new_len", new_len, cache, (B,)),
+                                   _int32("tree_mask", tree_mask, cache, (B, T, (T + 31) // 32)),
+                                   D ** -0.5 if scale is None else scale, o.data_ptr(), _ptr(lse),
+                                   _int32("status", status, cache, (B,)), ws.buffer.data_ptr(), ws.nbytes,
+                                   _stream(stream))
+    _check("asd_tree_attention", rc)
+    return out
+
+
+def kv_compact(cache: KVCache, kv_len: torch.Tensor, path: torch.Tensor, path_len: torch.Tensor,
+               status: torch.Tensor | None = None, stream=None) -> None:
+    """asd_kv_compact: move a verified path's keys and values next to the context, in every layer (in place).
+
+    path int32 [B, P], ascending tree nodes with path[b, i] >= i; path_len int32 [B].
+    """
+    B, P = path.shape
+    rc = load().asd_kv_compact(cache._ref, P, _int32("kv_len", kv_len, cache, (cache.B,)),
+                               _int32("path", path, cache, (cache.B, P)),
+                               _int32("path_len", path_len, cache, (cache.B,)),
+                               _int32("status", status, cache, (cache.B,)), _stream(stream))
+    _check("asd_kv_compact", rc)

@@ -1,0 +1,421 @@
+// libasd: attention of a draft chain's or tree's tokens over a paged cache
+// (asd_tree_attention), on the CUDA cores.
+//
+// out = softmax(scale q k^T) v over the slots that each row sees, in one pass
+// over the keys and values: per row the running maximum m and sum l of
+// exp2(s - m), and the output's sum rescaled when m grows.
+//
+// A CTA of 256 threads has kRows query rows that share a key/value head (16 or
+// 64) against tiles of 64 slots. Thread (y, x) of 16 x 16 computes the scores of
+// rows y + 16 i and slots x + 16 j, four elements of the head at a time from
+// shared memory, and holds the output's columns 4 x + 64 c .. + 3 of its rows.
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <atomic>
+
+#include "asd.h"
+#include "asd_attention.cuh"
+#include "asd_launch.cuh"
+
+namespace {
+
+using namespace asd_detail;
+
+constexpr int kSimtThreads = 256;
+constexpr int kSimtTile = 64;
+
+// Shared memory, in floats: rows of the head padded to a multiple of four and
+// one more vector, so that a warp's sixteen rows start in different banks.
+__host__ __device__ constexpr int simt_pitch(int dim) { return (dim + 3) / 4 * 4 + 4; }
+constexpr int kScorePitch = kSimtTile + 4;
+constexpr size_t simt_smem(int rows, int dim) {
+  return sizeof(float) * (static_cast<size_t>(rows + kSimtTile) * simt_pitch(dim) + rows * kScorePitch) +
+         2 * sizeof(long long) * kSimtTile;
+}
+
+template <typename T>
+__device__ __forceinline__ void load4(const T* p, bool vec, int valid, float (&x)[4]) {
+  if (vec) {
+    if constexpr (sizeof(T) == 4) {
+      const float4 w = __ldcg(reinterpret_cast<const float4*>(p));
+      x[0] = w.x, x[1] = w.y, x[2] = w.z, x[3] = w.w;
+    } else {
+      const uint2 w = __ldcg(reinterpret_cast<const uint2*>(p));
+      T e[4];
+      memcpy(e, &w, 8);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = Store<T>::widen(e[i]);
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = i < valid ? Store<T>::widen(p[i]) : 0.0f;
+}
+
+// kRows: query rows of a unit. kCols: the output's groups of 64 columns.
+template <typename T, int kRows, int kCols>
+__global__ void __launch_bounds__(kSimtThreads)
+    attention_kernel(const __grid_constant__ AttnParams p, bool vec_q, bool vec_kv) {
+  constexpr int kI = kRows / 16;
+  extern __shared__ __align__(16) float smem[];
+  __shared__ AttnDeal deal;
+  __shared__ int s_last;
+  const int D = p.D, pitch = simt_pitch(D), quads = (D + 3) / 4;
+  float* sq = smem;                        // [kRows][pitch]
+  float* skv = sq + kRows * pitch;         // [kSimtTile][pitch]: keys, then values
+  float* sp = skv + kSimtTile * pitch;     // [kRows][kScorePitch]
+  long long* s_off = reinterpret_cast<long long*>(sp + kRows * kScorePitch);  // [kSimtTile] slots' offsets
+
+  const int tid = threadIdx.x, x = tid & 15, y = tid >> 4;
+  pdl_signal_dependents();
+  pdl_wait_prerequisites();
+  if (__ldcg(p.error)) {
+    if (blockIdx.x == 0 && p.status)
+      for (int b = tid; b < p.B; b += kSimtThreads) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_INCOMPLETE));
+    return;
+  }
+  if (!attn_deal<kSimtTile>(p, deal)) return;
+
+  for (AttnWalk<kSimtTile> w(p, deal); w.more(); w.next()) {
+    const int row0 = w.row0(), rows = w.rows(), live = w.live_rows();
+    const int span = w.span();
+    __syncthreads();  // the unit before is done with shared memory
+    for (int i = tid; i < kRows * quads; i += kSimtThreads) {
+      const int r = i / quads, d4 = i - r * quads;
+      float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (r < live) {
+        const int t = (row0 + r) / p.group, g = row0 + r - t * p.group;
+        load4(reinterpret_cast<const T*>(p.q) + w.b * p.q_batch + t * p.q_token + (w.h * p.group + g) * p.q_head +
+                  4 * d4,
+              vec_q, D - 4 * d4, f);
+      }
+      *reinterpret_cast<float4*>(sq + r * pitch + 4 * d4) =
+          make_float4(f[0] * p.scale_log2, f[1] * p.scale_log2, f[2] * p.scale_log2, f[3] * p.scale_log2);
+    }
+    float m[kI], l[kI], o[kI][kCols][4];
+#pragma unroll
+    for (int i = 0; i < kI; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) o[i][c][0] = o[i][c][1] = o[i][c][2] = o[i][c][3] = 0.0f;
+    }
+
+    auto load_tile = [&](const char* base, int slots) {
+      const T* src = reinterpret_cast<const T*>(base) + w.h * p.cache.head_stride;
+      for (int i = tid; i < kSimtTile * quads; i += kSimtThreads) {
+        const int s = i / quads, d4 = i - s * quads;
+        float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (s < slots && s_off[s] >= 0) load4(src + s_off[s] + 4 * d4, vec_kv, D - 4 * d4, f);
+        *reinterpret_cast<float4*>(skv + s * pitch + 4 * d4) = make_float4(f[0], f[1], f[2], f[3]);
+      }
+    };
+    for (int j = w.j0; j < w.j1 && span > 0; ++j) {
+      const int slot0 = j * kSimtTile;
+      const int slots = min(kSimtTile, span - slot0);
+      __syncthreads();  // the tile before has been read
+      if (tid < slots) {
+        const long long off = slot_offset(p.cache, w.b, slot0 + tid);
+        if (off < 0 && p.status) atomicOr(p.status + w.b, static_cast<int>(ASD_STATUS_PAGE));
+        s_off[tid] = off;
+      }
+      __syncthreads();
+      load_tile(p.cache.k, slots);
+      __syncthreads();
+      float s[kI][4];
+#pragma unroll
+      for (int i = 0; i < kI; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.0f;
+      for (int d4 = 0; d4 < quads; ++d4) {
+        float4 a[kI], kk[4];
+#pragma unroll
+        for (int i = 0; i < kI; ++i) a[i] = *reinterpret_cast<const float4*>(sq + (y + 16 * i) * pitch + 4 * d4);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) kk[c] = *reinterpret_cast<const float4*>(skv + (x + 16 * c) * pitch + 4 * d4);
+#pragma unroll
+        for (int i = 0; i < kI; ++i)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            s[i][c] = fmaf(a[i].x, kk[c].x, s[i][c]);
+            s[i][c] = fmaf(a[i].y, kk[c].y, s[i][c]);
+            s[i][c] = fmaf(a[i].z, kk[c].z, s[i][c]);
+            s[i][c] = fmaf(a[i].w, kk[c].w, s[i][c]);
+          }
+      }
+      // the tile's mask where it reaches past the context (or the span)
+      const bool masked = slot0 + kSimtTile > w.r.ctx;
+#pragma unroll
+      for (int i = 0; i < kI; ++i) {
+        const int r = y + 16 * i;
+        if (masked) {
+          uint32_t lo = 0, hi = 0;
+          if (r < live) {
+            const int t = (row0 + r) / p.group;
+            lo = attn_sees(p, w.r, w.b, t, slot0);
+            hi = attn_sees(p, w.r, w.b, t, slot0 + 32);
+          }
+          if (!((lo >> x) & 1u)) s[i][0] = -INFINITY;
+          if (!((lo >> (x + 16)) & 1u)) s[i][1] = -INFINITY;
+          if (!((hi >> x) & 1u)) s[i][2] = -INFINITY;
+          if (!((hi >> (x + 16)) & 1u)) s[i][3] = -INFINITY;
+        }
+        float top = fmax_nan(fmax_nan(s[i][0], s[i][1]), fmax_nan(s[i][2], s[i][3]));
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) top = fmax_nan(top, __shfl_xor_sync(kFull, top, off));
+        const float m_new = fmax_nan(m[i], top);
+        const float ref = m_new == -INFINITY ? 0.0f : m_new;  // nothing seen yet: every weight is exp2(-inf) = 0
+        const float fade = exp2f(m[i] - ref);
+        float sum = 0.0f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const float e = exp2f(s[i][c] - ref);
+          sum += e;
+          sp[r * kScorePitch + x + 16 * c] = e;
+        }
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) sum += __shfl_xor_sync(kFull, sum, off);
+        l[i] = l[i] * fade + sum;
+        m[i] = m_new;
+#pragma unroll
+        for (int c = 0; c < kCols; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][c][e] *= fade;
+      }
+      __syncthreads();  // the scores are written, the keys read
+      load_tile(p.cache.v, slots);
+      __syncthreads();
+      for (int s4 = 0; s4 < kSimtTile; s4 += 4) {
+        float4 a[kI];
+#pragma unroll
+        for (int i = 0; i < kI; ++i) a[i] = *reinterpret_cast<const float4*>(sp + (y + 16 * i) * kScorePitch + s4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float4 v[kCols];
+#pragma unroll
+          for (int c = 0; c < kCols; ++c)
+            if (4 * x + 64 * c < D) v[c] = *reinterpret_cast<const float4*>(skv + (s4 + e) * pitch + 4 * x + 64 * c);
+#pragma unroll
+          for (int i = 0; i < kI; ++i) {
+            const float f = e == 0 ? a[i].x : e == 1 ? a[i].y : e == 2 ? a[i].z : a[i].w;
+            // what a row does not see does not reach it: 0 * NaN would
+            if (masked && f == 0.0f) continue;
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) {
+              o[i][c][0] = fmaf(f, v[c].x, o[i][c][0]);
+              o[i][c][1] = fmaf(f, v[c].y, o[i][c][1]);
+              o[i][c][2] = fmaf(f, v[c].z, o[i][c][2]);
+              o[i][c][3] = fmaf(f, v[c].w, o[i][c][3]);
+            }
+          }
+        }
+      }
+    }
+
+    // the rows' results, or this CTA's piece of them
+    auto write_row = [&](int r, const float (&acc)[kCols][4], float ml, float sum) {
+      const int t = (row0 + r) / p.group, g = row0 + r - t * p.group;
+      const long long at = (static_cast<long long>(w.b) * p.T + t) * p.q_heads + w.h * p.group + g;
+      if (r >= live) sum = 0.0f;  // a token that does not exist
+      const float inv = sum > 0.0f ? 1.0f / sum : sum;  // a row that sees nothing: 0; a NaN stays one
+      T* dst = reinterpret_cast<T*>(p.out) + at * D;
+#pragma unroll
+      for (int c = 0; c < kCols; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (4 * x + 64 * c + e < D) dst[4 * x + 64 * c + e] = Store<T>::narrow(sum == 0.0f ? 0.0f : acc[c][e] * inv);
+      if (x == 0 && p.lse) p.lse[at] = sum == 0.0f ? -INFINITY : 0.6931471805599453f * (ml + log2f(sum));
+    };
+    if (w.whole()) {
+#pragma unroll
+      for (int i = 0; i < kI; ++i)
+        if (y + 16 * i < rows) write_row(y + 16 * i, o[i], m[i], l[i]);
+      continue;
+    }
+    const int slot = w.piece();
+#pragma unroll
+    for (int i = 0; i < kI; ++i) {
+      const int r = y + 16 * i;
+      if (r >= rows) continue;
+      const long long at = static_cast<long long>(slot) * kRows + r;
+      if (x == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(m[i], l[i]);
+#pragma unroll
+      for (int c = 0; c < kCols; ++c)
+        if (4 * x + 64 * c < D)
+          *reinterpret_cast<float4*>(p.part_o + at * (quads * 4) + 4 * x + 64 * c) =
+              make_float4(o[i][c][0], o[i][c][1], o[i][c][2], o[i][c][3]);
+    }
+    __threadfence();
+    __syncthreads();
+    const int c0 = w.first_cta(), c1 = w.last_cta();
+    if (tid == 0) {
+      const unsigned pieces = static_cast<unsigned>(c1 - c0 + 1);
+      const bool last = atomicAdd(p.counters + c0, 1u) == pieces - 1;
+      if (last) p.counters[c0] = 0u;  // zero again for the next call
+      s_last = last;
+    }
+    __syncthreads();
+    if (!s_last) continue;
+    __threadfence();
+#pragma unroll
+    for (int i = 0; i < kI; ++i) {
+      const int r = y + 16 * i;
+      if (r >= rows) continue;
+      float top = -INFINITY;
+      for (int c = c0; c <= c1; ++c) {
+        const long long at = static_cast<long long>(c == c0 ? 2 * c + 1 : 2 * c) * kRows + r;
+        top = fmax_nan(top, __ldcg(p.part_ml + 2 * at));
+      }
+      const float ref = top == -INFINITY ? 0.0f : top;
+      float sum = 0.0f, acc[kCols][4];
+#pragma unroll
+      for (int k = 0; k < kCols; ++k) acc[k][0] = acc[k][1] = acc[k][2] = acc[k][3] = 0.0f;
+      for (int c = c0; c <= c1; ++c) {
+        const long long at = static_cast<long long>(c == c0 ? 2 * c + 1 : 2 * c) * kRows + r;
+        const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml + 2 * at));
+        const float f = exp2f(ml.x - ref);
+        sum += f * ml.y;
+#pragma unroll
+        for (int k = 0; k < kCols; ++k)
+          if (4 * x + 64 * k < D) {
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * (quads * 4) + 4 * x + 64 * k));
+            acc[k][0] += f * v.x, acc[k][1] += f * v.y, acc[k][2] += f * v.z, acc[k][3] += f * v.w;
+          }
+      }
+      write_row(r, acc, top, sum);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- host side
+
+constexpr int kMaxDevices = 64;
+
+// How many CTAs of a launch run at once, per kernel and head width (0: not asked yet).
+template <typename T, int kRows, int kCols>
+int launch_simt(AttnParams p, char* workspace, cudaStream_t stream) {
+  auto kernel = attention_kernel<T, kRows, kCols>;
+  static std::atomic<int> resident[kMaxDevices];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return ASD_ERR_CUDA;
+  if (dev < 0 || dev >= kMaxDevices) return ASD_ERR_DEVICE;
+  int ctas = resident[dev].load(std::memory_order_acquire);
+  const size_t most = simt_smem(kRows, kCols * 64);  // of this instance's head widths
+  if (ctas == 0) {
+    int sms = 0, per = 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most)) !=
+            cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, kSimtThreads, most) != cudaSuccess || per < 1)
+      return ASD_ERR_CUDA;
+    ctas = sms * per < kAttnMaxCtas ? sms * per : kAttnMaxCtas;
+    resident[dev].store(ctas, std::memory_order_release);
+  }
+  const AttnLayout l = attn_layout(kAttnMaxCtas, kRows, simt_pitch(p.D) - 4);
+  p.counters = reinterpret_cast<unsigned*>(workspace + l.counters);
+  p.part_ml = reinterpret_cast<float*>(workspace + l.ml);
+  p.part_o = reinterpret_cast<float*>(workspace + l.o);
+  p.unit_rows = kRows;
+  p.row_tiles = (p.T * p.group + kRows - 1) / kRows;
+  const size_t es = sizeof(T), four = 4 * es;
+  const bool vec_q = p.D % 4 == 0 && rows_aligned(p.q, es, four, p.q_batch, p.q_token, p.q_head);
+  const bool vec_kv = p.D % 4 == 0 &&
+                      rows_aligned(p.cache.k, es, four, p.cache.page_stride, p.cache.token_stride,
+                                   p.cache.head_stride) &&
+                      reinterpret_cast<uintptr_t>(p.cache.v) % four == 0;
+  cudaLaunchAttribute attr;
+  cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(ctas)), dim3(kSimtThreads), stream, &attr);
+  cfg.dynamicSmemBytes = simt_smem(kRows, p.D);
+  if (cudaLaunchKernelEx(&cfg, kernel, p, vec_q, vec_kv) != cudaSuccess) return ASD_ERR_CUDA;
+  return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;
+}
+
+// Rows of a unit: 64 where that many share a key/value head, else 16.
+int simt_rows(long long rows) { return rows > 16 ? 64 : 16; }
+
+template <typename T, int kRows>
+int launch_cols(const AttnParams& p, char* workspace, cudaStream_t stream) {
+  if (p.D <= 64) return launch_simt<T, kRows, 1>(p, workspace, stream);
+  if (p.D <= 128) return launch_simt<T, kRows, 2>(p, workspace, stream);
+  return launch_simt<T, kRows, 4>(p, workspace, stream);
+}
+
+template <typename T>
+int launch_rows(const AttnParams& p, char* workspace, cudaStream_t stream) {
+  if (simt_rows(static_cast<long long>(p.T) * p.group) == 64) return launch_cols<T, 64>(p, workspace, stream);
+  return launch_cols<T, 16>(p, workspace, stream);
+}
+
+int check_attention(const asd_kv_cache* cache, int T, int q_heads) {
+  const int rc = check_cache(cache);
+  if (rc != ASD_OK) return rc;
+  if (T < 0 || q_heads < 1 || q_heads % cache->heads != 0) return ASD_ERR_SHAPE;
+  // rows and tiles are counted in 32 bits
+  if (static_cast<long long>(T) * (q_heads / cache->heads) > (1 << 28)) return ASD_ERR_SHAPE;
+  return ASD_OK;
+}
+
+size_t attention_bytes(const asd_kv_cache* cache, int T, int q_heads) {
+  const long long rows = static_cast<long long>(T) * (q_heads / cache->heads);
+  return attn_layout(kAttnMaxCtas, simt_rows(rows), simt_pitch(cache->head_dim) - 4).total;
+}
+
+}  // namespace
+
+extern "C" {
+
+int asd_attention_workspace_size(const asd_kv_cache* cache, int T, int q_heads, size_t* bytes) {
+  if (!bytes) return ASD_ERR_NULL;
+  const int rc = check_attention(cache, T, q_heads);
+  if (rc != ASD_OK) return rc;
+  *bytes = attention_bytes(cache, T, q_heads);
+  return ASD_OK;
+}
+
+int asd_tree_attention(const asd_kv_cache* cache, int layer, int T, const void* q, int64_t q_batch, int64_t q_token,
+                       int64_t q_head, int q_heads, const int32_t* kv_len, const int32_t* new_len,
+                       const uint32_t* tree_mask, float scale, void* out, float* lse, int32_t* status,
+                       void* workspace, size_t workspace_bytes, asd_stream_t stream) {
+  const int rc = check_attention(cache, T, q_heads);
+  if (rc != ASD_OK) return rc;
+  if (layer < 0 || layer >= cache->layers) return ASD_ERR_SHAPE;
+  if (!(scale - scale == 0.0f)) return ASD_ERR_CONTROL;  // infinite or NaN
+  if (cache->B == 0 || T == 0) return ASD_OK;
+  if (!q || !kv_len || !out || !workspace) return ASD_ERR_NULL;
+  const size_t es = store_bytes(cache->dtype);
+  if (reinterpret_cast<uintptr_t>(q) % es != 0 || reinterpret_cast<uintptr_t>(out) % es != 0) return ASD_ERR_ALIGN;
+  const void* const words[] = {kv_len, new_len, tree_mask, lse, status};
+  for (const void* x : words)
+    if (reinterpret_cast<uintptr_t>(x) % 4 != 0) return ASD_ERR_ALIGN;
+  if (workspace_bytes < attention_bytes(cache, T, q_heads)) return ASD_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return ASD_ERR_ALIGN;
+  AttnParams p = {};
+  p.cache = cache_view(cache, layer);
+  p.q = static_cast<const char*>(q);
+  p.q_batch = q_batch;
+  p.q_token = q_token;
+  p.q_head = q_head;
+  p.out = static_cast<char*>(out);
+  p.lse = lse;
+  p.kv_len = kv_len;
+  p.new_len = new_len;
+  p.mask = tree_mask;
+  p.mask_words = (T + 31) / 32;
+  p.status = status;
+  p.error = reinterpret_cast<unsigned*>(workspace);
+  p.B = cache->B;
+  p.T = T;
+  p.q_heads = q_heads;
+  p.heads = cache->heads;
+  p.group = q_heads / cache->heads;
+  p.D = cache->head_dim;
+  p.scale = scale;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  char* ws = static_cast<char*>(workspace);
+  const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (cache->dtype == ASD_F32) return launch_rows<float>(p, ws, s);
+  if (cache->dtype == ASD_BF16) return launch_rows<__nv_bfloat16>(p, ws, s);
+  return launch_rows<__half>(p, ws, s);
+}
+
+}  // extern "C"
