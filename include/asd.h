@@ -457,7 +457,10 @@ int asd_kv_append(const asd_kv_cache* cache, int layer, int T, const void* k, in
  * mask row) is 0 with lse = -INFINITY. What a row does not see does not reach
  * it, NaN and infinities included.
  * Arithmetic: scores, softmax statistics and sums in fp32, one rounding at the
- * end. The result does not depend on the order in which CTAs finish.
+ * end. 16-bit types with head_dim <= 128 and a multiple of 8, rows on 16-byte
+ * boundaries and scale > 0 run on the tensor cores, where the softmax weights
+ * are rounded to the 16-bit type for the second product. The result does not
+ * depend on the order in which CTAs finish.
  */
 int asd_attention_workspace_size(const asd_kv_cache* cache, int T, int q_heads, size_t* bytes);
 int asd_tree_attention(const asd_kv_cache* cache, int layer, int T, const void* q, int64_t q_batch, int64_t q_token,

@@ -1,5 +1,7 @@
 // libasd: attention of a draft chain's or tree's tokens over a paged cache
-// (asd_tree_attention), on the CUDA cores.
+// (asd_tree_attention): the entry point, and the kernel on the CUDA cores, for
+// 32-bit caches, wide heads and layouts that the tensor-core kernel does not
+// take.
 //
 // out = softmax(scale q k^T) v over the slots that each row sees, in one pass
 // over the keys and values: per row the running maximum m and sum l of
@@ -17,6 +19,7 @@
 
 #include "asd.h"
 #include "asd_attention.cuh"
+#include "asd_attention_tc.h"
 #include "asd_launch.cuh"
 
 namespace {
@@ -71,7 +74,7 @@ __global__ void __launch_bounds__(kSimtThreads)
   const int tid = threadIdx.x, x = tid & 15, y = tid >> 4;
   pdl_signal_dependents();
   pdl_wait_prerequisites();
-  if (__ldcg(p.error)) {
+  if (__syncthreads_or(tid == 0 && __ldcg(p.error) != 0)) {
     if (blockIdx.x == 0 && p.status)
       for (int b = tid; b < p.B; b += kSimtThreads) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_INCOMPLETE));
     return;
@@ -357,7 +360,9 @@ int check_attention(const asd_kv_cache* cache, int T, int q_heads) {
 
 size_t attention_bytes(const asd_kv_cache* cache, int T, int q_heads) {
   const long long rows = static_cast<long long>(T) * (q_heads / cache->heads);
-  return attn_layout(kAttnMaxCtas, simt_rows(rows), simt_pitch(cache->head_dim) - 4).total;
+  const size_t simt = attn_layout(kAttnMaxCtas, simt_rows(rows), simt_pitch(cache->head_dim) - 4).total;
+  const size_t tc = attention_tc_bytes(cache, T, q_heads);
+  return simt > tc ? simt : tc;
 }
 
 }  // namespace
@@ -413,6 +418,7 @@ int asd_tree_attention(const asd_kv_cache* cache, int layer, int T, const void* 
   p.scale_log2 = scale * 1.4426950408889634f;
   char* ws = static_cast<char*>(workspace);
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (attention_tc_takes(cache, p)) return launch_attention_tc(cache, p, ws, s);
   if (cache->dtype == ASD_F32) return launch_rows<float>(p, ws, s);
   if (cache->dtype == ASD_BF16) return launch_rows<__nv_bfloat16>(p, ws, s);
   return launch_rows<__half>(p, ws, s);

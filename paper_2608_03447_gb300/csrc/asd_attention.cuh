@@ -1,4 +1,6 @@
-// libasd: the attention kernel's parameters and the deal of the work to CTAs.
+// libasd: what the two attention kernels (asd_attention.cu on the CUDA cores,
+// asd_attention_tc.cu on the tensor cores) share: parameters and the deal of the
+// work to CTAs.
 //
 // Work. A unit is one row tile (some of a request's T * group query rows that
 // share a key/value head, row t * group + g) against all the tiles of key/value
