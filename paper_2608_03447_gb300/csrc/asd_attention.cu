@@ -74,11 +74,6 @@ __global__ void __launch_bounds__(kSimtThreads)
   const int tid = threadIdx.x, x = tid & 15, y = tid >> 4;
   pdl_signal_dependents();
   pdl_wait_prerequisites();
-  if (__syncthreads_or(tid == 0 && __ldcg(p.error) != 0)) {
-    if (blockIdx.x == 0 && p.status)
-      for (int b = tid; b < p.B; b += kSimtThreads) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_INCOMPLETE));
-    return;
-  }
   if (!attn_deal<kSimtTile>(p, deal)) return;
 
   for (AttnWalk<kSimtTile> w(p, deal); w.more(); w.next()) {
@@ -115,7 +110,7 @@ __global__ void __launch_bounds__(kSimtThreads)
         *reinterpret_cast<float4*>(skv + s * pitch + 4 * d4) = make_float4(f[0], f[1], f[2], f[3]);
       }
     };
-    for (int j = w.j0; j < w.j1 && span > 0; ++j) {
+    for (int j = w.j0, j1 = w.j1(); j < j1 && span > 0; ++j) {
       const int slot0 = j * kSimtTile;
       const int slots = min(kSimtTile, span - slot0);
       __syncthreads();  // the tile before has been read

@@ -92,6 +92,7 @@ struct AttnDeal {
   int b;              // request of the first tile
   long long b_first;  // that request's first tile
   int cached;         // requests b .. b + cached - 1 are in `request`
+  unsigned error;     // the workspace's error word
   AttnRequest request[kAttnScan];
   long long sums[33];  // scratch of the scan
 };
@@ -103,13 +104,15 @@ __device__ __forceinline__ int attn_cta_of(long long x, long long total, int cta
 
 // By the whole CTA: adds up the requests' tiles, a chunk of blockDim.x requests
 // at a time, and finds where this CTA's range begins. Returns false where it has
-// none. Flags requests whose lengths are out of range.
+// none, or where the workspace's error word is set, with the requests flagged.
+// Flags requests whose lengths are out of range.
 template <int kTile>
 __device__ bool attn_deal(const AttnParams& p, AttnDeal& d) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nwarps = blockDim.x >> 5;
   // total, and what comes before this thread's request of the last chunk
   long long total = 0, before = 0, mine = 0;
   AttnRequest r = {0, 0};
+  if (tid == 0) d.error = __ldcg(p.error);  // in one round trip with the lengths
   const int chunks = (p.B + blockDim.x - 1) / blockDim.x;
   auto scan = [&](int chunk) {
     const int b = chunk * static_cast<int>(blockDim.x) + tid;
@@ -138,6 +141,11 @@ __device__ bool attn_deal(const AttnParams& p, AttnDeal& d) {
     total += all;
   };
   for (int c = 0; c < chunks; ++c) scan(c);
+  if (d.error) {
+    if (blockIdx.x == 0 && p.status)
+      for (int b = tid; b < p.B; b += blockDim.x) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_INCOMPLETE));
+    return false;
+  }
   const long long w = total;
   const int ctas = w < static_cast<long long>(gridDim.x) ? static_cast<int>(w) : static_cast<int>(gridDim.x);
   const long long c = blockIdx.x;
@@ -160,7 +168,9 @@ __device__ bool attn_deal(const AttnParams& p, AttnDeal& d) {
     }
   }
   __syncthreads();
-  if (tid < kAttnScan && d.b + tid < p.B) {
+  if (chunks == 1) {
+    if (tid < p.B && tid >= d.b && tid < d.b + kAttnScan) d.request[tid - d.b] = r;
+  } else if (tid < kAttnScan && d.b + tid < p.B) {
     bool bad;
     d.request[tid] = attn_request(p, d.b + tid, &bad);
   }
@@ -175,55 +185,48 @@ __device__ bool attn_deal(const AttnParams& p, AttnDeal& d) {
   return true;
 }
 
-// One role's walk over the CTA's range, unit by unit.
+// One role's walk over the CTA's range, unit by unit. Few words of state: the
+// roles of the tensor-core kernel keep it in registers beside their tiles.
 template <int kTile>
 struct AttnWalk {
   const AttnParams& p;
   const AttnDeal& d;
-  long long at;       // next tile
-  long long b_first;  // the request's first tile
   int b, h, row_tile;
   AttnRequest r;
-  long long unit_first;  // the unit's first tile
-  int tiles;             // the unit's
-  int j0, j1;            // of which this CTA has j0 .. j1 - 1
+  int tiles;  // the unit's
+  int j0;     // the first of them that is this CTA's
+  int left;   // tiles of the CTA's range from there on
 
   __device__ __forceinline__ AttnWalk(const AttnParams& p_, const AttnDeal& d_) : p(p_), d(d_) {
-    at = d.begin;
     b = d.b;
-    b_first = d.b_first;
     load();
     // find the unit that holds the first tile
-    long long left = at - b_first;
+    long long at = d.begin - d.b_first;
     long long per_head = 0;
     for (int i = 0; i < p.row_tiles; ++i) per_head += attn_tiles<kTile>(p, r, i);
-    h = static_cast<int>(left / per_head);
-    left -= h * per_head;
+    h = static_cast<int>(at / per_head);
+    at -= h * per_head;
     row_tile = 0;
     for (;;) {
       tiles = attn_tiles<kTile>(p, r, row_tile);
-      if (left < tiles) break;
-      left -= tiles;
+      if (at < tiles) break;
+      at -= tiles;
       ++row_tile;
     }
-    unit_first = at - left;
-    cut();
+    j0 = static_cast<int>(at);
+    left = static_cast<int>(d.end - d.begin);
   }
   __device__ __forceinline__ void load() {
     const int i = b - d.b;
     bool bad;
     r = i < d.cached ? d.request[i] : attn_request(p, b, &bad);
   }
-  __device__ __forceinline__ void cut() {
-    j0 = static_cast<int>(at - unit_first);
-    const long long rest = d.end - unit_first;
-    j1 = rest < tiles ? static_cast<int>(rest) : tiles;
-  }
-  __device__ __forceinline__ bool more() const { return at < d.end; }
+  __device__ __forceinline__ bool more() const { return left > 0; }
+  __device__ __forceinline__ int j1() const { return min(tiles, j0 + left); }  // this CTA has tiles j0 .. j1 - 1
   __device__ __forceinline__ void next() {
-    at = unit_first + j1;
-    if (at >= d.end) return;
-    unit_first = at;
+    left -= j1() - j0;
+    if (left <= 0) return;
+    j0 = 0;
     if (++row_tile == p.row_tiles) {
       row_tile = 0;
       if (++h == p.heads) {
@@ -233,9 +236,8 @@ struct AttnWalk {
       }
     }
     tiles = attn_tiles<kTile>(p, r, row_tile);
-    cut();
   }
-  __device__ __forceinline__ bool whole() const { return j0 == 0 && j1 == tiles; }
+  __device__ __forceinline__ bool whole() const { return j0 == 0 && left >= tiles; }
   __device__ __forceinline__ int span() const { return attn_span(p, r, row_tile); }
   __device__ __forceinline__ int row0() const { return row_tile * p.unit_rows; }
   // rows of the unit that exist in the output, and those of tokens that exist
@@ -243,8 +245,9 @@ struct AttnWalk {
   __device__ __forceinline__ int live_rows() const { return min(rows(), max(0, r.n * p.group - row0())); }
   // the workspace slot of this CTA's piece, and the unit's CTAs
   __device__ __forceinline__ int piece() const { return 2 * static_cast<int>(blockIdx.x) + (j0 == 0 ? 1 : 0); }
-  __device__ __forceinline__ int first_cta() const { return attn_cta_of(unit_first, d.total, d.ctas); }
-  __device__ __forceinline__ int last_cta() const { return attn_cta_of(unit_first + tiles - 1, d.total, d.ctas); }
+  __device__ __forceinline__ long long unit_first() const { return d.end - left - j0; }
+  __device__ __forceinline__ int first_cta() const { return attn_cta_of(unit_first(), d.total, d.ctas); }
+  __device__ __forceinline__ int last_cta() const { return attn_cta_of(unit_first() + tiles - 1, d.total, d.ctas); }
 };
 
 // Bit i: whether a row of token t sees slot j0 + i (i < 32; r.n > t). Slots past the span are not seen.

@@ -1,4 +1,5 @@
-"""Plain 64-bit implementations of the cache operators, on the CPU, and the tolerances their tests use.
+"""Plain 64-bit implementations of the cache operators, in elementary torch operations, and the tolerances their
+tests use.
 
 Written from the definitions: token by token, head by head, no shared code with the library.
 """
@@ -24,15 +25,16 @@ def sees_matrix(n, mask_row_words, T):
 
 
 def attention(q, k, v, table, kv_len, new_len, mask, scale):
-    """q [B, T, Hq, D], k, v [pages, page, Hkv, D] (any type, CPU). Returns out, lse and the tolerance's two
+    """q [B, T, Hq, D], k, v [pages, page, Hkv, D] (any type). Returns out, lse and the tolerance's two
     magnitudes per row: the weighted sum of |v| and the largest sum of |q_d k_d| * scale, all in 64 bits."""
     B, T, Hq, D = q.shape
     page, Hkv = k.shape[1], k.shape[2]
     G = Hq // Hkv
-    out = torch.zeros(B, T, Hq, D, dtype=torch.float64)
-    lse = torch.full((B, T, Hq), -math.inf, dtype=torch.float64)
-    weight = torch.zeros(B, T, Hq, D, dtype=torch.float64)
-    reach = torch.zeros(B, T, Hq, dtype=torch.float64)
+    dev = q.device
+    out = torch.zeros(B, T, Hq, D, dtype=torch.float64, device=dev)
+    lse = torch.full((B, T, Hq), -math.inf, dtype=torch.float64, device=dev)
+    weight = torch.zeros(B, T, Hq, D, dtype=torch.float64, device=dev)
+    reach = torch.zeros(B, T, Hq, dtype=torch.float64, device=dev)
     for b in range(B):
         ctx, n = int(kv_len[b]), int(new_len[b]) if new_len is not None else T
         if n == 0:
@@ -43,18 +45,20 @@ def attention(q, k, v, table, kv_len, new_len, mask, scale):
         tree = sees_matrix(n, None if mask is None else mask[b], T)
         sees = torch.cat([torch.ones(n, ctx, dtype=torch.bool), tree], 1)
         for t in range(n):
-            at = sees[t].nonzero().flatten()
+            at = sees[t].nonzero().flatten().to(dev)
             if at.numel() == 0:
                 continue
-            for h in range(Hq):
-                x = q[b, t, h].double()
-                key, val = kk[at, h // G], vv[at, h // G]
-                z = (key @ x) * scale
-                w = torch.softmax(z, 0)
-                out[b, t, h] = w @ val
-                lse[b, t, h] = torch.logsumexp(z, 0)
-                weight[b, t, h] = w @ val.abs()
-                reach[b, t, h] = ((key * x).abs().sum(1) * abs(scale)).max()
+            for h in range(Hkv):  # the group's G query heads at once
+                x = q[b, t, h * G:(h + 1) * G].double()
+                key, val = kk[at, h], vv[at, h]
+                z = (x @ key.T) * scale
+                w = torch.exp(z - z.max(1, keepdim=True).values)
+                w = w / w.sum(1, keepdim=True)
+                heads = slice(h * G, (h + 1) * G)
+                out[b, t, heads] = w @ val
+                lse[b, t, heads] = torch.logsumexp(z, 1)
+                weight[b, t, heads] = w @ val.abs()
+                reach[b, t, heads] = ((x.abs() @ key.abs().T) * abs(scale)).max(1).values
     return out, lse, weight, reach
 
 

@@ -56,7 +56,10 @@ class Problem:
         return ref.slot_place(self.table[b], slot, self.page)
 
     def reference(self):
-        return ref.attention(self.q, self.k, self.v, self.table, self.kv_len, self.new_len, self.mask, self.scale)
+        dev = "cuda" if int(self.kv_len.max()) > 2000 else "cpu"  # in 64 bits either way
+        got = ref.attention(self.q.to(dev), self.k.to(dev), self.v.to(dev), self.table, self.kv_len, self.new_len,
+                            self.mask, self.scale)
+        return [x.cpu() for x in got]
 
     def device(self, asd, layout="tokens"):
         if layout == "tokens":
@@ -137,6 +140,40 @@ def test_long_context_is_split(asd, dtype, T, Hq, Hkv, D):
     p = Problem(dtype, T, Hq, Hkv, D, 32, ctx=[9000, 3, 0, 700], tree=True, seed=5)
     out, lse, _ = p.run(asd)
     p.check(out, lse)
+
+
+class Filled(Problem):
+    """Contexts of tens of thousands of slots: the cache is filled at once, unused places included."""
+
+    def __init__(self, dtype, T, Hq, Hkv, D, page, ctx, seed):
+        Problem.__init__(self, dtype, T, Hq, Hkv, D, page, [0] * len(ctx), tree=True, seed=seed)
+        g = torch.Generator().manual_seed(seed + 1)
+        self.kv_len = torch.tensor(ctx, dtype=torch.int32)
+        self.width = max(-(-(c + T) // page) for c in ctx)
+        self.pages = self.B * self.width
+        self.table = torch.randperm(self.pages, generator=g).to(torch.int32).view(self.B, self.width)
+        self.k = torch.randn(self.pages, page, Hkv, D, generator=g).to(dtype)
+        self.v = torch.randn(self.pages, page, Hkv, D, generator=g).to(dtype)
+
+
+@pytest.mark.parametrize("page", [64, 48, 16, 128, 20, 256])
+@pytest.mark.parametrize("T,Hq,Hkv,D", [(1, 3, 1, 128), (7, 8, 2, 64), (44, 5, 1, 128), (61, 5, 1, 128)])
+def test_ranges_of_many_tiles(asd, T, Hq, Hkv, D, page):
+    """Every CTA works through tens of tiles: rings and barriers wrap many times."""
+    p = Filled(BF16, T, Hq, Hkv, D, page, [150000, 20000, 90000], seed=page)
+    out, lse, _ = p.run(asd)
+    p.check(out, lse)
+
+
+def test_ranges_of_many_tiles_of_short_requests(asd):
+    """Every CTA works through tens of units of one to four tiles, shared and not."""
+    g = torch.Generator().manual_seed(2)
+    for T, Hq, Hkv, D, page in ((5, 16, 8, 64, 16), (33, 8, 2, 128, 32), (1, 8, 8, 128, 64)):
+        ctx = torch.randint(0, 400, (256,), generator=g).tolist()
+        p = Filled(BF16, T, Hq, Hkv, D, page, ctx, seed=T)
+        p.new_len = torch.randint(0, T + 1, (256,), generator=g).to(torch.int32)
+        out, lse, _ = p.run(asd)
+        p.check(out, lse)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
