@@ -437,7 +437,8 @@ int asd_kv_append(const asd_kv_cache* cache, int layer, int T, const void* k, in
  *
  * q             [B, T, q_heads, head_dim] of the cache's dtype, strides as above;
  *               q_heads a multiple of the cache's heads: query head h reads
- *               key/value head h / (q_heads / heads)
+ *               key/value head h / (q_heads / heads). B * heads * (T * group / 16
+ *               + 1) * (slots of the page table's row / 64 + 1) < 2^31
  * kv_len        [B] int32: the context, without the T new tokens
  * new_len       [B] int32 (0..T), or NULL: T
  * tree_mask     [B, T, ceil(T / 32)] uint32, or NULL: a chain (u <= t)

@@ -74,16 +74,19 @@ __global__ void __launch_bounds__(kSimtThreads)
   const int tid = threadIdx.x, x = tid & 15, y = tid >> 4;
   pdl_signal_dependents();
   pdl_wait_prerequisites();
-  if (!attn_deal<kSimtTile>(p, deal)) return;
+  attn_zero_rows<T>(p, tid, kSimtThreads);
+  if (tid < 32) attn_deal<kSimtTile>(p, deal);
+  __syncthreads();
+  if (deal.begin == deal.end) return;
 
   for (AttnWalk<kSimtTile> w(p, deal); w.more(); w.next()) {
-    const int row0 = w.row0(), rows = w.rows(), live = w.live_rows();
+    const int row0 = w.row0(), rows = w.rows();
     const int span = w.span();
     __syncthreads();  // the unit before is done with shared memory
     for (int i = tid; i < kRows * quads; i += kSimtThreads) {
       const int r = i / quads, d4 = i - r * quads;
       float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (r < live) {
+      if (r < rows) {
         const int t = (row0 + r) / p.group, g = row0 + r - t * p.group;
         load4(reinterpret_cast<const T*>(p.q) + w.b * p.q_batch + t * p.q_token + (w.h * p.group + g) * p.q_head +
                   4 * d4,
@@ -110,7 +113,7 @@ __global__ void __launch_bounds__(kSimtThreads)
         *reinterpret_cast<float4*>(skv + s * pitch + 4 * d4) = make_float4(f[0], f[1], f[2], f[3]);
       }
     };
-    for (int j = w.j0, j1 = w.j1(); j < j1 && span > 0; ++j) {
+    for (int j = w.j0, j1 = w.j1(); j < j1; ++j) {
       const int slot0 = j * kSimtTile;
       const int slots = min(kSimtTile, span - slot0);
       __syncthreads();  // the tile before has been read
@@ -148,7 +151,7 @@ __global__ void __launch_bounds__(kSimtThreads)
         const int r = y + 16 * i;
         if (masked) {
           uint32_t lo = 0, hi = 0;
-          if (r < live) {
+          if (r < rows) {
             const int t = (row0 + r) / p.group;
             lo = attn_sees(p, w.r, w.b, t, slot0);
             hi = attn_sees(p, w.r, w.b, t, slot0 + 32);
@@ -214,7 +217,6 @@ __global__ void __launch_bounds__(kSimtThreads)
     auto write_row = [&](int r, const float (&acc)[kCols][4], float ml, float sum) {
       const int t = (row0 + r) / p.group, g = row0 + r - t * p.group;
       const long long at = (static_cast<long long>(w.b) * p.T + t) * p.q_heads + w.h * p.group + g;
-      if (r >= live) sum = 0.0f;  // a token that does not exist
       const float inv = sum > 0.0f ? 1.0f / sum : sum;  // a row that sees nothing: 0; a NaN stays one
       T* dst = reinterpret_cast<T*>(p.out) + at * D;
 #pragma unroll
@@ -349,7 +351,12 @@ int check_attention(const asd_kv_cache* cache, int T, int q_heads) {
   if (rc != ASD_OK) return rc;
   if (T < 0 || q_heads < 1 || q_heads % cache->heads != 0) return ASD_ERR_SHAPE;
   // rows and tiles are counted in 32 bits
-  if (static_cast<long long>(T) * (q_heads / cache->heads) > (1 << 28)) return ASD_ERR_SHAPE;
+  const long long rows = static_cast<long long>(T) * (q_heads / cache->heads);
+  if (rows > (1 << 28)) return ASD_ERR_SHAPE;
+  const long long slots = static_cast<long long>(cache->table_width) * cache->page_size;
+  const double tiles = static_cast<double>(slots < 0x7fffffffll ? slots : 0x7fffffffll) / kSimtTile + 1;
+  if (tiles * static_cast<double>(rows / simt_rows(rows) + 1) * cache->heads * cache->B > 2147483647.0)
+    return ASD_ERR_SHAPE;
   return ASD_OK;
 }
 

@@ -3,8 +3,8 @@
 // work to CTAs.
 //
 // Work. A unit is one row tile (some of a request's T * group query rows that
-// share a key/value head, row t * group + g) against all the tiles of key/value
-// slots that it sees. All units' tiles, one request after the other, form one
+// share a key/value head, row t * group + g; those of tokens that exist) against
+// all the tiles of key/value slots that it sees. All units' tiles, one request after the other, form one
 // sequence that is cut into equal contiguous ranges, one a CTA, whatever the
 // requests' lengths: no CTA has more than one tile more than another. Lengths
 // are device data, so every CTA adds them up itself. A unit that a range's end
@@ -23,7 +23,7 @@
 namespace asd_detail {
 
 constexpr int kAttnMaxCtas = 320;  // of one launch: a counter and two pieces each
-constexpr int kAttnScan = 32;      // requests of a CTA's range whose lengths it keeps
+constexpr int kAttnScan = 32;      // requests of a CTA's range whose lengths it keeps: one a lane
 
 struct AttnParams {
   CacheView cache;
@@ -61,8 +61,8 @@ __device__ __forceinline__ AttnRequest attn_request(const AttnParams& p, int b, 
   return r;
 }
 
-// Slots that a row tile of a request sees: none where it has no rows; a chain's
-// rows see nothing past their own token.
+// Slots that a row tile of a request sees: none where it has no rows of tokens
+// that exist; a chain's rows see nothing past their own token.
 __device__ __forceinline__ int attn_span(const AttnParams& p, const AttnRequest& r, int row_tile) {
   const int row0 = row_tile * p.unit_rows;
   if (row0 >= r.n * p.group) return 0;
@@ -74,119 +74,132 @@ __device__ __forceinline__ int attn_span(const AttnParams& p, const AttnRequest&
 template <int kTile>
 __device__ __forceinline__ int attn_tiles(const AttnParams& p, const AttnRequest& r, int row_tile) {
   const int span = attn_span(p, r, row_tile);
-  return span > kTile ? (span - 1) / kTile + 1 : 1;  // a unit that sees nothing still has its rows to write
+  return span > 0 ? (span - 1) / kTile + 1 : 0;
 }
 
 template <int kTile>
-__device__ __forceinline__ long long attn_request_tiles(const AttnParams& p, const AttnRequest& r) {
-  long long w = 0;
+__device__ __forceinline__ int attn_request_tiles(const AttnParams& p, const AttnRequest& r) {
+  int w = 0;
+#pragma unroll 1
   for (int i = 0; i < p.row_tiles; ++i) w += attn_tiles<kTile>(p, r, i);
   return w * p.heads;
 }
 
-// What a CTA works out before it starts.
+// The output rows of tokens that do not exist, which no unit has: zeros and
+// -infinity. Threads `tid` of `threads` of every CTA.
+template <typename T>
+__device__ __forceinline__ void attn_zero_rows(const AttnParams& p, int tid, int threads) {
+  for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
+    bool bad;
+    const AttnRequest r = attn_request(p, b, &bad);
+    if (r.n == p.T || __ldcg(p.error)) continue;
+    const long long row = (static_cast<long long>(b) * p.T + r.n) * p.q_heads;
+    const long long rows = static_cast<long long>(p.T - r.n) * p.q_heads, bytes = rows * p.D * sizeof(T);
+    char* dst = p.out + row * p.D * sizeof(T);
+    if (((reinterpret_cast<uintptr_t>(dst) | static_cast<uintptr_t>(bytes)) & 15) == 0) {
+      for (long long i = tid; i < bytes / 16; i += threads) reinterpret_cast<uint4*>(dst)[i] = make_uint4(0, 0, 0, 0);
+    } else {
+      for (long long i = tid; i < rows * p.D; i += threads) reinterpret_cast<T*>(dst)[i] = Store<T>::narrow(0.0f);
+    }
+    if (p.lse)
+      for (long long i = tid; i < rows; i += threads) p.lse[row + i] = -INFINITY;
+  }
+}
+
+// What a CTA works out before it starts. Tiles are counted in 32 bits (the entry
+// point refuses what would not fit).
 struct AttnDeal {
-  long long total;    // tiles of all units
-  long long begin, end;  // this CTA's
-  int ctas;           // that have any
-  int b;              // request of the first tile
-  long long b_first;  // that request's first tile
-  int cached;         // requests b .. b + cached - 1 are in `request`
-  unsigned error;     // the workspace's error word
+  int total;       // tiles of all units
+  int begin, end;  // this CTA's; none where begin == end
+  int ctas;        // that have any
+  int b;           // request of the first tile
+  int b_first;     // that request's first tile
+  int cached;      // requests b .. b + cached - 1 are in `request`
   AttnRequest request[kAttnScan];
-  long long sums[33];  // scratch of the scan
 };
 
-// The CTA that holds tile x of `total` dealt to `ctas`: cta c has tiles from floor(c * total / ctas) on.
-__device__ __forceinline__ int attn_cta_of(long long x, long long total, int ctas) {
-  return static_cast<int>(((x + 1) * ctas - 1) / total);
+// Of w tiles dealt to `ctas` CTAs the first w % ctas get one more than the others.
+__device__ __forceinline__ int attn_first_tile(int cta, int w, int ctas) {
+  return cta * (w / ctas) + min(cta, w % ctas);
+}
+__device__ __forceinline__ int attn_cta_of(int tile, int w, int ctas) {
+  const int each = w / ctas, more = w - each * ctas, cut = more * (each + 1);
+  return tile < cut ? tile / (each + 1) : more + (tile - cut) / each;
 }
 
-// By the whole CTA: adds up the requests' tiles, a chunk of blockDim.x requests
-// at a time, and finds where this CTA's range begins. Returns false where it has
-// none, or where the workspace's error word is set, with the requests flagged.
-// Flags requests whose lengths are out of range.
+// By one warp: adds up the requests' tiles, 32 requests at a time, and finds
+// where this CTA's range begins. Flags requests whose lengths are out of range;
+// where the workspace's error word is set, all requests, and the range is empty.
 template <int kTile>
-__device__ bool attn_deal(const AttnParams& p, AttnDeal& d) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nwarps = blockDim.x >> 5;
-  // total, and what comes before this thread's request of the last chunk
-  long long total = 0, before = 0, mine = 0;
+__device__ __forceinline__ void attn_deal(const AttnParams& p, AttnDeal& d) {
+  const int lane = threadIdx.x & 31;
+  const unsigned error = __ldcg(p.error);  // in one round trip with the first lengths
   AttnRequest r = {0, 0};
-  if (tid == 0) d.error = __ldcg(p.error);  // in one round trip with the lengths
-  const int chunks = (p.B + blockDim.x - 1) / blockDim.x;
-  auto scan = [&](int chunk) {
-    const int b = chunk * static_cast<int>(blockDim.x) + tid;
+  int mine = 0, before = 0, total = 0;
+  auto scan = [&](int b0, bool report) {  // requests b0 .. b0 + 31
     mine = 0;
-    if (b < p.B) {
+    r.ctx = r.n = 0;
+    if (b0 + lane < p.B) {
       bool bad;
-      r = attn_request(p, b, &bad);
+      r = attn_request(p, b0 + lane, &bad);
       mine = attn_request_tiles<kTile>(p, r);
-      if (bad && blockIdx.x == 0 && p.status) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_LENGTH));
+      if (bad && report && blockIdx.x == 0 && p.status)
+        atomicOr(p.status + b0 + lane, static_cast<int>(ASD_STATUS_LENGTH));
     }
-    long long inc = mine;
+    int inc = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-      const long long o = __shfl_up_sync(kFull, inc, off);
+      const int o = __shfl_up_sync(kFull, inc, off);
       if (lane >= off) inc += o;
     }
-    __syncthreads();
-    if (lane == 31) d.sums[warp] = inc;
-    __syncthreads();
-    long long base = total, all = 0;
-    for (int w = 0; w < nwarps; ++w) {
-      if (w < warp) base += d.sums[w];
-      all += d.sums[w];
-    }
-    before = base + inc - mine;
-    total += all;
+    before = total + inc - mine;
+    total += __shfl_sync(kFull, inc, 31);
   };
-  for (int c = 0; c < chunks; ++c) scan(c);
-  if (d.error) {
-    if (blockIdx.x == 0 && p.status)
-      for (int b = tid; b < p.B; b += blockDim.x) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_INCOMPLETE));
-    return false;
+#pragma unroll 1
+  for (int b0 = 0; b0 < p.B; b0 += 32) scan(b0, !error);
+  const int w = total;
+  const int ctas = min(w, static_cast<int>(gridDim.x));
+  const int c = blockIdx.x;
+  if (error || c >= ctas) {
+    if (error && c == 0 && p.status)
+      for (int b = lane; b < p.B; b += 32) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_INCOMPLETE));
+    if (lane == 0) d.begin = d.end = 0;
+    __syncwarp();
+    return;
   }
-  const long long w = total;
-  const int ctas = w < static_cast<long long>(gridDim.x) ? static_cast<int>(w) : static_cast<int>(gridDim.x);
-  const long long c = blockIdx.x;
-  if (c >= ctas) return false;
-  const long long begin = c * w / ctas, end = (c + 1) * w / ctas;
-  auto place = [&](int chunk) {
-    const int b = chunk * static_cast<int>(blockDim.x) + tid;
-    if (b < p.B && mine > 0 && before <= begin && begin < before + mine) {
-      d.b = b;
-      d.b_first = before;
-    }
-  };
-  if (chunks == 1) {
-    place(0);
-  } else {
-    total = 0;
-    for (int k = 0; k < chunks; ++k) {
-      scan(k);
-      place(k);
-    }
+  const int begin = attn_first_tile(c, w, ctas);
+  int b0 = 0;
+  unsigned holds = 0;
+  if (p.B > 32) total = 0;
+#pragma unroll 1
+  for (; b0 < p.B; b0 += 32) {
+    if (p.B > 32) scan(b0, false);
+    holds = __ballot_sync(kFull, mine > 0 && before <= begin && begin < before + mine);
+    if (holds) break;
   }
-  __syncthreads();
-  if (chunks == 1) {
-    if (tid < p.B && tid >= d.b && tid < d.b + kAttnScan) d.request[tid - d.b] = r;
-  } else if (tid < kAttnScan && d.b + tid < p.B) {
+  const int at = __ffs(holds) - 1, b = b0 + at;
+  const int b_first = __shfl_sync(kFull, before, at);
+  // the lengths of the next requests: the scan's own where it has them all
+  const int from = min(lane + at, 31);
+  AttnRequest next = {__shfl_sync(kFull, r.ctx, from), __shfl_sync(kFull, r.n, from)};
+  if (lane + at > 31 && b + lane < p.B) {
     bool bad;
-    d.request[tid] = attn_request(p, d.b + tid, &bad);
+    next = attn_request(p, b + lane, &bad);
   }
-  if (tid == 0) {
+  d.request[lane] = next;
+  if (lane == 0) {
     d.total = w;
     d.begin = begin;
-    d.end = end;
+    d.end = attn_first_tile(c + 1, w, ctas);
     d.ctas = ctas;
-    d.cached = p.B - d.b < kAttnScan ? p.B - d.b : kAttnScan;
+    d.b = b;
+    d.b_first = b_first;
+    d.cached = min(p.B - b, kAttnScan);
   }
-  __syncthreads();
-  return true;
+  __syncwarp();
 }
 
-// One role's walk over the CTA's range, unit by unit. Few words of state: the
-// roles of the tensor-core kernel keep it in registers beside their tiles.
+// A walk over the CTA's range, unit by unit.
 template <int kTile>
 struct AttnWalk {
   const AttnParams& p;
@@ -201,10 +214,9 @@ struct AttnWalk {
     b = d.b;
     load();
     // find the unit that holds the first tile
-    long long at = d.begin - d.b_first;
-    long long per_head = 0;
-    for (int i = 0; i < p.row_tiles; ++i) per_head += attn_tiles<kTile>(p, r, i);
-    h = static_cast<int>(at / per_head);
+    const int per_head = attn_request_tiles<kTile>(p, r) / p.heads;
+    int at = d.begin - d.b_first;
+    h = at / per_head;
     at -= h * per_head;
     row_tile = 0;
     for (;;) {
@@ -213,8 +225,8 @@ struct AttnWalk {
       at -= tiles;
       ++row_tile;
     }
-    j0 = static_cast<int>(at);
-    left = static_cast<int>(d.end - d.begin);
+    j0 = at;
+    left = d.end - d.begin;
   }
   __device__ __forceinline__ void load() {
     const int i = b - d.b;
@@ -227,25 +239,26 @@ struct AttnWalk {
     left -= j1() - j0;
     if (left <= 0) return;
     j0 = 0;
-    if (++row_tile == p.row_tiles) {
-      row_tile = 0;
-      if (++h == p.heads) {
-        h = 0;
-        ++b;
-        load();
+    do {
+      if (++row_tile == p.row_tiles) {
+        row_tile = 0;
+        if (++h == p.heads) {
+          h = 0;
+          ++b;
+          load();
+        }
       }
-    }
-    tiles = attn_tiles<kTile>(p, r, row_tile);
+      tiles = attn_tiles<kTile>(p, r, row_tile);
+    } while (tiles == 0);  // no rows of tokens that exist
   }
   __device__ __forceinline__ bool whole() const { return j0 == 0 && left >= tiles; }
   __device__ __forceinline__ int span() const { return attn_span(p, r, row_tile); }
   __device__ __forceinline__ int row0() const { return row_tile * p.unit_rows; }
-  // rows of the unit that exist in the output, and those of tokens that exist
-  __device__ __forceinline__ int rows() const { return min(p.unit_rows, p.T * p.group - row0()); }
-  __device__ __forceinline__ int live_rows() const { return min(rows(), max(0, r.n * p.group - row0())); }
+  // rows of the unit, of tokens that exist
+  __device__ __forceinline__ int rows() const { return min(p.unit_rows, r.n * p.group - row0()); }
   // the workspace slot of this CTA's piece, and the unit's CTAs
   __device__ __forceinline__ int piece() const { return 2 * static_cast<int>(blockIdx.x) + (j0 == 0 ? 1 : 0); }
-  __device__ __forceinline__ long long unit_first() const { return d.end - left - j0; }
+  __device__ __forceinline__ int unit_first() const { return d.end - left - j0; }
   __device__ __forceinline__ int first_cta() const { return attn_cta_of(unit_first(), d.total, d.ctas); }
   __device__ __forceinline__ int last_cta() const { return attn_cta_of(unit_first() + tiles - 1, d.total, d.ctas); }
 };

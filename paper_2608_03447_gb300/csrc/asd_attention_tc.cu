@@ -47,25 +47,41 @@ constexpr int kLoadWarp = 8, kMmaWarp = 9, kQueryWarp = 10, kTailWarp = 11;
 constexpr int kThreads = 12 * 32;  // three warps a scheduler: 168 registers each
 constexpr int kTmemCols = 512;
 constexpr int kMaxStages = 12;
+constexpr unsigned long long kLandNs = 10000000;  // longer than any load takes
 constexpr float kGrowth = 8.0f; // log2: how far the maximum may outgrow the reference
 
 constexpr int slab_bytes(int dim) { return kTile * dim * 2; }  // 128 rows of a padded head
 constexpr int kHalfSlab = kTile * 128;                         // 64 elements of all of them
 constexpr size_t kSmemMax = 232448;
 
+// What the roles know of a unit: the loading warp walks the CTA's range and
+// publishes its units through a small ring, so that the walk's code exists once
+// (the roles' code has to fit the instruction cache beside one another).
+struct alignas(16) TcUnit {
+  int b, h, row0, rows;      // request, key/value head, first row and rows
+  int span, ctx, n, valid;   // slots that the rows see; the request's lengths; 0: there are no more units
+  int j0, j1, whole, piece;  // this CTA's tiles, whether they are all of the unit's, the piece's place in the workspace
+  int c0, c1, pad[2];        // the CTAs that have a piece each
+};
+constexpr int kUnits = 8;
+constexpr int kUnitReaders = 11;  // warps
+
 struct TcShared {
   unsigned long long full[kMaxStages];   // a stage's loads have landed
   unsigned long long empty[kMaxStages];  // the MMAs have read it, and the tail warp has seen it
   unsigned long long clean[kMaxStages];  // values of a tile with new tokens or a request's end: gone over
+  unsigned long long unit_full[kUnits], unit_empty[kUnits];
   unsigned long long q_full[2], q_empty[2];  // a query slab is there; is no longer needed
   unsigned long long s_full[2];          // per group: its scores are in tensor memory
   unsigned long long p_ready[2];         // per group: its weights are, and the sum so far is rescaled
   unsigned long long o_done[2];          // per group: the unit's last product is complete
+  unsigned long long meet;               // the softmax warps
   unsigned long long drain;
   uint32_t tmem_base;
   int abort;
   int last;         // this CTA arrived last at a unit in pieces
   int poison[4];    // of unit u, at u % 4: u + 1 if a new token's values hold NaN or infinities
+  TcUnit unit[kUnits];
   AttnDeal deal;
 };
 constexpr int stages_for(int dim) {
@@ -181,18 +197,22 @@ __device__ __forceinline__ void copies_wait() {
 // Shared memory that this thread wrote, or whose copies it saw land, is the tensor cores' to read.
 __device__ __forceinline__ void fence_for_mma() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// A bounded wait by a whole warp, one answer for all of it. After one wait has
-// given up the others return at once, so that every role still runs through its
-// loops and meets the others at the barriers.
-__device__ __forceinline__ bool warp_wait(unsigned long long* bar, uint32_t parity, TcShared& sh, const AttnParams& p) {
-  const bool got = __all_sync(kFull, mbar_wait(bar, parity, &sh.abort));
+// A bounded wait by a whole warp, one answer for all of it. What follows the
+// first look is out of line: the roles' code has to stay small. Where a wait
+// gives up, the others do too, and every role leaves its loop; all waits between
+// roles are of this kind.
+__device__ __noinline__ bool warp_wait_on(unsigned long long* bar, uint32_t parity, int* abort, unsigned* error) {
+  const bool got = __all_sync(kFull, mbar_wait(bar, parity, abort));
   if (!got) {
-    *const_cast<volatile int*>(&sh.abort) = 1;
-    atomicExch(p.error, static_cast<unsigned>(ASD_ERR_TIMEOUT));
+    *const_cast<volatile int*>(abort) = 1;
+    atomicExch(error, static_cast<unsigned>(ASD_ERR_TIMEOUT));
   }
   return got;
 }
-__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory"); }
+__device__ __forceinline__ bool warp_wait(unsigned long long* bar, uint32_t parity, TcShared& sh, const AttnParams& p) {
+  if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
+  return warp_wait_on(bar, parity, &sh.abort, p.error);
+}
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -233,33 +253,53 @@ enum : int {
   kLate = 16,    // one of the last two
   kPair = 32,    // the unit has rows for both groups, which share its tiles
   kTail = 64,    // new tokens, or the request's end
-  kUnit = 128,   // the unit's number among the CTA's units with work starts here
+};
+__device__ __forceinline__ int tile_flags(int j, int j0, int j1, int rows, int ctx) {
+  return kValid | (j == j0 ? kFirst : 0) | (j - j0 < 2 ? kEarly : 0) | (j == j1 - 1 ? kLast : 0) |
+         (j1 - j <= 2 ? kLate : 0) | (rows > kGroupRows ? kPair : 0) | (j * kTile + kTile > ctx ? kTail : 0);
+}
+
+// A warp's place in the ring of units.
+struct UnitFeed {
+  int slot = 0;
+  uint32_t phase = 0;
+  // the next unit, or null after the last one (or a wait that gave up); done() when it has been read
+  __device__ __forceinline__ const TcUnit* wait(TcShared& sh, const AttnParams& p) {
+    if (!warp_wait(&sh.unit_full[slot], phase, sh, p) || !sh.unit[slot].valid) return nullptr;
+    return &sh.unit[slot];
+  }
+  __device__ __forceinline__ void done(TcShared& sh) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.unit_empty[slot]);
+    if (++slot == kUnits) {
+      slot = 0;
+      phase ^= 1u;
+    }
+  }
 };
 
-// The CTA's tiles one after the other, over the units that see anything. The
-// fields tell of the tile that `flags` describes; advance() goes to the next.
-struct TileWalk {
-  AttnWalk<kTile> w;
-  int j, unit, span;
-  __device__ __forceinline__ TileWalk(const AttnParams& p, const AttnDeal& d) : w(p, d), unit(-1) { enter(); }
-  __device__ __forceinline__ void enter() {
-    span = 0;
-    while (w.more() && (span = w.span()) == 0) w.next();
-    j = w.j0;
-    ++unit;
-  }
-  __device__ __forceinline__ int slot0() const { return j * kTile; }
-  __device__ __forceinline__ int flags() const {
-    if (!w.more()) return 0;
-    const int from = j - w.j0, to = w.j1() - 1 - j;
-    return kValid | (from == 0 ? kFirst : 0) | (from < 2 ? kEarly : 0) | (to == 0 ? kLast : 0) | (to < 2 ? kLate : 0) |
-           (w.live_rows() > kGroupRows ? kPair : 0) | (slot0() + kTile > w.r.ctx ? kTail : 0) | unit * kUnit;
-  }
-  __device__ __forceinline__ void advance() {
-    if (++j == w.j1()) {
-      w.next();
-      enter();
+// The CTA's tiles one after the other, from the ring of units.
+struct TileFeed {
+  UnitFeed units;
+  int j = 0, j0 = 0, j1 = 0, rows = 0, ctx = 0, span = 0, number = -1;
+  // the next tile's flags, 0 after the last; lo: its first row of a new token, end: of nothing
+  __device__ __forceinline__ int take(TcShared& sh, const AttnParams& p, int& lo, int& end) {
+    if (j == j1) {
+      const TcUnit* u = units.wait(sh, p);
+      if (!u) return 0;
+      j = j0 = u->j0;
+      j1 = u->j1;
+      rows = u->rows;
+      ctx = u->ctx;
+      span = u->span;
+      ++number;
+      units.done(sh);
     }
+    lo = max(0, ctx - j * kTile);
+    end = span - j * kTile;
+    const int flags = tile_flags(j, j0, j1, rows, ctx);
+    ++j;
+    return flags;
   }
 };
 
@@ -308,22 +348,30 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = __shfl_sync(kFull, static_cast<int>(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
   pdl_signal_dependents();
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
+  if (warp == kTailWarp) {  // a barrier or two a lane
+    for (int s = lane; s < kStages; s += 32) {
       mbar_init(&sh.full[s], kTma ? 1 : 32);
       mbar_init(&sh.empty[s], 1 + 32);
       mbar_init(&sh.clean[s], 32);
     }
-    for (int g = 0; g < 2; ++g) {
+    if (lane < kUnits) {
+      mbar_init(&sh.unit_full[lane], 1);
+      mbar_init(&sh.unit_empty[lane], kUnitReaders);
+    }
+    if (lane >= 16 && lane < 18) {
+      const int g = lane - 16;
       mbar_init(&sh.q_full[g], 32);
       mbar_init(&sh.q_empty[g], kSoftmaxThreads);
       mbar_init(&sh.s_full[g], 1);
       mbar_init(&sh.p_ready[g], 128);
       mbar_init(&sh.o_done[g], 1);
     }
-    mbar_init(&sh.drain, 1);
-    sh.abort = 0;
-    for (int i = 0; i < 4; ++i) sh.poison[i] = 0;
+    if (lane == 18) {
+      mbar_init(&sh.meet, kSoftmaxThreads / 32);
+      mbar_init(&sh.drain, 1);
+      sh.abort = 0;
+    }
+    if (lane < 4) sh.poison[lane] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_for_mma();
   }
@@ -345,7 +393,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto tmem_o = [&](int g) { return tmem + static_cast<uint32_t>(2 * kTile + g * kDim); };
 
   pdl_wait_prerequisites();
-  const bool work = attn_deal<kTile>(p, sh.deal);  // the same for all threads
   const int chunk = lane % kChunks, sub = lane / kChunks;
   // where chunk `chunk` of row r lies in a slab
   auto place = [&](int r) {
@@ -354,7 +401,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const bool has_chunk = chunk * 8 < p.D;
   // 32 rows of a slab from row0 on; off: of row row0 + lane, elements of `src`
   auto copy_rows = [&](uint32_t dst, int row0, const char* src, long long off, int rows) {
-#pragma unroll
+#pragma unroll 4
     for (int i = 0; i < 32 / kRowsAtOnce; ++i) {
       const int r = i * kRowsAtOnce + sub;
       const long long o = __shfl_sync(kFull, off, r);
@@ -363,136 +410,161 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   };
 
-  if (work && warp == kLoadWarp) {
-    // ---------------- keys and values
-    Ring<kStages> ring;
+  if (warp == kLoadWarp) {
+    // ---------------- units, keys and values
+    attn_deal<kTile>(p, sh.deal);
     bool ok = true;
-    if constexpr (kTma) {
-      const int boxes = kTile / box;  // of a tile, each in kDim / 64 halves: one a lane
+    UnitFeed out;  // the next free slot
+    auto publish = [&](const TcUnit& u) {
+      if (ok) ok = warp_wait(&sh.unit_empty[out.slot], out.phase ^ 1u, sh, p);
+      if (lane == 0) {
+        sh.unit[out.slot] = u;
+        mbar_arrive(&sh.unit_full[out.slot]);
+      }
+      __syncwarp();
+      if (++out.slot == kUnits) {
+        out.slot = 0;
+        out.phase ^= 1u;
+      }
+    };
+    if (sh.deal.begin == sh.deal.end) {
+      publish(TcUnit{});
+    } else {
+      AttnWalk<kTile> w(p, sh.deal);
+      int j = 0, j1 = 0, span = 0;  // the next tile of the unit that w is at
+      bool fresh = true;            // that has not been published
+      Ring<kStages> ring;
+      // this lane's share of a tile: a TMA box, or four rows' worth of copies
+      struct Share {
+        int flags, b, h;
+        int page, at;  // TMA: and the place in it; the page table is read two tiles ahead
+        bool has;
+        int slot0, rows;
+      };
+      const int boxes = kTma ? kTile / box : 1;  // of a tile, each in kDim / 64 halves: one a lane
       const int part = lane % boxes, half = lane / boxes;
       const uint32_t dst0 = static_cast<uint32_t>(half * kHalfSlab + part * box * 128);
-      // this lane's box of a tile
-      struct Box {
-        int flags, b, h;
-        int page, at;  // and the place in it; page is read ahead
-        bool has;
-      };
-      TileWalk walk(p, sh.deal);
-      auto look_up = [&] {
-        Box x = {walk.flags(), walk.w.b, walk.w.h, 0, 0, false};
-        if (x.flags & kValid) {
-          const int slot = walk.slot0() + part * box;
-          if (slot < walk.span && half < kDim / 64) {
+      auto take = [&] {
+        Share x = {0, 0, 0, 0, 0, false, 0, 0};
+        if (ok && j == j1) {
+          if (!fresh) w.next();
+          fresh = false;
+          TcUnit u = {};
+          if (!w.more()) {
+            publish(u);
+            return x;
+          }
+          span = w.span();
+          j1 = w.j1();
+          u.b = w.b, u.h = w.h, u.row0 = w.row0(), u.rows = w.rows();
+          u.span = span, u.ctx = w.r.ctx, u.n = w.r.n, u.valid = 1;
+          u.j0 = w.j0, u.j1 = j1, u.whole = w.whole(), u.piece = w.piece();
+          if (!u.whole) {
+            u.c0 = w.first_cta();
+            u.c1 = w.last_cta();
+          }
+          publish(u);
+          j = w.j0;
+        }
+        if (!ok) return x;
+        x.flags = tile_flags(j, w.j0, j1, w.rows(), w.r.ctx);
+        x.b = w.b, x.h = w.h;
+        x.slot0 = j * kTile;
+        x.rows = min(kTile, span - x.slot0);
+        if (kTma) {
+          const int slot = x.slot0 + part * box;
+          if (slot < span && half < kDim / 64) {
             const int n = p.cache.div.quot(slot);
             x.page = __ldcg(p.cache.table + static_cast<long long>(x.b) * p.cache.table_width + n);
             x.at = slot - n * p.cache.div.size;
             x.has = true;
           }
-          walk.advance();
         }
+        ++j;
         return x;
       };
-      auto fill = [&](const CUtensorMap* map, const Box& x) {
-        if (ok) ok = warp_wait(&sh.empty[ring.stage], ring.phase ^ 1u, sh, p);
-        if (ok) {
-          const uint32_t bytes = __popc(__ballot_sync(kFull, x.has)) * box * 128u;
-          if (lane == 0) mbar_expect_tx(&sh.full[ring.stage], bytes);
-          __syncwarp();
-          // a page out of range lies outside the tensor: the box is filled with zeros
-          if (x.has) load_box(skv + ring.stage * kSlab + dst0, map, &sh.full[ring.stage], half * 64, x.at, x.h, x.page);
-          __syncwarp();
-        }
-        ring.next();
-      };
-      Box cur = look_up(), next = cur;
-      if (cur.flags) {
-        next = look_up();
-        fill(&map_k, cur);
-      }
-      while (cur.flags) {
-        if (cur.has && static_cast<unsigned>(cur.page) >= static_cast<unsigned>(p.cache.pages) && p.status)
-          atomicOr(p.status + cur.b, static_cast<int>(ASD_STATUS_PAGE));
-        const bool before = values_first(next.flags, cur.flags);
-        if (before) fill(&map_v, cur);
-        Box after = next;
-        if (next.flags) {
-          after = look_up();
-          fill(&map_k, next);
-        }
-        if (!before) fill(&map_v, cur);
-        cur = next;
-        next = after;
-      }
-    } else {
       constexpr int kLag = lag_for(kDim);
       int issued = 0, arrived = 0, stage_out = 0;
-      auto arrive = [&] {  // this thread's copies of the stage have landed
+      auto arrive = [&] {  // copies: this thread's of the stage have landed
         fence_for_mma();
         mbar_arrive(&sh.full[stage_out]);
         if (++stage_out == kStages) stage_out = 0;
         ++arrived;
       };
-      struct Rows {
-        int flags, b, h, slot0, rows;
-      };
-      TileWalk walk(p, sh.deal);
-      auto take = [&] {
-        const Rows x = {walk.flags(), walk.w.b, walk.w.h, walk.slot0(), min(kTile, walk.span - walk.slot0())};
-        if (x.flags) walk.advance();
-        return x;
-      };
-      auto fill = [&](const char* src, const Rows& x, bool report) {
+      auto fill = [&](bool values, const Share& x) {
         if (ok) ok = warp_wait(&sh.empty[ring.stage], ring.phase ^ 1u, sh, p);
-#pragma unroll 1
-        for (int q = 0; ok && q < x.rows; q += 32) {
-          long long off = -1;
-          if (q + lane < x.rows) {
-            off = slot_offset(p.cache, x.b, x.slot0 + q + lane);
-            if (off < 0 && report && p.status) atomicOr(p.status + x.b, static_cast<int>(ASD_STATUS_PAGE));
-            if (off >= 0) off += x.h * p.cache.head_stride;
+        if (!ok) return;
+        const uint32_t dst = skv + ring.stage * kSlab;
+        if constexpr (kTma) {
+          const uint32_t bytes = __popc(__ballot_sync(kFull, x.has)) * box * 128u;
+          if (lane == 0) mbar_expect_tx(&sh.full[ring.stage], bytes);
+          __syncwarp();
+          if (x.has) {
+            // a page out of range lies outside the tensor: the box is filled with zeros
+            load_box(dst + dst0, values ? &map_v : &map_k, &sh.full[ring.stage], half * 64, x.at, x.h, x.page);
+            if (!values && static_cast<unsigned>(x.page) >= static_cast<unsigned>(p.cache.pages) && p.status)
+              atomicOr(p.status + x.b, static_cast<int>(ASD_STATUS_PAGE));
           }
-          copy_rows(skv + ring.stage * kSlab, q, src, off, x.rows - q);
+          __syncwarp();
+        } else {
+#pragma unroll 1
+          for (int q = 0; q < x.rows; q += 32) {
+            long long off = -1;
+            if (q + lane < x.rows) {
+              off = slot_offset(p.cache, x.b, x.slot0 + q + lane);
+              if (off < 0 && !values && p.status) atomicOr(p.status + x.b, static_cast<int>(ASD_STATUS_PAGE));
+              if (off >= 0) off += x.h * p.cache.head_stride;
+            }
+            copy_rows(dst, q, values ? p.cache.v : p.cache.k, off, x.rows - q);
+          }
+          copies_commit();
+          ++issued;
+          if (issued - arrived > kLag) {
+            copies_wait<kLag>();
+            arrive();
+          }
         }
-        copies_commit();
         ring.next();
-        ++issued;
-        if (issued - arrived > kLag) {
-          copies_wait<kLag>();
-          arrive();
-        }
       };
-      Rows cur = take();
-      if (cur.flags) fill(p.cache.k, cur, true);
-      while (cur.flags) {
-        const Rows next = take();
-        const bool before = values_first(next.flags, cur.flags);
-        if (before) fill(p.cache.v, cur, false);
-        if (next.flags) fill(p.cache.k, next, true);
-        if (!before) fill(p.cache.v, cur, false);
+      Share cur = {0, 0, 0, 0, 0, false, 0, 0};  // its keys are in the ring
+      Share next = take();
+      while (ok && (cur.flags | next.flags)) {
+        const Share after = next.flags ? take() : next;
+        const bool before = cur.flags && values_first(next.flags, cur.flags);
+#pragma unroll 1
+        for (int i = 0; i < 2; ++i) {
+          const bool values = (i == 0) == before;
+          if (values ? cur.flags : next.flags) fill(values, values ? cur : next);
+        }
         cur = next;
+        next = after;
       }
-      copies_wait<0>();
-      while (arrived < issued) arrive();
+      if (!kTma) {
+        copies_wait<0>();
+        while (arrived < issued) arrive();
+      }
     }
-  } else if (work && warp == kQueryWarp) {
+  } else if (warp == kQueryWarp) {
     // ---------------- queries: a unit's slab, or both slabs of a unit that the groups share
+    UnitFeed feed;
     bool ok = true;
     uint32_t uses = 0;  // a bit a slab: whether an odd number of fills
     int slab = 0;
-    for (AttnWalk<kTile> w(p, sh.deal); w.more(); w.next()) {
-      if (w.span() == 0) continue;
-      const int live = w.live_rows();
-      const bool pair = live > kGroupRows;
-      for (int tile = 0; tile * kGroupRows < live; ++tile) {
+    while (const TcUnit* u = feed.wait(sh, p)) {
+      const int b = u->b, h = u->h, row0 = u->row0, rows = u->rows;
+      feed.done(sh);
+      const bool pair = rows > kGroupRows;
+      for (int tile = 0; ok && tile * kGroupRows < rows; ++tile) {
         const int to = pair ? tile : slab;
-        if (ok) ok = warp_wait(&sh.q_empty[to], ((uses >> to) & 1u) ^ 1u, sh, p);
+        ok = warp_wait(&sh.q_empty[to], ((uses >> to) & 1u) ^ 1u, sh, p);
         uses ^= 1u << to;
-        for (int r0 = 0; ok && r0 < kGroupRows && tile * kGroupRows + r0 < live; r0 += 32) {
+#pragma unroll 1
+        for (int r0 = 0; ok && r0 < kGroupRows && tile * kGroupRows + r0 < rows; r0 += 32) {
           const int r = tile * kGroupRows + r0 + lane;
           long long off = -1;
-          if (r < live) {
-            const int row = w.row0() + r, t = row / p.group;
-            off = w.b * p.q_batch + t * p.q_token + (w.h * p.group + (row - t * p.group)) * p.q_head;
+          if (r < rows) {
+            const int row = row0 + r, t = row / p.group;
+            off = b * p.q_batch + t * p.q_token + (h * p.group + (row - t * p.group)) * p.q_head;
           }
           copy_rows(sq + to * kSlab, r0, p.q, off, 32);
         }
@@ -503,7 +575,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!pair) slab ^= 1;
     }
-  } else if (work && warp == kTailWarp) {
+  } else if (warp == kTailWarp) {
     // ---------------- tiles with new tokens or a request's end
     // Rows past the end become zeros (what lies there may be anything, and 0 times NaN is NaN). Of a new token some
     // rows may see nothing, so its values' NaN and infinities become zeros too and the unit is marked: its rows look
@@ -511,66 +583,45 @@ __global__ void __launch_bounds__(kThreads, 1)
     // This warp follows every fill, one by one, and a stage is filled again only when it has: a wait by parity must
     // never be a round of the ring away from the barrier.
     Ring<kStages> ring;
+    TileFeed feed;
     bool ok = true;
-    auto seen = [&] {
-      if (ok) ok = warp_wait(&sh.full[ring.stage], ring.phase, sh, p);
-    };
-    auto done = [&] {
-      mbar_arrive(&sh.empty[ring.stage]);
-      ring.next();
-    };
-    struct Range {
-      int flags, lo, end;  // rows of the tile: new tokens from lo on, nothing from end on
-    };
-    TileWalk walk(p, sh.deal);
-    auto take = [&] {
-      const Range x = {walk.flags(), max(0, walk.w.r.ctx - walk.slot0()), walk.span - walk.slot0()};
-      if (x.flags) walk.advance();
-      return x;
-    };
-    auto keys = [&] {
-      seen();
-      done();
-    };
-    auto values = [&](const Range& x) {
-      seen();
-      if (x.flags & kTail) {
-        if (ok) {
+    int cur = 0, cur_lo = 0, cur_end = 0, cur_number = 0;
+    int next_lo = 0, next_end = 0;
+    int next = feed.take(sh, p, next_lo, next_end);
+    while (ok && (cur | next)) {
+      const int next_number = feed.number;
+      const bool before = cur && values_first(next, cur);
+#pragma unroll 1
+      for (int i = 0; ok && i < 2; ++i) {
+        const bool values = (i == 0) == before;
+        if (!(values ? cur : next)) continue;
+        ok = warp_wait(&sh.full[ring.stage], ring.phase, sh, p);
+        if (ok && values && (cur & kTail)) {
           bool found = false;
-          for (int r = x.lo + sub; r < kTile; r += kRowsAtOnce) {
+#pragma unroll 1
+          for (int r = cur_lo + sub; r < kTile; r += kRowsAtOnce) {
             uint4* at = reinterpret_cast<uint4*>(gbase + (2 + ring.stage) * kSlab + place(r));
-            if (r >= x.end) {
-              *at = make_uint4(0u, 0u, 0u, 0u);
-              continue;
-            }
-            const uint4 was = *at;
-            const uint4 now = {finite_pair<T>(was.x), finite_pair<T>(was.y), finite_pair<T>(was.z),
-                               finite_pair<T>(was.w)};
+            const uint4 was = r < cur_end ? *at : make_uint4(~0u, ~0u, ~0u, ~0u);
+            uint4 now = make_uint4(0u, 0u, 0u, 0u);
+            if (r < cur_end)
+              now = {finite_pair<T>(was.x), finite_pair<T>(was.y), finite_pair<T>(was.z), finite_pair<T>(was.w)};
             if (now.x != was.x || now.y != was.y || now.z != was.z || now.w != was.w) {
               *at = now;
-              found = true;
+              found |= r < cur_end;
             }
           }
-          const int unit = x.flags / kUnit;
-          if (found) sh.poison[unit & 3] = unit + 1;
+          if (found) sh.poison[cur_number & 3] = cur_number + 1;
           fence_for_mma();
+          __syncwarp();
+          mbar_arrive(&sh.clean[ring.stage]);
         }
-        __syncwarp();
-        mbar_arrive(&sh.clean[ring.stage]);
+        mbar_arrive(&sh.empty[ring.stage]);
+        ring.next();
       }
-      done();
-    };
-    Range cur = take();
-    if (cur.flags) keys();
-    while (cur.flags) {
-      const Range next = take();
-      const bool before = values_first(next.flags, cur.flags);
-      if (before) values(cur);
-      if (next.flags) keys();
-      if (!before) values(cur);
-      cur = next;
+      cur = next, cur_lo = next_lo, cur_end = next_end, cur_number = next_number;
+      if (next) next = feed.take(sh, p, next_lo, next_end);
     }
-  } else if (work && warp == kMmaWarp) {
+  } else if (warp == kMmaWarp) {
     // ---------------- MMAs
     constexpr uint32_t kDescS = instr_desc(kBf16, kTile, false);
     constexpr uint32_t kDescO = instr_desc(kBf16, kDim, true);
@@ -582,21 +633,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     bool ok = true;
     Ring<kStages> ring;
+    TileFeed feed;
     int k_stage = 0, v_stage = 0;       // of the tiles whose scores and whose product are being issued
     uint32_t p_phase = 0, q_phase = 0, clean_phase = 0;  // a bit a group, slab, stage
     int slab = 1;                       // of the unit that the groups take in turn
-    TileWalk walk(p, sh.deal);
-    auto take = [&] {
-      const int flags = walk.flags();
-      if (flags) walk.advance();
-      return flags;
-    };
 
     // the scores of one group's rows against a tile; `second`: the other group has done so with the same tile
     auto scores = [&](int tile, bool second, int g) {
       const bool pair = tile & kPair;
       if ((tile & kFirst) && !second) {
         if (!pair) slab ^= 1;
+#pragma unroll 1
         for (int s = pair ? 0 : slab; s <= (pair ? 1 : slab); ++s) {
           if (ok) ok = warp_wait(&sh.q_full[s], (q_phase >> s) & 1u, sh, p);
           q_phase ^= 1u << s;
@@ -645,20 +692,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!pair || second) mma_commit(&sh.empty[v_stage]);
       }
     };
-    int a = take();
-    bool a_second = false;
-    int g = 0;
-    if (a) scores(a, false, 0);
-    while (a) {
-      const bool b_second = (a & kPair) && !a_second;
-      const int b = b_second ? a : take();
-      const bool later = !b_second && starts_after(b, a);
-      if (b && !later) scores(b, b_second, g ^ 1);
-      product(a, a_second, g);
-      if (later) scores(b, false, g ^ 1);
+    int a = 0, b_lo, b_end;  // a: the tile whose product is next
+    int b = feed.take(sh, p, b_lo, b_end);
+    bool a_second = false, b_second = false;
+    int g = 1;               // a's group
+    while (ok && (a | b)) {
+      const bool later = a && !b_second && starts_after(b, a);
+#pragma unroll 1
+      for (int i = 0; i < 2; ++i) {
+        const bool of_a = (i == 0) == later;
+        if (of_a && a) product(a, a_second, g);
+        if (!of_a && b) scores(b, b_second, g ^ 1);
+      }
       a = b;
       a_second = b_second;
       g ^= 1;
+      b_second = (a & kPair) && !a_second;
+      if (a && !b_second) b = feed.take(sh, p, b_lo, b_end);
     }
     if (elected) {
       mma_commit(&sh.drain);
@@ -667,66 +717,106 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
     __syncwarp();
-  } else if (work) {
+  } else {
     // ---------------- softmax: thread `row` of group g
     const int g = warp >> 2;
     const int row = threadIdx.x & 127;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t ts = tmem_s(g) + lanes, tw = ts + kTile / 2, to = tmem_o(g) + lanes;  // scores, weights, sum
     bool ok = true;
-    uint32_t s_phase = 0, o_phase = 0;
-    int turn = 0, unit = 0, slab = 0;
-    for (AttnWalk<kTile> w(p, sh.deal); w.more(); w.next()) {
-      const int span = w.span(), rows = w.rows(), live = w.live_rows();
-      const bool pair = live > kGroupRows;
-      const bool shares = rows > kGroupRows;                       // rows for both groups to write
-      const int group_row0 = shares ? g * kGroupRows : 0;
-      const int r = group_row0 + row;                              // of the unit
-      const int rl = (pair ? g * kGroupRows : 0) + row;            // whose scores this thread has
-      const bool warp_live = (pair ? g * kGroupRows : 0) + (warp & 3) * 32 < live;  // the same for the warp
-      const int t = (w.row0() + min(rl, max(live - 1, 0))) / p.group;
+    uint32_t s_phase = 0, o_phase = 0, meet_phase = 0;
+    int turn = 0, number = 0, slab = 0;
+    auto meet = [&] {  // the two groups
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.meet);
+      if (ok) ok = warp_wait(&sh.meet, meet_phase, sh, p);
+      meet_phase ^= 1u;
+    };
+    attn_zero_rows<T>(p, threadIdx.x, kSoftmaxThreads);
+    UnitFeed feed;
+    while (ok) {
+      const TcUnit* u = feed.wait(sh, p);
+      if (!u) break;
+      const AttnRequest req = {u->ctx, u->n};
+      const int rows = u->rows, row0 = u->row0, j0 = u->j0, j1 = u->j1;
+      const bool pair = rows > kGroupRows;               // each group has rows of its own; else both have the same
+      const int r = (pair ? g * kGroupRows : 0) + row;   // of the unit
+      const bool lives = r < rows;
+      const bool warp_lives = r - lane < rows;           // the same for the warp
+      const int t = (row0 + min(r, rows - 1)) / p.group;
       float m = -INFINITY, l = 0.0f;
       bool had = false;
-      const int j1 = w.j1();
-      for (int j = w.j0; span > 0 && j < j1; ++j) {
+#pragma unroll 1
+      for (int j = j0; j < j1; ++j) {
         const int whose = turn & 1;
         turn += pair ? 2 : 1;
         if (!pair && whose != g) continue;
-        const int slot0 = j * kTile;
-        const bool masked = slot0 + kTile > w.r.ctx;
-        uint32_t sees[4];
-        if (masked && warp_live) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) sees[c] = attn_sees(p, w.r, w.b, t, slot0 + 32 * c);
+        const bool masked = (j + 1) * kTile > req.ctx;
+        uint32_t sees0 = 0, sees1 = 0, sees2 = 0, sees3 = 0;
+        if (masked && warp_lives) {
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            sees0 = sees1, sees1 = sees2, sees2 = sees3;
+            sees3 = attn_sees(p, req, u->b, t, j * kTile + 32 * c);
+          }
         }
         if (ok) ok = warp_wait(&sh.s_full[g], s_phase, sh, p);
         s_phase ^= 1u;
         tc_fence_after();
-        if (ok && warp_live) {
+        if (ok && warp_lives) {
           float x[2][32];
-          auto read_half = [&](int half) {
+          float ref = 0.0f;
+          // four chains each: one warp a scheduler has little else to cover an operation's latency with
+          float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          // The maximum over the first and the second half of the slots; then the weights of the second, which is
+          // still in registers, and of the first. The weights lie over the second half's scores. A loop, not four
+          // stretches of code: see TcUnit.
+#pragma unroll 1
+          for (int step = 0; step < 3; ++step) {
+            const int half = step & 1;
             tmem_ld32(ts + 64 * half, x[0]);
             tmem_ld32(ts + 64 * half + 32, x[1]);
             tmem_ld_wait();
-          };
-          auto hide = [&](int half) {
+            if (masked) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+              for (int c = 0; c < 2; ++c) {
+                const uint32_t sees = half ? (c ? sees3 : sees2) : (c ? sees1 : sees0);
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (!((sees[2 * half + c] >> i) & 1u)) x[c][i] = -INFINITY;
-          };
-          // four chains: one warp a scheduler has little else to cover an operation's latency with
-          float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          auto top_half = [&] {
+                for (int i = 0; i < 32; ++i)
+                  if (!((sees >> i) & 1u)) x[c][i] = -INFINITY;
+              }
+            }
+            if (step < 2) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 4)
+              for (int i = 0; i < 32; i += 4)
 #pragma unroll
-              for (int k = 0; k < 4; ++k) tops[k] = fmaxf(tops[k], fmaxf(x[0][i + k], x[1][i + k]));
-          };
-          // weights of 64 slots, over scores that are in registers or have been read
-          float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-          auto weigh_half = [&](int half, float ref) {
+                for (int k = 0; k < 4; ++k) tops[k] = fmaxf(tops[k], fmaxf(x[0][i + k], x[1][i + k]));
+            }
+            if (step == 0) continue;
+            if (step == 1) {
+              const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * p.scale_log2;
+              if (__any_sync(kFull, lives && top > m + kGrowth)) {
+                const float m_new = fmaxf(m, top);
+                const float fade = exp2_fast(m - (m_new == -INFINITY ? 0.0f : m_new));
+                l *= fade;
+                m = m_new;
+                if (had) {
+                  // every product of this group so far has completed: it came before these scores
+#pragma unroll 1
+                  for (int c = 0; c < kDim; c += 16) {
+                    float o[16];
+                    tmem_ld16(to + c, o);
+                    tmem_ld_wait();
+                    uint32_t bits[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) bits[i] = __float_as_uint(o[i] * fade);
+                    tmem_st16(to + c, bits);
+                  }
+                }
+              }
+              ref = m == -INFINITY ? 0.0f : m;
+            }
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
               uint32_t w2[16];
@@ -740,40 +830,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
               tmem_st16(tw + 32 * half + 16 * c, w2);
             }
-          };
-          read_half(0);
-          if (masked) hide(0);
-          top_half();
-          read_half(1);
-          if (masked) hide(1);
-          top_half();
-          const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * p.scale_log2;
-          if (__any_sync(kFull, rl < live && top > m + kGrowth)) {
-            const float m_new = fmaxf(m, top);
-            const float fade = exp2_fast(m - (m_new == -INFINITY ? 0.0f : m_new));
-            l *= fade;
-            m = m_new;
-            if (had) {
-              // every product of this group so far has completed: it came before these scores
-#pragma unroll 1
-              for (int c = 0; c < kDim; c += 16) {
-                float o[16];
-                tmem_ld16(to + c, o);
-                tmem_ld_wait();
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[i] *= fade;
-                uint32_t bits[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) bits[i] = __float_as_uint(o[i]);
-                tmem_st16(to + c, bits);
-              }
-            }
           }
-          const float ref = m == -INFINITY ? 0.0f : m;
-          weigh_half(1, ref);  // still in registers; the weights lie over the second half's scores
-          read_half(0);
-          if (masked) hide(0);
-          weigh_half(0, ref);
           l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
           tmem_st_wait();
         }
@@ -783,53 +840,53 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
 
       // the unit's rows, or this CTA's piece of them
-      const bool whole = w.whole();
+      const bool whole = u->whole;
       float f_self = 1.0f, f_other = 1.0f;  // what the groups' sums are multiplied with
       bool other_had = false;
-      if (span > 0) {
-        if (had) {
-          if (ok) ok = warp_wait(&sh.o_done[g], o_phase, sh, p);
-          o_phase ^= 1u;
-          tc_fence_after();
-        }
-        if (!pair) {
-          // both groups' statistics, in the slab of the unit's queries, which no MMA reads any more
-          other_had = !had || j1 - w.j0 > 1;
-          float2* stat = reinterpret_cast<float2*>(gbase + slab * kSlab);
-          tc_fence_before();
-          softmax_sync();  // both groups' products are complete, the queries have been read
-          stat[g * kGroupRows + row] = make_float2(m, l);
-          softmax_sync();
-          tc_fence_after();
-          const float2 other = stat[(g ^ 1) * kGroupRows + row];
-          const float top = fmaxf(m, other.x);
-          const float ref = top == -INFINITY ? 0.0f : top;
-          f_self = exp2_fast(m - ref);
-          f_other = exp2_fast(other.x - ref);
-          l = l * f_self + other.y * f_other;
-          m = top;
-        }
+      if (had) {
+        if (ok) ok = warp_wait(&sh.o_done[g], o_phase, sh, p);
+        o_phase ^= 1u;
+        tc_fence_after();
       }
-      const bool poisoned = span > 0 && *const_cast<volatile int*>(&sh.poison[unit & 3]) == unit + 1;
-      // Who writes what: of shared rows each group its own; else row `row`'s halves of the head, one each. In a unit
-      // that has rows for both groups but tokens for one, the second group's rows are zeros.
-      const bool split = !shares;
-      const bool lives = r < live;
-      const bool mine = ok && r < rows;
-      const int row_t = (w.row0() + r) / p.group;
-      const long long at = (static_cast<long long>(w.b) * p.T + row_t) * p.q_heads + w.h * p.group + w.row0() + r -
-                           row_t * p.group;
-      const float inv = lives && l > 0.0f ? 1.0f / l : lives ? l : 0.0f;
-      const int cols = split ? kDim / 2 : kDim;
-      const int col0 = split ? g * cols : 0;
+      if (!pair) {
+        // both groups' statistics, in the slab of the unit's queries, which no MMA reads any more
+        other_had = !had || j1 - j0 > 1;
+        float2* stat = reinterpret_cast<float2*>(gbase + slab * kSlab);
+        tc_fence_before();
+        meet();  // both groups' products are complete, the queries have been read
+        stat[g * kGroupRows + row] = make_float2(m, l);
+        meet();
+        tc_fence_after();
+        const float2 other = stat[(g ^ 1) * kGroupRows + row];
+        const float top = fmaxf(m, other.x);
+        const float ref = top == -INFINITY ? 0.0f : top;
+        f_self = exp2_fast(m - ref);
+        f_other = exp2_fast(other.x - ref);
+        l = l * f_self + other.y * f_other;
+        m = top;
+      }
+      // Who writes what: each group its own rows, or of the rows that both have each group a half of the head.
+      const bool mine = ok && lives;
+      const long long at = (static_cast<long long>(u->b) * p.T + t) * p.q_heads + u->h * p.group + row0 + r -
+                           t * p.group;
+      const int cols = pair ? kDim : kDim / 2;
+      const int col0 = pair ? 0 : g * cols;
+      const bool zero = l == 0.0f;  // sees nothing
+      if (whole) {
+        const float inv = l > 0.0f ? 1.0f / l : l;  // a NaN stays one
+        f_self *= inv;
+        f_other *= inv;
+      }
+      T* const dst = reinterpret_cast<T*>(p.out) + at * p.D;
+      // [piece][column / 4][row]: a warp's rows lie side by side
+      float* const part = p.part_o + static_cast<long long>(u->piece) * kDim * p.unit_rows + r * 4;
 #pragma unroll 1
-      for (int c = 0; c < cols; c += 32) {
-        const int col = col0 + c;
+      for (int col = col0; col < col0 + cols; col += 32) {
         __syncwarp();
         float v[32];
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] = 0.0f;
-        if (ok && span > 0 && group_row0 + (warp & 3) * 32 < live) {
+        if (ok && warp_lives) {
           float x[32];
           if (had) {
             tmem_ld32(to + col, x);
@@ -843,121 +900,139 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = fmaf(f_other, x[i], v[i]);
           }
-          if (poisoned && lives) {
-            const int end = min(span, j1 * kTile);
-            for (int slot = max(w.r.ctx, w.j0 * kTile); slot < end; ++slot) {
-              if (!(attn_sees(p, w.r, w.b, t, slot) & 1u)) continue;
-              const long long off = slot_offset(p.cache, w.b, slot);
-              if (off < 0) continue;
-              const T* src = reinterpret_cast<const T*>(p.cache.v) + off + w.h * p.cache.head_stride + col;
-              for (int i = 0; i < 32 && col + i < p.D; ++i) {
-                const float e = Store<T>::widen(src[i]);
-                if (!(e - e == 0.0f)) {
-#pragma unroll
-                  for (int k = 0; k < 32; ++k)
-                    if (k == i) v[k] += e;
-                }
-              }
-            }
-          }
         }
         if (mine && whole) {
-          T* dst = reinterpret_cast<T*>(p.out) + at * p.D + col;
-          const bool zero = !lives || l == 0.0f;
 #pragma unroll
           for (int i = 0; i < 32; i += 8) {
             if (col + i >= p.D) break;
             uint4 o;
-            o.x = zero ? 0u : pack2<T>(v[i] * inv, v[i + 1] * inv);
-            o.y = zero ? 0u : pack2<T>(v[i + 2] * inv, v[i + 3] * inv);
-            o.z = zero ? 0u : pack2<T>(v[i + 4] * inv, v[i + 5] * inv);
-            o.w = zero ? 0u : pack2<T>(v[i + 6] * inv, v[i + 7] * inv);
-            *reinterpret_cast<uint4*>(dst + i) = o;
+            o.x = zero ? 0u : pack2<T>(v[i], v[i + 1]);
+            o.y = zero ? 0u : pack2<T>(v[i + 2], v[i + 3]);
+            o.z = zero ? 0u : pack2<T>(v[i + 4], v[i + 5]);
+            o.w = zero ? 0u : pack2<T>(v[i + 6], v[i + 7]);
+            *reinterpret_cast<uint4*>(dst + col + i) = o;
           }
-        } else if (mine && lives) {
-          // [piece][column / 4][row]: a warp's rows lie side by side
-          float* dst =
-              p.part_o + (static_cast<long long>(w.piece()) * (kDim / 4) + col / 4) * (p.unit_rows * 4) + r * 4;
+        } else if (mine) {
 #pragma unroll
           for (int i = 0; i < 32; i += 4)
-            *reinterpret_cast<float4*>(dst + i * p.unit_rows) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+            *reinterpret_cast<float4*>(part + (col + i) * p.unit_rows) =
+                make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
         }
       }
-      if (mine && (!split || g == 0)) {
+      if (mine && (pair || g == 0)) {
         if (whole) {
-          if (p.lse) p.lse[at] = !lives || l == 0.0f ? -INFINITY : 0.6931471805599453f * (m + log2f(l));
-        } else if (lives) {
-          *reinterpret_cast<float2*>(p.part_ml + 2 * (static_cast<long long>(w.piece()) * p.unit_rows + r)) =
+          if (p.lse) p.lse[at] = zero ? -INFINITY : 0.6931471805599453f * (m + log2f(l));
+        } else {
+          *reinterpret_cast<float2*>(p.part_ml + 2 * (static_cast<long long>(u->piece) * p.unit_rows + r)) =
               make_float2(m, l);
         }
       }
-      if (span > 0) {
-        tc_fence_before();
-        if (pair) {
-          mbar_arrive(&sh.q_empty[0]);
-          mbar_arrive(&sh.q_empty[1]);
-        } else {
-          softmax_sync();  // both sums and the statistics have been read
-          mbar_arrive(&sh.q_empty[slab]);
-          slab ^= 1;
-        }
-        tc_fence_after();
-        ++unit;
-      }
-      if (whole) continue;
-
-      // a unit in pieces
-      __threadfence();
-      softmax_sync();
-      const int c0 = w.first_cta(), c1 = w.last_cta();
-      if (threadIdx.x == 0) {
-        bool last = false;
-        if (ok) {
-          last = atomicAdd(p.counters + c0, 1u) == static_cast<unsigned>(c1 - c0);
-          if (last) p.counters[c0] = 0u;  // zero again for the next call
-        }
-        sh.last = last;
-      }
-      softmax_sync();
-      if (!*const_cast<volatile int*>(&sh.last)) continue;
-      __threadfence();
-      const int quads = p.D / 4;
-      for (int i = threadIdx.x; i < rows * quads; i += kSoftmaxThreads) {
-        const int rr = i % rows, d4 = i / rows;
-        const int tt = (w.row0() + rr) / p.group;
-        const long long dst = (static_cast<long long>(w.b) * p.T + tt) * p.q_heads + w.h * p.group + w.row0() + rr -
-                              tt * p.group;
-        float top = -INFINITY, sum = 0.0f;
-        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (rr < live) {
-#pragma unroll 4
-          for (int c = c0; c <= c1; ++c) {
-            const long long piece = c == c0 ? 2 * c + 1 : 2 * c;
-            top = fmaxf(top, __ldcg(p.part_ml + 2 * (piece * p.unit_rows + rr)));
-          }
-          const float ref = top == -INFINITY ? 0.0f : top;
-#pragma unroll 4
-          for (int c = c0; c <= c1; ++c) {
-            const long long piece = c == c0 ? 2 * c + 1 : 2 * c;
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml + 2 * (piece * p.unit_rows + rr)));
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(
-                p.part_o + (piece * (kDim / 4) + d4) * (p.unit_rows * 4) + rr * 4));
-            const float e = exp2_fast(ml.x - ref);
-            sum += e * ml.y;
-            acc.x += e * v.x, acc.y += e * v.y, acc.z += e * v.z, acc.w += e * v.w;
+      if (mine && *const_cast<volatile int*>(&sh.poison[number & 3]) == number + 1) {
+        // NaN and infinities that the row does see, onto what this thread has just written
+#pragma unroll 1
+        for (int slot = max(req.ctx, j0 * kTile); slot < min(u->span, j1 * kTile); ++slot) {
+          if (!(attn_sees(p, req, u->b, t, slot) & 1u)) continue;
+          const long long off = slot_offset(p.cache, u->b, slot);
+          if (off < 0) continue;
+          const T* src = reinterpret_cast<const T*>(p.cache.v) + off + u->h * p.cache.head_stride;
+#pragma unroll 1
+          for (int c = col0; c < min(col0 + cols, p.D); ++c) {
+            const float e = Store<T>::widen(src[c]);
+            if (e - e == 0.0f) continue;
+            if (whole)
+              dst[c] = Store<T>::narrow(Store<T>::widen(dst[c]) + e);
+            else
+              part[(c & ~3) * p.unit_rows + (c & 3)] += e;
           }
         }
-        const float k = sum > 0.0f ? 1.0f / sum : sum;
-        const uint2 o = sum == 0.0f ? make_uint2(0u, 0u)
-                                    : make_uint2(pack2<T>(acc.x * k, acc.y * k), pack2<T>(acc.z * k, acc.w * k));
-        *reinterpret_cast<uint2*>(reinterpret_cast<T*>(p.out) + dst * p.D + 4 * d4) = o;
-        if (d4 == 0 && p.lse) p.lse[dst] = sum == 0.0f ? -INFINITY : 0.6931471805599453f * (top + log2f(sum));
       }
+      tc_fence_before();
+      if (pair) {
+        mbar_arrive(&sh.q_empty[0]);
+        mbar_arrive(&sh.q_empty[1]);
+      } else {
+        meet();  // both sums and the statistics have been read
+        mbar_arrive(&sh.q_empty[slab]);
+        slab ^= 1;
+      }
+      tc_fence_after();
+      ++number;
+      if (!whole && ok) {
+        // a unit in pieces
+        const int c0 = u->c0, c1 = u->c1;
+        __threadfence();
+        meet();
+        if (threadIdx.x == 0) {
+          bool last = false;
+          if (ok) {
+            last = atomicAdd(p.counters + c0, 1u) == static_cast<unsigned>(c1 - c0);
+            if (last) p.counters[c0] = 0u;  // zero again for the next call
+          }
+          sh.last = last;
+        }
+        meet();
+        if (ok && *const_cast<volatile int*>(&sh.last)) {
+          __threadfence();
+          const int quads = p.D / 4;
+#pragma unroll 1
+          for (int i = threadIdx.x; i < rows * quads; i += kSoftmaxThreads) {
+            const int d4 = i / rows, rr = i - d4 * rows;
+            const int tt = (row0 + rr) / p.group;
+            const long long to_row = (static_cast<long long>(u->b) * p.T + tt) * p.q_heads + u->h * p.group + row0 + rr -
+                                     tt * p.group;
+            const float* ml = p.part_ml + 2 * rr;
+            const float* o4 = p.part_o + static_cast<long long>(d4) * (p.unit_rows * 4) + rr * 4;
+            float top = -INFINITY, sum = 0.0f;
+            float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            // so many pieces in flight at once
+            constexpr int kBatch = 8;
+#pragma unroll 1
+            for (int c = c0; c <= c1; c += kBatch) {
+              float2 s[kBatch];
+              float4 v[kBatch];
+              float most = top;
+#pragma unroll
+              for (int k = 0; k < kBatch; ++k) {
+                s[k] = make_float2(-INFINITY, 0.0f);
+                v[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (c + k <= c1) {
+                  const long long piece = c + k == c0 ? 2 * (c + k) + 1 : 2 * (c + k);
+                  s[k] = __ldcg(reinterpret_cast<const float2*>(ml + 2 * piece * p.unit_rows));
+                  v[k] = __ldcg(reinterpret_cast<const float4*>(o4 + piece * kDim * p.unit_rows));
+                }
+              }
+#pragma unroll
+              for (int k = 0; k < kBatch; ++k) most = fmaxf(most, s[k].x);
+              const float ref = most == -INFINITY ? 0.0f : most;
+              const float fade = exp2_fast(top - ref);
+              sum *= fade, acc.x *= fade, acc.y *= fade, acc.z *= fade, acc.w *= fade;
+#pragma unroll
+              for (int k = 0; k < kBatch; ++k) {
+                const float e = exp2_fast(s[k].x - ref);
+                sum += e * s[k].y;
+                acc.x += e * v[k].x, acc.y += e * v[k].y, acc.z += e * v[k].z, acc.w += e * v[k].w;
+              }
+              top = most;
+            }
+            const float k = sum > 0.0f ? 1.0f / sum : sum;
+            const uint2 o = sum == 0.0f ? make_uint2(0u, 0u)
+                                        : make_uint2(pack2<T>(acc.x * k, acc.y * k), pack2<T>(acc.z * k, acc.w * k));
+            *reinterpret_cast<uint2*>(reinterpret_cast<T*>(p.out) + to_row * p.D + 4 * d4) = o;
+            if (d4 == 0 && p.lse) p.lse[to_row] = sum == 0.0f ? -INFINITY : 0.6931471805599453f * (top + log2f(sum));
+          }
+        }
+      }
+      feed.done(sh);
     }
   }
 
   tc_fence_before();
   __syncthreads();
+  if (sh.abort) {  // loads that nobody waited for: give them time to land before the CTA's memory is another's
+    const unsigned long long t0 = global_ns();
+    while (global_ns() - t0 < kLandNs) {
+    }
+  }
   if (warp == kMmaWarp) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
