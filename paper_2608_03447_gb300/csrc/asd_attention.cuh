@@ -42,6 +42,7 @@ struct AttnParams {
   float* part_o;       // [2 * grid][rows of a unit][D], in the kernel's own order
   int B, T, q_heads, heads, group, D;
   int unit_rows, row_tiles;
+  int group_rows;  // tensor cores: rows of a softmax group
   float scale;
   float scale_log2;
 };

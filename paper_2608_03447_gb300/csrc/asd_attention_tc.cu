@@ -15,12 +15,11 @@
 // and every tile of keys and values serves both.
 //
 // A CTA per SM: warps 0-3 and 4-7 are the softmax groups (a warp reads the TMEM
-// lanes of its quarter), warp 8 loads keys and values into a ring of stages in
-// the order in which they are used, warp 9 issues the MMAs, warp 10 loads
-// queries, warp 11 goes over the tiles that hold new tokens or a request's end
-// before their values are used. Loads are TMA boxes of as many slots as the page
-// size and the tile have as a common divisor (a page of 48 is three boxes of 16);
-// where that is less than the swizzle's eight rows, 16-byte copies.
+// lanes of its quarter), warp 8 loads keys and values into two rings of stages,
+// warp 9 issues the MMAs of the scores, warp 10 those of the products, warp 11
+// loads queries. Loads are TMA boxes of as many slots as the page size and the
+// tile have as a common divisor (a page of 48 is three boxes of 16); where that
+// is less than the swizzle's eight rows, 16-byte copies.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -30,6 +29,7 @@
 
 #include <atomic>
 #include <mutex>
+#include <type_traits>
 
 #include "asd.h"
 #include "asd_attention.cuh"
@@ -41,9 +41,9 @@ namespace {
 using namespace asd_detail;
 
 constexpr int kTile = 128;      // slots
-constexpr int kGroupRows = 128;
+constexpr int kGroupRows = 128;  // that a softmax group has threads for; a call may use fewer (AttnParams::group_rows)
 constexpr int kSoftmaxThreads = 256;
-constexpr int kLoadWarp = 8, kMmaWarp = 9, kQueryWarp = 10, kTailWarp = 11;
+constexpr int kLoadWarp = 8, kScoreWarp = 9, kProductWarp = 10, kQueryWarp = 11;
 constexpr int kThreads = 12 * 32;  // three warps a scheduler: 168 registers each
 constexpr int kTmemCols = 512;
 constexpr int kMaxStages = 12;
@@ -67,16 +67,15 @@ constexpr int kUnits = 8;
 constexpr int kUnitReaders = 11;  // warps
 
 struct TcShared {
-  unsigned long long full[kMaxStages];   // a stage's loads have landed
-  unsigned long long empty[kMaxStages];  // the MMAs have read it, and the tail warp has seen it
-  unsigned long long clean[kMaxStages];  // values of a tile with new tokens or a request's end: gone over
+  unsigned long long k_full[kMaxStages], k_empty[kMaxStages];  // loads have landed; the MMAs have read them
+  unsigned long long v_full[kMaxStages], v_empty[kMaxStages];
   unsigned long long unit_full[kUnits], unit_empty[kUnits];
   unsigned long long q_full[2], q_empty[2];  // a query slab is there; is no longer needed
   unsigned long long s_full[2];          // per group: its scores are in tensor memory
   unsigned long long p_ready[2];         // per group: its weights are, and the sum so far is rescaled
-  unsigned long long o_done[2];          // per group: the unit's last product is complete
+  unsigned long long pv_done[2];         // per group: their product is complete
   unsigned long long meet;               // the softmax warps
-  unsigned long long drain;
+  unsigned long long drain[2];
   uint32_t tmem_base;
   int abort;
   int last;         // this CTA arrived last at a unit in pieces
@@ -84,17 +83,23 @@ struct TcShared {
   TcUnit unit[kUnits];
   AttnDeal deal;
 };
+// Slabs of a CTA: two of queries, then a ring of keys and one of values, which
+// are held longer (their product waits for the softmax).
 constexpr int stages_for(int dim) {
   const size_t fit = (kSmemMax - 1024 - sizeof(TcShared) - 2 * slab_bytes(dim)) / slab_bytes(dim);
   return fit < static_cast<size_t>(kMaxStages) ? static_cast<int>(fit) : kMaxStages;
 }
+constexpr int key_stages(int dim) { return stages_for(dim) / 2; }
+constexpr int value_stages(int dim) { return stages_for(dim) - key_stages(dim); }
 constexpr size_t smem_for(int dim) {
   return 1024 + static_cast<size_t>(2 + stages_for(dim)) * slab_bytes(dim) + sizeof(TcShared);
 }
-// With 16-byte copies: fills in flight before the warp waits for the oldest. A
-// shared tile's values are released after the next tile's keys have landed, so at
-// least two stages of the ring are not in flight.
-constexpr int lag_for(int dim) { return stages_for(dim) - 2 < 8 ? stages_for(dim) - 2 : 8; }
+// With 16-byte copies: fills in flight before the warp waits for the oldest and
+// announces it. A fill must not wait for a stage whose own fill, or one that its
+// release depends on, has not been announced: keys 0 are fill 0 and their stage's
+// next keys fill 2 n - 1 (n: stages), and a shared tile's keys i + 1 are used after
+// values i, which were loaded after them.
+constexpr int lag_for(int dim) { return 2 * key_stages(dim) - 2 < 8 ? 2 * key_stages(dim) - 2 : 8; }
 static_assert(stages_for(128) == 5, "ring depth at the widest head");
 
 // ---------------------------------------------------------------- tcgen05
@@ -103,9 +108,9 @@ static_assert(stages_for(128) == 5, "ring depth at the widest head");
 // eight rows 1024 bytes apart, the next 64 elements of all 128 rows a half slab
 // on. Along the rows (keys, queries: K-major) the leading offset is not used; the
 // values are read across them (MN-major), where it steps over the half slab.
-__device__ __forceinline__ uint64_t tile_desc(uint32_t saddr, bool across) {
+__device__ __forceinline__ uint64_t tile_desc(uint32_t saddr16, bool across) {  // saddr16: in 16-byte words
   uint64_t d = 0;
-  d |= static_cast<uint64_t>((saddr >> 4) & 0x3FFFu);
+  d |= static_cast<uint64_t>(saddr16);  // shared memory ends below 2^18: the field's 14 bits hold it
   d |= static_cast<uint64_t>(across ? kHalfSlab >> 4 : 1) << 16;
   d |= static_cast<uint64_t>(1024 >> 4) << 32;
   d |= static_cast<uint64_t>(1) << 46;  // descriptor version
@@ -189,6 +194,16 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, u
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(d), "r"(at), "r"(head), "r"(page)
       : "memory");
 }
+// A TMA box of queries: 64 elements of a group's heads of consecutive tokens.
+__device__ __forceinline__ void load_queries(uint32_t dst, const CUtensorMap* map, unsigned long long* bar, int d,
+                                             int head, int token, int request) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}],"
+      " [%2];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(d), "r"(0), "r"(head), "r"(token),
+        "r"(request)
+      : "memory");
+}
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kLeft>
 __device__ __forceinline__ void copies_wait() {
@@ -202,22 +217,60 @@ __device__ __forceinline__ void fence_for_mma() { asm volatile("fence.proxy.asyn
 // gives up, the others do too, and every role leaves its loop; all waits between
 // roles are of this kind.
 __device__ __noinline__ bool warp_wait_on(unsigned long long* bar, uint32_t parity, int* abort, unsigned* error) {
-  const bool got = __all_sync(kFull, mbar_wait(bar, parity, abort));
-  if (!got) {
-    *const_cast<volatile int*>(abort) = 1;
-    atomicExch(error, static_cast<unsigned>(ASD_ERR_TIMEOUT));
+  const unsigned long long t0 = global_ns();
+  for (unsigned it = 1;; ++it) {
+    if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
+    if ((it & 255u) == 0 &&
+        __any_sync(kFull, *const_cast<volatile int*>(abort) != 0 || global_ns() - t0 > kWaitLimitNs))
+      break;
   }
-  return got;
+  *const_cast<volatile int*>(abort) = 1;
+  atomicExch(error, static_cast<unsigned>(ASD_ERR_TIMEOUT));
+  return false;
 }
 __device__ __forceinline__ bool warp_wait(unsigned long long* bar, uint32_t parity, TcShared& sh, const AttnParams& p) {
   if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
-  return warp_wait_on(bar, parity, &sh.abort, p.error);
+  return __all_sync(kFull, warp_wait_on(bar, parity, &sh.abort, p.error));
+}
+// Waits (bounded) for all MMAs of this warp.
+__device__ __forceinline__ void drain(unsigned long long* bar, bool elected) {
+  if (elected) {
+    mma_commit(bar);
+    const unsigned long long t0 = global_ns();
+    while (!mbar_try_wait(bar, 0) && global_ns() - t0 < kWaitLimitNs) {
+    }
+  }
+  __syncwarp();
+}
+// The same value in every lane, to the compiler too: MMAs and TMA loads take their operands from uniform registers.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_or_sync(kFull, x); }
+__device__ __forceinline__ int uniform(int x) { return static_cast<int>(__reduce_or_sync(kFull, static_cast<unsigned>(x))); }
+__device__ __forceinline__ bool elect_lane() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
 }
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// Two fp32 operations an instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(r)
+      : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)),
+        "l"(*reinterpret_cast<unsigned long long*>(&c)));
+  return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(r)
+      : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
+  return *reinterpret_cast<float2*>(&r);
 }
 template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
 template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
@@ -244,21 +297,6 @@ __device__ __forceinline__ uint32_t finite_pair(uint32_t w) {
 
 // ---------------------------------------------------------------- kernel
 
-// What the roles know of a tile, in one word.
-enum : int {
-  kValid = 1,
-  kFirst = 2,    // of the CTA's tiles of the unit
-  kEarly = 4,    // one of the first two
-  kLast = 8,     // the last
-  kLate = 16,    // one of the last two
-  kPair = 32,    // the unit has rows for both groups, which share its tiles
-  kTail = 64,    // new tokens, or the request's end
-};
-__device__ __forceinline__ int tile_flags(int j, int j0, int j1, int rows, int ctx) {
-  return kValid | (j == j0 ? kFirst : 0) | (j - j0 < 2 ? kEarly : 0) | (j == j1 - 1 ? kLast : 0) |
-         (j1 - j <= 2 ? kLate : 0) | (rows > kGroupRows ? kPair : 0) | (j * kTile + kTile > ctx ? kTail : 0);
-}
-
 // A warp's place in the ring of units.
 struct UnitFeed {
   int slot = 0;
@@ -278,44 +316,7 @@ struct UnitFeed {
   }
 };
 
-// The CTA's tiles one after the other, from the ring of units.
-struct TileFeed {
-  UnitFeed units;
-  int j = 0, j0 = 0, j1 = 0, rows = 0, ctx = 0, span = 0, number = -1;
-  // the next tile's flags, 0 after the last; lo: its first row of a new token, end: of nothing
-  __device__ __forceinline__ int take(TcShared& sh, const AttnParams& p, int& lo, int& end) {
-    if (j == j1) {
-      const TcUnit* u = units.wait(sh, p);
-      if (!u) return 0;
-      j = j0 = u->j0;
-      j1 = u->j1;
-      rows = u->rows;
-      ctx = u->ctx;
-      span = u->span;
-      ++number;
-      units.done(sh);
-    }
-    lo = max(0, ctx - j * kTile);
-    end = span - j * kTile;
-    const int flags = tile_flags(j, j0, j1, rows, ctx);
-    ++j;
-    return flags;
-  }
-};
-
-// Whether a unit's first scores wait for the last product of the unit before:
-// where one of the two is shared, its queries need the slab of the other.
-__device__ __forceinline__ bool starts_after(int next, int cur) { return (next & kFirst) && ((next | cur) & kPair); }
-
-// The order in which a CTA's tiles of keys and values go through the ring. The
-// MMAs run S(0), then S(i + 1) P V(i), where i counts a tile that the groups take
-// in turn once and a tile that they share twice; a tile is loaded when it is
-// first needed. Whether the values of `cur` go before the keys of `next`:
-__device__ __forceinline__ bool values_first(int next, int cur) {
-  return (cur & kPair) || !(next & kValid) || starts_after(next, cur);
-}
-
-// A position in the ring.
+// A position in a ring of stages.
 template <int kStages>
 struct Ring {
   int stage = 0;
@@ -332,8 +333,7 @@ struct Ring {
 template <typename T, int kDim, bool kTma>
 __global__ void __launch_bounds__(kThreads, 1)
     attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                        const __grid_constant__ AttnParams p, int box) {
-  constexpr int kStages = stages_for(kDim);
+                        const __grid_constant__ CUtensorMap map_q, const __grid_constant__ AttnParams p, int box) {
   constexpr int kSlab = slab_bytes(kDim);
   constexpr bool kBf16 = kExponent<T> == 0x7f807f80u;
   constexpr int kChunks = kDim / 8;          // 16-byte chunks of a row
@@ -342,17 +342,19 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t raw = smem_u32(tc_smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   unsigned char* gbase = tc_smem_raw + (base - raw);
-  const uint32_t sq = base, skv = base + 2 * kSlab;
-  TcShared& sh = *reinterpret_cast<TcShared*>(gbase + (2 + kStages) * kSlab);
+  constexpr int kKeys = key_stages(kDim), kValues = value_stages(kDim);
+  const uint32_t sq = base, sk = base + 2 * kSlab, sv = sk + kKeys * kSlab;
+  TcShared& sh = *reinterpret_cast<TcShared*>(gbase + (2 + kKeys + kValues) * kSlab);
 
   const int warp = __shfl_sync(kFull, static_cast<int>(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
   pdl_signal_dependents();
-  if (warp == kTailWarp) {  // a barrier or two a lane
-    for (int s = lane; s < kStages; s += 32) {
-      mbar_init(&sh.full[s], kTma ? 1 : 32);
-      mbar_init(&sh.empty[s], 1 + 32);
-      mbar_init(&sh.clean[s], 32);
+  if (warp == kQueryWarp) {  // a barrier or two a lane
+    if (lane < kMaxStages) {
+      mbar_init(&sh.k_full[lane], kTma ? 1 : 32);
+      mbar_init(&sh.k_empty[lane], 1);
+      mbar_init(&sh.v_full[lane], kTma ? 1 : 32);
+      mbar_init(&sh.v_empty[lane], 1);
     }
     if (lane < kUnits) {
       mbar_init(&sh.unit_full[lane], 1);
@@ -360,22 +362,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (lane >= 16 && lane < 18) {
       const int g = lane - 16;
-      mbar_init(&sh.q_full[g], 32);
-      mbar_init(&sh.q_empty[g], kSoftmaxThreads);
+      mbar_init(&sh.q_full[g], kTma ? 1 : 32);
+      mbar_init(&sh.q_empty[g], kSoftmaxThreads / 32);
       mbar_init(&sh.s_full[g], 1);
-      mbar_init(&sh.p_ready[g], 128);
-      mbar_init(&sh.o_done[g], 1);
+      mbar_init(&sh.p_ready[g], 4);
+      mbar_init(&sh.pv_done[g], 1);
+      mbar_init(&sh.drain[g], 1);
     }
     if (lane == 18) {
       mbar_init(&sh.meet, kSoftmaxThreads / 32);
-      mbar_init(&sh.drain, 1);
       sh.abort = 0;
     }
     if (lane < 4) sh.poison[lane] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_for_mma();
   }
-  if (warp == kMmaWarp) {
+  if (warp == kScoreWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)),
                  "r"(kTmemCols)
                  : "memory");
@@ -384,6 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (kTma && warp == kLoadWarp && lane == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_k)) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_v)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_q)) : "memory");
   }
   tc_fence_before();
   __syncthreads();
@@ -433,19 +436,17 @@ __global__ void __launch_bounds__(kThreads, 1)
       AttnWalk<kTile> w(p, sh.deal);
       int j = 0, j1 = 0, span = 0;  // the next tile of the unit that w is at
       bool fresh = true;            // that has not been published
-      Ring<kStages> ring;
-      // this lane's share of a tile: a TMA box, or four rows' worth of copies
+      Ring<kKeys> keys;
+      Ring<kValues> values;
       struct Share {
-        int flags, b, h;
-        int page, at;  // TMA: and the place in it; the page table is read two tiles ahead
-        bool has;
-        int slot0, rows;
+        int b, h;
+        int slot0, rows;  // of the tile: rows exist; 0: there is no tile
+        int page, at;     // TMA: where this lane's box begins; the page table is read two tiles ahead
       };
-      const int boxes = kTma ? kTile / box : 1;  // of a tile, each in kDim / 64 halves: one a lane
-      const int part = lane % boxes, half = lane / boxes;
-      const uint32_t dst0 = static_cast<uint32_t>(half * kHalfSlab + part * box * 128);
+      const bool elected = elect_lane();
+      const Share none = {0, 0, 0, 0, 0, 0};
       auto take = [&] {
-        Share x = {0, 0, 0, 0, 0, false, 0, 0};
+        Share x = none;
         if (ok && j == j1) {
           if (!fresh) w.next();
           fresh = false;
@@ -467,44 +468,56 @@ __global__ void __launch_bounds__(kThreads, 1)
           j = w.j0;
         }
         if (!ok) return x;
-        x.flags = tile_flags(j, w.j0, j1, w.rows(), w.r.ctx);
         x.b = w.b, x.h = w.h;
         x.slot0 = j * kTile;
         x.rows = min(kTile, span - x.slot0);
-        if (kTma) {
-          const int slot = x.slot0 + part * box;
-          if (slot < span && half < kDim / 64) {
-            const int n = p.cache.div.quot(slot);
-            x.page = __ldcg(p.cache.table + static_cast<long long>(x.b) * p.cache.table_width + n);
-            x.at = slot - n * p.cache.div.size;
-            x.has = true;
-          }
+        if (kTma && lane * box < x.rows) {
+          const int slot = x.slot0 + lane * box, n = p.cache.div.quot(slot);
+          x.page = __ldcg(p.cache.table + static_cast<long long>(x.b) * p.cache.table_width + n);
+          x.at = slot - n * p.cache.div.size;
         }
         ++j;
         return x;
       };
       constexpr int kLag = lag_for(kDim);
-      int issued = 0, arrived = 0, stage_out = 0;
-      auto arrive = [&] {  // copies: this thread's of the stage have landed
-        fence_for_mma();
-        mbar_arrive(&sh.full[stage_out]);
-        if (++stage_out == kStages) stage_out = 0;
-        ++arrived;
+      int issued = 0, arrived = 0;
+      // Tiles go K(0), then K(i + 1) V(i): the scores of a tile are computed while the one before is weighed.
+      auto bar_of = [&](int fill) {  // copies: the barrier of the fill of that number
+        const bool of_v = fill >= 2 && (fill & 1) == 0;
+        return of_v ? &sh.v_full[(fill / 2 - 1) % kValues] : &sh.k_full[((fill + 1) / 2) % kKeys];
       };
-      auto fill = [&](bool values, const Share& x) {
-        if (ok) ok = warp_wait(&sh.empty[ring.stage], ring.phase ^ 1u, sh, p);
+      auto arrive = [&] {  // copies: this thread's of the oldest fill have landed
+        fence_for_mma();
+        mbar_arrive(bar_of(arrived++));
+      };
+      auto fill = [&](bool of_v, const Share& x) {
+        const int stage = of_v ? values.stage : keys.stage;
+        const uint32_t phase = of_v ? values.phase : keys.phase;
+        if (ok) ok = warp_wait(of_v ? &sh.v_empty[stage] : &sh.k_empty[stage], phase ^ 1u, sh, p);
         if (!ok) return;
-        const uint32_t dst = skv + ring.stage * kSlab;
+        const uint32_t dst = (of_v ? sv : sk) + stage * kSlab;
+        if (of_v)
+          values.next();
+        else
+          keys.next();
         if constexpr (kTma) {
-          const uint32_t bytes = __popc(__ballot_sync(kFull, x.has)) * box * 128u;
-          if (lane == 0) mbar_expect_tx(&sh.full[ring.stage], bytes);
+          unsigned long long* bar = of_v ? &sh.v_full[stage] : &sh.k_full[stage];
+          const int n = uniform((x.rows + box - 1) / box), h = uniform(x.h);
+          if (elected) mbar_expect_tx(bar, static_cast<uint32_t>(n * box) * (kDim * 2));
           __syncwarp();
-          if (x.has) {
-            // a page out of range lies outside the tensor: the box is filled with zeros
-            load_box(dst + dst0, values ? &map_v : &map_k, &sh.full[ring.stage], half * 64, x.at, x.h, x.page);
-            if (!values && static_cast<unsigned>(x.page) >= static_cast<unsigned>(p.cache.pages) && p.status)
-              atomicOr(p.status + x.b, static_cast<int>(ASD_STATUS_PAGE));
+          // a page out of range lies outside the tensor: the box is filled with zeros
+          const CUtensorMap* map = of_v ? &map_v : &map_k;
+#pragma unroll 4
+          for (int i = 0; i < n; ++i) {
+            const int page = __shfl_sync(kFull, x.page, i), at = __shfl_sync(kFull, x.at, i);
+            if (elected) {
+#pragma unroll
+              for (int half = 0; half < kDim / 64; ++half)
+                load_box(dst + half * kHalfSlab + i * box * 128, map, bar, half * 64, at, h, page);
+            }
           }
+          if (!of_v && lane < n && static_cast<unsigned>(x.page) >= static_cast<unsigned>(p.cache.pages) && p.status)
+            atomicOr(p.status + x.b, static_cast<int>(ASD_STATUS_PAGE));
           __syncwarp();
         } else {
 #pragma unroll 1
@@ -512,211 +525,206 @@ __global__ void __launch_bounds__(kThreads, 1)
             long long off = -1;
             if (q + lane < x.rows) {
               off = slot_offset(p.cache, x.b, x.slot0 + q + lane);
-              if (off < 0 && !values && p.status) atomicOr(p.status + x.b, static_cast<int>(ASD_STATUS_PAGE));
+              if (off < 0 && !of_v && p.status) atomicOr(p.status + x.b, static_cast<int>(ASD_STATUS_PAGE));
               if (off >= 0) off += x.h * p.cache.head_stride;
             }
-            copy_rows(dst, q, values ? p.cache.v : p.cache.k, off, x.rows - q);
+            copy_rows(dst, q, of_v ? p.cache.v : p.cache.k, off, x.rows - q);
           }
           copies_commit();
-          ++issued;
-          if (issued - arrived > kLag) {
+          if (++issued - arrived > kLag) {
             copies_wait<kLag>();
             arrive();
           }
         }
-        ring.next();
       };
-      Share cur = {0, 0, 0, 0, 0, false, 0, 0};  // its keys are in the ring
-      Share next = take();
-      while (ok && (cur.flags | next.flags)) {
-        const Share after = next.flags ? take() : next;
-        const bool before = cur.flags && values_first(next.flags, cur.flags);
+      Share cur = none, next = take();  // cur: its keys have been loaded
+      while (ok && (cur.rows | next.rows)) {
+        const Share after = next.rows ? take() : next;
 #pragma unroll 1
         for (int i = 0; i < 2; ++i) {
-          const bool values = (i == 0) == before;
-          if (values ? cur.flags : next.flags) fill(values, values ? cur : next);
+          const Share& x = i ? cur : next;
+          if (x.rows) fill(i, x);
         }
         cur = next;
         next = after;
       }
       if (!kTma) {
+        // the last fill is a tile's values with no keys between them and the values before
         copies_wait<0>();
-        while (arrived < issued) arrive();
+        while (arrived < issued - 1) arrive();
+        if (issued > 0) {
+          fence_for_mma();
+          mbar_arrive(&sh.v_full[(issued / 2 - 1) % kValues]);
+        }
       }
     }
   } else if (warp == kQueryWarp) {
     // ---------------- queries: a unit's slab, or both slabs of a unit that the groups share
     UnitFeed feed;
+    const bool elected = elect_lane();
     bool ok = true;
     uint32_t uses = 0;  // a bit a slab: whether an odd number of fills
     int slab = 0;
     while (const TcUnit* u = feed.wait(sh, p)) {
       const int b = u->b, h = u->h, row0 = u->row0, rows = u->rows;
       feed.done(sh);
-      const bool pair = rows > kGroupRows;
-      for (int tile = 0; ok && tile * kGroupRows < rows; ++tile) {
-        const int to = pair ? tile : slab;
+      const bool pair = rows > p.group_rows;
+#pragma unroll 1
+      for (int tile = 0; ok && tile * p.group_rows < rows; ++tile) {
+        const int to = pair ? tile : slab, first = row0 + tile * p.group_rows;
         ok = warp_wait(&sh.q_empty[to], ((uses >> to) & 1u) ^ 1u, sh, p);
         uses ^= 1u << to;
-#pragma unroll 1
-        for (int r0 = 0; ok && r0 < kGroupRows && tile * kGroupRows + r0 < rows; r0 += 32) {
-          const int r = tile * kGroupRows + r0 + lane;
-          long long off = -1;
-          if (r < rows) {
-            const int row = row0 + r, t = row / p.group;
-            off = b * p.q_batch + t * p.q_token + (h * p.group + (row - t * p.group)) * p.q_head;
+        if (!ok) break;
+        if constexpr (kTma) {
+          // whole tokens: [element][head of the group][key/value head][token][request]
+          if (elected) {
+            mbar_expect_tx(&sh.q_full[to], static_cast<uint32_t>(p.group_rows) * (kDim * 2));
+#pragma unroll
+            for (int half = 0; half < kDim / 64; ++half)
+              load_queries(sq + to * kSlab + half * kHalfSlab, &map_q, &sh.q_full[to], half * 64, h, first / p.group, b);
           }
-          copy_rows(sq + to * kSlab, r0, p.q, off, 32);
+          __syncwarp();
+        } else {
+          const int end = min(p.group_rows, rows - tile * p.group_rows);
+#pragma unroll 1
+          for (int r0 = 0; r0 < end; r0 += 32) {
+            const int row = first + r0 + lane, t = row / p.group;
+            const long long off =
+                r0 + lane < end ? b * p.q_batch + t * p.q_token + (h * p.group + (row - t * p.group)) * p.q_head : -1;
+            copy_rows(sq + to * kSlab, r0, p.q, off, 32);
+          }
+          copies_commit();
+          copies_wait<0>();
+          fence_for_mma();
+          mbar_arrive(&sh.q_full[to]);
         }
-        copies_commit();
-        copies_wait<0>();
-        fence_for_mma();
-        mbar_arrive(&sh.q_full[to]);
       }
       if (!pair) slab ^= 1;
     }
-  } else if (warp == kTailWarp) {
-    // ---------------- tiles with new tokens or a request's end
-    // Rows past the end become zeros (what lies there may be anything, and 0 times NaN is NaN). Of a new token some
-    // rows may see nothing, so its values' NaN and infinities become zeros too and the unit is marked: its rows look
-    // at the end for those that they do see.
-    // This warp follows every fill, one by one, and a stage is filled again only when it has: a wait by parity must
-    // never be a round of the ring away from the barrier.
-    Ring<kStages> ring;
-    TileFeed feed;
+  } else if (warp == kScoreWarp) {
+    // ---------------- S = Q K^T
+    constexpr uint32_t kDesc = instr_desc(kBf16, kTile, false);
+    const bool elected = elect_lane();
+    UnitFeed feed;
+    Ring<kKeys> ring;
     bool ok = true;
-    int cur = 0, cur_lo = 0, cur_end = 0, cur_number = 0;
-    int next_lo = 0, next_end = 0;
-    int next = feed.take(sh, p, next_lo, next_end);
-    while (ok && (cur | next)) {
-      const int next_number = feed.number;
-      const bool before = cur && values_first(next, cur);
+    uint32_t q_phase = 0, pv_phase = 3;  // a bit a slab; a group
+    int turn = 0, slab = 0;              // the group whose turn it is; the slab of the unit that the groups take in turn
+    while (ok) {
+      const TcUnit* u = feed.wait(sh, p);
+      if (!u) break;
+      const bool pair = uniform(u->rows) > p.group_rows;
+      int left = uniform(u->j1 - u->j0);
+      feed.done(sh);
 #pragma unroll 1
-      for (int i = 0; ok && i < 2; ++i) {
-        const bool values = (i == 0) == before;
-        if (!(values ? cur : next)) continue;
-        ok = warp_wait(&sh.full[ring.stage], ring.phase, sh, p);
-        if (ok && values && (cur & kTail)) {
+      for (int s = pair ? 0 : slab; s <= (pair ? 1 : slab); ++s) {
+        if (ok) ok = warp_wait(&sh.q_full[s], (q_phase >> s) & 1u, sh, p);
+        q_phase ^= 1u << s;
+      }
+#pragma unroll 1
+      for (bool second = false; ok && left > 0;) {
+        // the group's scores and weights so far lie where these go
+        ok = warp_wait(&sh.pv_done[turn], (pv_phase >> turn) & 1u, sh, p);
+        pv_phase ^= 1u << turn;
+        if (ok && !second) ok = warp_wait(&sh.k_full[ring.stage], ring.phase, sh, p);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t a = uniform((sq + (pair ? turn : slab) * kSlab) >> 4);
+        const uint32_t b = uniform((sk + ring.stage * kSlab) >> 4);
+        const uint32_t d = uniform(tmem_s(turn));
+        const bool ends = !pair || second;  // no group needs the tile's keys any more
+        if (elected) {
+#pragma unroll
+          for (int k = 0; k < kDim / 16; ++k) {
+            const uint32_t at = ((k >> 2) * kHalfSlab + (k & 3) * 32) >> 4;
+            mma_smem(d, tile_desc(a + at, false), tile_desc(b + at, false), kDesc, k > 0 ? 1u : 0u);
+          }
+          mma_commit(&sh.s_full[turn]);
+          if (ends) mma_commit(&sh.k_empty[ring.stage]);
+        }
+        __syncwarp();
+        turn ^= 1;
+        second = !ends;
+        if (ends) {
+          ring.next();
+          --left;
+        }
+      }
+      if (!pair) slab ^= 1;
+    }
+    drain(&sh.drain[0], elected);
+  } else if (warp == kProductWarp) {
+    // ---------------- O += P V
+    constexpr uint32_t kDesc = instr_desc(kBf16, kDim, true);
+    const bool elected = elect_lane();
+    UnitFeed feed;
+    Ring<kValues> ring;
+    bool ok = true;
+    uint32_t p_phase = 0;  // a bit a group
+    int turn = 0;
+    for (int number = 0; ok; ++number) {
+      const TcUnit* u = feed.wait(sh, p);
+      if (!u) break;
+      const bool pair = uniform(u->rows) > p.group_rows;
+      const int j0 = uniform(u->j0), j1 = uniform(u->j1), span = uniform(u->span), ctx = uniform(u->ctx);
+      feed.done(sh);
+#pragma unroll 1
+      for (int j = j0; ok && j < j1; ++j) {
+        ok = warp_wait(&sh.v_full[ring.stage], ring.phase, sh, p);
+        if (!ok) break;
+        const int end = min(kTile, span - j * kTile);  // rows of the tile that exist
+        if ((j + 1) * kTile > ctx) {
+          // New tokens, or the request's end. Rows past the end become zeros (what lies there may be anything, and 0
+          // times NaN is NaN); of a new token some rows may see nothing, so its values' NaN and infinities become
+          // zeros too and the unit is marked: its rows look at the end for those that they do see.
+          unsigned char* tile = gbase + (sv - base) + ring.stage * kSlab;
+          // of the rows past the end the product reads only the rest of the last 16
+          for (int r = end + sub; r < min(kTile, (end + 15) & ~15); r += kRowsAtOnce)
+            *reinterpret_cast<uint4*>(tile + place(r)) = make_uint4(0u, 0u, 0u, 0u);
           bool found = false;
-#pragma unroll 1
-          for (int r = cur_lo + sub; r < kTile; r += kRowsAtOnce) {
-            uint4* at = reinterpret_cast<uint4*>(gbase + (2 + ring.stage) * kSlab + place(r));
-            const uint4 was = r < cur_end ? *at : make_uint4(~0u, ~0u, ~0u, ~0u);
-            uint4 now = make_uint4(0u, 0u, 0u, 0u);
-            if (r < cur_end)
-              now = {finite_pair<T>(was.x), finite_pair<T>(was.y), finite_pair<T>(was.z), finite_pair<T>(was.w)};
+#pragma unroll 4
+          for (int r = max(0, ctx - j * kTile) + sub; r < end; r += kRowsAtOnce) {
+            uint4* at = reinterpret_cast<uint4*>(tile + place(r));
+            const uint4 was = *at;
+            const uint4 now = {finite_pair<T>(was.x), finite_pair<T>(was.y), finite_pair<T>(was.z),
+                               finite_pair<T>(was.w)};
             if (now.x != was.x || now.y != was.y || now.z != was.z || now.w != was.w) {
               *at = now;
-              found |= r < cur_end;
+              found = true;
             }
           }
-          if (found) sh.poison[cur_number & 3] = cur_number + 1;
+          if (found) sh.poison[number & 3] = number + 1;
           fence_for_mma();
           __syncwarp();
-          mbar_arrive(&sh.clean[ring.stage]);
         }
-        mbar_arrive(&sh.empty[ring.stage]);
-        ring.next();
-      }
-      cur = next, cur_lo = next_lo, cur_end = next_end, cur_number = next_number;
-      if (next) next = feed.take(sh, p, next_lo, next_end);
-    }
-  } else if (warp == kMmaWarp) {
-    // ---------------- MMAs
-    constexpr uint32_t kDescS = instr_desc(kBf16, kTile, false);
-    constexpr uint32_t kDescO = instr_desc(kBf16, kDim, true);
-    bool elected;
-    {
-      uint32_t one;
-      asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
-      elected = one != 0;
-    }
-    bool ok = true;
-    Ring<kStages> ring;
-    TileFeed feed;
-    int k_stage = 0, v_stage = 0;       // of the tiles whose scores and whose product are being issued
-    uint32_t p_phase = 0, q_phase = 0, clean_phase = 0;  // a bit a group, slab, stage
-    int slab = 1;                       // of the unit that the groups take in turn
-
-    // the scores of one group's rows against a tile; `second`: the other group has done so with the same tile
-    auto scores = [&](int tile, bool second, int g) {
-      const bool pair = tile & kPair;
-      if ((tile & kFirst) && !second) {
-        if (!pair) slab ^= 1;
 #pragma unroll 1
-        for (int s = pair ? 0 : slab; s <= (pair ? 1 : slab); ++s) {
-          if (ok) ok = warp_wait(&sh.q_full[s], (q_phase >> s) & 1u, sh, p);
-          q_phase ^= 1u << s;
+        for (bool second = false;;) {
+          ok = warp_wait(&sh.p_ready[turn], (p_phase >> turn) & 1u, sh, p);
+          p_phase ^= 1u << turn;
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t a = uniform(tmem_s(turn) + kTile / 2), d = uniform(tmem_o(turn));
+          const uint32_t b = uniform((sv + ring.stage * kSlab) >> 4);
+          const uint32_t fresh = j - j0 < (pair ? 1 : 2);  // the group's first tile of the unit
+          const int steps = uniform((end + 15) >> 4);
+          const bool ends = !pair || second;
+          if (elected) {
+#pragma unroll
+            for (int k = 0; k < kTile / 16; ++k)
+              if (k < steps)
+                mma_tmem(d, a + 8 * k, tile_desc(b + ((k * 16 * 128) >> 4), true), kDesc, k > 0 ? 1u : 1u - fresh);
+            mma_commit(&sh.pv_done[turn]);
+            if (ends) mma_commit(&sh.v_empty[ring.stage]);
+          }
+          __syncwarp();
+          turn ^= 1;
+          if (ends) break;
+          second = true;
         }
-      }
-      if (!second) {
-        k_stage = ring.stage;
-        if (ok) ok = warp_wait(&sh.full[k_stage], ring.phase, sh, p);
         ring.next();
       }
-      tc_fence_after();
-      if (ok && elected) {
-        const uint64_t a = tile_desc(sq + (pair ? g : slab) * kSlab, false);
-        const uint64_t b = tile_desc(skv + k_stage * kSlab, false);
-#pragma unroll
-        for (int k = 0; k < kDim / 16; ++k) {
-          const uint32_t at = ((k >> 2) * kHalfSlab + (k & 3) * 32) >> 4;
-          mma_smem(tmem_s(g), a + at, b + at, kDescS, k > 0 ? 1u : 0u);
-        }
-        mma_commit(&sh.s_full[g]);
-        if (!pair || second) mma_commit(&sh.empty[k_stage]);
-      }
-    };
-    auto product = [&](int tile, bool second, int g) {
-      const bool pair = tile & kPair;
-      if (!second) {
-        v_stage = ring.stage;
-        if (ok) ok = warp_wait(&sh.full[v_stage], ring.phase, sh, p);
-        ring.next();
-        if (tile & kTail) {
-          if (ok) ok = warp_wait(&sh.clean[v_stage], (clean_phase >> v_stage) & 1u, sh, p);
-          clean_phase ^= 1u << v_stage;
-        }
-      }
-      if (ok) ok = warp_wait(&sh.p_ready[g], (p_phase >> g) & 1u, sh, p);
-      p_phase ^= 1u << g;
-      tc_fence_after();
-      if (ok && elected) {
-        const bool first = tile & (pair ? kFirst : kEarly);  // of this group: the unit's first may be the other's
-        const uint64_t b = tile_desc(skv + v_stage * kSlab, true);
-#pragma unroll
-        for (int k = 0; k < kTile / 16; ++k)
-          mma_tmem(tmem_o(g), tmem_s(g) + kTile / 2 + 8 * k, b + ((k * 16 * 128) >> 4), kDescO,
-                   !first || k > 0 ? 1u : 0u);
-        if (tile & (pair ? kLast : kLate)) mma_commit(&sh.o_done[g]);
-        if (!pair || second) mma_commit(&sh.empty[v_stage]);
-      }
-    };
-    int a = 0, b_lo, b_end;  // a: the tile whose product is next
-    int b = feed.take(sh, p, b_lo, b_end);
-    bool a_second = false, b_second = false;
-    int g = 1;               // a's group
-    while (ok && (a | b)) {
-      const bool later = a && !b_second && starts_after(b, a);
-#pragma unroll 1
-      for (int i = 0; i < 2; ++i) {
-        const bool of_a = (i == 0) == later;
-        if (of_a && a) product(a, a_second, g);
-        if (!of_a && b) scores(b, b_second, g ^ 1);
-      }
-      a = b;
-      a_second = b_second;
-      g ^= 1;
-      b_second = (a & kPair) && !a_second;
-      if (a && !b_second) b = feed.take(sh, p, b_lo, b_end);
     }
-    if (elected) {
-      mma_commit(&sh.drain);
-      const unsigned long long t0 = global_ns();
-      while (!mbar_try_wait(&sh.drain, 0) && global_ns() - t0 < kWaitLimitNs) {
-      }
-    }
-    __syncwarp();
+    drain(&sh.drain[1], elected);
   } else {
     // ---------------- softmax: thread `row` of group g
     const int g = warp >> 2;
@@ -724,7 +732,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t ts = tmem_s(g) + lanes, tw = ts + kTile / 2, to = tmem_o(g) + lanes;  // scores, weights, sum
     bool ok = true;
-    uint32_t s_phase = 0, o_phase = 0, meet_phase = 0;
+    uint32_t s_phase = 0, meet_phase = 0;
     int turn = 0, number = 0, slab = 0;
     auto meet = [&] {  // the two groups
       __syncwarp();
@@ -739,10 +747,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!u) break;
       const AttnRequest req = {u->ctx, u->n};
       const int rows = u->rows, row0 = u->row0, j0 = u->j0, j1 = u->j1;
-      const bool pair = rows > kGroupRows;               // each group has rows of its own; else both have the same
-      const int r = (pair ? g * kGroupRows : 0) + row;   // of the unit
-      const bool lives = r < rows;
-      const bool warp_lives = r - lane < rows;           // the same for the warp
+      const bool pair = rows > p.group_rows;               // each group has rows of its own; else both have the same
+      const int r = (pair ? g * p.group_rows : 0) + row;   // of the unit
+      const bool lives = row < p.group_rows && r < rows;
+      const bool warp_lives = row - lane < p.group_rows && r - lane < rows;  // the same for the warp
       const int t = (row0 + min(r, rows - 1)) / p.group;
       float m = -INFINITY, l = 0.0f;
       bool had = false;
@@ -768,7 +776,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           float ref = 0.0f;
           // four chains each: one warp a scheduler has little else to cover an operation's latency with
           float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          float2 sums[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
           // The maximum over the first and the second half of the slots; then the weights of the second, which is
           // still in registers, and of the first. The weights lie over the second half's scores. A loop, not four
           // stretches of code: see TcUnit.
@@ -802,7 +810,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 l *= fade;
                 m = m_new;
                 if (had) {
-                  // every product of this group so far has completed: it came before these scores
+                  // every product of this group so far is complete: these scores were computed after it
 #pragma unroll 1
                   for (int c = 0; c < kDim; c += 16) {
                     float o[16];
@@ -822,21 +830,22 @@ __global__ void __launch_bounds__(kThreads, 1)
               uint32_t w2[16];
 #pragma unroll
               for (int i = 0; i < 32; i += 2) {
-                const float e0 = exp2_fast(fmaf(x[c][i], p.scale_log2, -ref));
-                const float e1 = exp2_fast(fmaf(x[c][i + 1], p.scale_log2, -ref));
-                sums[i & 2] += e0;
-                sums[(i & 2) + 1] += e1;
-                w2[i >> 1] = pack2<T>(e0, e1);
+                float2 e = fma2(make_float2(x[c][i], x[c][i + 1]), make_float2(p.scale_log2, p.scale_log2),
+                                make_float2(-ref, -ref));
+                e = make_float2(exp2_fast(e.x), exp2_fast(e.y));
+                sums[(i >> 1) & 1] = add2(sums[(i >> 1) & 1], e);
+                w2[i >> 1] = pack2<T>(e.x, e.y);
               }
               tmem_st16(tw + 32 * half + 16 * c, w2);
             }
           }
-          l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+          l += (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y);
           tmem_st_wait();
         }
         had = true;
         tc_fence_before();
-        mbar_arrive(&sh.p_ready[g]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.p_ready[g]);
       }
 
       // the unit's rows, or this CTA's piece of them
@@ -844,8 +853,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       float f_self = 1.0f, f_other = 1.0f;  // what the groups' sums are multiplied with
       bool other_had = false;
       if (had) {
-        if (ok) ok = warp_wait(&sh.o_done[g], o_phase, sh, p);
-        o_phase ^= 1u;
+        if (ok) ok = warp_wait(&sh.pv_done[g], s_phase ^ 1u, sh, p);  // of the group's last tile
         tc_fence_after();
       }
       if (!pair) {
@@ -887,18 +895,17 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] = 0.0f;
         if (ok && warp_lives) {
-          float x[32];
+          float x[32], y[32];
+          tmem_ld32(to + col, x);
+          tmem_ld32(tmem_o(g ^ 1) + lanes + col, y);
+          tmem_ld_wait();
           if (had) {
-            tmem_ld32(to + col, x);
-            tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = f_self * x[i];
           }
           if (other_had) {
-            tmem_ld32(tmem_o(g ^ 1) + lanes + col, x);
-            tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = fmaf(f_other, x[i], v[i]);
+            for (int i = 0; i < 32; ++i) v[i] = fmaf(f_other, y[i], v[i]);
           }
         }
         if (mine && whole) {
@@ -947,12 +954,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       tc_fence_before();
+      __syncwarp();
       if (pair) {
-        mbar_arrive(&sh.q_empty[0]);
-        mbar_arrive(&sh.q_empty[1]);
+        if (lane < 2) mbar_arrive(&sh.q_empty[lane]);
       } else {
         meet();  // both sums and the statistics have been read
-        mbar_arrive(&sh.q_empty[slab]);
+        if (lane == 0) mbar_arrive(&sh.q_empty[slab]);
         slab ^= 1;
       }
       tc_fence_after();
@@ -973,53 +980,78 @@ __global__ void __launch_bounds__(kThreads, 1)
         meet();
         if (ok && *const_cast<volatile int*>(&sh.last)) {
           __threadfence();
-          const int quads = p.D / 4;
+          // four columns of a row an item: many pieces of one at once, or some of several
+          auto merge = [&](auto many_items, auto many_pieces) {
+            constexpr int kItems = decltype(many_items)::value, kPieces = decltype(many_pieces)::value;
+            const int items = rows * (p.D / 4);
 #pragma unroll 1
-          for (int i = threadIdx.x; i < rows * quads; i += kSoftmaxThreads) {
-            const int d4 = i / rows, rr = i - d4 * rows;
-            const int tt = (row0 + rr) / p.group;
-            const long long to_row = (static_cast<long long>(u->b) * p.T + tt) * p.q_heads + u->h * p.group + row0 + rr -
-                                     tt * p.group;
-            const float* ml = p.part_ml + 2 * rr;
-            const float* o4 = p.part_o + static_cast<long long>(d4) * (p.unit_rows * 4) + rr * 4;
-            float top = -INFINITY, sum = 0.0f;
-            float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            // so many pieces in flight at once
-            constexpr int kBatch = 8;
-#pragma unroll 1
-            for (int c = c0; c <= c1; c += kBatch) {
-              float2 s[kBatch];
-              float4 v[kBatch];
-              float most = top;
+            for (int i0 = threadIdx.x; i0 < items; i0 += kItems * kSoftmaxThreads) {
+              float top[kItems], sum[kItems];
+              float4 acc[kItems];
 #pragma unroll
-              for (int k = 0; k < kBatch; ++k) {
-                s[k] = make_float2(-INFINITY, 0.0f);
-                v[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                if (c + k <= c1) {
-                  const long long piece = c + k == c0 ? 2 * (c + k) + 1 : 2 * (c + k);
-                  s[k] = __ldcg(reinterpret_cast<const float2*>(ml + 2 * piece * p.unit_rows));
-                  v[k] = __ldcg(reinterpret_cast<const float4*>(o4 + piece * kDim * p.unit_rows));
+              for (int i = 0; i < kItems; ++i) {
+                top[i] = -INFINITY;
+                sum[i] = 0.0f;
+                acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+              }
+#pragma unroll 1
+              for (int c = c0; c <= c1; c += kPieces) {
+                float2 s[kItems][kPieces];
+                float4 v[kItems][kPieces];
+#pragma unroll
+                for (int i = 0; i < kItems; ++i) {
+                  const int item = i0 + i * kSoftmaxThreads, d4 = item / rows, rr = item - d4 * rows;
+#pragma unroll
+                  for (int k = 0; k < kPieces; ++k) {
+                    s[i][k] = make_float2(-INFINITY, 0.0f);
+                    v[i][k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    if (item < items && c + k <= c1) {
+                      const long long piece = c + k == c0 ? 2 * (c + k) + 1 : 2 * (c + k);
+                      s[i][k] = __ldcg(reinterpret_cast<const float2*>(p.part_ml + 2 * (piece * p.unit_rows + rr)));
+                      v[i][k] = __ldcg(reinterpret_cast<const float4*>(p.part_o + piece * kDim * p.unit_rows +
+                                                                       d4 * (p.unit_rows * 4) + rr * 4));
+                    }
+                  }
+                }
+#pragma unroll
+                for (int i = 0; i < kItems; ++i) {
+                  float most = top[i];
+#pragma unroll
+                  for (int k = 0; k < kPieces; ++k) most = fmaxf(most, s[i][k].x);
+                  const float ref = most == -INFINITY ? 0.0f : most;
+                  const float fade = exp2_fast(top[i] - ref);
+                  sum[i] *= fade, acc[i].x *= fade, acc[i].y *= fade, acc[i].z *= fade, acc[i].w *= fade;
+#pragma unroll
+                  for (int k = 0; k < kPieces; ++k) {
+                    const float e = exp2_fast(s[i][k].x - ref);
+                    sum[i] += e * s[i][k].y;
+                    acc[i].x += e * v[i][k].x, acc[i].y += e * v[i][k].y;
+                    acc[i].z += e * v[i][k].z, acc[i].w += e * v[i][k].w;
+                  }
+                  top[i] = most;
                 }
               }
 #pragma unroll
-              for (int k = 0; k < kBatch; ++k) most = fmaxf(most, s[k].x);
-              const float ref = most == -INFINITY ? 0.0f : most;
-              const float fade = exp2_fast(top - ref);
-              sum *= fade, acc.x *= fade, acc.y *= fade, acc.z *= fade, acc.w *= fade;
-#pragma unroll
-              for (int k = 0; k < kBatch; ++k) {
-                const float e = exp2_fast(s[k].x - ref);
-                sum += e * s[k].y;
-                acc.x += e * v[k].x, acc.y += e * v[k].y, acc.z += e * v[k].z, acc.w += e * v[k].w;
+              for (int i = 0; i < kItems; ++i) {
+                const int item = i0 + i * kSoftmaxThreads, d4 = item / rows, rr = item - d4 * rows;
+                if (item >= items) break;
+                const int tt = (row0 + rr) / p.group;
+                const long long to_row = (static_cast<long long>(u->b) * p.T + tt) * p.q_heads + u->h * p.group + row0 +
+                                         rr - tt * p.group;
+                const float k = sum[i] > 0.0f ? 1.0f / sum[i] : sum[i];
+                const uint2 o = sum[i] == 0.0f ? make_uint2(0u, 0u)
+                                               : make_uint2(pack2<T>(acc[i].x * k, acc[i].y * k),
+                                                            pack2<T>(acc[i].z * k, acc[i].w * k));
+                *reinterpret_cast<uint2*>(reinterpret_cast<T*>(p.out) + to_row * p.D + 4 * d4) = o;
+                if (d4 == 0 && p.lse)
+                  p.lse[to_row] = sum[i] == 0.0f ? -INFINITY : 0.6931471805599453f * (top[i] + log2f(sum[i]));
               }
-              top = most;
             }
-            const float k = sum > 0.0f ? 1.0f / sum : sum;
-            const uint2 o = sum == 0.0f ? make_uint2(0u, 0u)
-                                        : make_uint2(pack2<T>(acc.x * k, acc.y * k), pack2<T>(acc.z * k, acc.w * k));
-            *reinterpret_cast<uint2*>(reinterpret_cast<T*>(p.out) + to_row * p.D + 4 * d4) = o;
-            if (d4 == 0 && p.lse) p.lse[to_row] = sum == 0.0f ? -INFINITY : 0.6931471805599453f * (top + log2f(sum));
-          }
+          };
+          if (c1 - c0 < 4)
+            merge(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
+          else
+            merge(std::integral_constant<int, 1>{}, std::integral_constant<int, 16>{});
         }
       }
       feed.done(sh);
@@ -1033,7 +1065,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     while (global_ns() - t0 < kLandNs) {
     }
   }
-  if (warp == kMmaWarp) {
+  if (warp == kScoreWarp) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
   }
@@ -1081,9 +1113,32 @@ bool make_map(CUtensorMap* map, bool bf16, const void* ptr, const asd_kv_cache* 
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Queries as [request][token][key/value head][head of its group][element], boxes
+// of one key/value head's heads of as many tokens as a softmax group has rows
+// for; tokens past the last read as zero.
+bool make_query_map(CUtensorMap* map, bool bf16, const AttnParams& p) {
+  EncodeTiledFn fn = encode_tiled();
+  if (!fn) return false;
+  auto stride = [&](long long elements, int size) -> cuuint64_t {  // of a dimension of one entry: any
+    return size == 1 ? 256u * 2u : static_cast<cuuint64_t>(elements) * 2;
+  };
+  const cuuint64_t dims[5] = {static_cast<cuuint64_t>(p.D), static_cast<cuuint64_t>(p.group),
+                              static_cast<cuuint64_t>(p.heads), static_cast<cuuint64_t>(p.T),
+                              static_cast<cuuint64_t>(p.B)};
+  const cuuint64_t strides[4] = {stride(p.q_head, p.group), stride(p.q_head * p.group, p.heads), stride(p.q_token, p.T),
+                                 stride(p.q_batch, p.B)};
+  for (const cuuint64_t s : strides)
+    if (s == 0) return false;  // one row for several: copied
+  const cuuint32_t boxes[5] = {64, static_cast<cuuint32_t>(p.group), 1, static_cast<cuuint32_t>(p.group_rows / p.group), 1};
+  const cuuint32_t steps[5] = {1, 1, 1, 1, 1};
+  return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5,
+            const_cast<char*>(p.q), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename T, int kDim, bool kTma>
-int launch(const CUtensorMap& map_k, const CUtensorMap& map_v, AttnParams p, int box, char* workspace,
-           cudaStream_t stream) {
+int launch(const CUtensorMap (&maps)[3], AttnParams p, int box, char* workspace, cudaStream_t stream) {
   auto kernel = attention_tc_kernel<T, kDim, kTma>;
   static std::atomic<int> grid_of[kMaxDevices];
   int dev = 0;
@@ -1109,12 +1164,15 @@ int launch(const CUtensorMap& map_k, const CUtensorMap& map_v, AttnParams p, int
   cudaLaunchAttribute attr;
   cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(kThreads), stream, &attr);
   cfg.dynamicSmemBytes = smem_for(kDim);
-  if (cudaLaunchKernelEx(&cfg, kernel, map_k, map_v, p, box) != cudaSuccess) return ASD_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, kernel, maps[0], maps[1], maps[2], p, box) != cudaSuccess) return ASD_ERR_CUDA;
   return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;
 }
 
+// Rows of a softmax group: whole tokens, so that a TMA box holds them (a group of
+// more than 128 heads has its rows copied).
+int group_rows(int group) { return group <= kGroupRows ? kGroupRows / group * group : kGroupRows; }
 // Rows of a unit: what one softmax group holds, or both where there are more.
-int unit_rows(long long rows) { return rows > kGroupRows ? 2 * kGroupRows : kGroupRows; }
+int unit_rows(long long rows, int group) { return rows > group_rows(group) ? 2 * group_rows(group) : group_rows(group); }
 
 // Slots of a TMA box: what the page size and the tile have in common, and at
 // least the swizzle's eight rows; 0: none.
@@ -1126,12 +1184,13 @@ int box_slots(const asd_kv_cache* c) {
 
 template <typename T, int kDim>
 int launch_dim(const asd_kv_cache* cache, const AttnParams& p, char* workspace, cudaStream_t stream) {
-  CUtensorMap map_k, map_v;
+  CUtensorMap maps[3];
   const int box = box_slots(cache);
   const bool bf16 = cache->dtype == ASD_BF16;
-  if (box && make_map(&map_k, bf16, p.cache.k, cache, box) && make_map(&map_v, bf16, p.cache.v, cache, box))
-    return launch<T, kDim, true>(map_k, map_v, p, box, workspace, stream);
-  return launch<T, kDim, false>(map_k, map_v, p, 0, workspace, stream);
+  if (box && p.group <= kGroupRows && make_map(&maps[0], bf16, p.cache.k, cache, box) &&
+      make_map(&maps[1], bf16, p.cache.v, cache, box) && make_query_map(&maps[2], bf16, p))
+    return launch<T, kDim, true>(maps, p, box, workspace, stream);
+  return launch<T, kDim, false>(maps, p, 0, workspace, stream);
 }
 
 }  // namespace
@@ -1150,13 +1209,14 @@ bool attention_tc_takes(const asd_kv_cache* cache, const AttnParams& p) {
 
 size_t attention_tc_bytes(const asd_kv_cache* cache, int T, int q_heads) {
   if (cache->dtype == ASD_F32 || cache->head_dim > 128) return 0;
-  return attn_layout(kAttnMaxCtas, unit_rows(static_cast<long long>(T) * (q_heads / cache->heads)),
-                     cache->head_dim <= 64 ? 64 : 128)
-      .total;
+  const int group = q_heads / cache->heads;
+  const bool shared = static_cast<long long>(T) * group > group_rows(group);
+  return attn_layout(kAttnMaxCtas, shared ? 2 * kGroupRows : kGroupRows, cache->head_dim <= 64 ? 64 : 128).total;
 }
 
 int launch_attention_tc(const asd_kv_cache* cache, AttnParams p, char* workspace, cudaStream_t stream) {
-  p.unit_rows = unit_rows(static_cast<long long>(p.T) * p.group);
+  p.group_rows = group_rows(p.group);
+  p.unit_rows = unit_rows(static_cast<long long>(p.T) * p.group, p.group);
   p.row_tiles = (p.T * p.group + p.unit_rows - 1) / p.unit_rows;
   if (cache->dtype == ASD_BF16)
     return p.D <= 64 ? launch_dim<__nv_bfloat16, 64>(cache, p, workspace, stream)

@@ -79,11 +79,12 @@ class Problem:
     def run(self, asd, layout="tokens", **kw):
         cache = self.device(asd, layout)
         status = torch.zeros(self.B, dtype=torch.int32, device="cuda")
+        ws = kw.pop("workspace", None) or asd.attention_workspace(cache, self.T, self.Hq)
         o = asd.tree_attention(self.q.cuda(), cache, self.kv_len.cuda(),
                                tree_mask=None if self.mask is None else self.mask.cuda(),
                                new_len=None if self.new_len is None else self.new_len.cuda(), scale=self.scale,
-                               status=status, **kw)
-        torch.cuda.synchronize()
+                               status=status, workspace=ws, **kw)
+        assert ws.error() == 0
         return o["out"].cpu(), o["lse"].cpu(), status.cpu()
 
     def check(self, out, lse):
