@@ -389,42 +389,45 @@ typedef struct {
  * norm per head and the position rotation on the way; the queries of the same
  * tokens take the same norm and rotation to q_out in the same pass.
  *
- * cache, layer  where the tokens go: token t of request b to slot kv_len[b] + t.
- *               kv_len is not changed (asd_commit advances it)
- * T             tokens per request, >= 0
- * k, v          [B, T, heads, head_dim] of the cache's dtype; strides in elements
- *               of the batch, token and head dimension (any, as in the rows of
- *               a fused projection); the last dimension is contiguous
- * q, q_heads    [B, T, q_heads, head_dim] the same way, or NULL and 0
- * q_out         [B, T, q_heads, head_dim] contiguous; may be q itself where q is
- *               contiguous
- * kv_len        [B] int32 tokens that each request has in the cache
- * new_len       [B] int32 how many of the T tokens exist (0..T), or NULL: all.
- *               Nothing is written for the others, q_out included
- * positions     [B, T] int32 rotation positions (a tree's nodes take their
- *               depth), or NULL: kv_len[b] + t
- * cos, sin      [rot_positions, rot_dim / 2] fp32, or both NULL: no rotation
- * rot_dim       even, 2 .. head_dim: the leading elements that turn; 0 without
- *               tables
- * interleaved   0: element i turns with i + rot_dim / 2; 1: 2i with 2i + 1
- * q_norm, k_norm [head_dim] weights of the cache's dtype, or NULL: no norm
- * eps           >= 0, of the norm
- * status        [B] int32, or NULL: ASD_STATUS_* bits are ORed in (zero it to
- *               start; one array can serve all layers of a pass). A request
- *               flagged ASD_STATUS_LENGTH writes nothing, a token whose position
- *               is out of range is left out, and one whose page is out of range
- *               leaves its key and value out.
+ * The tokens go to slots kv_len[b] + t (t < T) of request b. kv_len is not
+ * changed (asd_commit advances it). A request flagged ASD_STATUS_LENGTH writes
+ * nothing, a token whose position is out of range is left out, and one whose page
+ * is out of range leaves its key and value out.
  *
  * Arithmetic: x is widened to fp32; with a norm x <- x / sqrt(mean(x^2) + eps)
  * * w; then (a, b) <- (a cos - b sin, b cos + a sin); one rounding at the end.
  * Values are copied bit for bit.
  */
-int asd_kv_append(const asd_kv_cache* cache, int layer, int T, const void* k, int64_t k_batch, int64_t k_token,
-                  int64_t k_head, const void* v, int64_t v_batch, int64_t v_token, int64_t v_head, const void* q,
-                  int64_t q_batch, int64_t q_token, int64_t q_head, int q_heads, void* q_out, const int32_t* kv_len,
-                  const int32_t* new_len, const int32_t* positions, const float* cos, const float* sin, int rot_dim,
-                  int rot_positions, int interleaved, const void* q_norm, const void* k_norm, float eps,
-                  int32_t* status, asd_stream_t stream);
+typedef struct {
+  int64_t batch, token, head; /* strides in elements of a [B, T, heads, head_dim] array of the cache's dtype: any, as
+                               * in the rows of a fused projection; the last dimension is contiguous */
+} asd_strides;
+typedef struct {
+  const void* k; /* [B, T, heads, head_dim] */
+  const void* v;
+  const void* q; /* [B, T, q_heads, head_dim], or NULL with q_heads = 0 */
+  void* q_out;   /* [B, T, q_heads, head_dim] contiguous; may be q itself where q is contiguous */
+  asd_strides k_strides, v_strides, q_strides;
+  const int32_t* kv_len;    /* [B] tokens that each request has in the cache */
+  const int32_t* new_len;   /* [B] how many of the T tokens exist (0..T), or NULL: all. Nothing is written for the
+                             * others, q_out included */
+  const int32_t* positions; /* [B, T] rotation positions (a tree's nodes take their depth), or NULL: kv_len[b] + t */
+  const float* cos;         /* [rot_positions, rot_dim / 2], or both NULL: no rotation */
+  const float* sin;
+  const void* q_norm; /* [head_dim] weights of the cache's dtype, or NULL: no norm */
+  const void* k_norm;
+  int32_t* status;    /* [B] or NULL: ASD_STATUS_* bits are ORed in (zero it to start; one array can serve all
+                       * layers of a pass) */
+  int layer;
+  int T;              /* tokens per request, >= 0 */
+  int q_heads;        /* >= 0 */
+  int rot_dim;        /* even, 2 .. head_dim: the leading elements that turn; 0 without tables */
+  int rot_positions;  /* >= 0 */
+  int interleaved;    /* 0: element i turns with i + rot_dim / 2; 1: 2i with 2i + 1 */
+  float eps;          /* >= 0, of the norm */
+  int reserved;       /* 0 */
+} asd_append;
+int asd_kv_append(const asd_kv_cache* cache, const asd_append* args, asd_stream_t stream);
 
 /*
  * Attention of each request's T newest tokens over its paged cache: the tokens
@@ -435,24 +438,10 @@ int asd_kv_append(const asd_kv_cache* cache, int layer, int T, const void* k, in
  * kv_len[b] + u (u < new_len[b]) those with bit u % 32 of word u / 32 of its row
  * of tree_mask set (a node's row holds itself and its ancestors).
  *
- * q             [B, T, q_heads, head_dim] of the cache's dtype, strides as above;
- *               q_heads a multiple of the cache's heads: query head h reads
- *               key/value head h / (q_heads / heads). B * heads * (T * group / 16
- *               + 1) * (slots of the page table's row / 64 + 1) < 2^31
- * kv_len        [B] int32: the context, without the T new tokens
- * new_len       [B] int32 (0..T), or NULL: T
- * tree_mask     [B, T, ceil(T / 32)] uint32, or NULL: a chain (u <= t)
- * scale         finite; scores are scale * (q . k)
- * out           [B, T, q_heads, head_dim] contiguous, of the cache's dtype
- * lse           [B, T, q_heads] fp32 natural log of the sum of exp(score), or
- *               NULL
- * status        as for asd_kv_append; a request flagged ASD_STATUS_LENGTH counts
- *               as one without tokens, a slot on a page out of range as zeros
- * workspace     >= asd_attention_workspace_size bytes, 16-byte aligned, zeroed by
- *               asd_workspace_init before first use; one of the larger size
- *               serves any smaller shape. Its error word is read with
- *               asd_workspace_error; while it is set calls write nothing and
- *               flag their requests ASD_STATUS_INCOMPLETE
+ * Query head h reads key/value head h / group with group = q_heads / heads, a
+ * whole number. B * heads * (T * group / 16 + 1) * (slots of the page table's row
+ * / 64 + 1) < 2^31. A request flagged ASD_STATUS_LENGTH counts as one without
+ * tokens, a slot on a page out of range as zeros.
  *
  * A row that sees nothing (new_len[b] <= t, or an empty context and an empty
  * mask row) is 0 with lse = -INFINITY. What a row does not see does not reach
@@ -463,11 +452,26 @@ int asd_kv_append(const asd_kv_cache* cache, int layer, int T, const void* k, in
  * are rounded to the 16-bit type for the second product. The result does not
  * depend on the order in which CTAs finish.
  */
+typedef struct {
+  const void* q;             /* [B, T, q_heads, head_dim] of the cache's dtype */
+  void* out;                 /* [B, T, q_heads, head_dim] contiguous */
+  float* lse;                /* [B, T, q_heads] natural log of the sum of exp(score), or NULL */
+  asd_strides q_strides;
+  const int32_t* kv_len;     /* [B] the context, without the T new tokens */
+  const int32_t* new_len;    /* [B] (0..T), or NULL: T */
+  const uint32_t* tree_mask; /* [B, T, ceil(T / 32)], or NULL: a chain (u <= t) */
+  int32_t* status;           /* as in asd_append */
+  void* workspace;           /* 16-byte aligned, zeroed by asd_workspace_init before first use; one for a larger T or
+                              * cache serves any smaller one. While its error word (asd_workspace_error) is set calls
+                              * write nothing and flag their requests ASD_STATUS_INCOMPLETE */
+  size_t workspace_bytes;    /* >= asd_attention_workspace_size */
+  int layer;
+  int T;
+  int q_heads;
+  float scale;               /* finite; scores are scale * (q . k) */
+} asd_attention;
 int asd_attention_workspace_size(const asd_kv_cache* cache, int T, int q_heads, size_t* bytes);
-int asd_tree_attention(const asd_kv_cache* cache, int layer, int T, const void* q, int64_t q_batch, int64_t q_token,
-                       int64_t q_head, int q_heads, const int32_t* kv_len, const int32_t* new_len,
-                       const uint32_t* tree_mask, float scale, void* out, float* lse, int32_t* status,
-                       void* workspace, size_t workspace_bytes, asd_stream_t stream);
+int asd_tree_attention(const asd_kv_cache* cache, const asd_attention* args, asd_stream_t stream);
 
 /*
  * Moves the keys and values of a verified path next to the context, in place

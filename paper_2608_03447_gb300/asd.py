@@ -15,6 +15,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import struct
 import threading
 
 import torch
@@ -98,13 +99,11 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.asd_lmhead_logits.restype = i32
     lib.asd_lmhead_partials.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, sz, vp]
     lib.asd_lmhead_partials.restype = i32
-    i64 = ctypes.c_int64
-    lib.asd_kv_append.argtypes = [vp, i32, i32, vp, i64, i64, i64, vp, i64, i64, i64, vp, i64, i64, i64, i32, vp, vp, vp,
-                                  vp, vp, vp, i32, i32, i32, vp, vp, f32, vp, vp]
+    lib.asd_kv_append.argtypes = [vp, vp, vp]
     lib.asd_kv_append.restype = i32
     lib.asd_attention_workspace_size.argtypes = [vp, i32, i32, ctypes.POINTER(sz)]
     lib.asd_attention_workspace_size.restype = i32
-    lib.asd_tree_attention.argtypes = [vp, i32, i32, vp, i64, i64, i64, i32, vp, vp, vp, f32, vp, vp, vp, vp, sz, vp]
+    lib.asd_tree_attention.argtypes = [vp, vp, vp]
     lib.asd_tree_attention.restype = i32
     lib.asd_kv_compact.argtypes = [vp, i32, vp, vp, vp, vp, vp]
     lib.asd_kv_compact.restype = i32
@@ -601,7 +600,7 @@ class KVCache:
         if not (k.is_cuda and k.device == v.device == page_table.device):
             raise ValueError("k, v and page_table must be on one CUDA device")
         self.k, self.v, self.page_table = k, v, page_table
-        self.dtype, self.device = k.dtype, k.device
+        self.dtype, self.device, self.index = k.dtype, k.device, k.get_device()
         self.layers, self.pages, self.page_size, self.heads, self.head_dim = k.shape
         self.B, self.table_width = page_table.shape
         s = k.stride()
@@ -611,22 +610,26 @@ class KVCache:
         self._ref = ctypes.addressof(self._c)
 
 
-def _heads(name: str, t: torch.Tensor, cache: KVCache, T: int | None = None, heads: int | None = None):
+# The arguments of asd_append and asd_attention as they lie in memory. One packed block and a call of three arguments:
+# as 31 arguments of a ctypes call asd_append took 3.2 us of host time, packed 0.8.
+_APPEND = struct.Struct("4P 9q 3P 2P 2P P 6i f i")
+_ATTENTION = struct.Struct("3P 3q 3P P P N 3i f")
+_I32 = torch.int32
+
+
+def _check_heads(name: str, t: torch.Tensor, cache: KVCache, shape: tuple) -> tuple:
     """The strides of a [B, T, heads, head_dim] tensor of the cache's type."""
-    shape, st = t.shape, t.stride()
-    if len(shape) != 4 or t.dtype != cache.dtype or t.device != cache.device or shape[0] != cache.B or \
-            shape[3] != cache.head_dim or (st[3] != 1 and shape[3] > 1) or (T is not None and shape[1] != T) or \
-            (heads is not None and shape[2] != heads):
-        raise ValueError(f"{name} must be a [B, T, heads, head_dim] tensor of the cache's type and device, its last "
-                         "dimension contiguous")
+    st = t.stride()
+    if t.shape != shape or t.dtype is not cache.dtype or t.get_device() != cache.index or \
+            (st[3] != 1 and shape[3] > 1):
+        raise ValueError(f"{name} must be a {list(shape)} tensor of the cache's type and device, its last dimension "
+                         "contiguous")
     return st
 
 
-def _int32(name: str, t: torch.Tensor | None, cache: KVCache, shape: tuple) -> int | None:
-    if t is None:
-        return None
-    if t.dtype != torch.int32 or t.shape != shape or t.device != cache.device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 CUDA tensor {list(shape)}")
+def _check_vector(name: str, t: torch.Tensor, cache: KVCache, shape: tuple, dtype: torch.dtype = _I32) -> int:
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != cache.index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on the cache's device")
     return t.data_ptr()
 
 
@@ -641,34 +644,41 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, kv_len: torch.Te
     k, v [B, T, heads, D] and q [B, T, q_heads, D] may be strided views of a fused projection's rows. cos, sin
     [positions, rot_dim / 2] float32. Returns ``q_out`` (allocated if not given), or None without queries.
     """
-    ks = _heads("k", k, cache, heads=cache.heads)
-    B, T = cache.B, k.shape[1]
-    vs = _heads("v", v, cache, T, cache.heads)
-    qs, q_heads = (0, 0, 0, 0), 0
-    if q is not None:
-        qs, q_heads = _heads("q", q, cache, T), q.shape[2]
+    B, D = cache.B, cache.head_dim
+    T = k.shape[1] if k.dim() == 4 else -1
+    shape = (B, T, cache.heads, D)
+    ks = _check_heads("k", k, cache, shape)
+    vs = _check_heads("v", v, cache, shape)
+    if q is None:
+        qs, q_heads, qp, op = (0, 0, 0), 0, 0, 0
+    else:
+        q_heads = q.shape[2] if q.dim() == 4 else -1
+        shape = (B, T, q_heads, D)
+        qs = _check_heads("q", q, cache, shape)
         if q_out is None:
-            q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
-        elif q_out.shape != q.shape or q_out.dtype != q.dtype or q_out.device != q.device or not q_out.is_contiguous():
-            raise ValueError("q_out must be a contiguous tensor of q's shape, type and device")
-    rot, table = 0, 0
+            q_out = torch.zeros(shape, dtype=q.dtype, device=q.device)
+        op, qp = _check_vector("q_out", q_out, cache, shape, cache.dtype), q.data_ptr()
+    one = (B,)
+    cp = sp = table = rot = 0
     if cos is not None or sin is not None:
-        if cos is None or sin is None or cos.dim() != 2 or cos.shape != sin.shape or cos.dtype != torch.float32 or \
-                sin.dtype != torch.float32 or not cos.is_contiguous() or not sin.is_contiguous() or \
-                cos.device != cache.device or sin.device != cache.device:
-            raise ValueError("cos and sin must be contiguous float32 CUDA tensors [positions, rot_dim / 2] alike")
-        table, rot = cos.shape[0], 2 * cos.shape[1]
-    for w in (q_norm, k_norm):
-        if w is not None and (w.shape != (cache.head_dim,) or w.dtype != cache.dtype or w.device != cache.device or
-                              not w.is_contiguous()):
-            raise ValueError("q_norm and k_norm must be contiguous tensors [head_dim] of the cache's type")
-    rc = load().asd_kv_append(cache._ref, layer, T, k.data_ptr(), ks[0], ks[1], ks[2], v.data_ptr(), vs[0], vs[1],
-                              vs[2], _ptr(q), qs[0], qs[1], qs[2], q_heads, None if q is None else q_out.data_ptr(),
-                              _int32("kv_len", kv_len, cache, (B,)), _int32("new_len", new_len, cache, (B,)),
-                              _int32("positions", positions, cache, (B, T)), _ptr(cos), _ptr(sin), rot, table,
-                              int(interleaved), _ptr(q_norm), _ptr(k_norm), eps,
-                              _int32("status", status, cache, (B,)), _stream(stream))
-    _check("asd_kv_append", rc)
+        if cos is None or sin is None or cos.dim() != 2:
+            raise ValueError("cos and sin must be float32 tensors [positions, rot_dim / 2], both or neither")
+        shape = cos.shape
+        table, rot = shape[0], 2 * shape[1]
+        cp = _check_vector("cos", cos, cache, shape, torch.float32)
+        sp = _check_vector("sin", sin, cache, shape, torch.float32)
+    args = _APPEND.pack(
+        k.data_ptr(), v.data_ptr(), qp, op, ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], qs[0], qs[1], qs[2],
+        _check_vector("kv_len", kv_len, cache, one),
+        0 if new_len is None else _check_vector("new_len", new_len, cache, one),
+        0 if positions is None else _check_vector("positions", positions, cache, (B, T)), cp, sp,
+        0 if q_norm is None else _check_vector("q_norm", q_norm, cache, (D,), cache.dtype),
+        0 if k_norm is None else _check_vector("k_norm", k_norm, cache, (D,), cache.dtype),
+        0 if status is None else _check_vector("status", status, cache, one), layer, T, q_heads, rot, table,
+        1 if interleaved else 0, eps, 0)
+    rc = load().asd_kv_append(cache._ref, args, _stream(stream))
+    if rc:
+        raise AsdError("asd_kv_append", rc)
     return None if q is None else q_out
 
 
@@ -713,25 +723,26 @@ def tree_attention(q: torch.Tensor, cache: KVCache, kv_len: torch.Tensor, layer:
     for a chain; ``scale`` defaults to 1 / sqrt(D). Returns {"out": [B, T, q_heads, D], "lse": float32 [B, T, q_heads]};
     an ``out`` dict without "lse" leaves it out.
     """
-    qs = _heads("q", q, cache)
-    B, T, q_heads, D = q.shape
+    B, D = cache.B, cache.head_dim
+    T, q_heads = q.shape[1:3] if q.dim() == 4 else (-1, -1)
+    shape, rows = (B, T, q_heads, D), (B, T, q_heads)
+    qs = _check_heads("q", q, cache, shape)
     if out is None:
-        out = {"out": torch.empty(q.shape, dtype=q.dtype, device=q.device),
-               "lse": torch.empty(B, T, q_heads, dtype=torch.float32, device=q.device)}
-    o, lse = out["out"], out.get("lse")
-    if o.shape != q.shape or o.dtype != q.dtype or o.device != q.device or not o.is_contiguous():
-        raise ValueError("out must be a contiguous tensor of q's shape, type and device")
-    if lse is not None and (lse.shape != (B, T, q_heads) or lse.dtype != torch.float32 or lse.device != q.device or
-                            not lse.is_contiguous()):
-        raise ValueError("lse must be a contiguous float32 tensor [B, T, q_heads]")
+        out = {"out": torch.empty(shape, dtype=q.dtype, device=q.device),
+               "lse": torch.empty(rows, dtype=torch.float32, device=q.device)}
+    lse = out.get("lse")
     ws = workspace or attention_workspace(cache, T, q_heads, stream)
-    rc = load().asd_tree_attention(cache._ref, layer, T, q.data_ptr(), qs[0], qs[1], qs[2], q_heads,
-                                   _int32("kv_len", kv_len, cache, (B,)), _int32("new_len", new_len, cache, (B,)),
-                                   _int32("tree_mask", tree_mask, cache, (B, T, (T + 31) // 32)),
-                                   D ** -0.5 if scale is None else scale, o.data_ptr(), _ptr(lse),
-                                   _int32("status", status, cache, (B,)), ws.buffer.data_ptr(), ws.nbytes,
-                                   _stream(stream))
-    _check("asd_tree_attention", rc)
+    args = _ATTENTION.pack(
+        q.data_ptr(), _check_vector("out", out["out"], cache, shape, cache.dtype),
+        0 if lse is None else _check_vector("lse", lse, cache, rows, torch.float32), qs[0], qs[1], qs[2],
+        _check_vector("kv_len", kv_len, cache, (B,)),
+        0 if new_len is None else _check_vector("new_len", new_len, cache, (B,)),
+        0 if tree_mask is None else _check_vector("tree_mask", tree_mask, cache, (B, T, (T + 31) // 32)),
+        0 if status is None else _check_vector("status", status, cache, (B,)), ws.buffer.data_ptr(), ws.nbytes, layer,
+        T, q_heads, D ** -0.5 if scale is None else scale)
+    rc = load().asd_tree_attention(cache._ref, args, _stream(stream))
+    if rc:
+        raise AsdError("asd_tree_attention", rc)
     return out
 
 
@@ -741,9 +752,12 @@ def kv_compact(cache: KVCache, kv_len: torch.Tensor, path: torch.Tensor, path_le
 
     path int32 [B, P], ascending tree nodes with path[b, i] >= i; path_len int32 [B].
     """
-    B, P = path.shape
-    rc = load().asd_kv_compact(cache._ref, P, _int32("kv_len", kv_len, cache, (cache.B,)),
-                               _int32("path", path, cache, (cache.B, P)),
-                               _int32("path_len", path_len, cache, (cache.B,)),
-                               _int32("status", status, cache, (cache.B,)), _stream(stream))
-    _check("asd_kv_compact", rc)
+    B = cache.B
+    P = path.shape[1] if path.dim() == 2 else -1
+    rc = load().asd_kv_compact(cache._ref, P, _check_vector("kv_len", kv_len, cache, (B,)),
+                               _check_vector("path", path, cache, (B, P)),
+                               _check_vector("path_len", path_len, cache, (B,)),
+                               None if status is None else _check_vector("status", status, cache, (B,)),
+                               _stream(stream))
+    if rc:
+        raise AsdError("asd_kv_compact", rc)

@@ -7,10 +7,17 @@
 // over the keys and values: per row the running maximum m and sum l of
 // exp2(s - m), and the output's sum rescaled when m grows.
 //
-// A CTA of 256 threads has kRows query rows that share a key/value head (16 or
-// 64) against tiles of 64 slots. Thread (y, x) of 16 x 16 computes the scores of
-// rows y + 16 i and slots x + 16 j, four elements of the head at a time from
-// shared memory, and holds the output's columns 4 x + 64 c .. + 3 of its rows.
+// A CTA of 256 threads has 16 kI query rows that share a key/value head against
+// tiles of 64 slots. Thread (y, x) of 16 x 16 computes the scores of rows y + 16 i
+// and slots x + 16 j, four elements of the head at a time from shared memory, and
+// holds the output's columns 4 x + 64 c .. + 3 of its rows.
+//
+// What bounds it: fp32 multiply-adds from about 12 rows on (two for each element
+// that crosses from memory), so rows are cut into as few and as equal tiles of at
+// most 80 as hold them, and a tile's instance has no more than 15 to spare. Keys
+// and values have a buffer each: 32-bit rows are copied straight into shared
+// memory, values while the scores are computed and the next keys while the values
+// are used.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -34,7 +41,7 @@ constexpr int kSimtTile = 64;
 __host__ __device__ constexpr int simt_pitch(int dim) { return (dim + 3) / 4 * 4 + 4; }
 constexpr int kScorePitch = kSimtTile + 4;
 constexpr size_t simt_smem(int rows, int dim) {
-  return sizeof(float) * (static_cast<size_t>(rows + kSimtTile) * simt_pitch(dim) + rows * kScorePitch) +
+  return sizeof(float) * (static_cast<size_t>(rows + 2 * kSimtTile) * simt_pitch(dim) + rows * kScorePitch) +
          2 * sizeof(long long) * kSimtTile;
 }
 
@@ -57,19 +64,27 @@ __device__ __forceinline__ void load4(const T* p, bool vec, int valid, float (&x
   for (int i = 0; i < 4; ++i) x[i] = i < valid ? Store<T>::widen(p[i]) : 0.0f;
 }
 
-// kRows: query rows of a unit. kCols: the output's groups of 64 columns.
-template <typename T, int kRows, int kCols>
+__device__ __forceinline__ void copy16(float* dst, const float* src, bool has) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(has ? 16 : 0)
+               : "memory");
+}
+
+// kI: query rows of a thread. kCols: the output's groups of 64 columns.
+template <typename T, int kI, int kCols>
 __global__ void __launch_bounds__(kSimtThreads)
     attention_kernel(const __grid_constant__ AttnParams p, bool vec_q, bool vec_kv) {
-  constexpr int kI = kRows / 16;
+  constexpr int kRows = 16 * kI;
   extern __shared__ __align__(16) float smem[];
   __shared__ AttnDeal deal;
   __shared__ int s_last;
   const int D = p.D, pitch = simt_pitch(D), quads = (D + 3) / 4;
   float* sq = smem;                        // [kRows][pitch]
-  float* skv = sq + kRows * pitch;         // [kSimtTile][pitch]: keys, then values
-  float* sp = skv + kSimtTile * pitch;     // [kRows][kScorePitch]
-  long long* s_off = reinterpret_cast<long long*>(sp + kRows * kScorePitch);  // [kSimtTile] slots' offsets
+  float* sk = sq + kRows * pitch;          // [kSimtTile][pitch]
+  float* sv = sk + kSimtTile * pitch;      // [kSimtTile][pitch]
+  float* sp = sv + kSimtTile * pitch;      // [kRows][kScorePitch]
+  // [2][kSimtTile] the slots' offsets, of this tile and the next
+  long long* s_off = reinterpret_cast<long long*>(sp + kRows * kScorePitch);
+  const bool async = sizeof(T) == 4 && vec_kv;
 
   const int tid = threadIdx.x, x = tid & 15, y = tid >> 4;
   pdl_signal_dependents();
@@ -104,26 +119,41 @@ __global__ void __launch_bounds__(kSimtThreads)
       for (int c = 0; c < kCols; ++c) o[i][c][0] = o[i][c][1] = o[i][c][2] = o[i][c][3] = 0.0f;
     }
 
-    auto load_tile = [&](const char* base, int slots) {
+    // One tile's keys or values: copied in the background, or (types to widen, odd rows) by way of registers.
+    auto load_tile = [&](float* dst, const char* base, const long long* off, int slots) {
       const T* src = reinterpret_cast<const T*>(base) + w.h * p.cache.head_stride;
       for (int i = tid; i < kSimtTile * quads; i += kSimtThreads) {
         const int s = i / quads, d4 = i - s * quads;
+        const bool has = s < slots && off[s] >= 0;
+        if constexpr (sizeof(T) == 4) {
+          if (async) {
+            copy16(dst + s * pitch + 4 * d4, has ? src + off[s] + 4 * d4 : src, has);
+            continue;
+          }
+        }
         float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (s < slots && s_off[s] >= 0) load4(src + s_off[s] + 4 * d4, vec_kv, D - 4 * d4, f);
-        *reinterpret_cast<float4*>(skv + s * pitch + 4 * d4) = make_float4(f[0], f[1], f[2], f[3]);
+        if (has) load4(src + off[s] + 4 * d4, vec_kv, D - 4 * d4, f);
+        *reinterpret_cast<float4*>(dst + s * pitch + 4 * d4) = make_float4(f[0], f[1], f[2], f[3]);
       }
+      if (async) asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    for (int j = w.j0, j1 = w.j1(); j < j1; ++j) {
+    auto look_up = [&](int j) {  // the slots' offsets of tile j
+      const int slot = j * kSimtTile + tid;
+      if (tid >= kSimtTile || slot >= span) return;
+      const long long off = slot_offset(p.cache, w.b, slot);
+      if (off < 0 && p.status) atomicOr(p.status + w.b, static_cast<int>(ASD_STATUS_PAGE));
+      s_off[(j & 1) * kSimtTile + tid] = off;
+    };
+    const int j1 = w.j1();
+    look_up(w.j0);
+    __syncthreads();
+    load_tile(sk, p.cache.k, s_off + (w.j0 & 1) * kSimtTile, span - w.j0 * kSimtTile);
+    for (int j = w.j0; j < j1; ++j) {
       const int slot0 = j * kSimtTile;
-      const int slots = min(kSimtTile, span - slot0);
-      __syncthreads();  // the tile before has been read
-      if (tid < slots) {
-        const long long off = slot_offset(p.cache, w.b, slot0 + tid);
-        if (off < 0 && p.status) atomicOr(p.status + w.b, static_cast<int>(ASD_STATUS_PAGE));
-        s_off[tid] = off;
-      }
-      __syncthreads();
-      load_tile(p.cache.k, slots);
+      const long long* off = s_off + (j & 1) * kSimtTile;
+      if (j + 1 < j1) look_up(j + 1);
+      load_tile(sv, p.cache.v, off, span - slot0);
+      if (async) asm volatile("cp.async.wait_group 1;" ::: "memory");  // the keys
       __syncthreads();
       float s[kI][4];
 #pragma unroll
@@ -133,7 +163,7 @@ __global__ void __launch_bounds__(kSimtThreads)
 #pragma unroll
         for (int i = 0; i < kI; ++i) a[i] = *reinterpret_cast<const float4*>(sq + (y + 16 * i) * pitch + 4 * d4);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) kk[c] = *reinterpret_cast<const float4*>(skv + (x + 16 * c) * pitch + 4 * d4);
+        for (int c = 0; c < 4; ++c) kk[c] = *reinterpret_cast<const float4*>(sk + (x + 16 * c) * pitch + 4 * d4);
 #pragma unroll
         for (int i = 0; i < kI; ++i)
 #pragma unroll
@@ -184,7 +214,12 @@ __global__ void __launch_bounds__(kSimtThreads)
           for (int e = 0; e < 4; ++e) o[i][c][e] *= fade;
       }
       __syncthreads();  // the scores are written, the keys read
-      load_tile(p.cache.v, slots);
+      if (j + 1 < j1) {
+        load_tile(sk, p.cache.k, s_off + ((j + 1) & 1) * kSimtTile, span - slot0 - kSimtTile);
+        if (async) asm volatile("cp.async.wait_group 1;" ::: "memory");  // the values
+      } else if (async) {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+      }
       __syncthreads();
       for (int s4 = 0; s4 < kSimtTile; s4 += 4) {
         float4 a[kI];
@@ -195,7 +230,7 @@ __global__ void __launch_bounds__(kSimtThreads)
           float4 v[kCols];
 #pragma unroll
           for (int c = 0; c < kCols; ++c)
-            if (4 * x + 64 * c < D) v[c] = *reinterpret_cast<const float4*>(skv + (s4 + e) * pitch + 4 * x + 64 * c);
+            if (4 * x + 64 * c < D) v[c] = *reinterpret_cast<const float4*>(sv + (s4 + e) * pitch + 4 * x + 64 * c);
 #pragma unroll
           for (int i = 0; i < kI; ++i) {
             const float f = e == 0 ? a[i].x : e == 1 ? a[i].y : e == 2 ? a[i].z : a[i].w;
@@ -211,6 +246,7 @@ __global__ void __launch_bounds__(kSimtThreads)
           }
         }
       }
+      __syncthreads();  // the values have been read
     }
 
     // the rows' results, or this CTA's piece of them
@@ -290,33 +326,40 @@ __global__ void __launch_bounds__(kSimtThreads)
 // ---------------------------------------------------------------- host side
 
 constexpr int kMaxDevices = 64;
+constexpr size_t kSmemPerSm = 233472;
 
-// How many CTAs of a launch run at once, per kernel and head width (0: not asked yet).
-template <typename T, int kRows, int kCols>
+template <typename T, int kI, int kCols>
 int launch_simt(AttnParams p, char* workspace, cudaStream_t stream) {
-  auto kernel = attention_kernel<T, kRows, kCols>;
-  static std::atomic<int> resident[kMaxDevices];
+  constexpr int kRows = 16 * kI;
+  auto kernel = attention_kernel<T, kI, kCols>;
+  // CTAs that an SM's registers hold, and SMs (0: not asked yet)
+  static std::atomic<int> by_registers[kMaxDevices], sm_count[kMaxDevices];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return ASD_ERR_CUDA;
   if (dev < 0 || dev >= kMaxDevices) return ASD_ERR_DEVICE;
-  int ctas = resident[dev].load(std::memory_order_acquire);
-  const size_t most = simt_smem(kRows, kCols * 64);  // of this instance's head widths
-  if (ctas == 0) {
-    int sms = 0, per = 0;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most)) !=
-            cudaSuccess ||
+  int per = by_registers[dev].load(std::memory_order_acquire);
+  if (per == 0) {
+    int sms = 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(simt_smem(kRows, kCols * 64))) != cudaSuccess ||
         cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, kSimtThreads, most) != cudaSuccess || per < 1)
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, kSimtThreads, 0) != cudaSuccess || per < 1)
       return ASD_ERR_CUDA;
-    ctas = sms * per < kAttnMaxCtas ? sms * per : kAttnMaxCtas;
-    resident[dev].store(ctas, std::memory_order_release);
+    sm_count[dev].store(sms, std::memory_order_relaxed);
+    by_registers[dev].store(per, std::memory_order_release);
   }
+  const size_t smem = simt_smem(kRows, p.D);
+  const int by_smem = static_cast<int>(kSmemPerSm / (smem + 2048));  // the CTA's static part and the system's KB
+  per = by_smem < per ? by_smem : per;
+  int ctas = sm_count[dev].load(std::memory_order_relaxed) * (per < 1 ? 1 : per);
+  ctas = ctas < kAttnMaxCtas ? ctas : kAttnMaxCtas;
   const AttnLayout l = attn_layout(kAttnMaxCtas, kRows, simt_pitch(p.D) - 4);
   p.counters = reinterpret_cast<unsigned*>(workspace + l.counters);
   p.part_ml = reinterpret_cast<float*>(workspace + l.ml);
   p.part_o = reinterpret_cast<float*>(workspace + l.o);
+  const int rows = p.T * p.group;
+  p.row_tiles = (rows + kRows - 1) / kRows;
   p.unit_rows = kRows;
-  p.row_tiles = (p.T * p.group + kRows - 1) / kRows;
   const size_t es = sizeof(T), four = 4 * es;
   const bool vec_q = p.D % 4 == 0 && rows_aligned(p.q, es, four, p.q_batch, p.q_token, p.q_head);
   const bool vec_kv = p.D % 4 == 0 &&
@@ -325,25 +368,39 @@ int launch_simt(AttnParams p, char* workspace, cudaStream_t stream) {
                       reinterpret_cast<uintptr_t>(p.cache.v) % four == 0;
   cudaLaunchAttribute attr;
   cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(ctas)), dim3(kSimtThreads), stream, &attr);
-  cfg.dynamicSmemBytes = simt_smem(kRows, p.D);
+  cfg.dynamicSmemBytes = smem;
   if (cudaLaunchKernelEx(&cfg, kernel, p, vec_q, vec_kv) != cudaSuccess) return ASD_ERR_CUDA;
   return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;
 }
 
-// Rows of a unit: 64 where that many share a key/value head, else 16.
-int simt_rows(long long rows) { return rows > 16 ? 64 : 16; }
+// Rows of a thread: the fewest tiles of at most 80 rows, as equal as they go.
+// 16-bit types (what the tensor cores do not take) have two instances. Heads wider
+// than 128 leave shared memory for 64 rows.
+int simt_i(long long rows, int dtype, int dim) {
+  const int most = dim > 128 ? 4 : 5;
+  if (dtype != ASD_F32 || dim > 128) return rows > 16 ? 4 : 1;
+  const long long tiles = (rows + 16 * most - 1) / (16 * most);
+  const long long i = (rows + 16 * tiles - 1) / (16 * tiles);
+  return i < 1 ? 1 : static_cast<int>(i);
+}
 
-template <typename T, int kRows>
+template <typename T, int kI>
 int launch_cols(const AttnParams& p, char* workspace, cudaStream_t stream) {
-  if (p.D <= 64) return launch_simt<T, kRows, 1>(p, workspace, stream);
-  if (p.D <= 128) return launch_simt<T, kRows, 2>(p, workspace, stream);
-  return launch_simt<T, kRows, 4>(p, workspace, stream);
+  if (p.D <= 64) return launch_simt<T, kI, 1>(p, workspace, stream);
+  if (p.D <= 128) return launch_simt<T, kI, 2>(p, workspace, stream);
+  if constexpr (kI == 1 || kI == 4) return launch_simt<T, kI, 4>(p, workspace, stream);
+  return ASD_ERR_SHAPE;
 }
 
 template <typename T>
-int launch_rows(const AttnParams& p, char* workspace, cudaStream_t stream) {
-  if (simt_rows(static_cast<long long>(p.T) * p.group) == 64) return launch_cols<T, 64>(p, workspace, stream);
-  return launch_cols<T, 16>(p, workspace, stream);
+int launch_rows(const AttnParams& p, int dtype, char* workspace, cudaStream_t stream) {
+  const int i = simt_i(static_cast<long long>(p.T) * p.group, dtype, p.D);
+  if constexpr (sizeof(T) == 4) {
+    if (i == 2) return launch_cols<T, 2>(p, workspace, stream);
+    if (i == 3) return launch_cols<T, 3>(p, workspace, stream);
+    if (i == 5) return launch_cols<T, 5>(p, workspace, stream);
+  }
+  return i == 4 ? launch_cols<T, 4>(p, workspace, stream) : launch_cols<T, 1>(p, workspace, stream);
 }
 
 int check_attention(const asd_kv_cache* cache, int T, int q_heads) {
@@ -355,14 +412,15 @@ int check_attention(const asd_kv_cache* cache, int T, int q_heads) {
   if (rows > (1 << 28)) return ASD_ERR_SHAPE;
   const long long slots = static_cast<long long>(cache->table_width) * cache->page_size;
   const double tiles = static_cast<double>(slots < 0x7fffffffll ? slots : 0x7fffffffll) / kSimtTile + 1;
-  if (tiles * static_cast<double>(rows / simt_rows(rows) + 1) * cache->heads * cache->B > 2147483647.0)
+  if (tiles * static_cast<double>(rows / 16 + 1) * cache->heads * cache->B > 2147483647.0)
     return ASD_ERR_SHAPE;
   return ASD_OK;
 }
 
 size_t attention_bytes(const asd_kv_cache* cache, int T, int q_heads) {
   const long long rows = static_cast<long long>(T) * (q_heads / cache->heads);
-  const size_t simt = attn_layout(kAttnMaxCtas, simt_rows(rows), simt_pitch(cache->head_dim) - 4).total;
+  // the tile of a smaller T may have more rows
+  const size_t simt = attn_layout(kAttnMaxCtas, rows <= 16 ? 16 : rows <= 64 ? 64 : 80, simt_pitch(cache->head_dim) - 4).total;
   const size_t tc = attention_tc_bytes(cache, T, q_heads);
   return simt > tc ? simt : tc;
 }
@@ -379,51 +437,49 @@ int asd_attention_workspace_size(const asd_kv_cache* cache, int T, int q_heads, 
   return ASD_OK;
 }
 
-int asd_tree_attention(const asd_kv_cache* cache, int layer, int T, const void* q, int64_t q_batch, int64_t q_token,
-                       int64_t q_head, int q_heads, const int32_t* kv_len, const int32_t* new_len,
-                       const uint32_t* tree_mask, float scale, void* out, float* lse, int32_t* status,
-                       void* workspace, size_t workspace_bytes, asd_stream_t stream) {
-  const int rc = check_attention(cache, T, q_heads);
+int asd_tree_attention(const asd_kv_cache* cache, const asd_attention* args, asd_stream_t stream) {
+  if (!args) return cache ? ASD_ERR_NULL : check_cache(cache);
+  const asd_attention& a = *args;
+  const int rc = check_attention(cache, a.T, a.q_heads);
   if (rc != ASD_OK) return rc;
-  if (layer < 0 || layer >= cache->layers) return ASD_ERR_SHAPE;
-  if (!(scale - scale == 0.0f)) return ASD_ERR_CONTROL;  // infinite or NaN
-  if (cache->B == 0 || T == 0) return ASD_OK;
-  if (!q || !kv_len || !out || !workspace) return ASD_ERR_NULL;
+  if (a.layer < 0 || a.layer >= cache->layers) return ASD_ERR_SHAPE;
+  if (!(a.scale - a.scale == 0.0f)) return ASD_ERR_CONTROL;  // infinite or NaN
+  if (cache->B == 0 || a.T == 0) return ASD_OK;
+  if (!a.q || !a.kv_len || !a.out || !a.workspace) return ASD_ERR_NULL;
   const size_t es = store_bytes(cache->dtype);
-  if (reinterpret_cast<uintptr_t>(q) % es != 0 || reinterpret_cast<uintptr_t>(out) % es != 0) return ASD_ERR_ALIGN;
-  const void* const words[] = {kv_len, new_len, tree_mask, lse, status};
+  if (reinterpret_cast<uintptr_t>(a.q) % es != 0 || reinterpret_cast<uintptr_t>(a.out) % es != 0) return ASD_ERR_ALIGN;
+  const void* const words[] = {a.kv_len, a.new_len, a.tree_mask, a.lse, a.status};
   for (const void* x : words)
     if (reinterpret_cast<uintptr_t>(x) % 4 != 0) return ASD_ERR_ALIGN;
-  if (workspace_bytes < attention_bytes(cache, T, q_heads)) return ASD_ERR_WORKSPACE;
-  if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return ASD_ERR_ALIGN;
+  if (a.workspace_bytes < attention_bytes(cache, a.T, a.q_heads)) return ASD_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(a.workspace) % 16 != 0) return ASD_ERR_ALIGN;
   AttnParams p = {};
-  p.cache = cache_view(cache, layer);
-  p.q = static_cast<const char*>(q);
-  p.q_batch = q_batch;
-  p.q_token = q_token;
-  p.q_head = q_head;
-  p.out = static_cast<char*>(out);
-  p.lse = lse;
-  p.kv_len = kv_len;
-  p.new_len = new_len;
-  p.mask = tree_mask;
-  p.mask_words = (T + 31) / 32;
-  p.status = status;
-  p.error = reinterpret_cast<unsigned*>(workspace);
+  p.cache = cache_view(cache, a.layer);
+  p.q = static_cast<const char*>(a.q);
+  p.q_batch = a.q_strides.batch;
+  p.q_token = a.q_strides.token;
+  p.q_head = a.q_strides.head;
+  p.out = static_cast<char*>(a.out);
+  p.lse = a.lse;
+  p.kv_len = a.kv_len;
+  p.new_len = a.new_len;
+  p.mask = a.tree_mask;
+  p.mask_words = (a.T + 31) / 32;
+  p.status = a.status;
+  p.error = static_cast<unsigned*>(a.workspace);
   p.B = cache->B;
-  p.T = T;
-  p.q_heads = q_heads;
+  p.T = a.T;
+  p.q_heads = a.q_heads;
   p.heads = cache->heads;
-  p.group = q_heads / cache->heads;
+  p.group = a.q_heads / cache->heads;
   p.D = cache->head_dim;
-  p.scale = scale;
-  p.scale_log2 = scale * 1.4426950408889634f;
-  char* ws = static_cast<char*>(workspace);
+  p.scale_log2 = a.scale * 1.4426950408889634f;
+  char* ws = static_cast<char*>(a.workspace);
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (attention_tc_takes(cache, p)) return launch_attention_tc(cache, p, ws, s);
-  if (cache->dtype == ASD_F32) return launch_rows<float>(p, ws, s);
-  if (cache->dtype == ASD_BF16) return launch_rows<__nv_bfloat16>(p, ws, s);
-  return launch_rows<__half>(p, ws, s);
+  if (cache->dtype == ASD_F32) return launch_rows<float>(p, cache->dtype, ws, s);
+  if (cache->dtype == ASD_BF16) return launch_rows<__nv_bfloat16>(p, cache->dtype, ws, s);
+  return launch_rows<__half>(p, cache->dtype, ws, s);
 }
 
 }  // extern "C"

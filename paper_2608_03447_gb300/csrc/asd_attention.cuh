@@ -43,7 +43,6 @@ struct AttnParams {
   int B, T, q_heads, heads, group, D;
   int unit_rows, row_tiles;
   int group_rows;  // tensor cores: rows of a softmax group
-  float scale;
   float scale_log2;
 };
 

@@ -1201,7 +1201,7 @@ namespace asd_detail {
 // 16-byte boundaries, and scores that grow with q . k (the row's maximum is taken
 // before it is scaled).
 bool attention_tc_takes(const asd_kv_cache* cache, const AttnParams& p) {
-  return cache->dtype != ASD_F32 && p.D <= 128 && p.D % 8 == 0 && p.scale > 0.0f &&
+  return cache->dtype != ASD_F32 && p.D <= 128 && p.D % 8 == 0 && p.scale_log2 > 0.0f &&
          rows_aligned(p.cache.k, 2, 16, p.cache.page_stride, p.cache.token_stride, p.cache.head_stride) &&
          reinterpret_cast<uintptr_t>(p.cache.v) % 16 == 0 &&
          rows_aligned(p.q, 2, 16, p.q_batch, p.q_token, p.q_head) && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;

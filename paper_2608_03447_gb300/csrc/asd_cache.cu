@@ -41,6 +41,7 @@ struct AppendParams {
   int B, T, q_heads, kv_heads, D;
   int rot, rot_positions, interleaved;
   int q_slices, kv_slices;  // groups of kHeads heads
+  bool vec_tables;          // rows of cosines and sines start on 16 bytes and are read from multiples of 4
   long long items;          // B * T * (q_slices + 2 kv_slices)
 };
 
@@ -67,6 +68,21 @@ __device__ __forceinline__ Chunk<T, kVec> load_chunk(const T* p) {
     memcpy(&c, &w, 2);
   }
   return c;
+}
+
+// Cosines or sines, by ordinary loads: the heads of a token share them.
+template <int kCount>
+__device__ __forceinline__ void load_table(const float* p, float* x, bool vec) {
+  if (kCount % 4 == 0 && vec) {
+#pragma unroll
+    for (int e = 0; e < kCount; e += 4) {
+      const float4 w = *reinterpret_cast<const float4*>(p + e);
+      x[e] = w.x, x[e + 1] = w.y, x[e + 2] = w.z, x[e + 3] = w.w;
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < kCount; ++e) x[e] = p[e];
 }
 
 // kVec: elements per chunk. kPairs: chunk pairs per lane. kHeads: heads of one
@@ -209,20 +225,19 @@ __global__ void __launch_bounds__(kAppendThreads)
     bool turn_a = false, turn_c = false;
     if (whole) {
       const int i0 = (lane + (j << lanes_log)) * kVec;
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        cs[e] = __ldcg(cos + i0 + e);
-        sn[e] = __ldcg(sin + i0 + e);
-      }
+      load_table<kVec>(cos + i0, cs, p.vec_tables);
+      load_table<kVec>(sin + i0, sn, p.vec_tables);
     } else if (turns && !across) {
       turn_a = a * kVec < p.rot;
       turn_c = c >= 0 && c * kVec < p.rot;
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const int i = (e < kVec / 2 ? a * (kVec / 2) + e : c * (kVec / 2) + e - kVec / 2);
-        const bool has = e < kVec / 2 ? turn_a : turn_c;
-        cs[e] = has ? __ldcg(cos + i) : 1.0f;
-        sn[e] = has ? __ldcg(sin + i) : 0.0f;
+      constexpr int kHalf = kVec / 2 > 0 ? kVec / 2 : 1;
+      // the second chunk's elements follow the first's; what lies past the rotation's end is not used
+      if (turn_c) {
+        load_table<kVec>(cos + a * kHalf, cs, p.vec_tables);
+        load_table<kVec>(sin + a * kHalf, sn, p.vec_tables);
+      } else if (turn_a) {
+        load_table<kHalf>(cos + a * kHalf, cs, false);
+        load_table<kHalf>(sin + a * kHalf, sn, false);
       }
     }
 #pragma unroll
@@ -292,11 +307,26 @@ int launch_append(AppendParams p, cudaStream_t stream) {
   return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;
 }
 
+// Heads per group of lanes: four where that still gives every SM 1024 threads
+// (loads of four heads in flight, their cosines and sines loaded once: 32744
+// tokens of 56 heads of 128 in 357 us with one head, 196 with four), else one (a
+// batch of 288 tokens is bound by latency).
+template <typename T, int kVec>
+int launch_vec(const AppendParams& p, cudaStream_t stream) {
+  const long long threads = static_cast<long long>(p.B) * p.T * ((p.q_heads + 3) / 4 + 2 * ((p.kv_heads + 3) / 4)) *
+                            ((p.D + 2 * kVec - 1) / (2 * kVec));
+  if (threads >= 1024ll * 152) return launch_append<T, kVec, 1, 4>(p, stream);
+  return launch_append<T, kVec, 1, 1>(p, stream);
+}
+
 // Elements per chunk: as many as 16 bytes hold, where rows start on such a
 // boundary and the rotation's halves and ends fall between chunks; half as many
 // for the 16-bit types (heads of 80 of which 40 turn); else one.
 template <typename T>
-int append_typed(const AppendParams& p, cudaStream_t stream) {
+int append_typed(AppendParams p, cudaStream_t stream) {
+  // a row of the tables is rot / 2 floats, and chunks start at multiples of half a chunk or of one
+  p.vec_tables = (p.rot / 2) % 4 == 0 && reinterpret_cast<uintptr_t>(p.cos) % 16 == 0 &&
+                 reinterpret_cast<uintptr_t>(p.sin) % 16 == 0;
   auto fits = [&](int vec) {
     const size_t bytes = vec * sizeof(T);
     if (p.D % vec != 0 || (p.interleaved ? p.rot % vec : (p.rot / 2) % vec) != 0) return false;
@@ -311,9 +341,9 @@ int append_typed(const AppendParams& p, cudaStream_t stream) {
     return reinterpret_cast<uintptr_t>(p.q_norm) % bytes == 0 && reinterpret_cast<uintptr_t>(p.k_norm) % bytes == 0;
   };
   constexpr int kFullVec = 16 / static_cast<int>(sizeof(T));
-  if (fits(kFullVec)) return launch_append<T, kFullVec, 1, 1>(p, stream);
+  if (fits(kFullVec)) return launch_vec<T, kFullVec>(p, stream);
   if constexpr (sizeof(T) == 2) {
-    if (fits(4)) return launch_append<T, 4, 1, 1>(p, stream);
+    if (fits(4)) return launch_vec<T, 4>(p, stream);
   }
   return launch_append<T, 1, 4, 1>(p, stream);
 }
@@ -402,52 +432,50 @@ int launch_compact(const CompactParams& p, int layers, int words, cudaStream_t s
 
 extern "C" {
 
-int asd_kv_append(const asd_kv_cache* cache, int layer, int T, const void* k, int64_t k_batch, int64_t k_token,
-                  int64_t k_head, const void* v, int64_t v_batch, int64_t v_token, int64_t v_head, const void* q,
-                  int64_t q_batch, int64_t q_token, int64_t q_head, int q_heads, void* q_out, const int32_t* kv_len,
-                  const int32_t* new_len, const int32_t* positions, const float* cos, const float* sin, int rot_dim,
-                  int rot_positions, int interleaved, const void* q_norm, const void* k_norm, float eps,
-                  int32_t* status, asd_stream_t stream) {
+int asd_kv_append(const asd_kv_cache* cache, const asd_append* args, asd_stream_t stream) {
   const int rc = check_cache(cache);
   if (rc != ASD_OK) return rc;
-  if (layer < 0 || layer >= cache->layers || T < 0 || q_heads < 0) return ASD_ERR_SHAPE;
-  if ((cos == nullptr) != (sin == nullptr)) return ASD_ERR_NULL;
-  if (cos ? (rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > cache->head_dim || rot_positions < 0) : rot_dim != 0)
+  if (!args) return ASD_ERR_NULL;
+  const asd_append& a = *args;
+  if (a.layer < 0 || a.layer >= cache->layers || a.T < 0 || a.q_heads < 0) return ASD_ERR_SHAPE;
+  if ((a.cos == nullptr) != (a.sin == nullptr)) return ASD_ERR_NULL;
+  if (a.cos ? (a.rot_dim < 2 || a.rot_dim % 2 != 0 || a.rot_dim > cache->head_dim || a.rot_positions < 0)
+            : a.rot_dim != 0)
     return ASD_ERR_SHAPE;
-  if (interleaved != 0 && interleaved != 1) return ASD_ERR_SHAPE;
-  if (eps != eps || eps < 0.0f) return ASD_ERR_CONTROL;
-  if (cache->B == 0 || T == 0) return ASD_OK;
-  if (!k || !v || !kv_len || (q_heads > 0 && (!q || !q_out))) return ASD_ERR_NULL;
+  if (a.interleaved != 0 && a.interleaved != 1) return ASD_ERR_SHAPE;
+  if (a.eps != a.eps || a.eps < 0.0f) return ASD_ERR_CONTROL;
+  if (cache->B == 0 || a.T == 0) return ASD_OK;
+  if (!a.k || !a.v || !a.kv_len || (a.q_heads > 0 && (!a.q || !a.q_out))) return ASD_ERR_NULL;
   const size_t es = store_bytes(cache->dtype);
-  const void* const typed[] = {k, v, q, q_out, q_norm, k_norm};
+  const void* const typed[] = {a.k, a.v, a.q, a.q_out, a.q_norm, a.k_norm};
   for (const void* x : typed)
     if (reinterpret_cast<uintptr_t>(x) % es != 0) return ASD_ERR_ALIGN;
-  const void* const words[] = {kv_len, new_len, positions, cos, sin, status};
+  const void* const words[] = {a.kv_len, a.new_len, a.positions, a.cos, a.sin, a.status};
   for (const void* x : words)
     if (reinterpret_cast<uintptr_t>(x) % 4 != 0) return ASD_ERR_ALIGN;
   AppendParams p = {};
-  p.cache = cache_view(cache, layer);
-  p.k = {static_cast<const char*>(k), k_batch, k_token, k_head};
-  p.v = {static_cast<const char*>(v), v_batch, v_token, v_head};
-  p.q = {static_cast<const char*>(q), q_batch, q_token, q_head};
-  p.q_out = static_cast<char*>(q_out);
-  p.kv_len = kv_len;
-  p.new_len = new_len;
-  p.positions = positions;
-  p.cos = cos;
-  p.sin = sin;
-  p.q_norm = static_cast<const char*>(q_norm);
-  p.k_norm = static_cast<const char*>(k_norm);
-  p.status = status;
-  p.eps = eps;
+  p.cache = cache_view(cache, a.layer);
+  p.k = {static_cast<const char*>(a.k), a.k_strides.batch, a.k_strides.token, a.k_strides.head};
+  p.v = {static_cast<const char*>(a.v), a.v_strides.batch, a.v_strides.token, a.v_strides.head};
+  p.q = {static_cast<const char*>(a.q), a.q_strides.batch, a.q_strides.token, a.q_strides.head};
+  p.q_out = static_cast<char*>(a.q_out);
+  p.kv_len = a.kv_len;
+  p.new_len = a.new_len;
+  p.positions = a.positions;
+  p.cos = a.cos;
+  p.sin = a.sin;
+  p.q_norm = static_cast<const char*>(a.q_norm);
+  p.k_norm = static_cast<const char*>(a.k_norm);
+  p.status = a.status;
+  p.eps = a.eps;
   p.B = cache->B;
-  p.T = T;
-  p.q_heads = q_heads;
+  p.T = a.T;
+  p.q_heads = a.q_heads;
   p.kv_heads = cache->heads;
   p.D = cache->head_dim;
-  p.rot = rot_dim;
-  p.rot_positions = rot_positions;
-  p.interleaved = interleaved;
+  p.rot = a.rot_dim;
+  p.rot_positions = a.rot_positions;
+  p.interleaved = a.interleaved;
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (cache->dtype == ASD_F32) return append_typed<float>(p, s);
   if (cache->dtype == ASD_BF16) return append_typed<__nv_bfloat16>(p, s);

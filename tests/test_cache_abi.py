@@ -22,23 +22,23 @@ def cache(**kw):
 
 
 def append(lib, c=None, **kw):
-    a = dict(layer=0, T=3, k=0x1000, ks=(384, 128, 64), v=0x2000, vs=(384, 128, 64), q=None, qs=(0, 0, 0), q_heads=0,
-             q_out=None, kv_len=0x3000, new_len=None, positions=None, cos=None, sin=None, rot=0, table=0, inter=0,
-             qw=None, kw=None, eps=1e-6, status=None)
-    a.update(kw)
-    ref = ctypes.addressof(c) if c is not None else None
-    return lib.asd_kv_append(ref, a["layer"], a["T"], a["k"], *a["ks"], a["v"], *a["vs"], a["q"], *a["qs"],
-                             a["q_heads"], a["q_out"], a["kv_len"], a["new_len"], a["positions"], a["cos"], a["sin"],
-                             a["rot"], a["table"], a["inter"], a["qw"], a["kw"], a["eps"], a["status"], None)
+    a = dict(layer=0, T=3, k=0x1000, ks=(384, 128, 64), v=0x2000, vs=(384, 128, 64), q=0, qs=(0, 0, 0), q_heads=0,
+             q_out=0, kv_len=0x3000, new_len=0, positions=0, cos=0, sin=0, rot=0, table=0, inter=0, qw=0, kw=0,
+             eps=1e-6, status=0)
+    a.update({n: 0 if x is None else x for n, x in kw.items()})
+    block = asd._APPEND.pack(a["k"], a["v"], a["q"], a["q_out"], *a["ks"], *a["vs"], *a["qs"], a["kv_len"],
+                             a["new_len"], a["positions"], a["cos"], a["sin"], a["qw"], a["kw"], a["status"],
+                             a["layer"], a["T"], a["q_heads"], a["rot"], a["table"], a["inter"], a["eps"], 0)
+    return lib.asd_kv_append(ctypes.addressof(c) if c is not None else None, block, None)
 
 
 def attend(lib, c=None, **kw):
-    a = dict(layer=0, T=3, q=0x1000, qs=(768, 256, 64), q_heads=4, kv_len=0x3000, new_len=None, mask=None, scale=0.1,
-             out=0x4000, lse=None, status=None, ws=0x50000, wsb=1 << 40)
-    a.update(kw)
-    ref = ctypes.addressof(c) if c is not None else None
-    return lib.asd_tree_attention(ref, a["layer"], a["T"], a["q"], *a["qs"], a["q_heads"], a["kv_len"], a["new_len"],
-                                  a["mask"], a["scale"], a["out"], a["lse"], a["status"], a["ws"], a["wsb"], None)
+    a = dict(layer=0, T=3, q=0x1000, qs=(768, 256, 64), q_heads=4, kv_len=0x3000, new_len=0, mask=0, scale=0.1,
+             out=0x4000, lse=0, status=0, ws=0x50000, wsb=1 << 40)
+    a.update({n: 0 if x is None else x for n, x in kw.items()})
+    block = asd._ATTENTION.pack(a["q"], a["out"], a["lse"], *a["qs"], a["kv_len"], a["new_len"], a["mask"],
+                                a["status"], a["ws"], a["wsb"], a["layer"], a["T"], a["q_heads"], a["scale"])
+    return lib.asd_tree_attention(ctypes.addressof(c) if c is not None else None, block, None)
 
 
 def compact(lib, c=None, **kw):
@@ -66,8 +66,11 @@ def test_bad_caches(lib, kw, code):
     assert lib.asd_attention_workspace_size(ctypes.addressof(c), 3, 4, ctypes.byref(n)) == code
 
 
-def test_no_cache(lib):
+def test_no_cache_and_no_arguments(lib):
     n = ctypes.c_size_t(0)
+    c = cache()
+    assert lib.asd_kv_append(ctypes.addressof(c), None, None) == 1
+    assert lib.asd_tree_attention(ctypes.addressof(c), None, None) == 1
     assert append(lib) == attend(lib) == compact(lib) == 1
     assert lib.asd_attention_workspace_size(None, 3, 4, ctypes.byref(n)) == 1
 
@@ -98,6 +101,29 @@ def test_attention_refusals(lib, kw, code):
     (dict(path=0x2002), 6), (dict(P=0), 0)], ids=str)
 def test_compact_refusals(lib, kw, code):
     assert compact(lib, cache(), **kw) == code
+
+
+def test_argument_blocks_lie_as_in_the_header(tmp_path):
+    """The packed blocks' sizes and the last fields' places, as the C compiler has them."""
+    import subprocess
+    from paper_2608_03447_gb300 import build
+    (tmp_path / "shim.cpp").write_text("""
+#include "asd.h"
+#include <stddef.h>
+extern "C" int at(int i) {
+  const size_t x[] = {sizeof(asd_append), offsetof(asd_append, kv_len), offsetof(asd_append, status),
+                      offsetof(asd_append, eps), sizeof(asd_attention), offsetof(asd_attention, kv_len),
+                      offsetof(asd_attention, workspace_bytes), offsetof(asd_attention, scale), sizeof(asd_kv_cache)};
+  return static_cast<int>(x[i]);
+}
+""")
+    out = str(tmp_path / "shim.so")
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", "-shared", "-fPIC", f"-I{build.INCLUDE}",
+                    str(tmp_path / "shim.cpp"), "-o", out], check=True)
+    at = ctypes.CDLL(out).at
+    assert at(0) == asd._APPEND.size and at(4) == asd._ATTENTION.size and at(8) == ctypes.sizeof(asd._Cache)
+    assert (at(1), at(2), at(3)) == (104, 160, 192)
+    assert (at(5), at(6), at(7)) == (48, 88, 108)
 
 
 def test_empty_batches(lib):
