@@ -398,6 +398,7 @@ typedef struct {
  * * w; then (a, b) <- (a cos - b sin, b cos + a sin); one rounding at the end.
  * Values are copied bit for bit.
  */
+/* B * T * (q_heads + 2 * heads) <= 2^30. */
 typedef struct {
   int64_t batch, token, head; /* strides in elements of a [B, T, heads, head_dim] array of the cache's dtype: any, as
                                * in the rows of a fused projection; the last dimension is contiguous */

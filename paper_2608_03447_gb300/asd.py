@@ -583,7 +583,8 @@ class KVCache:
     k, v        [layers, pages, page_size, heads, head_dim], or without the first dimension for one layer; float32,
                 bfloat16 or float16, the last dimension contiguous, any strides otherwise (the same for both): a
                 [pages, heads, page_size, head_dim] cache is passed as its ``transpose(-3, -2)``.
-    page_table  int32 [B, table_width]: slot s of request b is place s % page_size of page page_table[b, s // page_size].
+    page_table  int32 [B, table_width]: slot s of request b is place s % page_size of page
+                page_table[b, s // page_size].
     """
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor):

@@ -420,7 +420,8 @@ int check_attention(const asd_kv_cache* cache, int T, int q_heads) {
 size_t attention_bytes(const asd_kv_cache* cache, int T, int q_heads) {
   const long long rows = static_cast<long long>(T) * (q_heads / cache->heads);
   // the tile of a smaller T may have more rows
-  const size_t simt = attn_layout(kAttnMaxCtas, rows <= 16 ? 16 : rows <= 64 ? 64 : 80, simt_pitch(cache->head_dim) - 4).total;
+  const int tile = rows <= 16 ? 16 : rows <= 64 ? 64 : 80;
+  const size_t simt = attn_layout(kAttnMaxCtas, tile, simt_pitch(cache->head_dim) - 4).total;
   const size_t tc = attention_tc_bytes(cache, T, q_heads);
   return simt > tc ? simt : tc;
 }

@@ -244,7 +244,9 @@ __device__ __forceinline__ void drain(unsigned long long* bar, bool elected) {
 }
 // The same value in every lane, to the compiler too: MMAs and TMA loads take their operands from uniform registers.
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_or_sync(kFull, x); }
-__device__ __forceinline__ int uniform(int x) { return static_cast<int>(__reduce_or_sync(kFull, static_cast<unsigned>(x))); }
+__device__ __forceinline__ int uniform(int x) {
+  return static_cast<int>(__reduce_or_sync(kFull, static_cast<unsigned>(x)));
+}
 __device__ __forceinline__ bool elect_lane() {
   uint32_t one;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
@@ -581,7 +583,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_expect_tx(&sh.q_full[to], static_cast<uint32_t>(p.group_rows) * (kDim * 2));
 #pragma unroll
             for (int half = 0; half < kDim / 64; ++half)
-              load_queries(sq + to * kSlab + half * kHalfSlab, &map_q, &sh.q_full[to], half * 64, h, first / p.group, b);
+              load_queries(sq + to * kSlab + half * kHalfSlab, &map_q, &sh.q_full[to], half * 64, h, first / p.group,
+                           b);
           }
           __syncwarp();
         } else {
@@ -609,7 +612,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     Ring<kKeys> ring;
     bool ok = true;
     uint32_t q_phase = 0, pv_phase = 3;  // a bit a slab; a group
-    int turn = 0, slab = 0;              // the group whose turn it is; the slab of the unit that the groups take in turn
+    int turn = 0;                        // the group whose turn it is
+    int slab = 0;                        // of a unit that the groups take in turn
     while (ok) {
       const TcUnit* u = feed.wait(sh, p);
       if (!u) break;
@@ -1129,7 +1133,8 @@ bool make_query_map(CUtensorMap* map, bool bf16, const AttnParams& p) {
                                  stride(p.q_batch, p.B)};
   for (const cuuint64_t s : strides)
     if (s == 0) return false;  // one row for several: copied
-  const cuuint32_t boxes[5] = {64, static_cast<cuuint32_t>(p.group), 1, static_cast<cuuint32_t>(p.group_rows / p.group), 1};
+  const cuuint32_t boxes[5] = {64, static_cast<cuuint32_t>(p.group), 1,
+                               static_cast<cuuint32_t>(p.group_rows / p.group), 1};
   const cuuint32_t steps[5] = {1, 1, 1, 1, 1};
   return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5,
             const_cast<char*>(p.q), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -1172,7 +1177,9 @@ int launch(const CUtensorMap (&maps)[3], AttnParams p, int box, char* workspace,
 // more than 128 heads has its rows copied).
 int group_rows(int group) { return group <= kGroupRows ? kGroupRows / group * group : kGroupRows; }
 // Rows of a unit: what one softmax group holds, or both where there are more.
-int unit_rows(long long rows, int group) { return rows > group_rows(group) ? 2 * group_rows(group) : group_rows(group); }
+int unit_rows(long long rows, int group) {
+  return rows > group_rows(group) ? 2 * group_rows(group) : group_rows(group);
+}
 
 // Slots of a TMA box: what the page size and the tile have in common, and at
 // least the swizzle's eight rows; 0: none.

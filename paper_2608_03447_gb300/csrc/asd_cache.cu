@@ -5,9 +5,14 @@
 // bounds it, or the launch where there are few tokens. A head's row is handled
 // by a group of lanes that holds it in registers: the norm needs its sum of
 // squares (shuffles within the group) and the rotation pairs elements half a
-// rotation apart, so a lane takes a chunk and the chunk that turns with it.
+// rotation apart, so a lane takes a chunk and the chunk that turns with it. Norm
+// weight, cosine and sine of an element make two factors, the same for every head
+// of the token: an output is r (x p + z q), z the element that x turns with, r
+// the head's 1 / sqrt(mean + eps).
 #include <cuda_runtime.h>
 #include <stdint.h>
+
+#include <atomic>
 
 #include "asd.h"
 #include "asd_cache.cuh"
@@ -37,12 +42,13 @@ struct AppendParams {
   const char* q_norm;
   const char* k_norm;
   int32_t* status;
-  float eps;
+  float eps, inv_dim;
   int B, T, q_heads, kv_heads, D;
   int rot, rot_positions, interleaved;
   int q_slices, kv_slices;  // groups of kHeads heads
   bool vec_tables;          // rows of cosines and sines start on 16 bytes and are read from multiples of 4
-  long long items;          // B * T * (q_slices + 2 kv_slices)
+  int items;                // B * T * (q_slices + 2 kv_slices)
+  PageDiv by_slices, by_tokens;
 };
 
 // kVec consecutive elements, as they are stored.
@@ -85,238 +91,371 @@ __device__ __forceinline__ void load_table(const float* p, float* x, bool vec) {
   for (int e = 0; e < kCount; ++e) x[e] = p[e];
 }
 
+// A chunk's elements in fp32, two to a register pair.
+template <int kVec> struct Wide {
+  static constexpr int kPairs = (kVec + 1) / 2;
+  float2 e[kPairs];  // a single element: the second is 0
+};
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(r)
+      : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
+  return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(r)
+      : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)),
+        "l"(*reinterpret_cast<unsigned long long*>(&c)));
+  return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 widen2(const float* x) { return make_float2(x[0], x[1]); }
+__device__ __forceinline__ float2 widen2(const __nv_bfloat16* x) {
+  return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(x));
+}
+__device__ __forceinline__ float2 widen2(const __half* x) {
+  return __half22float2(*reinterpret_cast<const __half2*>(x));
+}
+__device__ __forceinline__ void narrow2(float* x, float2 v) { x[0] = v.x, x[1] = v.y; }
+__device__ __forceinline__ void narrow2(__nv_bfloat16* x, float2 v) {
+  *reinterpret_cast<__nv_bfloat162*>(x) = __float22bfloat162_rn(v);
+}
+__device__ __forceinline__ void narrow2(__half* x, float2 v) { *reinterpret_cast<__half2*>(x) = __float22half2_rn(v); }
+
+template <typename T, int kVec>
+__device__ __forceinline__ Wide<kVec> widen(const Chunk<T, kVec>& c) {
+  Wide<kVec> w;
+  if constexpr (kVec == 1) {
+    w.e[0] = make_float2(Store<T>::widen(c.e[0]), 0.0f);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec / 2; ++i) w.e[i] = widen2(c.e + 2 * i);
+  }
+  return w;
+}
+
+// Which heads of which token an item is: head0 .. of the queries (which = 0), keys
+// or values.
+struct AppendItem {
+  int b, t, token, which, slice, head0, heads;
+  const char* src;  // of head0
+};
+template <typename T, int kHeads>
+__device__ __forceinline__ AppendItem append_item(const AppendParams& p, int item) {
+  AppendItem i;
+  i.token = p.by_slices.quot(item);
+  i.slice = item - i.token * p.by_slices.size;
+  i.b = p.by_tokens.quot(i.token);
+  i.t = i.token - i.b * p.T;
+  i.which = i.slice < p.q_slices ? 0 : i.slice < p.q_slices + p.kv_slices ? 1 : 2;
+  i.slice -= i.which == 0 ? 0 : i.which == 1 ? p.q_slices : p.q_slices + p.kv_slices;
+  const Rows& rows = i.which == 0 ? p.q : i.which == 1 ? p.k : p.v;
+  i.head0 = i.slice * kHeads;
+  i.heads = (i.which == 0 ? p.q_heads : p.kv_heads) - i.head0;  // the slice's, at most kHeads
+  i.src = rows.data + (i.b * rows.batch + i.t * rows.token + i.head0 * rows.head) * static_cast<long long>(sizeof(T));
+  return i;
+}
+
 // kVec: elements per chunk. kPairs: chunk pairs per lane. kHeads: heads of one
-// token that a group of lanes handles, their loads in flight together and their
-// cosines and sines loaded once.
-template <typename T, int kVec, int kPairs, int kHeads>
-__global__ void __launch_bounds__(kAppendThreads)
+// token that a group of lanes handles, their factors made once. kStages: 0: an
+// item per group of lanes, loaded into registers. Else a group works through items
+// one after the other, the next kStages - 1 on their way into shared memory: each
+// thread copies and reads its own chunks, so nothing has to meet.
+template <typename T, int kVec, int kPairs, int kHeads, int kStages>
+__global__ void __launch_bounds__(kAppendThreads, kStages > 0 ? 3 : 2)
     append_kernel(const __grid_constant__ AppendParams p, int lanes_log) {
+  static_assert(kStages == 0 || kPairs == 1, "a stage holds one chunk pair a lane and head");
+  constexpr int kWide = Wide<kVec>::kPairs;
+  constexpr int kChunk = static_cast<int>(sizeof(Chunk<T, kVec>));
+  extern __shared__ __align__(16) unsigned char append_smem[];
   pdl_signal_dependents();
   const int lanes = 1 << lanes_log;
   const int lane = threadIdx.x & (lanes - 1);
-  const long long item = static_cast<long long>(blockIdx.x) * (kAppendThreads >> lanes_log) + (threadIdx.x >> lanes_log);
-  bool live = item < p.items;
-  const int slices = p.q_slices + 2 * p.kv_slices;
-  const long long token = live ? item / slices : 0;
-  int slice = live ? static_cast<int>(item - token * slices) : 0;
-  const int b = static_cast<int>(token / p.T), t = static_cast<int>(token - static_cast<long long>(b) * p.T);
-  const int which = slice < p.q_slices ? 0 : slice < p.q_slices + p.kv_slices ? 1 : 2;  // q, k, v
-  slice -= which == 0 ? 0 : which == 1 ? p.q_slices : p.q_slices + p.kv_slices;
-  const Rows& rows = which == 0 ? p.q : which == 1 ? p.k : p.v;
-  const int head0 = slice * kHeads;
-  const int heads = (which == 0 ? p.q_heads : p.kv_heads) - head0;  // the slice's, at most kHeads
+  const int groups = kAppendThreads >> lanes_log, group = threadIdx.x >> lanes_log;
+  const int stride = static_cast<int>(gridDim.x) * groups;
   const int chunks = p.D / kVec;
   // chunk pairs: those that turn together first, then the rest two by two
   const int turning = p.rot / (2 * kVec);
   const bool across = !p.interleaved || kVec == 1;  // the two chunks of a pair turn with one another
-  const bool turns = which != 2 && p.rot > 0;
-
-  pdl_wait_prerequisites();
-
-  const int start = live ? __ldcg(p.kv_len + b) : 0;
-  const int n = live && p.new_len ? __ldcg(p.new_len + b) : p.T;
-  int pos = 0;
-  if (live && p.positions && p.rot > 0) pos = __ldcg(p.positions + token);
-
-  // the rows themselves do not wait for lengths and positions
-  Chunk<T, kVec> x[kHeads][kPairs][2];
   int at[kPairs][2];
 #pragma unroll
   for (int j = 0; j < kPairs; ++j) {
     const int q = lane + (j << lanes_log);
-    if (across && !p.interleaved && q < turning) {
-      at[j][0] = q;
-      at[j][1] = q + turning;
-    } else {
-      at[j][0] = 2 * q;
-      at[j][1] = 2 * q + 1;
-    }
+    const bool apart = !p.interleaved && q < turning;
+    at[j][0] = apart ? q : 2 * q;
+    at[j][1] = apart ? q + turning : 2 * q + 1;
     if (at[j][0] >= chunks) at[j][0] = -1;
     if (at[j][1] >= chunks) at[j][1] = -1;
   }
-  const T* src = reinterpret_cast<const T*>(rows.data) + b * rows.batch + t * rows.token;
+  auto stage_chunk = [&](int stage, int h, int s) {
+    return append_smem + (((stage * kHeads + h) * 2 + s) * kAppendThreads + threadIdx.x) * kChunk;
+  };
+  auto fetch = [&](int item, int stage) {
+    if (item < p.items) {
+      const AppendItem i = append_item<T, kHeads>(p, item);
+      const Rows& rows = i.which == 0 ? p.q : i.which == 1 ? p.k : p.v;
+      const T* src = reinterpret_cast<const T*>(i.src);
 #pragma unroll
-  for (int h = 0; h < kHeads; ++h)
+      for (int h = 0; h < kHeads; ++h)
 #pragma unroll
-    for (int j = 0; j < kPairs; ++j)
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-        if (live && h < heads && at[j][s] >= 0)
-          x[h][j][s] = load_chunk<T, kVec>(src + (head0 + h) * rows.head + at[j][s] * kVec);
-        else
-          for (int e = 0; e < kVec; ++e) x[h][j][s].e[e] = Store<T>::narrow(0.0f);
-
-  const bool bad_length = start < 0 || n < 0 || n > p.T || static_cast<long long>(start) + n > p.cache.slots;
-  const bool reports = live && which == 1 && slice == 0 && lane == 0 && p.status;
-  if (reports && t == 0 && bad_length) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_LENGTH));
-  live = live && !bad_length && t < n;
-  if (!p.positions) pos = start + t;
-  if (p.rot > 0 && live && static_cast<unsigned>(pos) >= static_cast<unsigned>(p.rot_positions)) {
-    if (reports) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_POSITION));
-    live = false;
-  }
-  T* dst = nullptr;
-  long long dst_head = p.D;
-  if (live) {
-    if (which == 0) {
-      dst = reinterpret_cast<T*>(p.q_out) + (token * p.q_heads + head0) * p.D;
-    } else {
-      const long long off = slot_offset(p.cache, b, start + t);
-      if (off < 0) {
-        if (reports) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_PAGE));
-        live = false;
-      } else {
-        dst_head = p.cache.head_stride;
-        dst = reinterpret_cast<T*>(which == 1 ? p.cache.k : p.cache.v) + off + head0 * dst_head;
-      }
+        for (int s = 0; s < 2; ++s)
+          if (h < i.heads && at[0][s] >= 0)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(stage_chunk(stage, h, s))),
+                         "l"(src + h * rows.head + at[0][s] * kVec), "n"(kChunk >= 4 ? kChunk : 4)
+                         : "memory");
     }
-  }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
 
-  const T* weight = reinterpret_cast<const T*>(which == 0 ? p.q_norm : which == 1 ? p.k_norm : nullptr);
-  if (which == 2 || (!weight && !turns)) {  // moved as they are (the groups of a warp may differ: no shuffle below)
-    if (live)
+  pdl_wait_prerequisites();
+  int item = static_cast<int>(blockIdx.x) * groups + group, stage = 0;
+  if constexpr (kStages > 0) {
+#pragma unroll
+    for (int k = 0; k < kStages - 1; ++k) fetch(item + k * stride, k);
+  }
+  // every lane of a warp goes as often round as its first group: the norm's shuffles need the whole group
+  for (int first = item - group; first < p.items; first += stride, item += stride) {
+    bool live = item < p.items;
+    const AppendItem it = append_item<T, kHeads>(p, live ? item : 0);
+    const int b = it.b, t = it.t, token = it.token, which = it.which, slice = it.slice, head0 = it.head0,
+              heads = it.heads;
+    const bool turns = which != 2 && p.rot > 0;
+
+    // lengths, positions, pages and tables serve many rows: ordinary loads, which find them in L1
+    const int start = live ? p.kv_len[b] : 0;
+    const int n = live && p.new_len ? p.new_len[b] : p.T;
+    int pos = 0;
+    if (live && p.positions && p.rot > 0) pos = p.positions[token];
+
+    // the rows themselves do not wait for lengths and positions
+    Chunk<T, kVec> x[kHeads][kPairs][2];
+    if constexpr (kStages > 0) {
+      const int next = stage == 0 ? kStages - 1 : stage - 1;
+      fetch(item + (kStages - 1) * stride, next);
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages > 0 ? kStages - 1 : 0) : "memory");
+    } else {
+      const Rows& rows = which == 0 ? p.q : which == 1 ? p.k : p.v;
+      const T* src = reinterpret_cast<const T*>(it.src);
 #pragma unroll
       for (int h = 0; h < kHeads; ++h)
 #pragma unroll
         for (int j = 0; j < kPairs; ++j)
 #pragma unroll
-          for (int s = 0; s < 2; ++s)
-            if (h < heads && at[j][s] >= 0)
-              *reinterpret_cast<Chunk<T, kVec>*>(dst + h * dst_head + at[j][s] * kVec) = x[h][j][s];
-  }
-  const bool norm = weight != nullptr;
-  const unsigned members = __ballot_sync(kFull, norm);  // whole groups
-  float r[kHeads];
-#pragma unroll
-  for (int h = 0; h < kHeads; ++h) r[h] = 1.0f;
-  if (norm) {
-#pragma unroll
-    for (int h = 0; h < kHeads; ++h) {
-      float sum = 0.0f;
-#pragma unroll
-      for (int j = 0; j < kPairs; ++j)
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) {
-            const float f = Store<T>::widen(x[h][j][s].e[e]);
-            sum = fmaf(f, f, sum);
+          for (int s = 0; s < 2; ++s) {
+            x[h][j][s] = Chunk<T, kVec>{};
+            if (live && h < heads && at[j][s] >= 0)
+              x[h][j][s] = load_chunk<T, kVec>(src + h * rows.head + at[j][s] * kVec);
           }
-      for (int off = lanes >> 1; off > 0; off >>= 1) sum += __shfl_xor_sync(members, sum, off);
-      r[h] = 1.0f / sqrtf(sum / static_cast<float>(p.D) + p.eps);
     }
-  }
-  if (!live || which == 2 || (!weight && !turns)) return;
+    auto own_chunk = [&](int h, int j, int s) -> Chunk<T, kVec> {
+      if constexpr (kStages > 0) {
+        if (item >= p.items || h >= heads || at[j][s] < 0) return Chunk<T, kVec>{};
+        return *reinterpret_cast<const Chunk<T, kVec>*>(stage_chunk(stage, h, s));
+      } else {
+        return x[h][j][s];
+      }
+    };
 
-  const float* cos = p.cos + static_cast<long long>(pos) * (p.rot / 2);
-  const float* sin = p.sin + static_cast<long long>(pos) * (p.rot / 2);
-#pragma unroll
-  for (int j = 0; j < kPairs; ++j) {
-    const int a = at[j][0], c = at[j][1];
-    if (a < 0) continue;
-    Chunk<T, kVec> wa = {}, wc = {};
-    if (norm) {
-      wa = *reinterpret_cast<const Chunk<T, kVec>*>(weight + a * kVec);
-      if (c >= 0) wc = *reinterpret_cast<const Chunk<T, kVec>*>(weight + c * kVec);
+    const bool bad_length = start < 0 || n < 0 || n > p.T || static_cast<long long>(start) + n > p.cache.slots;
+    const bool reports = live && which == 1 && slice == 0 && lane == 0 && p.status;
+    if (reports && t == 0 && bad_length) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_LENGTH));
+    live = live && !bad_length && t < n;
+    if (!p.positions) pos = start + t;
+    if (p.rot > 0 && live && static_cast<unsigned>(pos) >= static_cast<unsigned>(p.rot_positions)) {
+      if (reports) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_POSITION));
+      live = false;
     }
-    // the chunk pair's cosines and sines: one for each element of the first chunk, or one for every two of both
-    const bool whole = turns && across && lane + (j << lanes_log) < turning;
-    float cs[kVec], sn[kVec];
-    bool turn_a = false, turn_c = false;
-    if (whole) {
-      const int i0 = (lane + (j << lanes_log)) * kVec;
-      load_table<kVec>(cos + i0, cs, p.vec_tables);
-      load_table<kVec>(sin + i0, sn, p.vec_tables);
-    } else if (turns && !across) {
-      turn_a = a * kVec < p.rot;
-      turn_c = c >= 0 && c * kVec < p.rot;
-      constexpr int kHalf = kVec / 2 > 0 ? kVec / 2 : 1;
-      // the second chunk's elements follow the first's; what lies past the rotation's end is not used
-      if (turn_c) {
-        load_table<kVec>(cos + a * kHalf, cs, p.vec_tables);
-        load_table<kVec>(sin + a * kHalf, sn, p.vec_tables);
-      } else if (turn_a) {
-        load_table<kHalf>(cos + a * kHalf, cs, false);
-        load_table<kHalf>(sin + a * kHalf, sn, false);
+    T* dst = nullptr;
+    long long dst_head = p.D;
+    if (live) {
+      if (which == 0) {
+        dst = reinterpret_cast<T*>(p.q_out) + (static_cast<long long>(token) * p.q_heads + head0) * p.D;
+      } else {
+        const long long off = slot_offset(p.cache, b, start + t);
+        if (off < 0) {
+          if (reports) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_PAGE));
+          live = false;
+        } else {
+          dst_head = p.cache.head_stride;
+          dst = reinterpret_cast<T*>(which == 1 ? p.cache.k : p.cache.v) + off + head0 * dst_head;
+        }
       }
     }
+
+    const T* weight = reinterpret_cast<const T*>(which == 0 ? p.q_norm : which == 1 ? p.k_norm : nullptr);
+    const bool norm = weight != nullptr;
+    const unsigned members = __ballot_sync(kFull, norm);  // whole groups; the others of the warp may not be
+    if (!norm && !turns) {  // moved as they are
+      if (live)
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h) {
-      if (h >= heads) break;
-      float u[kVec], w[kVec];
+        for (int h = 0; h < kHeads; ++h)
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        u[e] = Store<T>::widen(x[h][j][0].e[e]);
-        w[e] = Store<T>::widen(x[h][j][1].e[e]);
+          for (int j = 0; j < kPairs; ++j)
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+              if (h < heads && at[j][s] >= 0)
+                *reinterpret_cast<Chunk<T, kVec>*>(dst + h * dst_head + at[j][s] * kVec) = own_chunk(h, j, s);
+    } else {
+      // The factors. Of chunk s of pair j: fp multiplies its own elements, fq those that they turn with (the other
+      // chunk's, or each element's neighbour).
+      Wide<kVec> fp[kPairs][2], fq[kPairs][2];
+      bool turned[kPairs][2];
+#pragma unroll
+      for (int j = 0; j < kPairs; ++j) {
+        const int a = at[j][0], c = at[j][1];
+        Wide<kVec> wa, wc;
+#pragma unroll
+        for (int i = 0; i < kWide; ++i) wa.e[i] = wc.e[i] = make_float2(1.0f, 1.0f);
+        if (norm && a >= 0) wa = widen<T, kVec>(*reinterpret_cast<const Chunk<T, kVec>*>(weight + a * kVec));
+        if (norm && c >= 0) wc = widen<T, kVec>(*reinterpret_cast<const Chunk<T, kVec>*>(weight + c * kVec));
+#pragma unroll
+        for (int i = 0; i < kWide; ++i) {
+          fp[j][0].e[i] = wa.e[i];
+          fp[j][1].e[i] = wc.e[i];
+        }
+        turned[j][0] = turned[j][1] = false;
+        if (!turns || !live) continue;
+        const float* cos = p.cos + static_cast<long long>(pos) * (p.rot / 2);
+        const float* sin = p.sin + static_cast<long long>(pos) * (p.rot / 2);
+        const int q = lane + (j << lanes_log);
+        if (across) {
+          if (q >= turning) continue;
+          turned[j][0] = turned[j][1] = true;
+          float cs[kVec + 1], sn[kVec + 1];
+          cs[kVec] = sn[kVec] = 0.0f;
+          load_table<kVec>(cos + q * kVec, cs, p.vec_tables);
+          load_table<kVec>(sin + q * kVec, sn, p.vec_tables);
+#pragma unroll
+          for (int i = 0; i < kWide; ++i) {
+            const float2 co = make_float2(cs[2 * i], cs[2 * i + 1]), si = make_float2(sn[2 * i], sn[2 * i + 1]);
+            fp[j][0].e[i] = mul2(wa.e[i], co);
+            fq[j][0].e[i] = mul2(wc.e[i], make_float2(-si.x, -si.y));
+            fp[j][1].e[i] = mul2(wc.e[i], co);
+            fq[j][1].e[i] = mul2(wa.e[i], si);
+          }
+        } else if constexpr (kVec > 1) {
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            if (at[j][s] < 0 || at[j][s] * kVec >= p.rot) continue;
+            turned[j][s] = true;
+            const Wide<kVec>& w = s ? wc : wa;
+            float cs[kVec / 2], sn[kVec / 2];
+            load_table<kVec / 2>(cos + at[j][s] * (kVec / 2), cs, p.vec_tables);
+            load_table<kVec / 2>(sin + at[j][s] * (kVec / 2), sn, p.vec_tables);
+#pragma unroll
+            for (int i = 0; i < kWide; ++i) {
+              fp[j][s].e[i] = mul2(w.e[i], make_float2(cs[i], cs[i]));
+              fq[j][s].e[i] = make_float2(-w.e[i].y * sn[i], w.e[i].x * sn[i]);
+            }
+          }
+        }
+      }
+
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h) {
+        Wide<kVec> y[kPairs][2];
+        float2 sum2 = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j)
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            y[j][s] = widen<T, kVec>(own_chunk(h, j, s));
+#pragma unroll
+            for (int i = 0; i < kWide; ++i) sum2 = fma2(y[j][s].e[i], y[j][s].e[i], sum2);
+          }
+        float r = 1.0f;
         if (norm) {
-          u[e] = u[e] * r[h] * Store<T>::widen(wa.e[e]);
-          w[e] = w[e] * r[h] * Store<T>::widen(wc.e[e]);
+          float sum = sum2.x + sum2.y;
+          for (int off = lanes >> 1; off > 0; off >>= 1) sum += __shfl_xor_sync(members, sum, off);
+          r = rsqrtf(fmaf(sum, p.inv_dim, p.eps));
         }
-      }
-      if (whole) {
+        if (!live || h >= heads) continue;
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const float f = u[e], g = w[e];
-          u[e] = f * cs[e] - g * sn[e];
-          w[e] = g * cs[e] + f * sn[e];
-        }
-      } else if (turn_a || turn_c) {
+        for (int j = 0; j < kPairs; ++j)
 #pragma unroll
-        for (int e = 0; e + 1 < kVec; e += 2) {
-          const float f = u[e], g = u[e + 1];
-          if (turn_a) {
-            u[e] = f * cs[e / 2] - g * sn[e / 2];
-            u[e + 1] = g * cs[e / 2] + f * sn[e / 2];
+          for (int s = 0; s < 2; ++s) {
+            if (at[j][s] < 0) continue;
+            Chunk<T, kVec> o;
+#pragma unroll
+            for (int i = 0; i < kWide; ++i) {
+              const float2 own = y[j][s].e[i];
+              const float2 with = across ? y[j][s ^ 1].e[i] : make_float2(own.y, own.x);
+              // an element that does not turn must not see another's NaN or infinity
+              const float2 made = turned[j][s] ? fma2(own, fp[j][s].e[i], mul2(with, fq[j][s].e[i]))
+                                               : mul2(own, fp[j][s].e[i]);
+              const float2 v = mul2(made, make_float2(r, r));
+              if constexpr (kVec == 1)
+                o.e[0] = Store<T>::narrow(v.x);
+              else
+                narrow2(o.e + 2 * i, v);
+            }
+            *reinterpret_cast<Chunk<T, kVec>*>(dst + h * dst_head + at[j][s] * kVec) = o;
           }
-          const float f2 = w[e], g2 = w[e + 1];
-          if (turn_c) {
-            w[e] = f2 * cs[kVec / 2 + e / 2] - g2 * sn[kVec / 2 + e / 2];
-            w[e + 1] = g2 * cs[kVec / 2 + e / 2] + f2 * sn[kVec / 2 + e / 2];
-          }
-        }
-      }
-      Chunk<T, kVec> o;
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) o.e[e] = Store<T>::narrow(u[e]);
-      *reinterpret_cast<Chunk<T, kVec>*>(dst + h * dst_head + a * kVec) = o;
-      if (c >= 0) {
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) o.e[e] = Store<T>::narrow(w[e]);
-        *reinterpret_cast<Chunk<T, kVec>*>(dst + h * dst_head + c * kVec) = o;
       }
     }
+    if constexpr (kStages > 0) stage = stage == kStages - 1 ? 0 : stage + 1;
   }
 }
 
-int div_up(int a, int b) { return (a + b - 1) / b; }
+constexpr int kSms = 152;
 
-template <typename T, int kVec, int kPairs, int kHeads>
+int div_up(int a, int b) { return a / b + (a % b != 0); }
+
+template <typename T, int kVec, int kPairs, int kHeads, int kStages>
 int launch_append(AppendParams p, cudaStream_t stream) {
+  auto kernel = append_kernel<T, kVec, kPairs, kHeads, kStages>;
   p.q_slices = div_up(p.q_heads, kHeads);
   p.kv_slices = div_up(p.kv_heads, kHeads);
-  p.items = static_cast<long long>(p.B) * p.T * (p.q_slices + 2 * p.kv_slices);
+  const int slices = p.q_slices + 2 * p.kv_slices;
+  p.items = p.B * p.T * slices;  // the entry point has seen that it fits
+  p.by_slices = page_div(slices);
+  p.by_tokens = page_div(p.T);
   int lanes_log = 0;
   while (lanes_log < 5 && (kPairs << lanes_log) * 2 * kVec < p.D) ++lanes_log;
-  const long long groups = kAppendThreads >> lanes_log;
-  const long long grid = (p.items + groups - 1) / groups;
-  if (grid > 0x7fffffffll) return ASD_ERR_SHAPE;
+  int grid = div_up(p.items, kAppendThreads >> lanes_log);
+  const size_t smem = static_cast<size_t>(kStages) * kHeads * 2 * kAppendThreads * sizeof(Chunk<T, kVec>);
+  if constexpr (kStages > 0) {
+    constexpr int kMaxDevices = 64;
+    static std::atomic<int> resident[kMaxDevices];  // CTAs at once; 0: not asked yet
+    int dev = 0, per = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return ASD_ERR_CUDA;
+    if (dev < 0 || dev >= kMaxDevices) return ASD_ERR_DEVICE;
+    int ctas = resident[dev].load(std::memory_order_acquire);
+    if (ctas == 0) {
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) !=
+              cudaSuccess ||
+          cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+          cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, kAppendThreads, smem) != cudaSuccess || per < 1)
+        return ASD_ERR_CUDA;
+      ctas = sms * per;
+      resident[dev].store(ctas, std::memory_order_release);
+    }
+    grid = grid < ctas ? grid : ctas;
+  }
   cudaLaunchAttribute attr;
-  const cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(kAppendThreads), stream, &attr);
-  if (cudaLaunchKernelEx(&cfg, append_kernel<T, kVec, kPairs, kHeads>, p, lanes_log) != cudaSuccess)
-    return ASD_ERR_CUDA;
+  cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(kAppendThreads), stream, &attr);
+  cfg.dynamicSmemBytes = smem;
+  if (cudaLaunchKernelEx(&cfg, kernel, p, lanes_log) != cudaSuccess) return ASD_ERR_CUDA;
   return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;
 }
 
-// Heads per group of lanes: four where that still gives every SM 1024 threads
-// (loads of four heads in flight, their cosines and sines loaded once: 32744
-// tokens of 56 heads of 128 in 357 us with one head, 196 with four), else one (a
-// batch of 288 tokens is bound by latency).
+// Large 16-bit calls go through shared memory, four heads per group of lanes: what
+// a row needs in registers beside its factors would leave too few threads to cover
+// memory's latency (32744 tokens of 56 heads of 128: 168 us against 309 with two
+// heads in registers; 512 tokens 5.5 against 6.1). Small ones are bound by latency
+// and take two heads in registers (256 tokens 3.7 us against 5.6), 32-bit ones too,
+// whose chunks hold half the elements (4206 tokens of 24 heads of 96 in 12.3 us
+// against 14.5). The line lies at 352 threads of the former kind per SM.
 template <typename T, int kVec>
 int launch_vec(const AppendParams& p, cudaStream_t stream) {
-  const long long threads = static_cast<long long>(p.B) * p.T * ((p.q_heads + 3) / 4 + 2 * ((p.kv_heads + 3) / 4)) *
-                            ((p.D + 2 * kVec - 1) / (2 * kVec));
-  if (threads >= 1024ll * 152) return launch_append<T, kVec, 1, 4>(p, stream);
-  return launch_append<T, kVec, 1, 1>(p, stream);
+  if constexpr (sizeof(T) == 2) {
+    const long long threads = static_cast<long long>(p.B) * p.T *
+                              (div_up(p.q_heads, 4) + 2 * div_up(p.kv_heads, 4)) * div_up(p.D, 2 * kVec);
+    if (threads >= 352ll * kSms) return launch_append<T, kVec, 1, 4, 2>(p, stream);
+  }
+  return launch_append<T, kVec, 1, 2, 0>(p, stream);
 }
 
 // Elements per chunk: as many as 16 bytes hold, where rows start on such a
@@ -345,7 +484,7 @@ int append_typed(AppendParams p, cudaStream_t stream) {
   if constexpr (sizeof(T) == 2) {
     if (fits(4)) return launch_vec<T, 4>(p, stream);
   }
-  return launch_append<T, 1, 4, 1>(p, stream);
+  return launch_append<T, 1, 4, 1, 0>(p, stream);
 }
 
 // ---------------------------------------------------------------- compaction
@@ -443,6 +582,7 @@ int asd_kv_append(const asd_kv_cache* cache, const asd_append* args, asd_stream_
             : a.rot_dim != 0)
     return ASD_ERR_SHAPE;
   if (a.interleaved != 0 && a.interleaved != 1) return ASD_ERR_SHAPE;
+  if (static_cast<double>(cache->B) * a.T * (a.q_heads + 2.0 * cache->heads) > 1073741824.0) return ASD_ERR_SHAPE;
   if (a.eps != a.eps || a.eps < 0.0f) return ASD_ERR_CONTROL;
   if (cache->B == 0 || a.T == 0) return ASD_OK;
   if (!a.k || !a.v || !a.kv_len || (a.q_heads > 0 && (!a.q || !a.q_out))) return ASD_ERR_NULL;
@@ -468,6 +608,7 @@ int asd_kv_append(const asd_kv_cache* cache, const asd_append* args, asd_stream_
   p.k_norm = static_cast<const char*>(a.k_norm);
   p.status = a.status;
   p.eps = a.eps;
+  p.inv_dim = 1.0f / static_cast<float>(cache->head_dim);
   p.B = cache->B;
   p.T = a.T;
   p.q_heads = a.q_heads;

@@ -68,10 +68,11 @@ struct CacheView {
 };
 
 // The element offset of a slot of request b (head 0), or -1 where its page id
-// is out of range. slot < slots.
+// is out of range. slot < slots. The page table is read by ordinary loads: a
+// page's entry serves its slots.
 __device__ __forceinline__ long long slot_offset(const CacheView& c, int b, int slot) {
   const int at = c.div.quot(slot);
-  const int page = __ldcg(c.table + static_cast<long long>(b) * c.table_width + at);
+  const int page = c.table[static_cast<long long>(b) * c.table_width + at];
   if (static_cast<unsigned>(page) >= static_cast<unsigned>(c.pages)) return -1;
   return page * c.page_stride + static_cast<long long>(slot - at * c.div.size) * c.token_stride;
 }

@@ -158,6 +158,61 @@ def test_layer_and_pages_past_32_bits(asd):
     a.check(q, k[1, -a.pages:].cpu(), v[1, -a.pages:].cpu())
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_infinities_and_nan_stay_with_the_elements_they_turn_with(asd, dtype, interleaved):
+    """Without a norm an element reaches itself and its partner, and one past the rotation itself alone."""
+    for D, rot in ((64, 32), (33, 10), (96, 48)):
+        a = Append(dtype, 2, 1, 1, D, rot, 8, ctx=[3], norm=False, interleaved=interleaved, seed=7)
+        clean, _, _, _ = a.run(asd)
+        bad_at = [1, rot // 2, rot, D - 1]
+        for bad in (math.nan, math.inf):
+            for at in bad_at:
+                rows = a.rows.clone()
+                rows[0, 0, 0, at] = bad
+                q, _, _, _ = a.run(asd, rows=rows.cuda())
+                if at >= rot:
+                    hit = {at}
+                elif interleaved:
+                    hit = {at, at ^ 1}
+                else:
+                    hit = {at, at + rot // 2 if at < rot // 2 else at - rot // 2}
+                for i in range(D):
+                    if i in hit:
+                        assert not math.isfinite(float(q[0, 0, 0, i]))
+                    else:
+                        assert torch.equal(q[0, 0, 0, i], clean[0, 0, 0, i]), (D, at, i)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype,D,rot", [(BF16, 128, 128), (F16, 64, 32), (F32, 96, 96), (BF16, 80, 40), (BF16, 66, 6)])
+def test_prompts(asd, dtype, D, rot, interleaved):
+    """Thousands of tokens: several items a group of lanes, the last round ragged."""
+    T, Hq, Hkv = 1501, 9, 3
+    a = Append(dtype, T, Hq, Hkv, D, rot, 16, ctx=[5, 0, 70], new=[T, 700, T - 1], interleaved=interleaved, seed=8)
+    q, k, v, status = a.run(asd)
+    assert not status.any()
+    x = a.rows.double()
+    w = torch.cat([a.q_norm.double().expand(Hq, D), a.k_norm.double().expand(Hkv, D)])
+    x = x[:, :, :Hq + Hkv] / (x[:, :, :Hq + Hkv].square().mean(-1, keepdim=True) + a.eps).sqrt() * w
+    cos, sin = a.cos.double()[a.positions.long()][:, :, None], a.sin.double()[a.positions.long()][:, :, None]
+    y = x.clone()
+    lo, hi = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
+    y[..., lo], y[..., hi] = x[..., lo] * cos - x[..., hi] * sin, x[..., hi] * cos + x[..., lo] * sin
+    big = y.abs().amax(-1, keepdim=True) * math.sqrt(2.0)
+    tol = ref.UNIT[dtype] * y.abs() + (D + 16) * 2.0 ** -24 * big + (2.0 ** -24 if dtype == F16 else 1e-30)
+    t = torch.arange(T)
+    for b in range(3):
+        n = int(a.new_len[b])
+        assert bool(((q[b, :n].double() - y[b, :n, :Hq]).abs() <= tol[b, :n, :Hq]).all())
+        assert bool((q[b, n:] == 7).all())
+        slots = int(a.kv_len[b]) + t[:n]
+        pages, places = a.table[b].long()[slots // 16], slots % 16
+        assert bool(((k[pages, places].double() - y[b, :n, Hq:]).abs() <= tol[b, :n, Hq:]).all())
+        assert torch.equal(v[pages, places], a.rows[b, :n, Hq + Hkv:])
+    assert int((k != 7).any(-1).any(-1).sum()) == int(a.new_len.sum())
+
+
 def test_append_data_errors(asd):
     a = Append(F32, 3, 2, 1, 32, 32, 8, ctx=[4, 5, 6, 7, 8, 9], new=[3, 3, 3, 3, 3, 3], seed=5)
     a.kv_len[0] = -2
@@ -252,7 +307,8 @@ def test_compact_data_errors(asd):
     table = torch.arange(B * width, dtype=torch.int32).view(B, width)
     table[5, 2] = -1
     kv_len = torch.tensor([-1, 0, 0, 0, 22, 5, 5], dtype=torch.int32)
-    path = torch.tensor([[0, 1, 2], [0, 2, 2], [0, 0, 5], [1, 2, 3], [0, 1, 2], [1, 4, 6], [0, 2, 4]], dtype=torch.int32)
+    path = torch.tensor([[0, 1, 2], [0, 2, 2], [0, 0, 5], [1, 2, 3], [0, 1, 2], [1, 4, 6], [0, 2, 4]],
+                        dtype=torch.int32)
     path_len = torch.tensor([3, 3, 3, 4, 3, 3, 3], dtype=torch.int32)
     k0, v0 = k.cpu(), v.cpu()
     status = torch.zeros(B, dtype=torch.int32, device="cuda")
