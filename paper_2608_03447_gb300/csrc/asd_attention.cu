@@ -98,7 +98,8 @@ __global__ void __launch_bounds__(kSimtThreads, kCols <= 2 ? 2 : 1)
   __syncthreads();
   if (deal.begin == deal.end) return;
 
-  for (AttnWalk<kSimtTile> w(p, deal); w.more(); w.next()) {
+  AttnWalk<kSimtTile> w(p, deal);
+  for (w.start(); w.more(); w.next()) {
     const int row0 = w.row0(), rows = w.rows();
     const int span = w.span();
     __syncthreads();  // the unit before is done with shared memory

@@ -208,9 +208,13 @@ struct AttnWalk {
   AttnRequest r;
   int tiles;  // the unit's
   int j0;     // the first of them that is this CTA's
-  int left;   // tiles of the CTA's range from there on
+  int left = 0;  // tiles of the CTA's range from there on
 
-  __device__ __forceinline__ AttnWalk(const AttnParams& p_, const AttnDeal& d_) : p(p_), d(d_) {
+  __device__ __forceinline__ AttnWalk(const AttnParams& p_, const AttnDeal& d_) : p(p_), d(d_) {}
+  // to the first unit, if the range has any
+  __device__ __forceinline__ void start() {
+    left = d.end - d.begin;
+    if (left == 0) return;
     b = d.b;
     load();
     // find the unit that holds the first tile
@@ -226,7 +230,6 @@ struct AttnWalk {
       ++row_tile;
     }
     j0 = at;
-    left = d.end - d.begin;
   }
   __device__ __forceinline__ void load() {
     const int i = b - d.b;

@@ -15,10 +15,10 @@
 // and every tile of keys and values serves both.
 //
 // A CTA per SM: warps 0-3 and 4-7 are the softmax groups (a warp reads the TMEM
-// lanes of its quarter), warp 8 loads keys and values into two rings of stages,
-// warp 9 issues the MMAs of the scores, warp 10 those of the products, warp 11
-// loads queries. Loads are TMA boxes of as many slots as the page size and the
-// tile have as a common divisor (a page of 48 is three boxes of 16); where that
+// lanes of its quarter), warp 8 walks the units and loads keys, warp 9 issues the
+// MMAs of the scores, warp 10 those of the products, warp 11 loads queries and
+// values. Loads are TMA boxes of as many slots as the page size and the tile have
+// as a common divisor (a page of 48 is three boxes of 16); where that
 // is less than the swizzle's eight rows, 16-byte copies.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -43,7 +43,7 @@ using namespace asd_detail;
 constexpr int kTile = 128;      // slots
 constexpr int kGroupRows = 128;  // that a softmax group has threads for; a call may use fewer (AttnParams::group_rows)
 constexpr int kSoftmaxThreads = 256;
-constexpr int kLoadWarp = 8, kScoreWarp = 9, kProductWarp = 10, kQueryWarp = 11;
+constexpr int kKeyWarp = 8, kScoreWarp = 9, kProductWarp = 10, kValueWarp = 11;
 constexpr int kThreads = 12 * 32;  // three warps a scheduler: 168 registers each
 constexpr int kTmemCols = 512;
 constexpr int kMaxStages = 12;
@@ -54,7 +54,7 @@ constexpr int slab_bytes(int dim) { return kTile * dim * 2; }  // 128 rows of a 
 constexpr int kHalfSlab = kTile * 128;                         // 64 elements of all of them
 constexpr size_t kSmemMax = 232448;
 
-// What the roles know of a unit: the loading warp walks the CTA's range and
+// What the roles know of a unit: the keys' warp walks the CTA's range and
 // publishes its units through a small ring, so that the walk's code exists once
 // (the roles' code has to fit the instruction cache beside one another).
 struct alignas(16) TcUnit {
@@ -94,12 +94,12 @@ constexpr int value_stages(int dim) { return stages_for(dim) - key_stages(dim); 
 constexpr size_t smem_for(int dim) {
   return 1024 + static_cast<size_t>(2 + stages_for(dim)) * slab_bytes(dim) + sizeof(TcShared);
 }
-// With 16-byte copies: fills in flight before the warp waits for the oldest and
-// announces it. A fill must not wait for a stage whose own fill, or one that its
-// release depends on, has not been announced: keys 0 are fill 0 and their stage's
-// next keys fill 2 n - 1 (n: stages), and a shared tile's keys i + 1 are used after
-// values i, which were loaded after them.
-constexpr int lag_for(int dim) { return 2 * key_stages(dim) - 2 < 8 ? 2 * key_stages(dim) - 2 : 8; }
+// With 16-byte copies: a warp's fills in flight before it waits for the oldest and
+// announces it. A fill must not wait for a stage whose own fill has not been
+// announced; and as the keys of tile i are released after the values of i - 1, the
+// two warps' lags together must stay below both rings' stages.
+constexpr int kLagMax = 8;
+constexpr int lag_for(int dim) { return key_stages(dim) - 1 < kLagMax ? key_stages(dim) - 1 : kLagMax; }
 static_assert(stages_for(128) == 5, "ring depth at the widest head");
 
 // ---------------------------------------------------------------- tcgen05
@@ -351,7 +351,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = __shfl_sync(kFull, static_cast<int>(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
   pdl_signal_dependents();
-  if (warp == kQueryWarp) {  // a barrier or two a lane
+  if (warp == kValueWarp) {  // a barrier or two a lane
     if (lane < kMaxStages) {
       mbar_init(&sh.k_full[lane], kTma ? 1 : 32);
       mbar_init(&sh.k_empty[lane], 1);
@@ -385,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  if (kTma && warp == kLoadWarp && lane == 0) {
+  if (kTma && warp == kKeyWarp && lane == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_k)) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_v)) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_q)) : "memory");
@@ -415,161 +415,48 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   };
 
-  if (warp == kLoadWarp) {
-    // ---------------- units, keys and values
-    attn_deal<kTile>(p, sh.deal);
+  if (warp == kKeyWarp || warp == kValueWarp) {
+    // ---------------- units and keys; queries and values
+    const bool of_v = warp == kValueWarp;
+    const bool elected = elect_lane();
+    if (!of_v) attn_deal<kTile>(p, sh.deal);
     bool ok = true;
-    UnitFeed out;  // the next free slot
+    UnitFeed feed;  // keys: the next free slot
     auto publish = [&](const TcUnit& u) {
-      if (ok) ok = warp_wait(&sh.unit_empty[out.slot], out.phase ^ 1u, sh, p);
+      if (ok) ok = warp_wait(&sh.unit_empty[feed.slot], feed.phase ^ 1u, sh, p);
       if (lane == 0) {
-        sh.unit[out.slot] = u;
-        mbar_arrive(&sh.unit_full[out.slot]);
+        sh.unit[feed.slot] = u;
+        mbar_arrive(&sh.unit_full[feed.slot]);
       }
       __syncwarp();
-      if (++out.slot == kUnits) {
-        out.slot = 0;
-        out.phase ^= 1u;
+      if (++feed.slot == kUnits) {
+        feed.slot = 0;
+        feed.phase ^= 1u;
       }
     };
-    if (sh.deal.begin == sh.deal.end) {
-      publish(TcUnit{});
-    } else {
-      AttnWalk<kTile> w(p, sh.deal);
-      int j = 0, j1 = 0, span = 0;  // the next tile of the unit that w is at
-      bool fresh = true;            // that has not been published
-      Ring<kKeys> keys;
-      Ring<kValues> values;
-      struct Share {
-        int b, h;
-        int slot0, rows;  // of the tile: rows exist; 0: there is no tile
-        int page, at;     // TMA: where this lane's box begins; the page table is read two tiles ahead
-      };
-      const bool elected = elect_lane();
-      const Share none = {0, 0, 0, 0, 0, 0};
-      auto take = [&] {
-        Share x = none;
-        if (ok && j == j1) {
-          if (!fresh) w.next();
-          fresh = false;
-          TcUnit u = {};
-          if (!w.more()) {
-            publish(u);
-            return x;
-          }
-          span = w.span();
-          j1 = w.j1();
-          u.b = w.b, u.h = w.h, u.row0 = w.row0(), u.rows = w.rows();
-          u.span = span, u.ctx = w.r.ctx, u.n = w.r.n, u.valid = 1;
-          u.j0 = w.j0, u.j1 = j1, u.whole = w.whole(), u.piece = w.piece();
-          if (!u.whole) {
-            u.c0 = w.first_cta();
-            u.c1 = w.last_cta();
-          }
-          publish(u);
-          j = w.j0;
-        }
-        if (!ok) return x;
-        x.b = w.b, x.h = w.h;
-        x.slot0 = j * kTile;
-        x.rows = min(kTile, span - x.slot0);
-        if (kTma && lane * box < x.rows) {
-          const int slot = x.slot0 + lane * box, n = p.cache.div.quot(slot);
-          x.page = __ldcg(p.cache.table + static_cast<long long>(x.b) * p.cache.table_width + n);
-          x.at = slot - n * p.cache.div.size;
-        }
-        ++j;
-        return x;
-      };
-      constexpr int kLag = lag_for(kDim);
-      int issued = 0, arrived = 0;
-      // Tiles go K(0), then K(i + 1) V(i): the scores of a tile are computed while the one before is weighed.
-      auto bar_of = [&](int fill) {  // copies: the barrier of the fill of that number
-        const bool of_v = fill >= 2 && (fill & 1) == 0;
-        return of_v ? &sh.v_full[(fill / 2 - 1) % kValues] : &sh.k_full[((fill + 1) / 2) % kKeys];
-      };
-      auto arrive = [&] {  // copies: this thread's of the oldest fill have landed
-        fence_for_mma();
-        mbar_arrive(bar_of(arrived++));
-      };
-      auto fill = [&](bool of_v, const Share& x) {
-        const int stage = of_v ? values.stage : keys.stage;
-        const uint32_t phase = of_v ? values.phase : keys.phase;
-        if (ok) ok = warp_wait(of_v ? &sh.v_empty[stage] : &sh.k_empty[stage], phase ^ 1u, sh, p);
-        if (!ok) return;
-        const uint32_t dst = (of_v ? sv : sk) + stage * kSlab;
-        if (of_v)
-          values.next();
-        else
-          keys.next();
-        if constexpr (kTma) {
-          unsigned long long* bar = of_v ? &sh.v_full[stage] : &sh.k_full[stage];
-          const int n = uniform((x.rows + box - 1) / box), h = uniform(x.h);
-          if (elected) mbar_expect_tx(bar, static_cast<uint32_t>(n * box) * (kDim * 2));
-          __syncwarp();
-          // a page out of range lies outside the tensor: the box is filled with zeros
-          const CUtensorMap* map = of_v ? &map_v : &map_k;
-#pragma unroll 4
-          for (int i = 0; i < n; ++i) {
-            const int page = __shfl_sync(kFull, x.page, i), at = __shfl_sync(kFull, x.at, i);
-            if (elected) {
-#pragma unroll
-              for (int half = 0; half < kDim / 64; ++half)
-                load_box(dst + half * kHalfSlab + i * box * 128, map, bar, half * 64, at, h, page);
-            }
-          }
-          if (!of_v && lane < n && static_cast<unsigned>(x.page) >= static_cast<unsigned>(p.cache.pages) && p.status)
-            atomicOr(p.status + x.b, static_cast<int>(ASD_STATUS_PAGE));
-          __syncwarp();
-        } else {
-#pragma unroll 1
-          for (int q = 0; q < x.rows; q += 32) {
-            long long off = -1;
-            if (q + lane < x.rows) {
-              off = slot_offset(p.cache, x.b, x.slot0 + q + lane);
-              if (off < 0 && !of_v && p.status) atomicOr(p.status + x.b, static_cast<int>(ASD_STATUS_PAGE));
-              if (off >= 0) off += x.h * p.cache.head_stride;
-            }
-            copy_rows(dst, q, of_v ? p.cache.v : p.cache.k, off, x.rows - q);
-          }
-          copies_commit();
-          if (++issued - arrived > kLag) {
-            copies_wait<kLag>();
-            arrive();
-          }
-        }
-      };
-      Share cur = none, next = take();  // cur: its keys have been loaded
-      while (ok && (cur.rows | next.rows)) {
-        const Share after = next.rows ? take() : next;
-#pragma unroll 1
-        for (int i = 0; i < 2; ++i) {
-          const Share& x = i ? cur : next;
-          if (x.rows) fill(i, x);
-        }
-        cur = next;
-        next = after;
-      }
-      if (!kTma) {
-        // the last fill is a tile's values with no keys between them and the values before
-        copies_wait<0>();
-        while (arrived < issued - 1) arrive();
-        if (issued > 0) {
-          fence_for_mma();
-          mbar_arrive(&sh.v_full[(issued / 2 - 1) % kValues]);
-        }
-      }
-    }
-  } else if (warp == kQueryWarp) {
-    // ---------------- queries: a unit's slab, or both slabs of a unit that the groups share
-    UnitFeed feed;
-    const bool elected = elect_lane();
-    bool ok = true;
-    uint32_t uses = 0;  // a bit a slab: whether an odd number of fills
-    int slab = 0;
-    while (const TcUnit* u = feed.wait(sh, p)) {
-      const int b = u->b, h = u->h, row0 = u->row0, rows = u->rows;
-      feed.done(sh);
+    // the ring
+    unsigned long long* const full = of_v ? sh.v_full : sh.k_full;
+    unsigned long long* const empty = of_v ? sh.v_empty : sh.k_empty;
+    const int stages = of_v ? kValues : kKeys;
+    int stage = 0;
+    uint32_t phase = 0;
+    // copies: fills that have not been announced, and the oldest one's stage
+    constexpr int kLag = lag_for(kDim);
+    int pending = 0, oldest = 0;
+    auto announce = [&] {  // this thread's part of the oldest has landed
+      fence_for_mma();
+      mbar_arrive(&full[oldest]);
+      if (++oldest == stages) oldest = 0;
+      --pending;
+    };
+    auto flush = [&] {
+      if (kTma || pending == 0) return;
+      copies_wait<0>();
+      while (pending > 0) announce();
+    };
+    uint32_t uses = 0;  // of the query slabs, a bit each: whether an odd number of fills
+    int slab = 0;       // of a unit that the groups take in turn
+    auto load_unit_queries = [&](int b, int h, int row0, int rows) {
       const bool pair = rows > p.group_rows;
 #pragma unroll 1
       for (int tile = 0; ok && tile * p.group_rows < rows; ++tile) {
@@ -603,7 +490,124 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (!pair) slab ^= 1;
+    };
+    struct Share {
+      int b, h;
+      int slot0, rows;  // of the tile: rows exist; 0: there is no tile
+      int page, at;     // TMA: where this lane's box begins; the page table is read a tile ahead
+    };
+    const Share none = {0, 0, 0, 0, 0, 0};
+    AttnWalk<kTile> w(p, sh.deal);       // keys
+    bool started = false;
+    int b = 0, h = 0, j = 0, j1 = 0, span = 0;  // the unit's next tile
+    auto take = [&] {
+      Share x = none;
+      int row0 = 0, rows = 0;  // a new unit's queries
+      if (ok && j == j1) {
+        // Where this warp waits for others, what it has copied has to be theirs.
+        flush();
+        if (of_v) {
+          const TcUnit* u = feed.wait(sh, p);
+          if (!u) return x;
+          b = u->b, h = u->h, j = u->j0, j1 = u->j1, span = u->span;
+          row0 = u->row0, rows = u->rows;
+          feed.done(sh);
+        } else {
+          if (started)
+            w.next();
+          else
+            w.start();
+          started = true;
+          TcUnit u = {};
+          if (!w.more()) {
+            publish(u);
+            return x;
+          }
+          b = w.b, h = w.h, j = w.j0, j1 = w.j1(), span = w.span();
+          u.b = b, u.h = h, u.row0 = w.row0(), u.rows = w.rows();
+          u.span = span, u.ctx = w.r.ctx, u.n = w.r.n, u.valid = 1;
+          u.j0 = j, u.j1 = j1, u.whole = w.whole(), u.piece = w.piece();
+          if (!u.whole) {
+            u.c0 = w.first_cta();
+            u.c1 = w.last_cta();
+          }
+          publish(u);
+        }
+      }
+      if (!ok) return x;
+      x.b = b, x.h = h;
+      x.slot0 = j * kTile;
+      x.rows = min(kTile, span - x.slot0);
+      if (kTma && lane * box < x.rows) {
+        const int slot = x.slot0 + lane * box, n = p.cache.div.quot(slot);
+        x.page = __ldcg(p.cache.table + static_cast<long long>(x.b) * p.cache.table_width + n);
+        x.at = slot - n * p.cache.div.size;
+      }
+      ++j;
+      if (rows) load_unit_queries(b, h, row0, rows);
+      return x;
+    };
+    auto fill = [&](const Share& x) {
+      if (ok) ok = warp_wait(&empty[stage], phase ^ 1u, sh, p);
+      if (!ok) return;
+      const uint32_t dst = (of_v ? sv : sk) + stage * kSlab;
+      if constexpr (kTma) {
+        unsigned long long* bar = &full[stage];
+        const int n = uniform((x.rows + box - 1) / box), head = uniform(x.h);
+        if (elected) mbar_expect_tx(bar, static_cast<uint32_t>(n * box) * (kDim * 2));
+        __syncwarp();
+        // a page out of range lies outside the tensor: the box is filled with zeros
+        const CUtensorMap* map = of_v ? &map_v : &map_k;
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+          const int page = __shfl_sync(kFull, x.page, i), at = __shfl_sync(kFull, x.at, i);
+          if (elected) {
+#pragma unroll
+            for (int half = 0; half < kDim / 64; ++half)
+              load_box(dst + half * kHalfSlab + i * box * 128, map, bar, half * 64, at, head, page);
+          }
+        }
+        if (!of_v && lane < n && static_cast<unsigned>(x.page) >= static_cast<unsigned>(p.cache.pages) && p.status)
+          atomicOr(p.status + x.b, static_cast<int>(ASD_STATUS_PAGE));
+        __syncwarp();
+      } else {
+#pragma unroll 1
+        for (int q = 0; q < x.rows; q += 32) {
+          long long off = -1;
+          if (q + lane < x.rows) {
+            off = slot_offset(p.cache, x.b, x.slot0 + q + lane);
+            if (off < 0 && !of_v && p.status) atomicOr(p.status + x.b, static_cast<int>(ASD_STATUS_PAGE));
+            if (off >= 0) off += x.h * p.cache.head_stride;
+          }
+          copy_rows(dst, q, of_v ? p.cache.v : p.cache.k, off, x.rows - q);
+        }
+        copies_commit();
+        if (++pending > kLag) {
+          copies_wait<kLag>();
+          announce();
+        }
+      }
+      if (++stage == stages) {
+        stage = 0;
+        phase ^= 1u;
+      }
+    };
+    Share cur = take();
+    while (ok && cur.rows) {
+      // The next tile is looked up first, but not over a unit's end by the values' warp: the unit's queries may have
+      // to wait for the one before, and that for this tile.
+      const bool late = of_v && j == j1;
+      Share next = none;
+#pragma unroll 1
+      for (int i = 0; i < 2; ++i) {
+        if ((i == 1) == late)
+          next = take();
+        else
+          fill(cur);
+      }
+      cur = next;
     }
+    flush();
   } else if (warp == kScoreWarp) {
     // ---------------- S = Q K^T
     constexpr uint32_t kDesc = instr_desc(kBf16, kTile, false);
