@@ -298,6 +298,19 @@ def test_more_requests_than_a_cta_has_threads(asd):
         p.check(out, lse)
 
 
+@pytest.mark.parametrize("B", [31, 32, 33, 64, 65, 97, 130])
+def test_any_number_of_requests(asd, B):
+    """A block of requests a lane: numbers at and around whole blocks, runs of requests without any work."""
+    g = torch.Generator().manual_seed(B)
+    ctx = [0 if i % 7 < 3 else int(torch.randint(0, 300, (1,), generator=g)) for i in range(B)]
+    new = [0 if i % 7 < 4 else i % 4 for i in range(B)]
+    for dtype in (BF16, F32):
+        p = Problem(dtype, 3, 4, 2, 64, 16, ctx=ctx, new=new, seed=B)
+        out, lse, status = p.run(asd)
+        p.check(out, lse)
+        assert not status.any()
+
+
 def test_layers(asd):
     p = Problem(BF16, 3, 4, 2, 64, 16, ctx=[40, 9], seed=11)
     k = torch.full((3, *p.k.shape), math.nan, dtype=BF16, device="cuda")
