@@ -376,7 +376,8 @@ int launch_simt(AttnParams p, char* workspace, cudaStream_t stream) {
   p.part_o = reinterpret_cast<float*>(workspace + l.o);
   const int rows = p.T * p.group;
   p.row_tiles = (rows + kRows - 1) / kRows;
-  p.unit_rows = kRows;
+  p.unit_rows = p.group_rows = kRows;
+  p.weighted = false;
   const size_t es = sizeof(T), four = 4 * es;
   const bool vec_q = p.D % 4 == 0 && rows_aligned(p.q, es, four, p.q_batch, p.q_token, p.q_head);
   const bool vec_kv = p.D % 4 == 0 &&

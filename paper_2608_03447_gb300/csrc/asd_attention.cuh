@@ -4,13 +4,18 @@
 //
 // Work. A unit is one row tile (some of a request's T * group query rows that
 // share a key/value head, row t * group + g; those of tokens that exist) against
-// all the tiles of key/value slots that it sees. All units' tiles, one request after the other, form one
-// sequence that is cut into equal contiguous ranges, one a CTA, whatever the
-// requests' lengths: no CTA has more than one tile more than another. Lengths
-// are device data, so every CTA adds them up itself. A unit that a range's end
-// cuts is in pieces: each CTA leaves its piece's softmax statistics and
-// unnormalised sums in the workspace, and the one that arrives last adds them up
-// in the order of the slots, so results do not depend on who that is.
+// all the tiles of key/value slots that it sees. All units' tiles, one request
+// after the other, form one sequence that is cut into contiguous ranges of equal
+// work, one a CTA, whatever the requests' lengths. A tile is one work item, but
+// three of a unit whose rows are too many for one softmax group and two of one
+// whose rows are not, where a call has both (61 tokens, 5 query heads on one, four
+// contexts of 90000: 348 us, with equal tiles 394). A tile belongs to the range
+// that its first item is in, and ranges have at least as many items as a tile, so
+// that none is without tiles. Lengths are device data, so every CTA adds them up
+// itself. A unit that a range's end cuts is in pieces: each CTA leaves its piece's
+// softmax statistics and unnormalised sums in the workspace, and the one that
+// arrives last adds them up in the order of the slots, so results do not depend on
+// who that is.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -24,6 +29,7 @@ namespace asd_detail {
 
 constexpr int kAttnMaxCtas = 320;  // of one launch: a counter and two pieces each
 constexpr int kAttnScan = 32;      // requests of a CTA's range whose lengths it keeps: one a lane
+constexpr int kAttnWorkMost = 3, kAttnWorkLeast = 2;  // of a tile, where a call has both kinds
 
 struct AttnParams {
   CacheView cache;
@@ -43,6 +49,7 @@ struct AttnParams {
   int B, T, q_heads, heads, group, D;
   int unit_rows, row_tiles;
   int group_rows;  // tensor cores: rows of a softmax group
+  bool weighted;   // whether a tile's work depends on that
   float scale_log2;
 };
 
@@ -77,11 +84,22 @@ __device__ __forceinline__ int attn_tiles(const AttnParams& p, const AttnRequest
   return span > 0 ? (span - 1) / kTile + 1 : 0;
 }
 
+__device__ __forceinline__ int attn_tile_work(const AttnParams& p, const AttnRequest& r, int row_tile) {
+  if (!p.weighted) return 1;
+  return r.n * p.group - row_tile * p.unit_rows > p.group_rows ? kAttnWorkMost : kAttnWorkLeast;
+}
+// Tiles that begin among a unit's first `items` items.
+__device__ __forceinline__ int attn_tiles_of(int items, int work) {
+  const unsigned n = static_cast<unsigned>(items);
+  return static_cast<int>(work == 1 ? n : work == kAttnWorkLeast ? (n + kAttnWorkLeast - 1) / kAttnWorkLeast
+                                                                 : (n + kAttnWorkMost - 1) / kAttnWorkMost);
+}
+
 template <int kTile>
-__device__ __forceinline__ int attn_request_tiles(const AttnParams& p, const AttnRequest& r) {
+__device__ __forceinline__ int attn_request_work(const AttnParams& p, const AttnRequest& r) {
   int w = 0;
 #pragma unroll 1
-  for (int i = 0; i < p.row_tiles; ++i) w += attn_tiles<kTile>(p, r, i);
+  for (int i = 0; i < p.row_tiles; ++i) w += attn_tiles<kTile>(p, r, i) * attn_tile_work(p, r, i);
   return w * p.heads;
 }
 
@@ -106,28 +124,28 @@ __device__ __forceinline__ void attn_zero_rows(const AttnParams& p, int tid, int
   }
 }
 
-// What a CTA works out before it starts. Tiles are counted in 32 bits (the entry
+// What a CTA works out before it starts. Work is counted in 32 bits (the entry
 // point refuses what would not fit).
 struct AttnDeal {
-  int total;       // tiles of all units
+  int total;       // work items of all units
   int begin, end;  // this CTA's; none where begin == end
   int ctas;        // that have any
-  int b;           // request of the first tile
-  int b_first;     // that request's first tile
+  int b;           // request of the first item
+  int b_first;     // that request's first item
   int cached;      // requests b .. b + cached - 1 are in `request`
   AttnRequest request[kAttnScan];
 };
 
-// Of w tiles dealt to `ctas` CTAs the first w % ctas get one more than the others.
-__device__ __forceinline__ int attn_first_tile(int cta, int w, int ctas) {
+// Of w items dealt to `ctas` CTAs the first w % ctas get one more than the others.
+__device__ __forceinline__ int attn_first_item(int cta, int w, int ctas) {
   return cta * (w / ctas) + min(cta, w % ctas);
 }
-__device__ __forceinline__ int attn_cta_of(int tile, int w, int ctas) {
+__device__ __forceinline__ int attn_cta_of(int item, int w, int ctas) {
   const int each = w / ctas, more = w - each * ctas, cut = more * (each + 1);
-  return tile < cut ? tile / (each + 1) : more + (tile - cut) / each;
+  return item < cut ? item / (each + 1) : more + (item - cut) / each;
 }
 
-// By one warp: adds up the requests' tiles, a block of consecutive requests a
+// By one warp: adds up the requests' work, a block of consecutive requests a
 // lane, finds the lane and then the request where this CTA's range begins. Two or
 // three rounds of loads for up to 256 requests: every CTA starts with this (160
 // requests took 4.5 us of 43 when a warp went through them 32 at a time, twice).
@@ -153,12 +171,12 @@ __device__ __forceinline__ void attn_deal(const AttnParams& p, AttnDeal& d) {
     for (int i = 0; i < kBatch; ++i) {
       const int b = from + i0 + i;
       if (b >= to) break;
-      mine += attn_request_tiles<kTile>(p, some[i]);
+      mine += attn_request_work<kTile>(p, some[i]);
       if (bad[i] && !error && blockIdx.x == 0 && p.status)
         atomicOr(p.status + b, static_cast<int>(ASD_STATUS_LENGTH));
     }
   }
-  // the tiles before the lane's
+  // the work before the lane's
   auto sum_before = [&](int x) {
     int inc = x;
 #pragma unroll
@@ -170,7 +188,7 @@ __device__ __forceinline__ void attn_deal(const AttnParams& p, AttnDeal& d) {
   };
   int before = sum_before(mine);
   const int w = __shfl_sync(kFull, before + mine, 31);
-  const int ctas = min(w, static_cast<int>(gridDim.x));
+  const int ctas = w == 0 ? 0 : max(1, min(p.weighted ? w / kAttnWorkMost : w, static_cast<int>(gridDim.x)));
   const int c = blockIdx.x;
   if (lane == 0) d.begin = d.end = 0;
   if (error || c >= ctas) {
@@ -179,7 +197,7 @@ __device__ __forceinline__ void attn_deal(const AttnParams& p, AttnDeal& d) {
     __syncwarp();
     return;
   }
-  const int begin = attn_first_tile(c, w, ctas);
+  const int begin = attn_first_item(c, w, ctas);
   unsigned holds = __ballot_sync(kFull, mine > 0 && before <= begin && begin < before + mine);
   int at = __ffs(holds) - 1;
   int b = at * per, b_first = __shfl_sync(kFull, before, at);
@@ -194,7 +212,7 @@ __device__ __forceinline__ void attn_deal(const AttnParams& p, AttnDeal& d) {
       bool bad;
       here = attn_request(p, min(b + lane, p.B - 1), &bad);
       then = attn_request(p, min(b + 32 + lane, p.B - 1), &bad);
-      mine = b + lane < end ? attn_request_tiles<kTile>(p, here) : 0;
+      mine = b + lane < end ? attn_request_work<kTile>(p, here) : 0;
       before = b_first + sum_before(mine);
       holds = __ballot_sync(kFull, mine > 0 && before <= begin && begin < before + mine);
       if (holds) break;
@@ -217,7 +235,7 @@ __device__ __forceinline__ void attn_deal(const AttnParams& p, AttnDeal& d) {
   if (lane == 0) {
     d.total = w;
     d.begin = begin;
-    d.end = attn_first_tile(c + 1, w, ctas);
+    d.end = attn_first_item(c + 1, w, ctas);
     d.ctas = ctas;
     d.b = b;
     d.b_first = b_first;
@@ -234,63 +252,75 @@ struct AttnWalk {
   int b, h, row_tile;
   AttnRequest r;
   int tiles;  // the unit's
-  int j0;     // the first of them that is this CTA's
-  int left = 0;  // tiles of the CTA's range from there on
+  int work;   // of each of them
+  int at;     // the unit's first item
+  int j0;     // the first tile that is this CTA's
 
   __device__ __forceinline__ AttnWalk(const AttnParams& p_, const AttnDeal& d_) : p(p_), d(d_) {}
   // to the first unit, if the range has any
   __device__ __forceinline__ void start() {
-    left = d.end - d.begin;
-    if (left == 0) return;
+    at = d.end;
+    if (d.begin == d.end) return;
     b = d.b;
     load();
-    // find the unit that holds the first tile
-    const int per_head = attn_request_tiles<kTile>(p, r) / p.heads;
-    int at = d.begin - d.b_first;
-    h = at / per_head;
-    at -= h * per_head;
+    // find the unit that holds the first item
+    const int per_head = attn_request_work<kTile>(p, r) / p.heads;
+    int in = d.begin - d.b_first;
+    h = in / per_head;
+    in -= h * per_head;
     row_tile = 0;
     for (;;) {
-      tiles = attn_tiles<kTile>(p, r, row_tile);
-      if (at < tiles) break;
-      at -= tiles;
+      measure();
+      if (in < tiles * work) break;
+      in -= tiles * work;
       ++row_tile;
     }
-    j0 = at;
+    at = d.begin - in;
+    j0 = attn_tiles_of(in, work);
+    if (j0 == tiles) next();  // inside its last tile, which is the range's before
+  }
+  __device__ __forceinline__ void measure() {
+    tiles = attn_tiles<kTile>(p, r, row_tile);
+    work = attn_tile_work(p, r, row_tile);
   }
   __device__ __forceinline__ void load() {
     const int i = b - d.b;
     bool bad;
     r = i < d.cached ? d.request[i] : attn_request(p, b, &bad);
   }
-  __device__ __forceinline__ bool more() const { return left > 0; }
-  __device__ __forceinline__ int j1() const { return min(tiles, j0 + left); }  // this CTA has tiles j0 .. j1 - 1
+  __device__ __forceinline__ bool more() const { return at < d.end; }
+  __device__ __forceinline__ int j1() const {  // this CTA has tiles j0 .. j1 - 1
+    const int in = d.end - at;
+    return in >= tiles * work ? tiles : attn_tiles_of(in, work);
+  }
   __device__ __forceinline__ void next() {
-    left -= j1() - j0;
-    if (left <= 0) return;
+    at += tiles * work;
+    if (at >= d.end) return;
     j0 = 0;
     do {
       if (++row_tile == p.row_tiles) {
         row_tile = 0;
         if (++h == p.heads) {
           h = 0;
-          ++b;
+          if (++b >= p.B) {  // the lengths have changed meanwhile
+            at = d.end;
+            return;
+          }
           load();
         }
       }
-      tiles = attn_tiles<kTile>(p, r, row_tile);
+      measure();
     } while (tiles == 0);  // no rows of tokens that exist
   }
-  __device__ __forceinline__ bool whole() const { return j0 == 0 && left >= tiles; }
+  __device__ __forceinline__ bool whole() const { return j0 == 0 && d.end - at >= (tiles - 1) * work + 1; }
   __device__ __forceinline__ int span() const { return attn_span(p, r, row_tile); }
   __device__ __forceinline__ int row0() const { return row_tile * p.unit_rows; }
   // rows of the unit, of tokens that exist
   __device__ __forceinline__ int rows() const { return min(p.unit_rows, r.n * p.group - row0()); }
   // the workspace slot of this CTA's piece, and the unit's CTAs
   __device__ __forceinline__ int piece() const { return 2 * static_cast<int>(blockIdx.x) + (j0 == 0 ? 1 : 0); }
-  __device__ __forceinline__ int unit_first() const { return d.end - left - j0; }
-  __device__ __forceinline__ int first_cta() const { return attn_cta_of(unit_first(), d.total, d.ctas); }
-  __device__ __forceinline__ int last_cta() const { return attn_cta_of(unit_first() + tiles - 1, d.total, d.ctas); }
+  __device__ __forceinline__ int first_cta() const { return attn_cta_of(at, d.total, d.ctas); }
+  __device__ __forceinline__ int last_cta() const { return attn_cta_of(at + (tiles - 1) * work, d.total, d.ctas); }
 };
 
 // Bit i: whether a row of token t sees slot j0 + i (i < 32; r.n > t). Slots past the span are not seen.

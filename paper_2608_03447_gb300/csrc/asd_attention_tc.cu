@@ -1229,6 +1229,7 @@ int launch_attention_tc(const asd_kv_cache* cache, AttnParams p, char* workspace
   p.group_rows = group_rows(p.group);
   p.unit_rows = unit_rows(static_cast<long long>(p.T) * p.group, p.group);
   p.row_tiles = (p.T * p.group + p.unit_rows - 1) / p.unit_rows;
+  p.weighted = p.unit_rows > p.group_rows;
   if (cache->dtype == ASD_BF16)
     return p.D <= 64 ? launch_dim<__nv_bfloat16, 64>(cache, p, workspace, stream)
                      : launch_dim<__nv_bfloat16, 128>(cache, p, workspace, stream);

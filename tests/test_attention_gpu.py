@@ -187,6 +187,18 @@ def test_many_rows(asd, dtype, T, G):
         p.check(out, lse)
 
 
+@pytest.mark.parametrize("tree", [False, True], ids=["chain", "tree"])
+@pytest.mark.parametrize("B,T,Hq,Hkv", [(1, 27, 10, 2), (3, 61, 10, 2), (40, 33, 8, 2), (9, 70, 6, 2)])
+def test_row_tiles_that_cost_differently(asd, B, T, Hq, Hkv, tree):
+    """Requests with more rows than a softmax group has threads for beside requests (and last row tiles) with fewer."""
+    g = torch.Generator().manual_seed(B + T)
+    ctx = torch.randint(0, 700, (B,), generator=g).tolist()
+    new = [T] + torch.randint(0, T + 1, (B - 1,), generator=g).tolist()
+    p = Problem(BF16, T, Hq, Hkv, 64, 16, ctx=ctx, new=new, tree=tree, seed=T)
+    out, lse, _ = p.run(asd)
+    p.check(out, lse)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
 def test_fewer_tokens_than_T_and_none(asd, dtype):
     p = Problem(dtype, 9, 10, 2, 128, 16, ctx=[100, 0, 0, 200, 77], new=[9, 3, 0, 0, 1], tree=True, seed=3)
