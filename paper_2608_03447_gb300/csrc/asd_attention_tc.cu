@@ -94,12 +94,6 @@ constexpr int value_stages(int dim) { return stages_for(dim) - key_stages(dim); 
 constexpr size_t smem_for(int dim) {
   return 1024 + static_cast<size_t>(2 + stages_for(dim)) * slab_bytes(dim) + sizeof(TcShared);
 }
-// With 16-byte copies: a warp's fills in flight before it waits for the oldest and
-// announces it. A fill must not wait for a stage whose own fill has not been
-// announced; and as the keys of tile i are released after the values of i - 1, the
-// two warps' lags together must stay below both rings' stages.
-constexpr int kLagMax = 8;
-constexpr int lag_for(int dim) { return key_stages(dim) - 1 < kLagMax ? key_stages(dim) - 1 : kLagMax; }
 static_assert(stages_for(128) == 5, "ring depth at the widest head");
 
 // ---------------------------------------------------------------- tcgen05
@@ -204,12 +198,11 @@ __device__ __forceinline__ void load_queries(uint32_t dst, const CUtensorMap* ma
         "r"(request)
       : "memory");
 }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int kLeft>
-__device__ __forceinline__ void copies_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+// This thread's arrival at the barrier once all copies that it has issued so far have landed.
+__device__ __forceinline__ void copies_arrive(unsigned long long* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-// Shared memory that this thread wrote, or whose copies it saw land, is the tensor cores' to read.
+// Shared memory that this thread wrote, or knows to be written, is the tensor cores' to read.
 __device__ __forceinline__ void fence_for_mma() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // A bounded wait by a whole warp, one answer for all of it. What follows the
@@ -440,20 +433,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int stages = of_v ? kValues : kKeys;
     int stage = 0;
     uint32_t phase = 0;
-    // copies: fills that have not been announced, and the oldest one's stage
-    constexpr int kLag = lag_for(kDim);
-    int pending = 0, oldest = 0;
-    auto announce = [&] {  // this thread's part of the oldest has landed
-      fence_for_mma();
-      mbar_arrive(&full[oldest]);
-      if (++oldest == stages) oldest = 0;
-      --pending;
-    };
-    auto flush = [&] {
-      if (kTma || pending == 0) return;
-      copies_wait<0>();
-      while (pending > 0) announce();
-    };
     uint32_t uses = 0;  // of the query slabs, a bit each: whether an odd number of fills
     int slab = 0;       // of a unit that the groups take in turn
     auto load_unit_queries = [&](int b, int h, int row0, int rows) {
@@ -483,10 +462,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 r0 + lane < end ? b * p.q_batch + t * p.q_token + (h * p.group + (row - t * p.group)) * p.q_head : -1;
             copy_rows(sq + to * kSlab, r0, p.q, off, 32);
           }
-          copies_commit();
-          copies_wait<0>();
-          fence_for_mma();
-          mbar_arrive(&sh.q_full[to]);
+          copies_arrive(&sh.q_full[to]);
         }
       }
       if (!pair) slab ^= 1;
@@ -494,9 +470,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     struct Share {
       int b, h;
       int slot0, rows;  // of the tile: rows exist; 0: there is no tile
-      int page, at;     // TMA: where this lane's box begins; the page table is read a tile ahead
+      // the page table is read a tile ahead
+      int page, at;                   // TMA: where this lane's box begins
+      long long off[kTile / 32];      // copies: where rows `lane`, 32 + lane .. lie, in elements; -1: none
     };
-    const Share none = {0, 0, 0, 0, 0, 0};
+    const Share none = {};
     AttnWalk<kTile> w(p, sh.deal);       // keys
     bool started = false;
     int b = 0, h = 0, j = 0, j1 = 0, span = 0;  // the unit's next tile
@@ -504,8 +482,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       Share x = none;
       int row0 = 0, rows = 0;  // a new unit's queries
       if (ok && j == j1) {
-        // Where this warp waits for others, what it has copied has to be theirs.
-        flush();
         if (of_v) {
           const TcUnit* u = feed.wait(sh, p);
           if (!u) return x;
@@ -543,6 +519,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         x.page = __ldcg(p.cache.table + static_cast<long long>(x.b) * p.cache.table_width + n);
         x.at = slot - n * p.cache.div.size;
       }
+      if constexpr (!kTma) {
+#pragma unroll
+        for (int q = 0; q < kTile / 32; ++q)
+          x.off[q] = 32 * q + lane < x.rows ? slot_offset(p.cache, x.b, x.slot0 + 32 * q + lane) : -1;
+      }
       ++j;
       if (rows) load_unit_queries(b, h, row0, rows);
       return x;
@@ -571,21 +552,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           atomicOr(p.status + x.b, static_cast<int>(ASD_STATUS_PAGE));
         __syncwarp();
       } else {
-#pragma unroll 1
-        for (int q = 0; q < x.rows; q += 32) {
-          long long off = -1;
-          if (q + lane < x.rows) {
-            off = slot_offset(p.cache, x.b, x.slot0 + q + lane);
-            if (off < 0 && !of_v && p.status) atomicOr(p.status + x.b, static_cast<int>(ASD_STATUS_PAGE));
-            if (off >= 0) off += x.h * p.cache.head_stride;
-          }
-          copy_rows(dst, q, of_v ? p.cache.v : p.cache.k, off, x.rows - q);
+#pragma unroll
+        for (int q = 0; q < kTile / 32; ++q) {
+          if (32 * q >= x.rows) break;
+          long long off = x.off[q];
+          if (off >= 0)
+            off += x.h * p.cache.head_stride;
+          else if (!of_v && 32 * q + lane < x.rows && p.status)
+            atomicOr(p.status + x.b, static_cast<int>(ASD_STATUS_PAGE));
+          copy_rows(dst, 32 * q, of_v ? p.cache.v : p.cache.k, off, x.rows - 32 * q);
         }
-        copies_commit();
-        if (++pending > kLag) {
-          copies_wait<kLag>();
-          announce();
-        }
+        copies_arrive(&full[stage]);
       }
       if (++stage == stages) {
         stage = 0;
@@ -607,7 +584,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       cur = next;
     }
-    flush();
+    if (!kTma) asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp == kScoreWarp) {
     // ---------------- S = Q K^T
     constexpr uint32_t kDesc = instr_desc(kBf16, kTile, false);
@@ -636,6 +613,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         pv_phase ^= 1u << turn;
         if (ok && !second) ok = warp_wait(&sh.k_full[ring.stage], ring.phase, sh, p);
         if (!ok) break;
+        if (!kTma) fence_for_mma();  // queries and keys were copied by threads
         tc_fence_after();
         const uint32_t a = uniform((sq + (pair ? turn : slab) * kSlab) >> 4);
         const uint32_t b = uniform((sk + ring.stage * kSlab) >> 4);
@@ -680,6 +658,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int j = j0; ok && j < j1; ++j) {
         ok = warp_wait(&sh.v_full[ring.stage], ring.phase, sh, p);
         if (!ok) break;
+        if (!kTma) fence_for_mma();
         const int end = min(kTile, span - j * kTile);  // rows of the tile that exist
         if ((j + 1) * kTile > ctx) {
           // New tokens, or the request's end. Rows past the end become zeros (what lies there may be anything, and 0
@@ -871,6 +850,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_before();
         meet();  // both groups' products are complete, the queries have been read
         stat[g * kGroupRows + row] = make_float2(m, l);
+        fence_for_mma();  // the slab's next queries come by TMA
         meet();
         tc_fence_after();
         const float2 other = stat[(g ^ 1) * kGroupRows + row];
