@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kSimtThreads, kCols <= 2 ? 2 : 1)
     const int span = w.span();
     __syncthreads();  // the unit before is done with shared memory
     for (int r = warp; r < kRows; r += kSimtThreads / 32) {
-      const int t = (row0 + r) / p.group, g = row0 + r - t * p.group;
+      const int t = p.by_group.quot(row0 + r), g = row0 + r - t * p.group;
       const T* src = reinterpret_cast<const T*>(p.q) + w.b * p.q_batch + t * p.q_token + (w.h * p.group + g) * p.q_head;
       for (int d4 = lane; d4 < quads; d4 += 32) {
         float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kSimtThreads, kCols <= 2 ? 2 : 1)
         if (masked) {
           uint32_t lo = 0, hi = 0;
           if (r < rows) {
-            const int t = (row0 + r) / p.group;
+            const int t = p.by_group.quot(row0 + r);
             lo = attn_sees(p, w.r, w.b, t, slot0);
             hi = attn_sees(p, w.r, w.b, t, slot0 + 32);
           }
@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(kSimtThreads, kCols <= 2 ? 2 : 1)
 
     // the rows' results, or this CTA's piece of them
     auto write_row = [&](int r, const float (&acc)[kCols][4], float ml, float sum) {
-      const int t = (row0 + r) / p.group, g = row0 + r - t * p.group;
+      const int t = p.by_group.quot(row0 + r), g = row0 + r - t * p.group;
       const long long at = (static_cast<long long>(w.b) * p.T + t) * p.q_heads + w.h * p.group + g;
       const float inv = sum > 0.0f ? 1.0f / sum : sum;  // a row that sees nothing: 0; a NaN stays one
       T* dst = reinterpret_cast<T*>(p.out) + at * D;
@@ -491,6 +491,7 @@ int asd_tree_attention(const asd_kv_cache* cache, const asd_attention* args, asd
   p.q_heads = a.q_heads;
   p.heads = cache->heads;
   p.group = a.q_heads / cache->heads;
+  p.by_group = page_div(p.group);
   p.D = cache->head_dim;
   p.scale_log2 = a.scale * 1.4426950408889634f;
   char* ws = static_cast<char*>(a.workspace);

@@ -47,6 +47,7 @@ struct AttnParams {
   float* part_ml;      // [2 * grid][rows of a unit][2] running maximum (log2 units) and sum
   float* part_o;       // [2 * grid][rows of a unit][D], in the kernel's own order
   int B, T, q_heads, heads, group, D;
+  PageDiv by_group;
   int unit_rows, row_tiles;
   int group_rows;  // tensor cores: rows of a softmax group
   bool weighted;   // whether a tile's work depends on that
@@ -74,7 +75,7 @@ __device__ __forceinline__ int attn_span(const AttnParams& p, const AttnRequest&
   const int row0 = row_tile * p.unit_rows;
   if (row0 >= r.n * p.group) return 0;
   if (p.mask) return r.ctx + r.n;
-  const int last = (row0 + p.unit_rows - 1) / p.group;
+  const int last = p.by_group.quot(row0 + p.unit_rows - 1);
   return r.ctx + (last < r.n ? last + 1 : r.n);
 }
 
@@ -96,11 +97,11 @@ __device__ __forceinline__ int attn_tiles_of(int items, int work) {
 }
 
 template <int kTile>
-__device__ __forceinline__ int attn_request_work(const AttnParams& p, const AttnRequest& r) {
+__device__ __forceinline__ int attn_head_work(const AttnParams& p, const AttnRequest& r) {  // of each of its heads
   int w = 0;
 #pragma unroll 1
   for (int i = 0; i < p.row_tiles; ++i) w += attn_tiles<kTile>(p, r, i) * attn_tile_work(p, r, i);
-  return w * p.heads;
+  return w;
 }
 
 // The output rows of tokens that do not exist, which no unit has: zeros and
@@ -127,119 +128,100 @@ __device__ __forceinline__ void attn_zero_rows(const AttnParams& p, int tid, int
 // What a CTA works out before it starts. Work is counted in 32 bits (the entry
 // point refuses what would not fit).
 struct AttnDeal {
-  int total;       // work items of all units
-  int begin, end;  // this CTA's; none where begin == end
-  int ctas;        // that have any
+  int begin, end;  // this CTA's work items; none where begin == end
+  int each, more;  // items of a CTA; that have one more
   int b;           // request of the first item
   int b_first;     // that request's first item
   int cached;      // requests b .. b + cached - 1 are in `request`
   AttnRequest request[kAttnScan];
 };
 
-// Of w items dealt to `ctas` CTAs the first w % ctas get one more than the others.
-__device__ __forceinline__ int attn_first_item(int cta, int w, int ctas) {
-  return cta * (w / ctas) + min(cta, w % ctas);
-}
-__device__ __forceinline__ int attn_cta_of(int item, int w, int ctas) {
-  const int each = w / ctas, more = w - each * ctas, cut = more * (each + 1);
-  return item < cut ? item / (each + 1) : more + (item - cut) / each;
-}
-
 // By one warp: adds up the requests' work, a block of consecutive requests a
-// lane, finds the lane and then the request where this CTA's range begins. Two or
-// three rounds of loads for up to 256 requests: every CTA starts with this (160
-// requests took 4.5 us of 43 when a warp went through them 32 at a time, twice).
+// lane, finds the lane where this CTA's range begins, and again in that block until
+// it is one request: two rounds of loads for up to 128 requests, three for 256.
+// Every CTA starts with this, so it is short, one loop for all rounds (code that
+// runs once comes from beyond the instruction cache), and the walk that follows
+// divides as little as it can. 160 requests took 4.5 us of 43 when a warp went
+// through them 32 at a time, twice.
 // Flags requests whose lengths are out of range; where the workspace's error word
 // is set, all requests, and the range is empty.
 template <int kTile>
 __device__ __forceinline__ void attn_deal(const AttnParams& p, AttnDeal& d) {
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, c = blockIdx.x;
   const unsigned error = __ldcg(p.error);  // in one round trip with the first lengths
-  const int per = (p.B - 1) / 32 + 1;
-  const int from = lane * per, to = min(from + per, p.B);
-  AttnRequest r = {0, 0};  // the block's first
-  int mine = 0;
-  constexpr int kBatch = 4;
+  if (lane == 0) d.begin = d.end = 0;
+  int b = 0, count = p.B, b_first = 0;  // the block, and the work before it
+  int total = 0, each = 0, more = 0, begin = 0, at = 0;
+  AttnRequest r = {0, 0};
 #pragma unroll 1
-  for (int i0 = 0; i0 < per; i0 += kBatch) {
-    AttnRequest some[kBatch];
-    bool bad[kBatch];
+  for (bool first = true;; first = false) {
+    const int per = (count - 1) / 32 + 1;
+    const int from = b + lane * per, to = min(from + per, b + count);
+    int mine = 0;
+    constexpr int kBatch = 4;
+#pragma unroll 1
+    for (int i0 = 0; i0 < per; i0 += kBatch) {
+      AttnRequest some[kBatch];
+      bool bad[kBatch];
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) some[i] = attn_request(p, min(from + i0 + i, p.B - 1), &bad[i]);
-    if (i0 == 0 && from < to) r = some[0];
+      for (int i = 0; i < kBatch; ++i) some[i] = attn_request(p, min(from + i0 + i, p.B - 1), &bad[i]);
+      if (i0 == 0) r = some[0];
+#pragma unroll 1
+      for (int i = 0; from + i0 + i < to && i < kBatch; ++i) {
+        const AttnRequest x = i == 0 ? some[0] : i == 1 ? some[1] : i == 2 ? some[2] : some[3];
+        mine += attn_head_work<kTile>(p, x) * p.heads;
+      }
+      if (first && !error && c == 0 && p.status)
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      const int b = from + i0 + i;
-      if (b >= to) break;
-      mine += attn_request_work<kTile>(p, some[i]);
-      if (bad[i] && !error && blockIdx.x == 0 && p.status)
-        atomicOr(p.status + b, static_cast<int>(ASD_STATUS_LENGTH));
+        for (int i = 0; i < kBatch; ++i)
+          if (bad[i] && from + i0 + i < to) atomicOr(p.status + from + i0 + i, static_cast<int>(ASD_STATUS_LENGTH));
     }
-  }
-  // the work before the lane's
-  auto sum_before = [&](int x) {
-    int inc = x;
+    int before = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-      const int o = __shfl_up_sync(kFull, inc, off);
-      if (lane >= off) inc += o;
+      const int o = __shfl_up_sync(kFull, before, off);
+      if (lane >= off) before += o;
     }
-    return inc - x;
-  };
-  int before = sum_before(mine);
-  const int w = __shfl_sync(kFull, before + mine, 31);
-  const int ctas = w == 0 ? 0 : max(1, min(p.weighted ? w / kAttnWorkMost : w, static_cast<int>(gridDim.x)));
-  const int c = blockIdx.x;
-  if (lane == 0) d.begin = d.end = 0;
-  if (error || c >= ctas) {
-    if (error && c == 0 && p.status)
-      for (int b = lane; b < p.B; b += 32) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_INCOMPLETE));
-    __syncwarp();
-    return;
-  }
-  const int begin = attn_first_item(c, w, ctas);
-  unsigned holds = __ballot_sync(kFull, mine > 0 && before <= begin && begin < before + mine);
-  int at = __ffs(holds) - 1;
-  int b = at * per, b_first = __shfl_sync(kFull, before, at);
-  AttnRequest next;  // request b + lane
-  if (per == 1) {
-    const int who = min(lane + at, 31);
-    next = {__shfl_sync(kFull, r.ctx, who), __shfl_sync(kFull, r.n, who)};
-  } else {
-    const int end = min(b + per, p.B);
-    AttnRequest here, then;
-    for (holds = 0; b < end;) {
-      bool bad;
-      here = attn_request(p, min(b + lane, p.B - 1), &bad);
-      then = attn_request(p, min(b + 32 + lane, p.B - 1), &bad);
-      mine = b + lane < end ? attn_request_work<kTile>(p, here) : 0;
-      before = b_first + sum_before(mine);
-      holds = __ballot_sync(kFull, mine > 0 && before <= begin && begin < before + mine);
-      if (holds) break;
-      b_first = __shfl_sync(kFull, before + mine, 31);
-      b += 32;
+    before += b_first - mine;
+    if (first) {
+      total = __shfl_sync(kFull, before + mine, 31);
+      const int ctas = total == 0 ? 0 : max(1, min(p.weighted ? total / kAttnWorkMost : total,
+                                                   static_cast<int>(gridDim.x)));
+      if (error || c >= ctas) {
+        if (error && c == 0 && p.status)
+          for (int i = lane; i < p.B; i += 32) atomicOr(p.status + i, static_cast<int>(ASD_STATUS_INCOMPLETE));
+        __syncwarp();
+        return;
+      }
+      each = total / ctas;
+      more = total - each * ctas;
+      begin = c * each + min(c, more);
     }
+    const unsigned holds = __ballot_sync(kFull, mine > 0 && before <= begin && begin < before + mine);
     if (!holds) {  // the lengths have changed meanwhile
       __syncwarp();
       return;
     }
     at = __ffs(holds) - 1;
-    b += at;
     b_first = __shfl_sync(kFull, before, at);
-    const int who = (lane + at) & 31;
-    const AttnRequest x = {__shfl_sync(kFull, here.ctx, who), __shfl_sync(kFull, here.n, who)};
-    const AttnRequest y = {__shfl_sync(kFull, then.ctx, who), __shfl_sync(kFull, then.n, who)};
-    next = lane + at < 32 ? x : y;
+    if (per == 1) break;
+    const int end = b + count;
+    b += at * per;
+    count = min(per, end - b);
   }
+  // the lengths of the request and of those after it that the last round has read
+  const int who = min(lane + at, 31);
+  const AttnRequest next = {__shfl_sync(kFull, r.ctx, who), __shfl_sync(kFull, r.n, who)};
+  b += at;
   d.request[lane] = next;
   if (lane == 0) {
-    d.total = w;
     d.begin = begin;
-    d.end = attn_first_item(c + 1, w, ctas);
-    d.ctas = ctas;
+    d.end = begin + each + (c < more ? 1 : 0);
+    d.each = each;
+    d.more = more;
     d.b = b;
     d.b_first = b_first;
-    d.cached = min(p.B - b, kAttnScan);
+    d.cached = min(p.B - b, kAttnScan - at);
   }
   __syncwarp();
 }
@@ -264,7 +246,7 @@ struct AttnWalk {
     b = d.b;
     load();
     // find the unit that holds the first item
-    const int per_head = attn_request_work<kTile>(p, r) / p.heads;
+    const int per_head = attn_head_work<kTile>(p, r);
     int in = d.begin - d.b_first;
     h = in / per_head;
     in -= h * per_head;
@@ -319,8 +301,14 @@ struct AttnWalk {
   __device__ __forceinline__ int rows() const { return min(p.unit_rows, r.n * p.group - row0()); }
   // the workspace slot of this CTA's piece, and the unit's CTAs
   __device__ __forceinline__ int piece() const { return 2 * static_cast<int>(blockIdx.x) + (j0 == 0 ? 1 : 0); }
-  __device__ __forceinline__ int first_cta() const { return attn_cta_of(at, d.total, d.ctas); }
-  __device__ __forceinline__ int last_cta() const { return attn_cta_of(at + (tiles - 1) * work, d.total, d.ctas); }
+  __device__ __forceinline__ int first_cta() const { return j0 == 0 ? static_cast<int>(blockIdx.x) : cta_of(at); }
+  __device__ __forceinline__ int last_cta() const {
+    return j1() == tiles ? static_cast<int>(blockIdx.x) : cta_of(at + (tiles - 1) * work);
+  }
+  __device__ __forceinline__ int cta_of(int item) const {
+    const int cut = d.more * (d.each + 1);
+    return item < cut ? item / (d.each + 1) : d.more + (item - cut) / d.each;
+  }
 };
 
 // Bit i: whether a row of token t sees slot j0 + i (i < 32; r.n > t). Slots past the span are not seen.

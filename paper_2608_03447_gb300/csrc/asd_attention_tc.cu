@@ -449,15 +449,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_expect_tx(&sh.q_full[to], static_cast<uint32_t>(p.group_rows) * (kDim * 2));
 #pragma unroll
             for (int half = 0; half < kDim / 64; ++half)
-              load_queries(sq + to * kSlab + half * kHalfSlab, &map_q, &sh.q_full[to], half * 64, h, first / p.group,
-                           b);
+              load_queries(sq + to * kSlab + half * kHalfSlab, &map_q, &sh.q_full[to], half * 64, h,
+                           p.by_group.quot(first), b);
           }
           __syncwarp();
         } else {
           const int end = min(p.group_rows, rows - tile * p.group_rows);
 #pragma unroll 1
           for (int r0 = 0; r0 < end; r0 += 32) {
-            const int row = first + r0 + lane, t = row / p.group;
+            const int row = first + r0 + lane, t = p.by_group.quot(row);
             const long long off =
                 r0 + lane < end ? b * p.q_batch + t * p.q_token + (h * p.group + (row - t * p.group)) * p.q_head : -1;
             copy_rows(sq + to * kSlab, r0, p.q, off, 32);
@@ -480,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     int b = 0, h = 0, j = 0, j1 = 0, span = 0;  // the unit's next tile
     auto take = [&] {
       Share x = none;
-      int row0 = 0, rows = 0;  // a new unit's queries
+      int row0 = 0, rows = 0;  // of a new unit
       if (ok && j == j1) {
         if (of_v) {
           const TcUnit* u = feed.wait(sh, p);
@@ -494,20 +494,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           else
             w.start();
           started = true;
-          TcUnit u = {};
           if (!w.more()) {
-            publish(u);
+            publish(TcUnit{});
             return x;
           }
           b = w.b, h = w.h, j = w.j0, j1 = w.j1(), span = w.span();
-          u.b = b, u.h = h, u.row0 = w.row0(), u.rows = w.rows();
-          u.span = span, u.ctx = w.r.ctx, u.n = w.r.n, u.valid = 1;
-          u.j0 = j, u.j1 = j1, u.whole = w.whole(), u.piece = w.piece();
-          if (!u.whole) {
-            u.c0 = w.first_cta();
-            u.c1 = w.last_cta();
-          }
-          publish(u);
+          row0 = w.row0(), rows = w.rows();
         }
       }
       if (!ok) return x;
@@ -525,7 +517,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           x.off[q] = 32 * q + lane < x.rows ? slot_offset(p.cache, x.b, x.slot0 + 32 * q + lane) : -1;
       }
       ++j;
-      if (rows) load_unit_queries(b, h, row0, rows);
+      if (rows && of_v) load_unit_queries(b, h, row0, rows);
+      if (rows && !of_v) {  // while the table is read
+        TcUnit u = {};
+        u.b = b, u.h = h, u.row0 = row0, u.rows = rows;
+        u.span = span, u.ctx = w.r.ctx, u.n = w.r.n, u.valid = 1;
+        u.j0 = w.j0, u.j1 = j1, u.whole = w.whole(), u.piece = w.piece();
+        if (!u.whole) {
+          u.c0 = w.first_cta();
+          u.c1 = w.last_cta();
+        }
+        publish(u);
+      }
       return x;
     };
     auto fill = [&](const Share& x) {
@@ -570,10 +573,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     };
     Share cur = take();
+    bool late = true;
     while (ok && cur.rows) {
       // The next tile is looked up first, but not over a unit's end by the values' warp: the unit's queries may have
-      // to wait for the one before, and that for this tile.
-      const bool late = of_v && j == j1;
+      // to wait for the one before, and that for this tile. Nothing holds up the CTA's first tile.
+      late = j == j1 && (late || of_v);
       Share next = none;
 #pragma unroll 1
       for (int i = 0; i < 2; ++i) {
@@ -583,6 +587,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           fill(cur);
       }
       cur = next;
+      late = false;
     }
     if (!kTma) asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp == kScoreWarp) {
@@ -738,7 +743,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int r = (pair ? g * p.group_rows : 0) + row;   // of the unit
       const bool lives = row < p.group_rows && r < rows;
       const bool warp_lives = row - lane < p.group_rows && r - lane < rows;  // the same for the warp
-      const int t = (row0 + min(r, rows - 1)) / p.group;
+      const int t = p.by_group.quot(row0 + min(r, rows - 1));
       float m = -INFINITY, l = 0.0f;
       bool had = false;
 #pragma unroll 1
@@ -1023,7 +1028,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int i = 0; i < kItems; ++i) {
                 const int item = i0 + i * kSoftmaxThreads, d4 = item / rows, rr = item - d4 * rows;
                 if (item >= items) break;
-                const int tt = (row0 + rr) / p.group;
+                const int tt = p.by_group.quot(row0 + rr);
                 const long long to_row = (static_cast<long long>(u->b) * p.T + tt) * p.q_heads + u->h * p.group + row0 +
                                          rr - tt * p.group;
                 const float k = sum[i] > 0.0f ? 1.0f / sum[i] : sum[i];
