@@ -8,7 +8,8 @@ missing the first call raises.
 Entry points mirror the C names: ``verify`` (asd_verify), ``verify_strict``
 (asd_verify_strict), ``workspace_size``, ``workspace_init``, ``status_string``.
 Ledgers are float32 tensors of shape [B, 2] holding (budget, spent), the
-memory layout of ``asd_ledger``.
+memory layout of ``asd_ledger``. The cache side of a block: ``KVCache``
+(asd_kv_cache), ``kv_append``, ``tree_mask``, ``tree_attention``, ``kv_compact``.
 """
 from __future__ import annotations
 

@@ -7,19 +7,29 @@
 // when it has grown by more than 2^8 in weight: O is then rescaled in tensor
 // memory, else left as it is (the quotient O / l does not depend on m).
 //
-// What bounds it: up to about 250 rows per key/value head the keys and values
-// stream from memory faster than they are used, beyond that the tensor cores set
-// the pace. Two softmax groups of 128 threads, each with its own S and O, keep
-// both busy: with at most 128 rows they take turns at the tiles and their results
-// are added at the end; with more, a unit is 256 rows, each group has 128 of them
-// and every tile of keys and values serves both.
+// What bounds it: up to 128 rows per key/value head memory, which the keys and
+// values leave once; with more the two MMAs and the softmax between them, and above
+// 256 rows memory again, since tensor memory holds two sums of 128 rows and the
+// next row tile reads the keys and values anew. Eight key/value heads of 128 in
+// bf16, five query heads on each: 32 requests of 9 tokens and 8000 cached ones 116
+// to 119 us (5.6 TB/s, 1 % more read than there is), a single token on 250000 158
+// to 162 us (6.4 TB/s); four trees on 90000, 50 tokens 244 to 252 us (930
+// TFLOP/s), 61 tokens 344 to 350 us (1.76 GB read, 5.1 TB/s). Short requests are
+// bound by what a unit costs at its ends (4 to 5 thousand cycles): 160 of five
+// tokens and up to 577 cached ones, heads of 64 in f16, 42 us.
+//
+// Two softmax groups of 128 threads, each with its own S and O, keep both pipes
+// busy: with at most 128 rows they take turns at the tiles and their results are
+// added at the end; with more, a unit is 256 rows, each group has 128 of them and
+// every tile of keys and values serves both.
 //
 // A CTA per SM: warps 0-3 and 4-7 are the softmax groups (a warp reads the TMEM
 // lanes of its quarter), warp 8 walks the units and loads keys, warp 9 issues the
 // MMAs of the scores, warp 10 those of the products, warp 11 loads queries and
 // values. Loads are TMA boxes of as many slots as the page size and the tile have
-// as a common divisor (a page of 48 is three boxes of 16); where that
-// is less than the swizzle's eight rows, 16-byte copies.
+// as a common divisor (a page of 48 is three boxes of 16); where that is less than
+// the swizzle's eight rows, 16-byte copies, whose own rate then bounds a call (the
+// 32 requests above: pages of 8 121 to 123 us, of 12 286, of 5 322).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

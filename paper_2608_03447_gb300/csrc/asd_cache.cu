@@ -443,11 +443,12 @@ int launch_append(AppendParams p, cudaStream_t stream) {
 
 // Large 16-bit calls go through shared memory, four heads per group of lanes: what
 // a row needs in registers beside its factors would leave too few threads to cover
-// memory's latency (32744 tokens of 56 heads of 128: 168 us against 309 with two
-// heads in registers; 512 tokens 5.5 against 6.1). Small ones are bound by latency
-// and take two heads in registers (256 tokens 3.7 us against 5.6), 32-bit ones too,
-// whose chunks hold half the elements (4206 tokens of 24 heads of 96 in 12.3 us
-// against 14.5). The line lies at 352 threads of the former kind per SM.
+// memory's latency (32744 tokens of 56 heads of 128: 179 us, 5.3 TB/s, against 319
+// with two heads in registers; 1024 tokens 7.5 against 9.1, 512 5.8 against 6.3).
+// Small ones are bound by latency and take two heads in registers (256 tokens 3.8
+// us against 6.0), 32-bit ones too, whose chunks hold half the elements (some 2000
+// tokens of 24 heads of 96 in 13.9 us against 15.0). The line lies at 352 threads
+// of the former kind per SM.
 template <typename T, int kVec>
 int launch_vec(const AppendParams& p, cudaStream_t stream) {
   if constexpr (sizeof(T) == 2) {
@@ -493,7 +494,9 @@ int append_typed(AppendParams p, cudaStream_t stream) {
 // first, checked and left in shared memory, then every thread walks the path
 // with its own chunk of the token. Sources lie at or past their destinations and
 // ascend, so what a thread stores for node i is never what it loads for a later
-// node, and a batch of loads can be in flight at once.
+// node, and a batch of loads can be in flight at once. Memory bounds it, and for a
+// few rows the launch: 32 requests' paths of 9 in 40 layers of 8 heads of 128 in
+// bf16 take 14.5 us (4.9 TB/s read and written), one request's path of 6 takes 3.8.
 
 constexpr int kCompactThreads = 128;
 constexpr int kCompactBatch = 8;
