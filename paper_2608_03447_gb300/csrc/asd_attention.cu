@@ -103,6 +103,8 @@ __global__ void __launch_bounds__(kSimtThreads, kCols <= 2 ? 2 : 1)
   for (w.start(); w.more(); w.next()) {
     const int row0 = w.row0(), rows = w.rows();
     const int span = w.span();
+    // With up to 16 rows a warp has two: where neither exists it only copies (a token of four heads 29 us, not 44).
+    const bool idle = kI == 1 && 2 * warp >= rows;
     __syncthreads();  // the unit before is done with shared memory
     for (int r = warp; r < kRows; r += kSimtThreads / 32) {
       const int t = p.by_group.quot(row0 + r), g = row0 + r - t * p.group;
@@ -169,7 +171,7 @@ __global__ void __launch_bounds__(kSimtThreads, kCols <= 2 ? 2 : 1)
       float s[kI][4];
 #pragma unroll
       for (int i = 0; i < kI; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.0f;
-      for (int d4 = 0; d4 < quads; ++d4) {
+      for (int d4 = idle ? quads : 0; d4 < quads; ++d4) {
         float4 a[kI], kk[4];
 #pragma unroll
         for (int i = 0; i < kI; ++i) a[i] = *reinterpret_cast<const float4*>(sq + (y + 16 * i) * pitch + 4 * d4);
@@ -189,6 +191,7 @@ __global__ void __launch_bounds__(kSimtThreads, kCols <= 2 ? 2 : 1)
       const bool masked = slot0 + kSimtTile > w.r.ctx;
 #pragma unroll
       for (int i = 0; i < kI; ++i) {
+        if (idle) break;
         const int r = y + 16 * i;
         if (masked) {
           uint32_t lo = 0, hi = 0;
@@ -232,7 +235,7 @@ __global__ void __launch_bounds__(kSimtThreads, kCols <= 2 ? 2 : 1)
         asm volatile("cp.async.wait_group 0;" ::: "memory");
       }
       __syncthreads();
-      for (int s4 = 0; s4 < kSimtTile; s4 += 4) {
+      for (int s4 = idle ? kSimtTile : 0; s4 < kSimtTile; s4 += 4) {
         float4 a[kI];
 #pragma unroll
         for (int i = 0; i < kI; ++i) a[i] = *reinterpret_cast<const float4*>(sp + (y + 16 * i) * kScorePitch + s4);
