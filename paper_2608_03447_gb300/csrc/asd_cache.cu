@@ -448,13 +448,17 @@ int launch_append(AppendParams p, cudaStream_t stream) {
 // Small ones are bound by latency and take two heads in registers (256 tokens 3.8
 // us against 6.0), 32-bit ones too, whose chunks hold half the elements (some 2000
 // tokens of 24 heads of 96 in 13.9 us against 15.0). The line lies at 352 threads
-// of the former kind per SM.
+// of the former kind per SM. Where four heads a group would be two or fewer on
+// average it is two (51212 tokens of 5 + 1 + 1 heads of 128: 68 us against 83; of
+// 8 + 2 + 2, three on average, 87 both ways).
 template <typename T, int kVec>
 int launch_vec(const AppendParams& p, cudaStream_t stream) {
   if constexpr (sizeof(T) == 2) {
-    const long long threads = static_cast<long long>(p.B) * p.T *
-                              (div_up(p.q_heads, 4) + 2 * div_up(p.kv_heads, 4)) * div_up(p.D, 2 * kVec);
-    if (threads >= 352ll * kSms) return launch_append<T, kVec, 1, 4, 2>(p, stream);
+    const int slices = div_up(p.q_heads, 4) + 2 * div_up(p.kv_heads, 4);
+    const long long threads = static_cast<long long>(p.B) * p.T * slices * div_up(p.D, 2 * kVec);
+    if (threads >= 352ll * kSms)
+      return p.q_heads + 2 * p.kv_heads <= 2 * slices ? launch_append<T, kVec, 1, 2, 2>(p, stream)
+                                                      : launch_append<T, kVec, 1, 4, 2>(p, stream);
   }
   return launch_append<T, kVec, 1, 2, 0>(p, stream);
 }

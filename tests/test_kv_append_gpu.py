@@ -188,12 +188,24 @@ def test_infinities_and_nan_stay_with_the_elements_they_turn_with(asd, dtype, in
 @pytest.mark.parametrize("dtype,D,rot", [(BF16, 128, 128), (F16, 64, 32), (F32, 96, 96), (BF16, 80, 40), (BF16, 66, 6)])
 def test_prompts(asd, dtype, D, rot, interleaved):
     """Thousands of tokens: several items a group of lanes, the last round ragged."""
-    T, Hq, Hkv = 1501, 9, 3
+    check_prompts(asd, dtype, D, rot, interleaved, 1501, 9, 3)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype,D,rot,Hq,Hkv", [(BF16, 128, 128, 5, 1), (F16, 64, 64, 1, 1), (BF16, 80, 40, 5, 1),
+                                                (BF16, 128, 64, 2, 2), (F16, 96, 48, 0, 1), (F32, 64, 64, 5, 1)])
+def test_prompts_of_few_heads(asd, dtype, D, rot, Hq, Hkv, interleaved):
+    """As many tokens, with fewer heads than a group of lanes takes at a time."""
+    check_prompts(asd, dtype, D, rot, interleaved, 4099, Hq, Hkv)
+
+
+def check_prompts(asd, dtype, D, rot, interleaved, T, Hq, Hkv):
     a = Append(dtype, T, Hq, Hkv, D, rot, 16, ctx=[5, 0, 70], new=[T, 700, T - 1], interleaved=interleaved, seed=8)
     q, k, v, status = a.run(asd)
     assert not status.any()
     x = a.rows.double()
     w = torch.cat([a.q_norm.double().expand(Hq, D), a.k_norm.double().expand(Hkv, D)])
+    q = q if Hq else torch.full((3, T, 0, D), 7.0, dtype=dtype)
     x = x[:, :, :Hq + Hkv] / (x[:, :, :Hq + Hkv].square().mean(-1, keepdim=True) + a.eps).sqrt() * w
     cos, sin = a.cos.double()[a.positions.long()][:, :, None], a.sin.double()[a.positions.long()][:, :, None]
     y = x.clone()
