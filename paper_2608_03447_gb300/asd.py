@@ -13,6 +13,7 @@ memory layout of ``asd_ledger``. The cache side of a block: ``KVCache``
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import re
@@ -187,6 +188,17 @@ def _stream(stream) -> int:
             return _raw_stream(torch.cuda.current_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _torch_on(stream):
+    """A context in which torch allocates and launches on a call's stream, as the call's own kernels do.
+
+    Memory that a call allocates belongs to that stream: its first fill is ordered before the kernels, and memory that
+    is dropped on return is handed out again only behind them.
+    """
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
 
 
 def _flag(resident: bool) -> int:
@@ -644,7 +656,8 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, kv_len: torch.Te
     """asd_kv_append: norm and rotate the new tokens' keys (and queries), append keys and values to one layer.
 
     k, v [B, T, heads, D] and q [B, T, q_heads, D] may be strided views of a fused projection's rows. cos, sin
-    [positions, rot_dim / 2] float32. Returns ``q_out`` (allocated if not given), or None without queries.
+    [positions, rot_dim / 2] float32. Returns ``q_out`` (allocated on ``stream`` and zeroed if not given), or None
+    without queries.
     """
     B, D = cache.B, cache.head_dim
     T = k.shape[1] if k.dim() == 4 else -1
@@ -658,7 +671,8 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, kv_len: torch.Te
         shape = (B, T, q_heads, D)
         qs = _check_heads("q", q, cache, shape)
         if q_out is None:
-            q_out = torch.zeros(shape, dtype=q.dtype, device=q.device)
+            with _torch_on(stream):
+                q_out = torch.zeros(shape, dtype=q.dtype, device=q.device)
         op, qp = _check_vector("q_out", q_out, cache, shape, cache.dtype), q.data_ptr()
     one = (B,)
     cp = sp = table = rot = 0
@@ -691,7 +705,8 @@ def attention_workspace(cache: KVCache, T: int, q_heads: int, stream=None) -> Wo
            load().asd_attention_workspace_size(cache._ref, T, q_heads, ctypes.byref(n)))
     ws = Workspace.__new__(Workspace)
     ws.nbytes = n.value
-    ws.buffer = torch.empty(ws.nbytes, dtype=torch.uint8, device=cache.device)
+    with _torch_on(stream):
+        ws.buffer = torch.empty(ws.nbytes, dtype=torch.uint8, device=cache.device)
     _check("asd_workspace_init", load().asd_workspace_init(ws.buffer.data_ptr(), ws.nbytes, _stream(stream)))
     return ws
 
@@ -723,15 +738,16 @@ def tree_attention(q: torch.Tensor, cache: KVCache, kv_len: torch.Tensor, layer:
 
     q [B, T, q_heads, D] (any strides, last dimension contiguous); ``tree_mask`` int32 [B, T, ceil(T / 32)] or None
     for a chain; ``scale`` defaults to 1 / sqrt(D). Returns {"out": [B, T, q_heads, D], "lse": float32 [B, T, q_heads]};
-    an ``out`` dict without "lse" leaves it out.
+    an ``out`` dict without "lse" leaves it out. Outputs and a workspace that are not given are allocated on ``stream``.
     """
     B, D = cache.B, cache.head_dim
     T, q_heads = q.shape[1:3] if q.dim() == 4 else (-1, -1)
     shape, rows = (B, T, q_heads, D), (B, T, q_heads)
     qs = _check_heads("q", q, cache, shape)
     if out is None:
-        out = {"out": torch.empty(shape, dtype=q.dtype, device=q.device),
-               "lse": torch.empty(rows, dtype=torch.float32, device=q.device)}
+        with _torch_on(stream):
+            out = {"out": torch.empty(shape, dtype=q.dtype, device=q.device),
+                   "lse": torch.empty(rows, dtype=torch.float32, device=q.device)}
     lse = out.get("lse")
     ws = workspace or attention_workspace(cache, T, q_heads, stream)
     args = _ATTENTION.pack(
