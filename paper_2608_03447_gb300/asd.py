@@ -240,7 +240,8 @@ class Workspace:
 
     def __init__(self, B: int, K: int, V: int, dtype: int, device=None, stream=None):
         self.nbytes = workspace_size(B, K, V, dtype)
-        self.buffer = torch.empty(self.nbytes, dtype=torch.uint8, device=device or "cuda")
+        with _torch_on(stream):
+            self.buffer = torch.empty(self.nbytes, dtype=torch.uint8, device=device or "cuda")
         _check("asd_workspace_init", load().asd_workspace_init(self.buffer.data_ptr(), self.nbytes, _stream(stream)))
 
     @property
@@ -272,16 +273,17 @@ def make_ledger(B: int, budget: float, spent: float = 0.0, device="cuda") -> tor
     return led
 
 
-def alloc_outputs(B: int, K: int, device="cuda", with_rows: bool = True) -> dict:
-    out = {
-        "accepted_len": torch.empty(B, dtype=torch.int32, device=device),
-        "committed": torch.empty(B, K + 1, dtype=torch.int32, device=device),
-        "recovery": torch.empty(B, dtype=torch.int32, device=device),
-        "status": torch.empty(B, dtype=torch.int32, device=device),
-    }
-    if with_rows:
-        out["row_argmax"] = torch.empty(B, K + 1, dtype=torch.int32, device=device)
-        out["row_regret"] = torch.empty(B, K, dtype=torch.float32, device=device)
+def alloc_outputs(B: int, K: int, device="cuda", with_rows: bool = True, stream=None) -> dict:
+    with _torch_on(stream):
+        out = {
+            "accepted_len": torch.empty(B, dtype=torch.int32, device=device),
+            "committed": torch.empty(B, K + 1, dtype=torch.int32, device=device),
+            "recovery": torch.empty(B, dtype=torch.int32, device=device),
+            "status": torch.empty(B, dtype=torch.int32, device=device),
+        }
+        if with_rows:
+            out["row_argmax"] = torch.empty(B, K + 1, dtype=torch.int32, device=device)
+            out["row_regret"] = torch.empty(B, K, dtype=torch.float32, device=device)
     return out
 
 
@@ -307,7 +309,7 @@ def verify(logits: torch.Tensor, draft: torch.Tensor, ledger: torch.Tensor, gate
         raise ValueError("ledger must be a contiguous float32 tensor [B, 2] of (budget, spent)")
     code = _dtype_code(logits)
     ws = workspace or Workspace(B, K, V, code, logits.device, stream)
-    o = out or alloc_outputs(B, K, logits.device)
+    o = out or alloc_outputs(B, K, logits.device, stream=stream)
     rc = load().asd_verify(_ptr(logits), code | _flag(resident), B, K, V, _ptr(draft), _ptr(ledger), float(gate),
                            int(cap),
                            _ptr(o["accepted_len"]), _ptr(o["committed"]), _ptr(o["recovery"]),
@@ -327,7 +329,7 @@ def verify_noalloc(logits: torch.Tensor, draft: torch.Tensor, ledger: torch.Tens
     B, K, V = _shape(logits, draft)
     if ledger.shape != (B, 2) or ledger.dtype != torch.float32 or not ledger.is_contiguous():
         raise ValueError("ledger must be a contiguous float32 tensor [B, 2] of (budget, spent)")
-    o = out or alloc_outputs(B, K, logits.device)
+    o = out or alloc_outputs(B, K, logits.device, stream=stream)
     rc = load().asd_verify_noalloc(_ptr(logits), _dtype_code(logits) | _flag(resident), B, K, V, _ptr(draft),
                                    _ptr(ledger),
                                    float(gate), int(cap), _ptr(o["accepted_len"]), _ptr(o["committed"]),
@@ -343,7 +345,7 @@ def verify_strict(logits: torch.Tensor, draft: torch.Tensor, workspace: Workspac
     B, K, V = _shape(logits, draft)
     code = _dtype_code(logits)
     ws = workspace or Workspace(B, K, V, code, logits.device, stream)
-    o = out or alloc_outputs(B, K, logits.device)
+    o = out or alloc_outputs(B, K, logits.device, stream=stream)
     rc = load().asd_verify_strict(_ptr(logits), code | _flag(resident), B, K, V, _ptr(draft),
                                   _ptr(o["accepted_len"]), _ptr(o["committed"]), _ptr(o["recovery"]),
                                   _ptr(o.get("row_argmax")), _ptr(o.get("row_regret")), _ptr(o.get("status")),
@@ -389,8 +391,9 @@ def verify_from_host(logits_host: torch.Tensor, draft_host: torch.Tensor, ledger
                            _ptr(out.get("row_argmax")), _ptr(out.get("row_regret")), _ptr(out.get("status")),
                            workspace.ptr, workspace.nbytes, _stream(stream))
     _check("asd_verify", rc)
-    for k in ("accepted_len", "committed", "recovery"):
-        host_out[k].copy_(out[k], non_blocking=True)
+    with _torch_on(stream):
+        for k in ("accepted_len", "committed", "recovery"):
+            host_out[k].copy_(out[k], non_blocking=True)
     return host_out
 
 
@@ -399,7 +402,8 @@ def lmhead_workspace(B: int, K: int, V: int, H: int, device=None, stream=None) -
     _check("asd_lmhead_workspace_size", load().asd_lmhead_workspace_size(B, K, V, H, ctypes.byref(n)))
     ws = Workspace.__new__(Workspace)
     ws.nbytes = n.value
-    ws.buffer = torch.empty(ws.nbytes, dtype=torch.uint8, device=device or "cuda")
+    with _torch_on(stream):
+        ws.buffer = torch.empty(ws.nbytes, dtype=torch.uint8, device=device or "cuda")
     _check("asd_workspace_init", load().asd_workspace_init(ws.buffer.data_ptr(), ws.nbytes, _stream(stream)))
     return ws
 
@@ -422,9 +426,10 @@ def lmhead_verify(hidden: torch.Tensor, weight: torch.Tensor, draft: torch.Tenso
     if T != B * (K + 1):
         raise ValueError("hidden must hold B*(K+1) rows")
     ws = workspace or lmhead_workspace(B, K, V, H, hidden.device, stream)
-    o = out or alloc_outputs(B, K, hidden.device)
+    o = out or alloc_outputs(B, K, hidden.device, stream=stream)
     if "row_top" not in o:
-        o["row_top"] = torch.empty(B, K + 1, dtype=torch.float32, device=hidden.device)
+        with _torch_on(stream):
+            o["row_top"] = torch.empty(B, K + 1, dtype=torch.float32, device=hidden.device)
     rc = load().asd_lmhead_verify(_ptr(hidden), _ptr(weight), H, B, K, V, _ptr(draft), _ptr(ledger), float(gate),
                                   int(cap), _ptr(o["accepted_len"]), _ptr(o["committed"]), _ptr(o["recovery"]),
                                   _ptr(o.get("row_argmax")), _ptr(o.get("row_regret")), _ptr(o.get("row_top")),
@@ -445,7 +450,8 @@ def lmhead_partials(hidden: torch.Tensor, weight_shard: torch.Tensor, draft: tor
     if T != B * (K + 1):
         raise ValueError("hidden must hold B*(K+1) rows")
     ws = workspace or lmhead_workspace(B, K, Vs, H, hidden.device, stream)
-    o = out if out is not None else torch.empty(T, PARTIAL_WORDS, dtype=torch.int32, device=hidden.device)
+    with _torch_on(stream):
+        o = out if out is not None else torch.empty(T, PARTIAL_WORDS, dtype=torch.int32, device=hidden.device)
     _check("asd_lmhead_partials", load().asd_lmhead_partials(_ptr(hidden), _ptr(weight_shard), H, B, K, Vs,
                                                              int(v_offset), int(V), _ptr(draft), _ptr(o), ws.ptr,
                                                              ws.nbytes, _stream(stream)))
@@ -456,7 +462,8 @@ def lmhead_logits(hidden: torch.Tensor, weight: torch.Tensor, out: torch.Tensor 
                   stream=None) -> torch.Tensor:
     """asd_lmhead_logits: the same tensor-core GEMM, writing the fp32 logits [T, V]."""
     T, V, H = _lm_shapes(hidden, weight)
-    o = out if out is not None else torch.empty(T, V, dtype=torch.float32, device=hidden.device)
+    with _torch_on(stream):
+        o = out if out is not None else torch.empty(T, V, dtype=torch.float32, device=hidden.device)
     _check("asd_lmhead_logits", load().asd_lmhead_logits(_ptr(hidden), _ptr(weight), H, T, V, _ptr(o),
                                                          _stream(stream)))
     return o
@@ -467,7 +474,8 @@ def blocks_workspace(nblk: int, B: int, K: int, V: int, dtype: int, device=None,
     _check("asd_blocks_workspace_size", load().asd_blocks_workspace_size(nblk, B, K, V, dtype, ctypes.byref(n)))
     ws = Workspace.__new__(Workspace)
     ws.nbytes = n.value
-    ws.buffer = torch.empty(max(ws.nbytes, 1), dtype=torch.uint8, device=device or "cuda")
+    with _torch_on(stream):
+        ws.buffer = torch.empty(max(ws.nbytes, 1), dtype=torch.uint8, device=device or "cuda")
     _check("asd_workspace_init", load().asd_workspace_init(ws.buffer.data_ptr(), ws.nbytes, _stream(stream)))
     return ws
 
@@ -491,7 +499,7 @@ def verify_blocks(logits: torch.Tensor, draft: torch.Tensor, ledger: torch.Tenso
     code = _dtype_code(logits)
     ws = workspace or blocks_workspace(nblk, B, K, V, code, logits.device, stream)
     if out is None:
-        flat = alloc_outputs(nblk * B, K, logits.device)
+        flat = alloc_outputs(nblk * B, K, logits.device, stream=stream)
         out = {k: v.view(nblk, B, *v.shape[1:]) for k, v in flat.items()}
     rc = load().asd_verify_blocks(_ptr(logits), code | _flag(resident), nblk, B, K, V, _ptr(draft), _ptr(ledger),
                                   float(gate),
@@ -513,7 +521,8 @@ def opportunity(row_argmax: torch.Tensor, draft: torch.Tensor, row_regret: torch
     tau = _np.ascontiguousarray(taus, dtype=_np.float32)
     pv = _np.ascontiguousarray(ps, dtype=_np.int32)
     if counts is None:
-        counts = torch.zeros(len(tau) * len(pv) + 1, dtype=torch.int64, device=row_argmax.device)
+        with _torch_on(stream):
+            counts = torch.zeros(len(tau) * len(pv) + 1, dtype=torch.int64, device=row_argmax.device)
     rc = load().asd_opportunity(_ptr(row_argmax), _ptr(draft), _ptr(row_regret), _ptr(status), n, K1 - 1,
                                 tau.ctypes.data, len(tau), pv.ctypes.data, len(pv), _ptr(counts), _stream(stream))
     _check("asd_opportunity", rc)
@@ -533,7 +542,9 @@ def shard_partials(logits: torch.Tensor, draft: torch.Tensor, v_offset: int, V: 
     B, K, Vs = _shape(logits, draft)
     code = _dtype_code(logits)
     ws = workspace or Workspace(B, K, Vs, code, logits.device, stream)
-    o = out if out is not None else torch.empty(B * (K + 1), PARTIAL_WORDS, dtype=torch.int32, device=logits.device)
+    with _torch_on(stream):
+        o = out if out is not None else torch.empty(B * (K + 1), PARTIAL_WORDS, dtype=torch.int32,
+                                                    device=logits.device)
     rc = load().asd_shard_partials(_ptr(logits), code | _flag(resident), B, K, Vs, int(v_offset), int(V), _ptr(draft),
                                    _ptr(o),
                                    ws.ptr, ws.nbytes, _stream(stream))
@@ -548,7 +559,7 @@ def shard_combine(partials: torch.Tensor, draft: torch.Tensor, ledger: torch.Ten
     B, K = draft.shape
     if words != PARTIAL_WORDS or R != B * (K + 1) or partials.dtype != torch.int32 or not partials.is_contiguous():
         raise ValueError("partials must be a contiguous int32 tensor [S, B*(K+1), 6]")
-    o = out or alloc_outputs(B, K, partials.device)
+    o = out or alloc_outputs(B, K, partials.device, stream=stream)
     rc = load().asd_shard_combine(_ptr(partials), S, B, K, int(V), _ptr(draft), _ptr(ledger), float(gate), int(cap),
                                   _ptr(o["accepted_len"]), _ptr(o["committed"]), _ptr(o["recovery"]),
                                   _ptr(o.get("row_argmax")), _ptr(o.get("row_regret")), _ptr(o.get("status")),

@@ -93,3 +93,64 @@ def test_nothing_is_allocated_beside_given_tensors(record):
     asd.kv_append(k, k, cpu_cache(), n, q=q, q_out=q, stream=STREAM)
     asd.kv_append(k, k, cpu_cache(), n, stream=STREAM)
     assert record.allocated == []
+
+
+@pytest.fixture
+def shapes(monkeypatch):
+    """The older calls check that logits are on a GPU; here they are not."""
+    monkeypatch.setattr(asd, "_shape", lambda logits, draft: (logits.shape[0], logits.shape[1] - 1, logits.shape[2]))
+    monkeypatch.setattr(asd, "_lm_shapes", lambda h, w: (h.shape[0], w.shape[0], h.shape[1]))
+
+
+def test_verification_allocates_on_the_stream(record, shapes):
+    B, K, V = 2, 3, 10
+    z, x, led = torch.ones(B, K + 1, V), torch.ones(B, K, dtype=torch.int32), torch.ones(B, 2)
+    h, w = torch.ones(B * (K + 1), 8), torch.ones(V, 8)
+    s = dict(stream=STREAM)
+    asd.verify(z, x, led, 1.0, 2, **s)
+    asd.verify_noalloc(z, x, led, 1.0, 2, **s)
+    asd.verify_strict(z, x, **s)
+    asd.lmhead_verify(h, w, x, led, 1.0, 2, **s)
+    asd.lmhead_partials(h, w, x, 0, V, **s)
+    asd.lmhead_logits(h, w, **s)
+    asd.shard_partials(z, x, 0, V, **s)
+    asd.shard_combine(torch.ones(1, B * (K + 1), asd.PARTIAL_WORDS, dtype=torch.int32), x, led, 1.0, 2, V, **s)
+    asd.blocks_workspace(2, B, K, V, asd.F32, device="cpu", **s)
+    assert len(record.allocated) > 30
+    assert [a for a in record.allocated if a[1] is not STREAM] == []
+    assert all(args[-1] == STREAM.cuda_stream for name, args in record.lib.calls if not name.endswith("_size"))
+
+
+def test_opportunity_counts_are_zeroed_on_the_stream(record):
+    rows, x, regret = torch.ones(4, 3, dtype=torch.int32), torch.ones(4, 2, dtype=torch.int32), torch.ones(4, 2)
+    asd.opportunity(rows, x, regret, [0.5], [1], stream=STREAM)
+    assert record.allocated == [("zeros", STREAM)]
+
+
+def test_results_are_copied_to_the_host_on_the_stream(record, monkeypatch):
+    copied = []
+
+    class Result:
+        def data_ptr(self):
+            return 64
+
+    class HostResult:
+        def copy_(self, src, non_blocking):
+            copied.append((non_blocking, record.stream))
+
+    class Pinned:
+        dtype, shape = torch.float32, (2, 4, 10)
+
+        def dim(self):
+            return 3
+
+        def is_pinned(self):
+            return True
+
+    monkeypatch.setattr(asd, "_alias", lambda t: 64)
+    monkeypatch.setattr(asd, "_ptr", lambda t: 64)
+    names = ("accepted_len", "committed", "recovery")
+    ws = types.SimpleNamespace(ptr=64, nbytes=1024)
+    asd.verify_from_host(Pinned(), Pinned(), Result(), 1.0, 2, ws, {n: Result() for n in names},
+                         {n: HostResult() for n in names}, stream=STREAM)
+    assert copied == [(True, STREAM)] * 3

@@ -72,3 +72,36 @@ def test_two_streams_with_a_workspace_each(asd):
             assert ws[i].error() == 0
             for o in got[i]:
                 assert torch.equal(o["out"], want[i]["out"]) and torch.equal(o["lse"], want[i]["lse"])
+
+
+def test_verification_on_another_stream(asd):
+    """Outputs, workspace, counts and host copies of calls on a side stream that is behind the current one."""
+    B, K, V = 4, 5, 5003
+    g = torch.Generator(device="cuda").manual_seed(2)
+    z = torch.randn(B, K + 1, V, generator=g, device="cuda")
+    x = z[:, :K].argmax(-1).to(torch.int32)
+    x[:, 2] = 7
+    ledger = asd.make_ledger(B, 100.0)
+    want = asd.verify(z, x, ledger.clone(), 100.0, 2)
+    counts = asd.opportunity(want["row_argmax"], x, want["row_regret"], [0.5, 100.0], [1, 2])
+    side = torch.cuda.Stream()
+    zh, xh = z.cpu().pin_memory(), x.cpu().pin_memory()
+    ws, out = asd.Workspace(B, K, V, asd.F32), asd.alloc_outputs(B, K)
+    host = {n: torch.zeros_like(out[n], device="cpu").pin_memory() for n in ("accepted_len", "committed", "recovery")}
+    ledgers = [ledger.clone(), ledger.clone()]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(SLEEP)
+    seen = asd.opportunity(want["row_argmax"], x, want["row_regret"], [0.5, 100.0], [1, 2], stream=side)
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(SLEEP)
+    got = asd.verify(z, x, ledgers[0], 100.0, 2, stream=side)
+    taken = [torch.full((ws.nbytes,), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    asd.verify_from_host(zh, xh, ledgers[1], 100.0, 2, ws, out, host, stream=side)
+    side.synchronize()
+    for n in host:
+        assert torch.equal(host[n], want[n].cpu()), n
+    torch.cuda.synchronize()
+    for n in want:
+        assert torch.equal(got[n], want[n]), n
+    assert torch.equal(seen, counts) and int(counts[-1]) > 0
+    assert all(bool((t == 255).all()) for t in taken)
