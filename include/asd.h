@@ -96,7 +96,8 @@ enum {
 #define ASD_STATUS_INCOMPLETE 16u /* the workspace's error word was set when the request was
                                    * selected (asd_workspace_error): a kernel gave up waiting on
                                    * its copy pipeline, so row results may be missing. Set for
-                                   * every request of such a call until asd_workspace_init. */
+                                   * every request of such a call until asd_workspace_init.
+                                   * asd_tree_attention: also by the call that gives up. */
 
 #define ASD_STATUS_LENGTH 32u     /* cache entry points: kv_len < 0, a token count outside its range, or
                                    * more slots than the request's row of the page table covers */
@@ -463,8 +464,9 @@ typedef struct {
   const uint32_t* tree_mask; /* [B, T, ceil(T / 32)], or NULL: a chain (u <= t) */
   int32_t* status;           /* as in asd_append */
   void* workspace;           /* 16-byte aligned, zeroed by asd_workspace_init before first use; one for a larger T or
-                              * cache serves any smaller one. While its error word (asd_workspace_error) is set calls
-                              * write nothing and flag their requests ASD_STATUS_INCOMPLETE */
+                              * cache serves any smaller one. A call that gives up waiting on its own pipeline sets
+                              * the error word (asd_workspace_error) and flags all its requests
+                              * ASD_STATUS_INCOMPLETE; while the word is set calls write nothing and flag theirs */
   size_t workspace_bytes;    /* >= asd_attention_workspace_size */
   int layer;
   int T;

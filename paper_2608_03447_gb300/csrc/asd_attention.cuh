@@ -125,6 +125,14 @@ __device__ __forceinline__ void attn_zero_rows(const AttnParams& p, int tid, int
   }
 }
 
+// Flags every request: a CTA has given up a wait, or the workspace says that one
+// has. What a CTA leaves out may be any request's (units in pieces have no last
+// CTA then), so it does not say which. Threads `tid` of `threads`.
+__device__ __forceinline__ void attn_incomplete(int32_t* status, int B, int tid, int threads) {
+  if (!status) return;
+  for (int b = tid; b < B; b += threads) atomicOr(status + b, static_cast<int>(ASD_STATUS_INCOMPLETE));
+}
+
 // What a CTA works out before it starts. Work is counted in 32 bits (the entry
 // point refuses what would not fit).
 struct AttnDeal {
@@ -188,8 +196,7 @@ __device__ __forceinline__ void attn_deal(const AttnParams& p, AttnDeal& d) {
       const int ctas = total == 0 ? 0 : max(1, min(p.weighted ? total / kAttnWorkMost : total,
                                                    static_cast<int>(gridDim.x)));
       if (error || c >= ctas) {
-        if (error && c == 0 && p.status)
-          for (int i = lane; i < p.B; i += 32) atomicOr(p.status + i, static_cast<int>(ASD_STATUS_INCOMPLETE));
+        if (error && c == 0) attn_incomplete(p.status, p.B, lane, 32);
         __syncwarp();
         return;
       }

@@ -1063,7 +1063,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   tc_fence_before();
   __syncthreads();
-  if (sh.abort) {  // loads that nobody waited for: give them time to land before the CTA's memory is another's
+  if (sh.abort) {
+    attn_incomplete(p.status, p.B, threadIdx.x, kThreads);
+    // loads that nobody waited for: give them time to land before the CTA's memory is another's
     const unsigned long long t0 = global_ns();
     while (global_ns() - t0 < kLandNs) {
     }
