@@ -3,9 +3,10 @@
 //
 // Per tile of 128 slots: S = Q K^T (128 query rows by 128 slots, fp32 in tensor
 // memory), P = exp2(scale S - m) by one thread per row, O += P V with P read from
-// tensor memory where S was. m is the row's running maximum, but follows it only
-// when it has grown by more than 2^8 in weight: O is then rescaled in tensor
-// memory, else left as it is (the quotient O / l does not depend on m).
+// tensor memory where S was. m is the row's running maximum (in f16 7 less, so that
+// small weights keep their bits), but follows it only when it has grown by more
+// than 2^8 in weight: O is then rescaled in tensor memory, else left as it is (the
+// quotient O / l does not depend on m).
 //
 // What bounds it: up to 128 rows per key/value head memory, which the keys and
 // values leave once; with more the two MMAs and the softmax between them, and above
@@ -59,6 +60,11 @@ constexpr int kTmemCols = 512;
 constexpr int kMaxStages = 12;
 constexpr unsigned long long kLandNs = 10000000;  // longer than any load takes
 constexpr float kGrowth = 8.0f; // log2: how far the maximum may outgrow the reference
+// log2: how far below the maximum the reference is set. f16 weights begin to lose bits at 2^-14 and vanish at 2^-25,
+// which the many small ones of a long context are, against a largest of 1 (one key ahead of 250000 at 2^-20.6 each: the
+// result off by 5.7e-3 of the values' size, with a reference 7 lower by 2e-5); the largest may be 2^15 all the same.
+template <typename T> constexpr float kLead = 0.0f;
+template <> constexpr float kLead<__half> = 7.0f;
 
 constexpr int slab_bytes(int dim) { return kTile * dim * 2; }  // 128 rows of a padded head
 constexpr int kHalfSlab = kTile * 128;                         // 64 elements of all of them
@@ -806,8 +812,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (step == 0) continue;
             if (step == 1) {
               const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * p.scale_log2;
-              if (__any_sync(kFull, lives && top > m + kGrowth)) {
-                const float m_new = fmaxf(m, top);
+              if (__any_sync(kFull, lives && top > m + (kGrowth + kLead<T>))) {
+                const float m_new = fmaxf(m, top - kLead<T>);
                 const float fade = exp2_fast(m - (m_new == -INFINITY ? 0.0f : m_new));
                 l *= fade;
                 m = m_new;
