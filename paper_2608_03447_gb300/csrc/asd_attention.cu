@@ -193,8 +193,9 @@ __global__ void __launch_bounds__(kSimtThreads, kCols <= 2 ? 2 : 1)
       for (int i = 0; i < kI; ++i) {
         if (idle) break;
         const int r = y + 16 * i;
+        uint32_t lo = ~0u, hi = ~0u;
         if (masked) {
-          uint32_t lo = 0, hi = 0;
+          lo = hi = 0;
           if (r < rows) {
             const int t = p.by_group.quot(row0 + r);
             lo = attn_sees(p, w.r, w.b, t, slot0);
@@ -216,7 +217,8 @@ __global__ void __launch_bounds__(kSimtThreads, kCols <= 2 ? 2 : 1)
         for (int c = 0; c < 4; ++c) {
           const float e = exp2f(s[i][c] - ref);
           sum += e;
-          sp[r * kScorePitch + x + 16 * c] = e;
+          // -0 stands for a slot that the row does not see; the weight of one that it sees may be too small and +0
+          sp[r * kScorePitch + x + 16 * c] = (((c & 2 ? hi : lo) >> (x + 16 * (c & 1))) & 1u) ? e : -0.0f;
         }
 #pragma unroll
         for (int off = 8; off > 0; off >>= 1) sum += __shfl_xor_sync(kFull, sum, off);
@@ -249,7 +251,7 @@ __global__ void __launch_bounds__(kSimtThreads, kCols <= 2 ? 2 : 1)
           for (int i = 0; i < kI; ++i) {
             const float f = e == 0 ? a[i].x : e == 1 ? a[i].y : e == 2 ? a[i].z : a[i].w;
             // what a row does not see does not reach it: 0 * NaN would
-            if (masked && f == 0.0f) continue;
+            if (masked && __float_as_uint(f) == 0x80000000u) continue;
 #pragma unroll
             for (int c = 0; c < kCols; ++c) {
               o[i][c][0] = fmaf(f, v[c].x, o[i][c][0]);
