@@ -151,8 +151,9 @@ __global__ void __launch_bounds__(kSimtThreads, kCols <= 2 ? 2 : 1)
       if (async) asm volatile("cp.async.commit_group;" ::: "memory");
     };
     auto look_up = [&](int j) {  // the slots' offsets of tile j
+      if (tid >= kSimtTile) return;
       const int slot = j * kSimtTile + tid;
-      if (tid >= kSimtTile || slot >= span) return;
+      if (slot >= span) return;
       const long long off = slot_offset(p.cache, w.b, slot);
       if (off < 0 && p.status) atomicOr(p.status + w.b, static_cast<int>(ASD_STATUS_PAGE));
       s_off[(j & 1) * kSimtTile + tid] = off;
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(kSimtThreads, kCols <= 2 ? 2 : 1)
           }
       }
       // the tile's mask where it reaches past the context (or the span)
-      const bool masked = slot0 + kSimtTile > w.r.ctx;
+      const bool masked = slot0 > w.r.ctx - kSimtTile;  // slot0 + kSimtTile may be 2^31
 #pragma unroll
       for (int i = 0; i < kI; ++i) {
         if (idle) break;

@@ -681,7 +681,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
         if (!kTma) fence_for_mma();
         const int end = min(kTile, span - j * kTile);  // rows of the tile that exist
-        if ((j + 1) * kTile > ctx) {
+        if (j * kTile > ctx - kTile) {  // (j + 1) * kTile may be 2^31
           // New tokens, or the request's end. Rows past the end become zeros (what lies there may be anything, and 0
           // times NaN is NaN); of a new token some rows may see nothing, so its values' NaN and infinities become
           // zeros too and the unit is marked: its rows look at the end for those that they do see.
@@ -767,7 +767,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int whose = turn & 1;
         turn += pair ? 2 : 1;
         if (!pair && whose != g) continue;
-        const bool masked = (j + 1) * kTile > req.ctx;
+        const bool masked = j * kTile > req.ctx - kTile;
         uint32_t sees0 = 0, sees1 = 0, sees2 = 0, sees3 = 0;
         if (masked && warp_lives) {
 #pragma unroll 1
@@ -946,7 +946,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (mine && *const_cast<volatile int*>(&sh.poison[number & 3]) == number + 1) {
         // NaN and infinities that the row does see, onto what this thread has just written
 #pragma unroll 1
-        for (int slot = max(req.ctx, j0 * kTile); slot < min(u->span, j1 * kTile); ++slot) {
+        const int last = (j1 - 1) * kTile + (kTile - 1);  // j1 * kTile may be 2^31
+        for (int slot = max(req.ctx, j0 * kTile); slot < u->span && slot <= last; ++slot) {
           if (!(attn_sees(p, req, u->b, t, slot) & 1u)) continue;
           const long long off = slot_offset(p.cache, u->b, slot);
           if (off < 0) continue;

@@ -40,3 +40,36 @@ def test_what_a_row_does_see_reaches_it_however_small_its_weight(asd, dtype, D, 
     hit[:, [1, 3] if new else slice(None), 2:, 9] = True
     assert not bool(out[hit].isfinite().any())
     assert torch.equal(out[~hit], good[~hit])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("tree", [False, True], ids=["chain", "tree"])
+def test_the_last_slots_that_31_bits_count(asd, dtype, tree):
+    """A context of 2^31 - 3 slots, nearly all of them on one page, and two new tokens: what is masked in the last tile
+    still is. The new tokens' keys outweigh the context by e^-40 a slot."""
+    page, width, D = 65536, 32768, 8
+    k = torch.zeros(2, page, 1, D, dtype=dtype)
+    v = torch.ones_like(k)
+    k[1, -1] = v[1, -1] = math.nan  # slot 2^31 - 1, which no length reaches
+    k[1, -3, 0, 0], k[1, -2, 0, 0] = 40.0, 48.0
+    v[1, -3], v[1, -2] = 3.0, 5.0
+    if tree:
+        v[1, -2, 0, 4] = math.nan
+    table = torch.zeros(1, width, dtype=torch.int32)
+    table[0, -1] = 1
+    q = torch.zeros(1, 2, 1, D, dtype=dtype)
+    q[..., 0] = 1
+    cache = asd.KVCache(k.cuda(), v.cuda(), table.cuda())
+    mask = asd.tree_mask(torch.tensor([[-1, 0]])).cuda() if tree else None
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    o = asd.tree_attention(q.cuda(), cache, torch.tensor([2 ** 31 - 3], dtype=torch.int32, device="cuda"), scale=1.0,
+                           tree_mask=mask, status=status)
+    out, lse = o["out"].cpu().double()[0, :, 0], o["lse"].cpu().double()[0, :, 0]
+    assert not status.any()
+    w = math.exp(-8)  # of token 0 for token 1; the context's weights are under 2^31 e^-40 = 1e-8 together
+    want = torch.tensor([3.0, (5.0 + 3.0 * w) / (1 + w)], dtype=torch.float64)[:, None].expand(2, D).clone()
+    if tree:
+        want[1, 4] = math.nan
+    assert torch.equal(out.isnan(), want.isnan())
+    assert float((out - want).nan_to_num(0).abs().max()) <= 5.0 * (2.0 ** -8 if dtype == BF16 else 1e-6)
+    assert float((lse - torch.tensor([40.0, 48 + math.log1p(w)], dtype=torch.float64)).abs().max()) <= 1e-4
