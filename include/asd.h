@@ -79,7 +79,8 @@ enum {
   ASD_ERR_SHAPE = 2,     /* B < 0, K < 0, K > 31, V < 1, or H invalid; cache entry points: a size, head
                           * count, stride or rotation out of its range */
   ASD_ERR_DTYPE = 3,     /* unknown dtype code */
-  ASD_ERR_CONTROL = 4,   /* gate < 0 or NaN, cap < 0; eps < 0 or NaN, scale not finite */
+  ASD_ERR_CONTROL = 4,   /* gate < 0 or NaN, cap < 0; eps < 0 or NaN, scale not finite or
+                          * past 2e38 */
   ASD_ERR_WORKSPACE = 5, /* workspace smaller than the size query returns */
   ASD_ERR_ALIGN = 6,     /* pointer not aligned as documented */
   ASD_ERR_CUDA = 7,      /* a CUDA call failed (launch or device query) */
@@ -471,7 +472,7 @@ typedef struct {
   int layer;
   int T;
   int q_heads;
-  float scale;               /* finite; scores are scale * (q . k) */
+  float scale;               /* |scale| <= 2e38; scores are scale * (q . k) */
 } asd_attention;
 int asd_attention_workspace_size(const asd_kv_cache* cache, int T, int q_heads, size_t* bytes);
 int asd_tree_attention(const asd_kv_cache* cache, const asd_attention* args, asd_stream_t stream);

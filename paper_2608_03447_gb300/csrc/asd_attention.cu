@@ -469,7 +469,8 @@ int asd_tree_attention(const asd_kv_cache* cache, const asd_attention* args, asd
   const int rc = check_attention(cache, a.T, a.q_heads);
   if (rc != ASD_OK) return rc;
   if (a.layer < 0 || a.layer >= cache->layers) return ASD_ERR_SHAPE;
-  if (!(a.scale - a.scale == 0.0f)) return ASD_ERR_CONTROL;  // infinite or NaN
+  const float scale_log2 = a.scale * 1.4426950408889634f;
+  if (!(scale_log2 - scale_log2 == 0.0f)) return ASD_ERR_CONTROL;  // infinite or NaN
   if (cache->B == 0 || a.T == 0) return ASD_OK;
   if (!a.q || !a.kv_len || !a.out || !a.workspace) return ASD_ERR_NULL;
   const size_t es = store_bytes(cache->dtype);
@@ -500,7 +501,7 @@ int asd_tree_attention(const asd_kv_cache* cache, const asd_attention* args, asd
   p.group = a.q_heads / cache->heads;
   p.by_group = page_div(p.group);
   p.D = cache->head_dim;
-  p.scale_log2 = a.scale * 1.4426950408889634f;
+  p.scale_log2 = scale_log2;
   char* ws = static_cast<char*>(a.workspace);
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (attention_tc_takes(cache, p)) return launch_attention_tc(cache, p, ws, s);
