@@ -73,3 +73,68 @@ def test_the_last_slots_that_31_bits_count(asd, dtype, tree):
     assert torch.equal(out.isnan(), want.isnan())
     assert float((out - want).nan_to_num(0).abs().max()) <= 5.0 * (2.0 ** -8 if dtype == BF16 else 1e-6)
     assert float((lse - torch.tensor([40.0, 48 + math.log1p(w)], dtype=torch.float64)).abs().max()) <= 1e-4
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_replayed_graph_follows_the_lengths(asd, dtype):
+    """Every replay against the 64-bit form of its own lengths, log-sum-exp included; a context that is shorter than at
+    capture lies in slots that are filled."""
+    p = Problem(dtype, 9, 10, 2, 128, 16, ctx=[3000, 0, 40], tree=True, seed=17)
+    cache = p.device(asd)
+    q, kv_len, mask = p.q.cuda(), p.kv_len.cuda(), p.mask.cuda()
+    new_len = torch.full((3,), 9, dtype=torch.int32, device="cuda")
+    ws = asd.attention_workspace(cache, p.T, p.Hq)
+    out = {"out": torch.zeros(3, 9, 10, 128, dtype=dtype, device="cuda"),
+           "lse": torch.zeros(3, 9, 10, dtype=torch.float32, device="cuda")}
+    asd.tree_attention(q, cache, kv_len, tree_mask=mask, new_len=new_len, scale=p.scale, workspace=ws, out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        asd.tree_attention(q, cache, kv_len, tree_mask=mask, new_len=new_len, scale=p.scale, workspace=ws, out=out)
+    for ctx, new in (([3000, 0, 40], [9, 9, 9]), ([10, 0, 40], [9, 1, 0]), ([2000, 0, 0], [3, 9, 9]),
+                     ([1, 0, 31], [0, 0, 9]), ([2990, 0, 17], [9, 5, 9])):
+        p.kv_len, p.new_len = (torch.tensor(x, dtype=torch.int32) for x in (ctx, new))
+        kv_len.copy_(p.kv_len)
+        new_len.copy_(p.new_len)
+        out["out"].fill_(7)
+        out["lse"].fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        p.check(out["out"].cpu(), out["lse"].cpu())
+    assert ws.error() == 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("T,Hq,Hkv,D", [(1, 130, 1, 64), (3, 150, 1, 128), (2, 600, 2, 64), (1, 128, 1, 64), (3, 127, 1, 64)])
+def test_wide_groups(asd, dtype, T, Hq, Hkv, D):
+    """Up to and more than 128 query heads on a key/value head: row tiles begin inside a token."""
+    for tree in (False, True):
+        p = Problem(dtype, T, Hq, Hkv, D, 16, ctx=[150, 0, 700], tree=tree, seed=Hq)
+        out, lse, status = p.run(asd)
+        p.check(out, lse)
+        assert not status.any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("T,Hq,Hkv,D", [(1000, 5, 1, 64), (517, 4, 2, 128), (300, 8, 1, 96)])
+def test_prompts(asd, dtype, T, Hq, Hkv, D):
+    """Hundreds of new tokens, with and without a context, fewer in one request than in the others."""
+    p = Problem(dtype, T, Hq, Hkv, D, 48, ctx=[0, 300, 77], new=[T, T - 131, 1], seed=T)
+    out, lse, status = p.run(asd)
+    p.check(out, lse)
+    assert not status.any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_prompts_under_a_mask_of_many_words(asd, dtype):
+    """The same as a chain where the mask is a chain's; and a tree of 300 nodes."""
+    T = 300
+    p = Problem(dtype, T, 6, 2, 64, 16, ctx=[40, 0], seed=3)
+    chain, chain_lse, _ = p.run(asd)
+    p.check(chain, chain_lse)
+    p.mask = asd.tree_mask(torch.arange(T)[None].expand(2, T) - 1)
+    out, lse, _ = p.run(asd)
+    p.check(out, lse)
+    p = Problem(dtype, T, 6, 2, 64, 16, ctx=[40, 0], tree=True, seed=4)
+    out, lse, _ = p.run(asd)
+    p.check(out, lse)
