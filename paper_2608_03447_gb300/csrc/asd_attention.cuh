@@ -9,7 +9,10 @@
 // work, one a CTA, whatever the requests' lengths. A tile is one work item, but
 // three of a unit whose rows are too many for one softmax group and two of one
 // whose rows are not, where a call has both (61 tokens, 5 query heads on one, four
-// contexts of 90000: 348 us, with equal tiles 394). A tile belongs to the range
+// contexts of 90000: 348 us, with equal tiles 394; four of 40000: heads of 64, 40
+// tokens, groups of 8, 89 against 97; heads of 128, 70 tokens, groups of 4, 192
+// against 217; 300 tokens, groups of one, 200 against 218; 32 requests of up to 30
+// tokens on up to 8000, groups of 8, 83.1 against 83.2). A tile belongs to the range
 // that its first item is in, and ranges have at least as many items as a tile, so
 // that none is without tiles. Lengths are device data, so every CTA adds them up
 // itself. A unit that a range's end cuts is in pieces: each CTA leaves its piece's

@@ -12,12 +12,13 @@
 // values leave once; with more the two MMAs and the softmax between them, and above
 // 256 rows memory again, since tensor memory holds two sums of 128 rows and the
 // next row tile reads the keys and values anew. Eight key/value heads of 128 in
-// bf16, five query heads on each: 32 requests of 9 tokens and 8000 cached ones 116
-// to 119 us (5.6 TB/s, 1 % more read than there is), a single token on 250000 158
-// to 162 us (6.4 TB/s); four trees on 90000, 50 tokens 244 to 252 us (930
-// TFLOP/s), 61 tokens 344 to 350 us (1.76 GB read, 5.1 TB/s). Short requests are
-// bound by what a unit costs at its ends (4 to 5 thousand cycles): 160 of five
-// tokens and up to 577 cached ones, heads of 64 in f16, 42 us.
+// bf16, five query heads on each: 32 requests of 9 tokens and 8000 cached ones 115
+// to 120 us (5.6 TB/s, 1 % more read than there is), a single token on 250000 158
+// to 163 us (6.4 TB/s); four trees on 90000, 50 tokens 244 to 252 us (930
+// TFLOP/s), 61 tokens 344 to 358 us (1.76 GB read, 5.1 TB/s); a prompt of 4093 513 us
+// (335 TFLOP/s). Short requests are bound by what a
+// unit costs at its ends (4 to 5 thousand cycles): 160 of five tokens and up to 577
+// cached ones, heads of 64 in f16, 41 to 44 us.
 //
 // Two softmax groups of 128 threads, each with its own S and O, keep both pipes
 // busy: with at most 128 rows they take turns at the tiles and their results are
@@ -30,7 +31,8 @@
 // values. Loads are TMA boxes of as many slots as the page size and the tile have
 // as a common divisor (a page of 48 is three boxes of 16); where that is less than
 // the swizzle's eight rows, 16-byte copies, whose own rate then bounds a call (the
-// 32 requests above: pages of 8 121 to 123 us, of 12 286, of 5 322).
+// 32 requests above: pages of 8 121 to 123 us, of 12 286 to 293, of 5 322 to 329, of
+// one 380).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -990,7 +992,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         meet();
         if (ok && *const_cast<volatile int*>(&sh.last)) {
           __threadfence();
-          // four columns of a row an item: many pieces of one at once, or some of several
+          // Four columns of a row an item: 16 pieces of one at once, or four of four. On five pieces and more the former,
+          // whose loads are in flight together (152 pieces of 5 rows 27 us for the call, with the latter 42); below it
+          // the latter (45 rows in 1.7 pieces on average, the 32 chains, 117.8, with the former 119.2). Each alone is
+          // smaller code than the choice: with the former alone other calls were 0 to 4 % faster (5 to 125 rows in 2 to
+          // 152 pieces), with the latter up to 8 % at 125 rows in few pieces and slower by half at 152.
           auto merge = [&](auto many_items, auto many_pieces) {
             constexpr int kItems = decltype(many_items)::value, kPieces = decltype(many_pieces)::value;
             const int items = rows * (p.D / 4);

@@ -447,7 +447,8 @@ int launch_append(AppendParams p, cudaStream_t stream) {
 // with two heads in registers; 1024 tokens 7.5 against 9.1, 512 5.8 against 6.3).
 // Small ones are bound by latency and take two heads in registers (256 tokens 3.8
 // us against 6.0), 32-bit ones too, whose chunks hold half the elements (some 2000
-// tokens of 24 heads of 96 in 13.9 us against 15.0). The line lies at 352 threads
+// tokens of 24 heads of 96 in 13.9 us against 15.0, their 49 MB in L2; from memory
+// 18.6, latency: DRAM 26 % and issue slots 40 % busy). The line lies at 352 threads
 // of the former kind per SM. Where four heads a group would be two or fewer on
 // average it is two (51212 tokens of 5 + 1 + 1 heads of 128: 68 us against 83; of
 // 8 + 2 + 2, three on average, 87 both ways).
@@ -498,9 +499,12 @@ int append_typed(AppendParams p, cudaStream_t stream) {
 // first, checked and left in shared memory, then every thread walks the path
 // with its own chunk of the token. Sources lie at or past their destinations and
 // ascend, so what a thread stores for node i is never what it loads for a later
-// node, and a batch of loads can be in flight at once. Memory bounds it, and for a
-// few rows the launch: 32 requests' paths of 9 in 40 layers of 8 heads of 128 in
-// bf16 take 14.5 us (4.9 TB/s read and written), one request's path of 6 takes 3.8.
+// node, and a batch of loads can be in flight at once. A few rows are bound by the
+// launch: one request's path of 6 in 40 layers of 8 heads of 128 in bf16 takes 3.8
+// us. 32 requests' paths of 9 take 17.9 us from memory and 14.7 where the 71 MB are
+// in L2 from the call before; what bounds them is instructions (7.4 million, the
+// 64-bit divisions by a word's elements among them; issue slots 31 % busy) and two
+// rounds of loads, not memory (DRAM 24 % busy).
 
 constexpr int kCompactThreads = 128;
 constexpr int kCompactBatch = 8;
