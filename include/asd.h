@@ -104,7 +104,9 @@ enum {
                                    * more slots than the request's row of the page table covers */
 #define ASD_STATUS_PAGE 64u       /* cache entry points: a page id outside [0, pages) */
 #define ASD_STATUS_POSITION 128u  /* asd_kv_append: a position outside the rotation's table */
-#define ASD_STATUS_PATH 256u      /* asd_kv_compact: path[i] < i or not ascending */
+#define ASD_STATUS_PATH 256u      /* asd_kv_compact: path[i] < i or not ascending; asd_kv_weigh: path[i] outside
+                                   * [0, T) */
+#define ASD_STATUS_TOKEN 512u     /* asd_tokens_record, asd_tokens_bias: a token id >= V */
 
 /* Largest draft length: one warp lane per target row of a block. */
 #define ASD_MAX_K 31
@@ -490,6 +492,169 @@ int asd_tree_attention(const asd_kv_cache* cache, const asd_attention* args, asd
  */
 int asd_kv_compact(const asd_kv_cache* cache, int P, const int32_t* kv_len, const int32_t* path,
                    const int32_t* path_len, int32_t* status, asd_stream_t stream);
+
+/*
+ * Which cached slots a request still needs: the attention weight that each slot of
+ * each key/value head has received. asd_kv_weigh adds up what the rows of one pass
+ * give (after asd_tree_attention, which leaves their lse; the rows of a verified
+ * path after asd_kv_compact has moved it), asd_kv_evict keeps the heaviest slots.
+ *
+ * weight_out[b][h][s] = w + sum of exp(scale * (q . k_s) - lse) over the rows of
+ * request b's heads h * group .. h * group + group - 1 that see slot s; w is decay *
+ * weight[b][h][s] for s < kv_len[b] and 0 for the new slots (kv_len[b] .. kv_len[b] +
+ * n - 1), whose weights begin here; with decay = 0 weight is not read. Slots from
+ * kv_len[b] + n on are left as they were.
+ *
+ * Row i (i < n = new_len[b]) sees the slots below kv_len[b] and the new slots
+ * kv_len[b] .. kv_len[b] + i: a chain. It is token i of q and lse, or with a path
+ * token path[b][i] (a tree's accepted nodes, as asd_kv_compact takes them). A row
+ * whose lse is infinite adds nothing (a token that saw nothing has -INFINITY).
+ * Slots that a row does not see do not reach it, NaN included.
+ *
+ * A request without rows (new_len 0) and one flagged ASD_STATUS_LENGTH write
+ * nothing; a row whose path entry is outside [0, T) (ASD_STATUS_PATH) adds nothing,
+ * and a slot on a page out of range (ASD_STATUS_PAGE) counts as a key of zeros.
+ * Arithmetic: scores, exponentials and sums in fp32, rows added in a fixed order.
+ * 16-bit types with head_dim <= 128 and a multiple of 8 and rows on 16-byte
+ * boundaries run on the tensor cores; a call that gives up waiting on its own
+ * pipeline flags all its requests ASD_STATUS_INCOMPLETE (pass a status array to
+ * see it). No workspace. Values of the cache are not read. The limits on sizes are
+ * those of asd_tree_attention, with `rows` for T.
+ */
+typedef struct {
+  const void* q;           /* [B, T, q_heads, head_dim] of the cache's dtype */
+  const float* lse;        /* [B, T, q_heads] as asd_tree_attention writes it */
+  asd_strides q_strides;
+  const float* weight;     /* [B, heads, width]; may be NULL with decay = 0 */
+  float* weight_out;       /* [B, heads, width]; may be weight itself */
+  const int32_t* kv_len;   /* [B] slots that all rows see */
+  const int32_t* new_len;  /* [B] (0..rows), or NULL: rows */
+  const int32_t* path;     /* [B, rows] or NULL: row i is token i, and rows = T */
+  int32_t* status;         /* as in asd_append */
+  int layer;
+  int T;                   /* tokens of q and lse */
+  int rows;                /* rows of a request, >= 0 */
+  int q_heads;
+  int width;               /* slots that a head's weights have room for, >= kv_len + new_len of every request */
+  float scale;             /* finite */
+  float decay;             /* finite, >= 0 */
+  int reserved;            /* 0 */
+} asd_weigh;
+int asd_kv_weigh(const asd_kv_cache* cache, const asd_weigh* args, asd_stream_t stream);
+
+/*
+ * Cuts every request's cache to its budget, in place and in every layer. Of
+ * request b's kv_len[b] slots n = min(keep[b], kv_len[b]) stay in each layer and
+ * head: the first f = min(first, n), the last r = min(last, n - f), and the n - f -
+ * r heaviest of those between (a NaN weighs as much as -INFINITY; of equal weights
+ * the lower slot stays). Different heads keep different slots.
+ *
+ * A slot that stays and lies below n is not moved; the others that stay go, in
+ * ascending order, to the places below n that became free, in ascending order,
+ * their weights with them. Attention does not depend on the order of the slots
+ * (keys are rotated by their positions when they are appended), so nothing else
+ * moves. Where at least `last` tokens are appended between two evictions, no token
+ * with fewer than `last` behind it ever goes. Later tokens take positions of their
+ * own (asd_append.positions): kv_len is no longer a token's number.
+ *
+ * weight        [layers, B, heads, width]; weight_out the same or weight itself. Slots
+ *               of weight_out from n on are left as they were.
+ * kv_len_out    [B] = n; not kv_len itself (every head reads that while the call runs)
+ * keep          [B] >= 0
+ * status        ASD_STATUS_LENGTH (kv_len < 0 or past the table or the width, keep <
+ *               0): such a request moves nothing and keeps its length.
+ *               ASD_STATUS_PAGE: a move from or to a page out of range is left out,
+ *               its weight is not.
+ * width         <= ASD_MAX_EVICT_SLOTS
+ */
+typedef struct {
+  const float* weight;
+  float* weight_out;
+  const int32_t* kv_len;
+  int32_t* kv_len_out;
+  const int32_t* keep;
+  int32_t* status;
+  int first, last; /* >= 0 */
+  int width;
+  int reserved;    /* 0 */
+} asd_evict;
+#define ASD_MAX_EVICT_SLOTS 360448
+int asd_kv_evict(const asd_kv_cache* cache, const asd_evict* args, asd_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Rules: what a request's own text, its caller and its grammar do to the logits
+ * of a draft block before they are compared. The paper verifies raw logits; a
+ * serving engine changes them first, and since row j of a block continues the
+ * drafts x_0 .. x_{j-1}, every row is changed differently.
+ *
+ * Token v of row j, all in fp32, each operation rounded:
+ *   c = times said (record) + #{ i < j : x_i = v }
+ *   if c > 0 or v is in the prompt:  z <- z > 0 ? z / repetition : z * repetition
+ *   if c > 0:                        z <- z - c * frequency, then z <- z - presence
+ *   if v has a record:               z <- z + bias
+ *   if the grammar does not allow v: z <- -INFINITY, whatever it was
+ *
+ * A record says what is known of a token; a set bit of `marks` (bit v % 32 of word
+ * v / 32) that token v has one. Records without a mark are not read, so marks and
+ * records of zeros are a request without text. asd_tokens_record and
+ * asd_tokens_bias write both.
+ */
+typedef struct {
+  uint32_t seen; /* ASD_TOKEN_PROMPT if the token is in the prompt | how often it has been said (below 2^31) */
+  float bias;
+} asd_token_record;
+#define ASD_TOKEN_PROMPT 0x80000000u
+typedef struct {
+  uint32_t* marks;           /* [B, ceil(V / 32)] */
+  asd_token_record* records; /* [B, V], 8-byte aligned */
+  const float* repetition;   /* [B], > 0, or NULL: 1 */
+  const float* frequency;    /* [B] or NULL: 0 */
+  const float* presence;     /* [B] or NULL: 0 */
+  const uint32_t* allow;     /* ceil(V / 32) words a row as in marks, or NULL: every token may come */
+  int64_t allow_batch;       /* words from a request's rows to the next one's, and from a row to the next (>= 0; 0: */
+  int64_t allow_row;         /* one for all) */
+  int B, V;
+} asd_token_rules;
+
+/*
+ * asd_verify of the logits under the rules, which are applied as the rows are read:
+ * no changed logits are written. Arguments, outputs, workspace and status as
+ * for asd_verify (or, with ledger = NULL, asd_verify_strict); a NaN counts where the
+ * grammar allows its token. Regrets are differences of changed logits, which stay
+ * fp32: a draft that is not allowed has an infinite one, NaN where no token is
+ * allowed (then y* = 0). ASD_RESIDENT_INPUTS is not taken.
+ */
+int asd_rules_verify(const asd_token_rules* rules, const void* logits, int dtype, int K, const int32_t* draft,
+                     asd_ledger* ledger, float gate, int cap, int32_t* accepted_len, int32_t* committed,
+                     int32_t* recovery, int32_t* row_argmax, float* row_regret, int32_t* status, void* workspace,
+                     size_t workspace_bytes, asd_stream_t stream);
+
+/*
+ * The changed logits themselves, for callers that sample: logits and out [B, rows,
+ * V] (1 <= rows <= ASD_MAX_K + 1; out may be logits itself) of dtype ASD_F32 or
+ * ASD_BF16, rounded once. draft [B, rows - 1], or NULL: no row has drafts before it.
+ * Draft ids outside [0, V) count for nothing. Logits that no rule names are copied
+ * bit for bit. No workspace.
+ */
+int asd_rules_logits(const asd_token_rules* rules, const void* logits, int dtype, int rows, const int32_t* draft,
+                     void* out, asd_stream_t stream);
+
+/*
+ * Adds tokens to the records: tokens [B, n] int32, of which request b has the first
+ * token_len[b] (0..n; NULL: n). Negative ids are skipped, so asd_verify's `committed`
+ * can be passed as it is. prompt = 0: each is said once more; 1: each is in the prompt.
+ * status [B] or NULL: ASD_STATUS_TOKEN (an id >= V, skipped) and ASD_STATUS_LENGTH
+ * (a token_len out of range: nothing of the request is recorded) are ORed in.
+ */
+int asd_tokens_record(const asd_token_rules* rules, const int32_t* tokens, int n, const int32_t* token_len, int prompt,
+                      int32_t* status, asd_stream_t stream);
+
+/* Sets the bias of tokens: ids and bias [B, n] (n <= ASD_MAX_BIAS), lengths, negative
+ * ids and status as above; where an id comes twice the later one counts. A bias of 0
+ * is one like any other; -INFINITY bans a token. */
+#define ASD_MAX_BIAS 1024
+int asd_tokens_bias(const asd_token_rules* rules, const int32_t* ids, const float* bias, int n, const int32_t* length,
+                    int32_t* status, asd_stream_t stream);
 
 /* The device address through which kernels read page-locked (pinned) host
  * memory, e.g. logits that stay in host memory and stream to the GPU over the

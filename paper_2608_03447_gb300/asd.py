@@ -9,7 +9,10 @@ Entry points mirror the C names: ``verify`` (asd_verify), ``verify_strict``
 (asd_verify_strict), ``workspace_size``, ``workspace_init``, ``status_string``.
 Ledgers are float32 tensors of shape [B, 2] holding (budget, spent), the
 memory layout of ``asd_ledger``. The cache side of a block: ``KVCache``
-(asd_kv_cache), ``kv_append``, ``tree_mask``, ``tree_attention``, ``kv_compact``.
+(asd_kv_cache), ``kv_append``, ``tree_mask``, ``tree_attention``, ``kv_compact``,
+``kv_weigh``, ``kv_evict``. Logits under penalties, biases and grammars:
+``TokenRules`` (asd_token_rules), ``rules_verify``, ``rules_logits``,
+``tokens_record``, ``tokens_bias``.
 """
 from __future__ import annotations
 
@@ -40,9 +43,13 @@ STATUS_LENGTH = 32
 STATUS_PAGE = 64
 STATUS_POSITION = 128
 STATUS_PATH = 256
+STATUS_TOKEN = 512
 MAX_K = 31
 MAX_HEAD_DIM = 256
 MAX_PATH = 256
+MAX_BIAS = 1024
+MAX_EVICT_SLOTS = 360448
+TOKEN_PROMPT = -2**31  # ASD_TOKEN_PROMPT as an int32, of a record's first word
 RESIDENT_INPUTS = 0x100  # ASD_RESIDENT_INPUTS, ORed into the dtype code
 INT32_MAX = 2**31 - 1
 
@@ -109,6 +116,18 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.asd_tree_attention.restype = i32
     lib.asd_kv_compact.argtypes = [vp, i32, vp, vp, vp, vp, vp]
     lib.asd_kv_compact.restype = i32
+    lib.asd_kv_weigh.argtypes = [vp, vp, vp]
+    lib.asd_kv_weigh.restype = i32
+    lib.asd_kv_evict.argtypes = [vp, vp, vp]
+    lib.asd_kv_evict.restype = i32
+    lib.asd_rules_verify.argtypes = [vp, vp, i32, i32, vp, vp, f32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.asd_rules_verify.restype = i32
+    lib.asd_rules_logits.argtypes = [vp, vp, i32, i32, vp, vp, vp]
+    lib.asd_rules_logits.restype = i32
+    lib.asd_tokens_record.argtypes = [vp, vp, i32, vp, i32, vp, vp]
+    lib.asd_tokens_record.restype = i32
+    lib.asd_tokens_bias.argtypes = [vp, vp, vp, i32, vp, vp, vp]
+    lib.asd_tokens_bias.restype = i32
     lib.asd_set_launch_options.argtypes = [vp]
     lib.asd_set_launch_options.restype = i32
     lib.asd_get_launch_options.argtypes = [vp]
@@ -790,3 +809,222 @@ def kv_compact(cache: KVCache, kv_len: torch.Tensor, path: torch.Tensor, path_le
                                _stream(stream))
     if rc:
         raise AsdError("asd_kv_compact", rc)
+
+
+# asd_weigh and asd_evict as they lie in memory
+_WEIGH = struct.Struct("2P 3q 2P 3P P 5i 2f i")
+_EVICT = struct.Struct("6P 4i")
+
+
+def kv_weigh(q: torch.Tensor, lse: torch.Tensor, cache: KVCache, kv_len: torch.Tensor, weight: torch.Tensor | None,
+             layer: int = 0, decay: float = 1.0, new_len: torch.Tensor | None = None,
+             path: torch.Tensor | None = None, scale: float | None = None, out: torch.Tensor | None = None,
+             status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """asd_kv_weigh: add to every cached slot's weight what the rows of a pass gave it.
+
+    q [B, T, q_heads, D] and lse [B, T, q_heads] as tree_attention took and left them; weight float32 [B, heads,
+    width], one layer's, is written in place or to ``out`` (``None`` with ``decay=0`` and ``out``). Row i of a request
+    is token i, or token ``path[b, i]`` of int32 [B, rows], and sees the new slots kv_len .. kv_len + i; ``new_len``
+    int32 [B] counts a request's rows.
+    """
+    B, D = cache.B, cache.head_dim
+    T, q_heads = q.shape[1:3] if q.dim() == 4 else (-1, -1)
+    qs = _check_heads("q", q, cache, (B, T, q_heads, D))
+    if out is None:
+        out = weight
+    if out is None:
+        raise ValueError("kv_weigh needs a weight tensor or out")
+    width = out.shape[2] if out.dim() == 3 else -1
+    shape = (B, cache.heads, width)
+    rows = T
+    if path is not None:
+        rows = path.shape[1] if path.dim() == 2 else -1
+    args = _WEIGH.pack(
+        q.data_ptr(), _check_vector("lse", lse, cache, (B, T, q_heads), torch.float32), qs[0], qs[1], qs[2],
+        0 if weight is None else _check_vector("weight", weight, cache, shape, torch.float32),
+        _check_vector("out", out, cache, shape, torch.float32), _check_vector("kv_len", kv_len, cache, (B,)),
+        0 if new_len is None else _check_vector("new_len", new_len, cache, (B,)),
+        0 if path is None else _check_vector("path", path, cache, (B, rows)),
+        0 if status is None else _check_vector("status", status, cache, (B,)), layer, T, rows, q_heads, width,
+        D ** -0.5 if scale is None else scale, decay, 0)
+    rc = load().asd_kv_weigh(cache._ref, args, _stream(stream))
+    if rc:
+        raise AsdError("asd_kv_weigh", rc)
+    return out
+
+
+def kv_evict(cache: KVCache, kv_len: torch.Tensor, weight: torch.Tensor, keep: torch.Tensor, first: int = 0,
+             last: int = 0, out: torch.Tensor | None = None, new_len: torch.Tensor | None = None,
+             status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """asd_kv_evict: cut every request's cache to ``keep[b]`` slots, in every layer and in place.
+
+    weight float32 [layers, B, heads, width] (or without the first dimension for one layer), moved with the slots in
+    place or to ``out``. The first ``first`` and the last ``last`` slots stay. Returns the new lengths, int32 [B]
+    (``new_len``, allocated on ``stream`` if not given; not ``kv_len`` itself).
+    """
+    B = cache.B
+    one = (B,)
+    shape = (cache.layers, B, cache.heads, weight.shape[-1] if weight.dim() else -1)
+    if weight.dim() == 3 and cache.layers == 1:
+        shape = shape[1:]
+    to = weight if out is None else out
+    if new_len is None:
+        with _torch_on(stream):
+            new_len = torch.empty(one, dtype=_I32, device=cache.device)
+    args = _EVICT.pack(_check_vector("weight", weight, cache, shape, torch.float32),
+                       _check_vector("out", to, cache, shape, torch.float32),
+                       _check_vector("kv_len", kv_len, cache, one), _check_vector("new_len", new_len, cache, one),
+                       _check_vector("keep", keep, cache, one),
+                       0 if status is None else _check_vector("status", status, cache, one), first, last, shape[-1], 0)
+    rc = load().asd_kv_evict(cache._ref, args, _stream(stream))
+    if rc:
+        raise AsdError("asd_kv_evict", rc)
+    return new_len
+
+
+# ---------------------------------------------------------------- logits under rules
+
+_RULES = struct.Struct("6P 2q 2i")  # asd_token_rules
+
+
+class TokenRules:
+    """What a batch's requests know of their tokens, and their penalties (asd_token_rules).
+
+    marks       int32 [B, ceil(V / 32)]: bit v % 32 of word v / 32 set where token v has a record
+    records     int32 [B, V, 2]: (TOKEN_PROMPT if in the prompt | times said, the bits of a float32 bias)
+    repetition, frequency, presence  float32 [B] or None (no such penalty)
+
+    The tensors stay the caller's; tokens_record and tokens_bias write the first two. ``TokenRules.empty(B, V)`` makes
+    them, ``clear(b)`` empties a request's row for its next user.
+    """
+
+    def __init__(self, marks: torch.Tensor, records: torch.Tensor, repetition: torch.Tensor | None = None,
+                 frequency: torch.Tensor | None = None, presence: torch.Tensor | None = None):
+        if records.dim() != 3 or records.shape[2] != 2 or records.dtype is not _I32 or not records.is_contiguous():
+            raise ValueError("records must be a contiguous int32 tensor [B, V, 2]")
+        B, V = records.shape[:2]
+        words = (V + 31) // 32
+        if marks.shape != (B, words) or marks.dtype is not _I32 or not marks.is_contiguous():
+            raise ValueError("marks must be a contiguous int32 tensor [B, ceil(V / 32)]")
+        if not (records.is_cuda and marks.device == records.device):
+            raise ValueError("marks and records must be on one CUDA device")
+        for name, t in (("repetition", repetition), ("frequency", frequency), ("presence", presence)):
+            if t is not None and (t.shape != (B,) or t.dtype is not torch.float32 or not t.is_contiguous() or
+                                  t.device != records.device):
+                raise ValueError(f"{name} must be a contiguous float32 tensor [B] on the records' device")
+        self.marks, self.records = marks, records
+        self.repetition, self.frequency, self.presence = repetition, frequency, presence
+        self.B, self.V, self.words = B, V, words
+        self.device, self.index = records.device, records.get_device()
+        self._head = (marks.data_ptr(), records.data_ptr(), _ptr(repetition) or 0, _ptr(frequency) or 0,
+                      _ptr(presence) or 0)
+        self._plain = _RULES.pack(*self._head, 0, 0, 0, B, V)
+
+    @classmethod
+    def empty(cls, B: int, V: int, repetition: torch.Tensor | None = None, frequency: torch.Tensor | None = None,
+              presence: torch.Tensor | None = None, device="cuda", stream=None) -> "TokenRules":
+        with _torch_on(stream):
+            marks = torch.zeros(B, (V + 31) // 32, dtype=_I32, device=device)
+            records = torch.zeros(B, V, 2, dtype=_I32, device=device)
+        return cls(marks, records, repetition, frequency, presence)
+
+    def clear(self, b: int, stream=None) -> None:
+        """Forget what is known of request b's tokens."""
+        with _torch_on(stream):
+            self.marks[b].zero_()
+            self.records[b].zero_()
+
+    def _pack(self, allow: torch.Tensor | None, rows: int) -> bytes:
+        if allow is None:
+            return self._plain
+        if allow.shape != (self.B, rows, self.words) or allow.dtype is not _I32 or allow.get_device() != self.index or                 (allow.stride(2) != 1 and self.words > 1):
+            raise ValueError(f"allow must be an int32 tensor {[self.B, rows, self.words]} on the rules' device, its "
+                             "last dimension contiguous")
+        return _RULES.pack(*self._head, allow.data_ptr(), allow.stride(0), allow.stride(1), self.B, self.V)
+
+
+def _check_rules(rules: TokenRules, name: str, t: torch.Tensor, shape: tuple, dtype: torch.dtype = _I32) -> int:
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != rules.index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on the rules' device")
+    return t.data_ptr()
+
+
+def rules_verify(logits: torch.Tensor, draft: torch.Tensor, ledger: torch.Tensor | None, gate: float, cap: int,
+                 rules: TokenRules, allow: torch.Tensor | None = None, workspace: Workspace | None = None,
+                 out: dict | None = None, stream=None) -> dict:
+    """asd_rules_verify: ``verify`` of the logits under the rules (``verify_strict`` with ``ledger=None``).
+
+    logits [B, K+1, V] float32 or bfloat16; row j counts the drafts before it. ``allow`` int32 [B, K+1, ceil(V / 32)]:
+    a bit a token that the grammar lets come (strides of 0 for masks that several rows share). Workspaces are verify's.
+    """
+    B, K, V = _shape(logits, draft)
+    if (B, V) != (rules.B, rules.V):
+        raise ValueError(f"logits must be [{rules.B}, K+1, {rules.V}] like the rules")
+    code = _dtype_code(logits)
+    zp = _check_rules(rules, "logits", logits, (B, K + 1, V), logits.dtype)
+    xp = _check_rules(rules, "draft", draft, (B, K))
+    lp = None if ledger is None else _check_rules(rules, "ledger", ledger, (B, 2), torch.float32)
+    packed = rules._pack(allow, K + 1)
+    ws = workspace or Workspace(B, K, V, code, logits.device, stream)
+    o = out or alloc_outputs(B, K, logits.device, stream=stream)
+    rc = load().asd_rules_verify(packed, zp, code, K, xp, lp, float(gate), int(cap), _ptr(o["accepted_len"]),
+                                 _ptr(o["committed"]), _ptr(o["recovery"]), _ptr(o.get("row_argmax")),
+                                 _ptr(o.get("row_regret")), _ptr(o.get("status")), ws.ptr, ws.nbytes, _stream(stream))
+    if rc:
+        raise AsdError("asd_rules_verify", rc)
+    return o
+
+
+def rules_logits(logits: torch.Tensor, draft: torch.Tensor | None, rules: TokenRules,
+                 allow: torch.Tensor | None = None, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """asd_rules_logits: the logits [B, rows, V] under the rules, in ``out`` (which may be ``logits`` itself).
+
+    draft int32 [B, rows - 1], or None where no row continues drafts; ``allow`` as in rules_verify.
+    """
+    if logits.dim() != 3 or logits.shape[0] != rules.B or logits.shape[2] != rules.V:
+        raise ValueError(f"logits must be [{rules.B}, rows, {rules.V}] like the rules")
+    shape = tuple(logits.shape)
+    rows = shape[1]
+    code = _dtype_code(logits)
+    zp = _check_rules(rules, "logits", logits, shape, logits.dtype)
+    xp = None if draft is None else _check_rules(rules, "draft", draft, (rules.B, rows - 1))
+    packed = rules._pack(allow, rows)
+    if out is None:
+        with _torch_on(stream):
+            out = torch.empty(shape, dtype=logits.dtype, device=logits.device)
+    rc = load().asd_rules_logits(packed, zp, code, rows, xp, _check_rules(rules, "out", out, shape, logits.dtype),
+                                 _stream(stream))
+    if rc:
+        raise AsdError("asd_rules_logits", rc)
+    return out
+
+
+def tokens_record(tokens: torch.Tensor, rules: TokenRules, prompt: bool = False,
+                  token_len: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None) -> None:
+    """asd_tokens_record: add int32 tokens [B, n] to the records, as said or as the prompt's; negative ids are skipped.
+
+    ``verify``'s "committed" can be passed as it is; ``token_len`` int32 [B] says how many of the n a request has.
+    """
+    n = tokens.shape[1] if tokens.dim() == 2 else -1
+    one = (rules.B,)
+    rc = load().asd_tokens_record(rules._plain, _check_rules(rules, "tokens", tokens, (rules.B, n)), n,
+                                  None if token_len is None else _check_rules(rules, "token_len", token_len, one),
+                                  int(bool(prompt)),
+                                  None if status is None else _check_rules(rules, "status", status, one),
+                                  _stream(stream))
+    if rc:
+        raise AsdError("asd_tokens_record", rc)
+
+
+def tokens_bias(ids: torch.Tensor, bias: torch.Tensor, rules: TokenRules, length: torch.Tensor | None = None,
+                status: torch.Tensor | None = None, stream=None) -> None:
+    """asd_tokens_bias: set the bias of int32 ids [B, n] to float32 values [B, n]; the later one of an id counts."""
+    n = ids.shape[1] if ids.dim() == 2 else -1
+    one = (rules.B,)
+    rc = load().asd_tokens_bias(rules._plain, _check_rules(rules, "ids", ids, (rules.B, n)),
+                                _check_rules(rules, "bias", bias, (rules.B, n), torch.float32), n,
+                                None if length is None else _check_rules(rules, "length", length, one),
+                                None if status is None else _check_rules(rules, "status", status, one),
+                                _stream(stream))
+    if rc:
+        raise AsdError("asd_tokens_bias", rc)

@@ -1,0 +1,411 @@
+// libasd: eviction from a paged cache (asd_kv_evict).
+//
+// Per layer, request and key/value head: n of len slots stay, the first and the
+// last ones and the heaviest between them. Kept slots at or past n fill the free
+// places below n in ascending order, so sources and places never overlap, no two
+// moves depend on one another, and what already lies below n is not touched.
+//
+// A cluster of CTAs has a head: each keeps the weights of a part of its slots in
+// shared memory, as integers that grow with them, and finds the lightest weight
+// that stays digit by digit (11, 11, 10 bits), from histograms that the cluster
+// adds up. Two words of bits per 32 slots say which stay; their counts, added up
+// over the CTA and the cluster, give every move its number, and the moves are dealt
+// in equal shares to the cluster's CTAs, into the memory the weights were in.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <atomic>
+
+#include "asd.h"
+#include "asd_cache.cuh"
+#include "asd_device.cuh"
+#include "asd_launch.cuh"
+
+namespace {
+
+using namespace asd_detail;
+
+constexpr int kThreads = 512;
+constexpr int kWarps = kThreads / 32;
+constexpr int kBins = 2048;
+constexpr int kDigits = 3;
+constexpr int kMaxCluster = 8;
+constexpr int kMaxPart = ASD_MAX_EVICT_SLOTS / kMaxCluster;  // slots of a CTA
+constexpr int kBatch = 8;                                    // moves of a warp at once
+static_assert(kMaxPart % 32 == 0, "parts are whole words of bits");
+
+// Dynamic shared memory: weights (then moves), two words of bits per 32 slots, histograms.
+constexpr size_t evict_smem(int part) {
+  return 4 * static_cast<size_t>(part) + 8 * static_cast<size_t>(part / 32) + sizeof(unsigned) * kDigits * kBins;
+}
+static_assert(evict_smem(kMaxPart) <= 232448 - 1024, "shared memory of the longest part");
+
+struct EvictParams {
+  CacheView cache;  // of layer 0
+  long long layer_bytes;
+  const float* weight;
+  float* weight_out;
+  const int32_t* kv_len;
+  int32_t* kv_len_out;
+  const int32_t* keep;
+  int32_t* status;
+  int B, H;
+  int width, first, last;
+  int ctas;       // of a cluster
+  int part;       // slots that a CTA has room for
+  int element;    // bytes
+  int words;      // copy words of a row
+  int lane_bits;  // log2 of the lanes that copy a row
+};
+
+__device__ __forceinline__ void cluster_sync(int ctas) {
+  if (ctas == 1) {
+    __syncthreads();
+  } else {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+}
+__device__ __forceinline__ uint32_t at_rank(const void* smem, int rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(smem)), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ unsigned load_cluster(uint32_t addr) {
+  unsigned v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void store_cluster(uint32_t addr, unsigned v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+// The sum of x over the threads before this one; *total over all. A barrier on either side.
+__device__ __forceinline__ unsigned block_scan(unsigned x, unsigned* warp_sums, unsigned* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  unsigned sum = x;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const unsigned o = __shfl_up_sync(kFull, sum, off);
+    if (lane >= off) sum += o;
+  }
+  __syncthreads();
+  if (lane == 31) warp_sums[warp] = sum;
+  __syncthreads();
+  unsigned before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    const unsigned s = warp_sums[w];
+    if (w < warp) before += s;
+    all += s;
+  }
+  *total = all;
+  return before + sum - x;
+}
+
+// Word: what a row is copied in.
+template <typename Word>
+__global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__ EvictParams p) {
+  extern __shared__ __align__(16) unsigned s_mem[];
+  __shared__ unsigned s_warp[kWarps];
+  __shared__ unsigned s_found[3];  // the digit, how many of its slots stay, how many there are
+  __shared__ unsigned s_total[2];  // this CTA's counts, for the cluster
+  unsigned* s_key = s_mem;                    // [part]
+  unsigned* s_above = s_key + p.part;         // [part / 32] bits of slots heavier than the lightest that stays
+  unsigned* s_equal = s_above + p.part / 32;  // as heavy; then the bits of the slots that stay
+  unsigned* s_hist = s_equal + p.part / 32;   // [kDigits][kBins]
+
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, C = p.ctas;
+  const int head_id = blockIdx.x / C, rank = blockIdx.x - head_id * C;
+  const int h = head_id % p.H, lb = head_id / p.H, b = lb % p.B, layer = lb / p.B;
+  pdl_signal_dependents();
+  pdl_wait_prerequisites();
+
+  const int len = __ldcg(p.kv_len + b), keep = __ldcg(p.keep + b);
+  const bool bad = len < 0 || len > p.cache.slots || len > p.width || keep < 0;
+  const int n = bad ? 0 : min(keep, len);
+  if (layer == 0 && h == 0 && rank == 0 && tid == 0) {
+    if (bad && p.status) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_LENGTH));
+    p.kv_len_out[b] = bad ? len : n;
+  }
+  if (bad || n == 0) return;
+  const float* weight = p.weight + static_cast<long long>(head_id) * p.width;
+  float* weight_out = p.weight_out + static_cast<long long>(head_id) * p.width;
+  const bool copies = p.weight != p.weight_out;
+  const int per = ((len + C - 1) / C + 31) & ~31;
+  const int s0 = min(rank * per, len), count = min(per, len - s0);
+  if (n == len) {
+    if (copies)
+      for (int i = tid; i < count; i += kThreads) weight_out[s0 + i] = __ldcg(weight + s0 + i);
+    return;
+  }
+  const int first = min(p.first, n), last = min(p.last, n - first);
+
+  for (int i = tid; i < kDigits * kBins; i += kThreads) s_hist[i] = 0;
+  __syncthreads();
+#pragma unroll 4
+  for (int i = tid; i < count; i += kThreads) {
+    const int s = s0 + i;
+    const float w = __ldcg(weight + s);
+    if (copies && s < n) weight_out[s] = w;
+    unsigned key = w == w ? ordered_bits(w) : ordered_bits(-INFINITY);
+    if (s < first || s >= len - last) key = 0xffffffffu;  // above every weight
+    s_key[i] = key;
+    atomicAdd(&s_hist[key >> 21], 1u);
+  }
+
+  // the lightest weight that stays, digit by digit from the top
+  unsigned prefix = 0, need = static_cast<unsigned>(n), equal = 0;
+  int shift = 21;
+  for (int digit = 0;; ++digit) {
+    unsigned* hist = s_hist + digit * kBins;
+    cluster_sync(C);
+    constexpr int kEach = kBins / kThreads;
+    unsigned mine[kEach], sum = 0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int bin = kBins - 1 - (tid * kEach + k);
+      mine[k] = 0;
+      if (C == 1) {
+        mine[k] = hist[bin];
+      } else {
+        for (int r = 0; r < C; ++r) mine[k] += load_cluster(at_rank(hist + bin, r));
+      }
+      sum += mine[k];
+    }
+    unsigned all;
+    unsigned before = block_scan(sum, s_warp, &all);
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      if (before < need && before + mine[k] >= need) {
+        s_found[0] = static_cast<unsigned>(kBins - 1 - (tid * kEach + k));
+        s_found[1] = need - before;
+        s_found[2] = mine[k];
+      }
+      before += mine[k];
+    }
+    __syncthreads();
+    const int bits = digit == 2 ? 10 : 11;
+    prefix = digit == 0 ? s_found[0] : (prefix << bits) | s_found[0];
+    need = s_found[1];
+    equal = s_found[2];
+    if (digit == 2 || need == equal) break;  // all of the digit's slots stay: no need to look closer
+    const int next = digit == 0 ? 10 : 0;
+    for (int i = tid; i < count; i += kThreads) {
+      const unsigned key = s_key[i];
+      if (key >> shift == prefix) atomicAdd(&s_hist[(digit + 1) * kBins + ((key >> next) & (digit == 0 ? 2047u : 1023u))], 1u);
+    }
+    shift = next;
+  }
+
+  // the slots that stay: all above, of the equal ones the lowest
+  const int words = (count + 31) / 32;
+  for (int i = warp; i < words; i += kWarps) {
+    const int at = 32 * i + lane;
+    const unsigned key = at < count ? s_key[at] >> shift : 0u;
+    const unsigned above = __ballot_sync(kFull, at < count && key > prefix);
+    const unsigned same = __ballot_sync(kFull, at < count && key == prefix);
+    if (lane == 0) s_above[i] = above, s_equal[i] = same;
+  }
+  __syncthreads();
+  const int each = (words + kThreads - 1) / kThreads;  // consecutive words of a thread
+  const int w0 = min(tid * each, words), w1 = min(w0 + each, words);
+  unsigned before = 0, all;
+  if (need < equal) {
+    unsigned sum = 0;
+    for (int i = w0; i < w1; ++i) sum += __popc(s_equal[i]);
+    before = block_scan(sum, s_warp, &all);
+    if (C > 1) {
+      if (tid == 0) s_total[0] = all;
+      cluster_sync(C);
+      for (int r = 0; r < rank; ++r) before += load_cluster(at_rank(&s_total[0], r));
+      cluster_sync(C);  // read by all before it is written again
+    }
+  }
+  unsigned places = 0, sources = 0;
+  for (int i = w0; i < w1; ++i) {
+    unsigned same = s_equal[i];
+    if (need < equal) {
+      unsigned take = before < need ? need - before : 0u;  // how many of these stay
+      before += __popc(same);
+      for (unsigned left = same; left; left &= left - 1) {
+        if (take > 0)
+          --take;
+        else
+          same &= ~(left & (0u - left));
+      }
+    }
+    const unsigned stays = s_above[i] | same;
+    const int at = s0 + 32 * i, low_bits = n - at;
+    const unsigned low = low_bits >= 32 ? kFull : low_bits <= 0 ? 0u : (1u << low_bits) - 1u;
+    const unsigned free = ~stays & low, moves = stays & ~low;
+    s_above[i] = moves, s_equal[i] = free;
+    places += __popc(free), sources += __popc(moves);
+  }
+  unsigned place_all, source_all;
+  unsigned place = block_scan(places, s_warp, &place_all);
+  unsigned source = block_scan(sources, s_warp, &source_all);
+  unsigned total = source_all;
+  if (C > 1) {
+    if (tid == 0) s_total[0] = place_all, s_total[1] = source_all;
+    cluster_sync(C);
+    total = 0;
+    for (int r = 0; r < C; ++r) {
+      const unsigned other = load_cluster(at_rank(&s_total[1], r));
+      total += other;
+      if (r < rank) source += other, place += load_cluster(at_rank(&s_total[0], r));
+    }
+  } else {
+    __syncthreads();
+  }
+  // The moves' list, a share a CTA, where the weights were: every CTA of the cluster is done with its own.
+  const unsigned share = (total + C - 1) / C;
+  auto put = [&](unsigned number, unsigned offset, unsigned slot) {
+    const unsigned to = share ? number / share : 0u;
+    unsigned* const where = s_key + offset + (number - to * share);
+    if (C == 1)
+      *where = slot;
+    else
+      store_cluster(at_rank(where, static_cast<int>(to)), slot);
+  };
+  for (int i = w0; i < w1; ++i) {
+    for (unsigned left = s_above[i]; left; left &= left - 1)
+      put(source++, 0u, static_cast<unsigned>(s0 + 32 * i + __ffs(left) - 1));
+    for (unsigned left = s_equal[i]; left; left &= left - 1)
+      put(place++, share, static_cast<unsigned>(s0 + 32 * i + __ffs(left) - 1));
+  }
+  cluster_sync(C);
+
+  const unsigned begin = min(share * rank, total);
+  const int moves = static_cast<int>(min(share, total - begin));
+  char* const k = p.cache.k + layer * p.layer_bytes;
+  char* const v = p.cache.v + layer * p.layer_bytes;
+  const int per_row = 1 << p.lane_bits, rows = 32 >> p.lane_bits;
+  const int sub = lane >> p.lane_bits, word0 = lane & (per_row - 1);
+  for (int m0 = warp * kBatch; m0 < moves; m0 += kWarps * kBatch) {
+    const int many = min(kBatch, moves - m0);
+    long long from = -1, to = -1;
+    if (lane < many) {
+      const int src = static_cast<int>(s_key[m0 + lane]), dst = static_cast<int>(s_key[share + m0 + lane]);
+      from = slot_offset(p.cache, b, src);
+      to = slot_offset(p.cache, b, dst);
+      if (from < 0 || to < 0) {
+        if (p.status) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_PAGE));
+        from = to = -1;
+      } else {
+        from = (from + h * p.cache.head_stride) * p.element;
+        to = (to + h * p.cache.head_stride) * p.element;
+      }
+      weight_out[dst] = __ldcg(weight + src);
+    }
+    for (int r0 = 0; r0 < many; r0 += 4 * rows) {
+      long long src[4], dst[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = r0 + i * rows + sub;
+        src[i] = __shfl_sync(kFull, from, r & 31);
+        dst[i] = __shfl_sync(kFull, to, r & 31);
+        if (r >= many) src[i] = -1;
+      }
+      for (int w = word0; w < p.words; w += per_row) {
+        Word kw[4], vw[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (src[i] >= 0) {
+            kw[i] = __ldcg(reinterpret_cast<const Word*>(k + src[i]) + w);
+            vw[i] = __ldcg(reinterpret_cast<const Word*>(v + src[i]) + w);
+          }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (src[i] >= 0) {
+            reinterpret_cast<Word*>(k + dst[i])[w] = kw[i];
+            reinterpret_cast<Word*>(v + dst[i])[w] = vw[i];
+          }
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- host side
+
+constexpr int kMaxDevices = 64;
+
+template <typename Word>
+int launch_evict(EvictParams p, int layers, cudaStream_t stream) {
+  static std::atomic<int> sms_of[kMaxDevices];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return ASD_ERR_CUDA;
+  if (dev < 0 || dev >= kMaxDevices) return ASD_ERR_DEVICE;
+  int sms = sms_of[dev].load(std::memory_order_acquire);
+  if (sms == 0) {
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+        cudaFuncSetAttribute(evict_kernel<Word>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(evict_smem(kMaxPart))) != cudaSuccess)
+      return ASD_ERR_CUDA;
+    sms_of[dev].store(sms, std::memory_order_release);
+  }
+  const long long heads = static_cast<long long>(layers) * p.B * p.H;
+  int ctas = 1;
+  while (ctas < kMaxCluster && (p.width > ctas * kMaxPart || (heads * ctas < 2 * sms && p.width > 2048 * ctas))) ctas *= 2;
+  if (heads * ctas > INT32_MAX) return ASD_ERR_SHAPE;
+  p.ctas = ctas;
+  p.part = ((p.width + ctas - 1) / ctas + 31) / 32 * 32;
+  p.lane_bits = 0;
+  while (p.lane_bits < 5 && (1 << p.lane_bits) < p.words) ++p.lane_bits;
+  cudaLaunchAttribute attr[2];
+  cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(heads * ctas)), dim3(kThreads), stream, attr);
+  cfg.dynamicSmemBytes = evict_smem(p.part);
+  if (ctas > 1) {
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(ctas);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.numAttrs = 2;
+  }
+  if (cudaLaunchKernelEx(&cfg, evict_kernel<Word>, p) != cudaSuccess) return ASD_ERR_CUDA;
+  return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" int asd_kv_evict(const asd_kv_cache* cache, const asd_evict* args, asd_stream_t stream) {
+  const int rc = check_cache(cache);
+  if (rc != ASD_OK) return rc;
+  if (!args) return ASD_ERR_NULL;
+  const asd_evict& a = *args;
+  if (a.first < 0 || a.last < 0 || a.width < 0 || a.width > ASD_MAX_EVICT_SLOTS || a.reserved != 0) return ASD_ERR_SHAPE;
+  if (cache->B == 0) return ASD_OK;
+  if (!a.kv_len || !a.kv_len_out || !a.keep || (a.width > 0 && (!a.weight || !a.weight_out))) return ASD_ERR_NULL;
+  if (a.kv_len == a.kv_len_out) return ASD_ERR_SHAPE;
+  const void* const words[] = {a.weight, a.weight_out, a.kv_len, a.kv_len_out, a.keep, a.status};
+  for (const void* x : words)
+    if (reinterpret_cast<uintptr_t>(x) % 4 != 0) return ASD_ERR_ALIGN;
+  const size_t es = store_bytes(cache->dtype);
+  EvictParams p = {};
+  p.cache = cache_view(cache, 0);
+  p.layer_bytes = cache->layer_stride * static_cast<long long>(es);
+  p.weight = a.weight;
+  p.weight_out = a.weight_out;
+  p.kv_len = a.kv_len;
+  p.kv_len_out = a.kv_len_out;
+  p.keep = a.keep;
+  p.status = a.status;
+  p.B = cache->B;
+  p.H = cache->heads;
+  p.element = static_cast<int>(es);
+  p.width = a.width;
+  p.first = a.first;
+  p.last = a.last;
+  const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  // whole 16-byte words where every row starts on one, else elements
+  const int per = static_cast<int>(16 / es);
+  if (cache->head_dim % per == 0 && cache->layer_stride % per == 0 &&
+      rows_aligned(p.cache.k, es, 16, cache->page_stride, cache->token_stride, cache->head_stride) &&
+      reinterpret_cast<uintptr_t>(p.cache.v) % 16 == 0) {
+    p.words = cache->head_dim / per;
+    return launch_evict<uint4>(p, cache->layers, s);
+  }
+  p.words = cache->head_dim;
+  if (es == 4) return launch_evict<unsigned>(p, cache->layers, s);
+  return launch_evict<unsigned short>(p, cache->layers, s);
+}
