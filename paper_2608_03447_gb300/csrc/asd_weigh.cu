@@ -267,6 +267,7 @@ extern "C" int asd_kv_weigh(const asd_kv_cache* cache, const asd_weigh* args, as
   p.width = a.width;
   p.decay = a.decay;
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (weigh_tc_takes(cache, p)) return launch_weigh_tc(cache, p, s);
   if (cache->dtype == ASD_F32) return launch_rows<float>(p, s);
   if (cache->dtype == ASD_BF16) return launch_rows<__nv_bfloat16>(p, s);
   return launch_rows<__half>(p, s);

@@ -1,0 +1,532 @@
+// libasd: the attention weight that each cached slot receives, on the tensor cores
+// (asd_kv_weigh for 16-bit types).
+//
+// Per tile of 128 slots: S = K Q^T, the slots as the 128 rows of tensor memory and
+// the query rows as columns, at most 128 at a time. One thread owns a slot: it reads
+// its lane's columns and adds up exp2(scale S - lse) over them, so a slot's weight
+// never leaves a register until it is written, and no threads exchange anything.
+//
+// Two groups of 128 threads take the tiles in turn, each with two accumulators, so
+// that the next product is there when one is added up. With more than 128 rows a
+// pair of tiles, one a group, meets every slab of queries.
+//
+// A CTA per SM: warps 0-3 and 4-7 are the groups, warp 8 walks the units and loads
+// keys, warp 9 issues the MMAs, warps 10 and 11 copy queries and the rows' scales.
+// Keys are TMA boxes of as many slots as the page size and the tile have as a common
+// divisor, or 16-byte copies where that is less than the swizzle's eight rows.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <atomic>
+#include <type_traits>
+
+#include "asd.h"
+#include "asd_launch.cuh"
+#include "asd_tcgen05.cuh"
+#include "asd_weigh.cuh"
+
+namespace {
+
+using namespace asd_detail;
+
+constexpr int kTile = kSlabRows;  // slots
+constexpr int kCols = 128;        // query rows of a slab
+constexpr int kSumThreads = 256;
+constexpr int kKeyWarp = 8, kMmaWarp = 9, kQueryWarp = 10;
+constexpr int kQueryThreads = 64;
+constexpr int kThreads = 12 * 32;
+constexpr int kTmemCols = 512;
+constexpr int kMaxStages = 12;
+constexpr int kQueries = 2;  // slabs of queries
+constexpr unsigned long long kLandNs = 10000000;  // longer than any load takes
+constexpr size_t kSmemMax = 232448;
+
+constexpr int slab_bytes(int dim) { return kTile * dim * 2; }  // 128 rows of a padded head
+
+// What the roles know of a unit; the keys' warp walks the CTA's range and publishes its units through a ring.
+struct alignas(16) WeighUnit {
+  int b, h, rows, valid;   // request, key/value head, query rows; 0: there are no more units
+  int span, ctx, j0, j1;   // slots that the last row sees, that all do; this CTA's tiles
+  int tiles, cols, pad[2]; // slabs of queries, and the columns of each (a multiple of 16)
+};
+constexpr int kUnits = 4;
+constexpr int kUnitReaders = 11;  // warps
+
+struct WeighShared {
+  unsigned long long k_full[kMaxStages], k_empty[kMaxStages];  // loads have landed; the MMAs have read them
+  unsigned long long unit_full[kUnits], unit_empty[kUnits];
+  unsigned long long q_full[kQueries], q_empty[kQueries];
+  unsigned long long s_full[4], s_empty[4];  // accumulator 2 g + i of group g: is complete; has been read
+  unsigned long long drain;
+  uint32_t tmem_base;
+  int abort;
+  WeighUnit unit[kUnits];
+  AttnDeal deal;
+  alignas(16) RowScale scale[kQueries][kCols];  // read two at a time
+};
+constexpr int stages_for(int dim) {
+  const size_t fit = (kSmemMax - 1024 - sizeof(WeighShared) - kQueries * slab_bytes(dim)) / slab_bytes(dim);
+  return fit < static_cast<size_t>(kMaxStages) ? static_cast<int>(fit) : kMaxStages;
+}
+constexpr size_t smem_for(int dim) {
+  return 1024 + static_cast<size_t>(kQueries + stages_for(dim)) * slab_bytes(dim) + sizeof(WeighShared);
+}
+static_assert(stages_for(128) >= 4, "ring depth at the widest head");
+
+__device__ __forceinline__ bool warp_wait(unsigned long long* bar, uint32_t parity, WeighShared& sh) {
+  if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
+  return __all_sync(kFull, warp_wait_on(bar, parity, &sh.abort, nullptr));
+}
+
+// A place in the ring of units.
+struct UnitFeed {
+  int slot = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next() {
+    if (++slot == kUnits) {
+      slot = 0;
+      phase ^= 1u;
+    }
+  }
+  // the next unit, or null after the last one (or a wait that gave up); done() when it has been read
+  __device__ __forceinline__ const WeighUnit* wait(WeighShared& sh) {
+    if (!warp_wait(&sh.unit_full[slot], phase, sh) || !sh.unit[slot].valid) return nullptr;
+    return &sh.unit[slot];
+  }
+  __device__ __forceinline__ void done(WeighShared& sh) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.unit_empty[slot]);
+    next();
+  }
+};
+// A place in a ring of stages or slabs.
+template <int kStages>
+struct Ring {
+  int at = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next() {
+    if (++at == kStages) {
+      at = 0;
+      phase ^= 1u;
+    }
+  }
+};
+
+// kDim: the head, padded. kTma: keys are loaded as TMA boxes.
+template <typename T, int kDim, bool kTma>
+__global__ void __launch_bounds__(kThreads, 1)
+    weigh_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ WeighParams p, int box) {
+  constexpr int kSlab = slab_bytes(kDim), kStages = stages_for(kDim);
+  constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+  constexpr int kChunks = kDim / 8;          // 16-byte chunks of a row
+  constexpr int kRowsAtOnce = 32 / kChunks;  // rows that a warp copies per instruction
+  extern __shared__ __align__(1024) unsigned char weigh_smem_raw[];
+  const uint32_t raw = smem_u32(weigh_smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  const uint32_t sq = base, sk = base + kQueries * kSlab;
+  WeighShared& sh = *reinterpret_cast<WeighShared*>(weigh_smem_raw + (base - raw) + (kQueries + kStages) * kSlab);
+
+  const int warp = __shfl_sync(kFull, static_cast<int>(threadIdx.x >> 5), 0);
+  const int lane = threadIdx.x & 31;
+  pdl_signal_dependents();
+  if (warp == kQueryWarp) {  // a barrier or two a lane
+    if (lane < kMaxStages) {
+      mbar_init(&sh.k_full[lane], kTma ? 1 : 32);
+      mbar_init(&sh.k_empty[lane], 1);
+    }
+    if (lane < kUnits) {
+      mbar_init(&sh.unit_full[lane], 1);
+      mbar_init(&sh.unit_empty[lane], kUnitReaders);
+    }
+    if (lane >= 16 && lane < 16 + kQueries) {
+      mbar_init(&sh.q_full[lane - 16], 2 * kQueryThreads);  // each thread's copies, and its scales
+      mbar_init(&sh.q_empty[lane - 16], 1 + kSumThreads / 32);
+    }
+    if (lane >= 20 && lane < 24) {
+      mbar_init(&sh.s_full[lane - 20], 1);
+      mbar_init(&sh.s_empty[lane - 20], 4);
+    }
+    if (lane == 31) {
+      mbar_init(&sh.drain, 1);
+      sh.abort = 0;
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_for_mma();
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)),
+                 "r"(kTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (kTma && warp == kKeyWarp && lane == 0)
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_k)) : "memory");
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = __reduce_max_sync(kFull, sh.tmem_base);
+
+  pdl_wait_prerequisites();
+  const int chunk = lane % kChunks, sub = lane / kChunks;
+  // where chunk `chunk` of row r lies in a slab
+  auto place = [&](int r) {
+    return static_cast<uint32_t>((chunk >> 3) * kHalfSlab + r * 128 + (((chunk & 7) ^ (r & 7)) << 4));
+  };
+  const bool has_chunk = chunk * 8 < p.a.D;
+
+  if (warp == kKeyWarp) {
+    // ---------------- units and keys
+    const AttnParams a = weigh_deal_params(p);
+    const bool elected = elect_lane();
+    attn_deal<kTile>(a, sh.deal);
+    bool ok = true;
+    UnitFeed feed;  // the next free slot
+    Ring<kStages> ring;
+    auto publish = [&](const WeighUnit& u) {
+      ok = ok && warp_wait(&sh.unit_empty[feed.slot], feed.phase ^ 1u, sh);
+      if (lane == 0) {
+        sh.unit[feed.slot] = u;
+        mbar_arrive(&sh.unit_full[feed.slot]);
+      }
+      __syncwarp();
+      feed.next();
+    };
+    AttnWalk<kTile> w(a, sh.deal);
+    for (w.start(); ok && w.more(); w.next()) {
+      WeighUnit u = {};
+      u.b = w.b, u.h = w.h, u.rows = w.rows(), u.valid = 1;
+      u.span = w.span(), u.ctx = w.r.ctx, u.j0 = w.j0, u.j1 = w.j1();
+      u.tiles = (u.rows + kCols - 1) / kCols;
+      u.cols = ((u.rows + u.tiles - 1) / u.tiles + 15) & ~15;
+      publish(u);
+      for (int j = u.j0; ok && j < u.j1; ++j) {
+        const int slot0 = j * kTile, rows = min(kTile, u.span - slot0);
+        const uint32_t dst = sk + ring.at * kSlab;
+        unsigned long long* const bar = &sh.k_full[ring.at];
+        if constexpr (kTma) {
+          int page = 0, at = 0;  // where this lane's box begins
+          if (lane * box < rows) {
+            const int slot = slot0 + lane * box, n = a.cache.div.quot(slot);
+            page = __ldcg(a.cache.table + static_cast<long long>(u.b) * a.cache.table_width + n);
+            at = slot - n * a.cache.div.size;
+          }
+          ok = warp_wait(&sh.k_empty[ring.at], ring.phase ^ 1u, sh);
+          if (!ok) break;
+          const int n = uniform((rows + box - 1) / box), head = uniform(u.h);
+          if (elected) mbar_expect_tx(bar, static_cast<uint32_t>(n * box) * (kDim * 2));
+          __syncwarp();
+          // a page out of range lies outside the tensor: the box is filled with zeros
+#pragma unroll 4
+          for (int i = 0; i < n; ++i) {
+            const int pg = __shfl_sync(kFull, page, i), first = __shfl_sync(kFull, at, i);
+            if (elected) {
+#pragma unroll
+              for (int half = 0; half < kDim / 64; ++half)
+                load_box(dst + half * kHalfSlab + i * box * 128, &map_k, bar, half * 64, first, head, pg);
+            }
+          }
+          if (lane < n && static_cast<unsigned>(page) >= static_cast<unsigned>(a.cache.pages) && a.status)
+            atomicOr(a.status + u.b, static_cast<int>(ASD_STATUS_PAGE));
+          __syncwarp();
+        } else {
+          ok = warp_wait(&sh.k_empty[ring.at], ring.phase ^ 1u, sh);
+          if (!ok) break;
+          for (int r0 = 0; r0 < rows; r0 += 32) {
+            long long off = -1;  // of row r0 + lane
+            if (r0 + lane < rows) {
+              off = slot_offset(a.cache, u.b, slot0 + r0 + lane);
+              if (off >= 0)
+                off += u.h * a.cache.head_stride;
+              else if (a.status)
+                atomicOr(a.status + u.b, static_cast<int>(ASD_STATUS_PAGE));
+            }
+#pragma unroll 4
+            for (int i = 0; i < 32 / kRowsAtOnce; ++i) {
+              const int r = i * kRowsAtOnce + sub;
+              const long long o = __shfl_sync(kFull, off, r);
+              const bool has = o >= 0 && has_chunk;
+              if (r0 + r < rows) copy16(dst + place(r0 + r), has ? a.cache.k + 2 * (o + chunk * 8) : a.q, has);
+            }
+          }
+          copies_arrive(bar);
+        }
+        ring.next();
+      }
+    }
+    publish(WeighUnit{});
+    if (!kTma) asm volatile("cp.async.wait_all;" ::: "memory");
+  } else if (warp >= kQueryWarp) {
+    // ---------------- queries, in as many slabs as they need; again for every pair of tiles where there are several
+    const int part = warp - kQueryWarp;
+    UnitFeed feed;
+    Ring<kQueries> ring;
+    bool ok = true;
+    while (ok) {
+      const WeighUnit* next = feed.wait(sh);
+      if (!next) break;
+      const WeighUnit u = *next;
+      feed.done(sh);
+      const int times = u.tiles > 1 ? (u.j1 - u.j0 + 1) / 2 : 1;
+      for (int i = 0; ok && i < times; ++i) {
+        for (int tile = 0; ok && tile < u.tiles; ++tile) {
+          ok = warp_wait(&sh.q_empty[ring.at], ring.phase ^ 1u, sh);
+          if (!ok) break;
+          // 32 rows at a time, a lane their tokens
+          for (int r0 = part * 32; r0 < u.cols; r0 += 64) {
+            const int r = r0 + lane, row = tile * u.cols + r, t = p.a.by_group.quot(row);
+            const int token = r < u.cols && row < u.rows ? weigh_token(p, u.b, t) : -1;
+            const int head = u.h * p.a.group + row - t * p.a.group;
+            const long long off = token < 0 ? -1 : u.b * p.a.q_batch + token * p.a.q_token + head * p.a.q_head;
+            if (r < u.cols) sh.scale[ring.at][r] = row_scale(p, u.b, token, head);
+#pragma unroll 4
+            for (int k = 0; k < 32 / kRowsAtOnce; ++k) {
+              const int to = k * kRowsAtOnce + sub;
+              const long long o = __shfl_sync(kFull, off, to);
+              const bool has = o >= 0 && has_chunk;
+              if (r0 + to < u.cols)
+                copy16(sq + ring.at * kSlab + place(r0 + to), has ? p.a.q + 2 * (o + chunk * 8) : p.a.q, has);
+            }
+          }
+          copies_arrive(&sh.q_full[ring.at]);
+          mbar_arrive(&sh.q_full[ring.at]);
+          ring.next();
+        }
+      }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else if (warp == kMmaWarp) {
+    // ---------------- S = K Q^T
+    const bool elected = elect_lane();
+    UnitFeed feed;
+    Ring<kStages> keys;
+    Ring<kQueries> queries;
+    uint32_t empty = 0xfu;  // per accumulator the parity to wait for
+    int turn = 0;           // of the groups
+    uint32_t which = 0;     // a bit a group: its next accumulator
+    bool ok = true;
+    auto product = [&](int g, int stage) {  // of a tile's keys with the slab of queries, for group g
+      const int acc = 2 * g + static_cast<int>((which >> g) & 1u);
+      ok = ok && warp_wait(&sh.s_empty[acc], (empty >> acc) & 1u, sh);
+      empty ^= 1u << acc;
+      which ^= 1u << g;
+      return acc;
+    };
+    while (ok) {
+      const WeighUnit* u = feed.wait(sh);
+      if (!u) break;
+      const int tiles = uniform(u->tiles);
+      const uint32_t desc = uniform(instr_desc(kBf16, u->cols, false));
+      int left = uniform(u->j1 - u->j0);
+      feed.done(sh);
+      if (tiles == 1) {
+        ok = warp_wait(&sh.q_full[queries.at], queries.phase, sh);
+        fence_for_mma();
+      }
+      while (ok && left > 0) {
+        const int pair = tiles == 1 ? 1 : min(left, 2);
+        int stage[2] = {keys.at, keys.at + 1 == kStages ? 0 : keys.at + 1};
+#pragma unroll 1
+        for (int tile = 0; ok && tile < tiles; ++tile) {
+          if (tiles > 1) {
+            ok = warp_wait(&sh.q_full[queries.at], queries.phase, sh);
+            fence_for_mma();
+          }
+#pragma unroll 1
+          for (int i = 0; ok && i < pair; ++i) {
+            if (tile == 0) {
+              ok = warp_wait(&sh.k_full[keys.at], keys.phase, sh);
+              if (!kTma) fence_for_mma();
+              keys.next();
+            }
+            const int s = uniform(i == 0 ? stage[0] : stage[1]);
+            const int acc = uniform(product(tiles == 1 ? turn : i, s));
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t ka = uniform((sk + s * kSlab) >> 4), qb = uniform((sq + queries.at * kSlab) >> 4);
+            const uint32_t d = uniform(tmem + static_cast<uint32_t>(acc * kCols));
+            if (elected) {
+#pragma unroll
+              for (int k = 0; k < kDim / 16; ++k) {
+                const uint32_t at = ((k >> 2) * kHalfSlab + (k & 3) * 32) >> 4;
+                mma_smem(d, tile_desc(ka + at, false), tile_desc(qb + at, false), desc, k > 0 ? 1u : 0u);
+              }
+              mma_commit(&sh.s_full[acc]);
+              if (tile == tiles - 1) mma_commit(&sh.k_empty[s]);
+            }
+            __syncwarp();
+          }
+          if (tiles > 1) {
+            if (elected) mma_commit(&sh.q_empty[queries.at]);
+            __syncwarp();
+            queries.next();
+          }
+        }
+        turn ^= 1;
+        left -= pair;
+      }
+      if (tiles == 1) {
+        if (elected) mma_commit(&sh.q_empty[queries.at]);
+        __syncwarp();
+        queries.next();
+      }
+    }
+    drain(&sh.drain, elected);
+  } else {
+    // ---------------- sums: thread `slot` of group g
+    const int g = warp >> 2;
+    const int slot_of = threadIdx.x & 127;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    UnitFeed feed;
+    Ring<kQueries> queries;
+    uint32_t full = 0;  // per accumulator the parity to wait for
+    uint32_t which = 0;
+    int turn = 0;
+    bool ok = true;
+    while (ok) {
+      const WeighUnit* next = feed.wait(sh);
+      if (!next) break;
+      const WeighUnit u = *next;
+      feed.done(sh);
+      const bool pairs = u.tiles > 1;
+      if (!pairs) ok = warp_wait(&sh.q_full[queries.at], queries.phase, sh);
+      for (int j = u.j0; ok && j < u.j1; j += pairs ? 2 : 1) {
+        const int mine = pairs ? j + g : j;
+        const bool has = pairs ? mine < u.j1 : turn == g;  // whether this group has a tile
+        turn ^= 1;
+        if (!has && !pairs) continue;
+        const int slot = mine * kTile + slot_of;
+        const bool exists = has && slot < u.span;
+        const long long at = (static_cast<long long>(u.b) * p.a.heads + u.h) * p.width + slot;
+        float before = 0.0f;
+        if (exists && slot < u.ctx && p.decay != 0.0f) before = __ldcg(p.weight + at);
+        const bool masked = mine * kTile > u.ctx - kTile;  // some slot is not seen by all rows
+        float2 sum = {0.0f, 0.0f};
+        for (int tile = 0; ok && tile < u.tiles; ++tile) {
+          if (pairs) ok = warp_wait(&sh.q_full[queries.at], queries.phase, sh);
+          if (ok && has) {
+            const int acc = 2 * g + static_cast<int>(which);
+            ok = warp_wait(&sh.s_full[acc], (full >> which) & 1u, sh);
+            full ^= 1u << which;
+            which ^= 1u;
+            if (ok) {
+              tc_fence_after();
+              const uint32_t from = tmem + static_cast<uint32_t>(acc * kCols) + lanes;
+              const float4* scale = reinterpret_cast<const float4*>(sh.scale[queries.at]);
+              // the slab's first row that sees the slot
+              const int first = masked && slot > u.ctx ? min((slot - u.ctx) * p.a.group - tile * u.cols, kCols) : 0;
+#pragma unroll 1
+              for (int c = 0; c < u.cols; c += 16) {
+                float z[16];
+                tmem_ld16(from + c, z);
+                tmem_ld_wait();
+#pragma unroll
+                for (int k = 0; k < 16; k += 2) {
+                  const float4 s = scale[(c + k) / 2];
+                  float e0 = exp2_fast(fmaf(z[k], p.a.scale_log2, -s.x));
+                  float e1 = exp2_fast(fmaf(z[k + 1], p.a.scale_log2, -s.z));
+                  // neither a row that adds nothing nor one that does not see the slot, whatever its product is
+                  if (s.y == 0.0f || c + k < first) e0 = 0.0f;
+                  if (s.w == 0.0f || c + k + 1 < first) e1 = 0.0f;
+                  sum.x = fmaf(e0, s.y, sum.x);
+                  sum.y = fmaf(e1, s.w, sum.y);
+                }
+              }
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&sh.s_empty[acc]);
+            }
+          }
+          if (pairs) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.q_empty[queries.at]);
+            queries.next();
+          }
+        }
+        if (ok && exists) p.weight_out[at] = fmaf(before, p.decay, sum.x + sum.y);
+      }
+      if (!pairs) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.q_empty[queries.at]);
+        queries.next();
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (sh.abort) {
+    attn_incomplete(p.a.status, p.a.B, threadIdx.x, kThreads);
+    // loads that nobody waited for: give them time to land before the CTA's memory is another's
+    const unsigned long long t0 = global_ns();
+    while (global_ns() - t0 < kLandNs) {
+    }
+  }
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------- host side
+
+constexpr int kMaxDevices = 64;
+
+template <typename T, int kDim, bool kTma>
+int launch(const CUtensorMap& map, const WeighParams& p, int box, cudaStream_t stream) {
+  auto kernel = weigh_tc_kernel<T, kDim, kTma>;
+  static std::atomic<int> grid_of[kMaxDevices];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return ASD_ERR_CUDA;
+  if (dev < 0 || dev >= kMaxDevices) return ASD_ERR_DEVICE;
+  int grid = grid_of[dev].load(std::memory_order_acquire);
+  if (grid == 0) {
+    int sms = 0, major = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+      return ASD_ERR_CUDA;
+    if (major != 10) return ASD_ERR_DEVICE;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(smem_for(kDim))) != cudaSuccess)
+      return ASD_ERR_CUDA;
+    grid = sms;
+    grid_of[dev].store(grid, std::memory_order_release);
+  }
+  cudaLaunchAttribute attr;
+  cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(kThreads), stream, &attr);
+  cfg.dynamicSmemBytes = smem_for(kDim);
+  if (cudaLaunchKernelEx(&cfg, kernel, map, p, box) != cudaSuccess) return ASD_ERR_CUDA;
+  return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;
+}
+
+template <typename T, int kDim>
+int launch_dim(const asd_kv_cache* cache, const WeighParams& p, cudaStream_t stream) {
+  CUtensorMap map;
+  const int box = box_slots(cache);
+  if (box && make_map(&map, cache->dtype == ASD_BF16, p.a.cache.k, cache, box))
+    return launch<T, kDim, true>(map, p, box, stream);
+  return launch<T, kDim, false>(map, p, 0, stream);
+}
+
+}  // namespace
+
+namespace asd_detail {
+
+// 16-bit types, heads of at most 128 whose rows are whole 16-byte words on 16-byte boundaries.
+bool weigh_tc_takes(const asd_kv_cache* cache, const WeighParams& p) {
+  return cache->dtype != ASD_F32 && p.a.D <= 128 && p.a.D % 8 == 0 &&
+         rows_aligned(p.a.cache.k, 2, 16, p.a.cache.page_stride, p.a.cache.token_stride, p.a.cache.head_stride) &&
+         rows_aligned(p.a.q, 2, 16, p.a.q_batch, p.a.q_token, p.a.q_head);
+}
+
+int launch_weigh_tc(const asd_kv_cache* cache, const WeighParams& p, cudaStream_t stream) {
+  if (cache->dtype == ASD_BF16)
+    return p.a.D <= 64 ? launch_dim<__nv_bfloat16, 64>(cache, p, stream)
+                       : launch_dim<__nv_bfloat16, 128>(cache, p, stream);
+  return p.a.D <= 64 ? launch_dim<__half, 64>(cache, p, stream) : launch_dim<__half, 128>(cache, p, stream);
+}
+
+}  // namespace asd_detail
