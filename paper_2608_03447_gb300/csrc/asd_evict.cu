@@ -5,12 +5,14 @@
 // places below n in ascending order, so sources and places never overlap, no two
 // moves depend on one another, and what already lies below n is not touched.
 //
-// A cluster of CTAs has a head: each keeps the weights of a part of its slots in
-// shared memory, as integers that grow with them, and finds the lightest weight
-// that stays digit by digit (11, 11, 10 bits), from histograms that the cluster
-// adds up. Two words of bits per 32 slots say which stay; their counts, added up
-// over the CTA and the cluster, give every move its number, and the moves are dealt
-// in equal shares to the cluster's CTAs, into the memory the weights were in.
+// A CTA, or for few long heads a cluster, has a head: it keeps the weights in shared
+// memory, as integers that grow with them, and finds the lightest weight that stays
+// digit by digit from histograms. Digits are of the distance to the smallest key and
+// as fine as 2048 bins allow: floats of like size share their upper bits, and
+// additions to the same few bins wait for one another. Two words of bits per 32 slots
+// say which stay and which are free; their counts, added up over the CTA and the
+// cluster, give every move its number, and the moves are dealt in equal shares to the
+// cluster's CTAs, into the memory the weights were in.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -27,18 +29,16 @@ namespace {
 
 using namespace asd_detail;
 
-constexpr int kThreads = 512;
-constexpr int kWarps = kThreads / 32;
-constexpr int kBins = 2048;
-constexpr int kDigits = 3;
+constexpr int kBinBits = 11, kBins = 1 << kBinBits;
+constexpr int kDigits = 3;  // that 32 bits have
 constexpr int kMaxCluster = 8;
 constexpr int kMaxPart = ASD_MAX_EVICT_SLOTS / kMaxCluster;  // slots of a CTA
-constexpr int kBatch = 8;                                    // moves of a warp at once
+constexpr int kAtOnce = 4;  // rows of keys and of values that a lane has in flight
 static_assert(kMaxPart % 32 == 0, "parts are whole words of bits");
 
-// Dynamic shared memory: weights (then moves), two words of bits per 32 slots, histograms.
+// Dynamic shared memory: histograms; weights (then moves); per 32 slots two words of bits and the counts before them.
 constexpr size_t evict_smem(int part) {
-  return 4 * static_cast<size_t>(part) + 8 * static_cast<size_t>(part / 32) + sizeof(unsigned) * kDigits * kBins;
+  return 4 * static_cast<size_t>(part) + 12 * static_cast<size_t>(part / 32) + sizeof(unsigned) * kDigits * kBins;
 }
 static_assert(evict_smem(kMaxPart) <= 232448 - 1024, "shared memory of the longest part");
 
@@ -82,6 +82,7 @@ __device__ __forceinline__ void store_cluster(uint32_t addr, unsigned v) {
 }
 
 // The sum of x over the threads before this one; *total over all. A barrier on either side.
+template <int kWarps>
 __device__ __forceinline__ unsigned block_scan(unsigned x, unsigned* warp_sums, unsigned* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   unsigned sum = x;
@@ -104,22 +105,26 @@ __device__ __forceinline__ unsigned block_scan(unsigned x, unsigned* warp_sums, 
   return before + sum - x;
 }
 
-// Word: what a row is copied in.
-template <typename Word>
-__global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__ EvictParams p) {
+// Word: what a row is copied in. Up to four CTAs an SM of 256 threads, two of 512.
+template <typename Word, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_kernel(const __grid_constant__ EvictParams p) {
+  constexpr int kWarps = kThreads / 32;
   extern __shared__ __align__(16) unsigned s_mem[];
   __shared__ unsigned s_warp[kWarps];
   __shared__ unsigned s_found[3];  // the digit, how many of its slots stay, how many there are
-  __shared__ unsigned s_total[2];  // this CTA's counts, for the cluster
-  unsigned* s_key = s_mem;                    // [part]
-  unsigned* s_above = s_key + p.part;         // [part / 32] bits of slots heavier than the lightest that stays
-  unsigned* s_equal = s_above + p.part / 32;  // as heavy; then the bits of the slots that stay
-  unsigned* s_hist = s_equal + p.part / 32;   // [kDigits][kBins]
+  __shared__ unsigned s_total[4];  // this CTA's counts, its smallest and largest key, for the cluster
+  unsigned* s_hist = s_mem;                   // [kDigits][kBins], cleared by 16-byte words
+  unsigned* s_key = s_hist + kDigits * kBins; // [part]
+  unsigned* s_above = s_key + p.part;         // [part / 32] bits: heavier than the lightest that stays; then moves
+  unsigned* s_equal = s_above + p.part / 32;  // as heavy; then free places
+  unsigned* s_base = s_equal + p.part / 32;   // [part / 32] how many come before: free places above, moves below
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, C = p.ctas;
   const int head_id = blockIdx.x / C, rank = blockIdx.x - head_id * C;
   const int h = head_id % p.H, lb = head_id / p.H, b = lb % p.B, layer = lb / p.B;
   pdl_signal_dependents();
+  for (int i = tid; i < kDigits * kBins / 4; i += kThreads)
+    reinterpret_cast<uint4*>(s_hist)[i] = make_uint4(0u, 0u, 0u, 0u);
   pdl_wait_prerequisites();
 
   const int len = __ldcg(p.kv_len + b), keep = __ldcg(p.keep + b);
@@ -142,40 +147,75 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
   }
   const int first = min(p.first, n), last = min(p.last, n - first);
 
-  for (int i = tid; i < kDigits * kBins; i += kThreads) s_hist[i] = 0;
-  __syncthreads();
-#pragma unroll 4
+  // keys; those that stay in any case are above every weight and in no histogram
+  constexpr unsigned kStays = 0xffffffffu;
+  unsigned smallest = kStays, largest = 0u;
+#pragma unroll 8
   for (int i = tid; i < count; i += kThreads) {
     const int s = s0 + i;
     const float w = __ldcg(weight + s);
     if (copies && s < n) weight_out[s] = w;
     unsigned key = w == w ? ordered_bits(w) : ordered_bits(-INFINITY);
-    if (s < first || s >= len - last) key = 0xffffffffu;  // above every weight
+    if (s < first || s >= len - last) {
+      key = kStays;
+    } else {
+      smallest = min(smallest, key);
+      largest = max(largest, key);
+    }
     s_key[i] = key;
-    atomicAdd(&s_hist[key >> 21], 1u);
+  }
+  smallest = __reduce_min_sync(kFull, smallest);
+  largest = __reduce_max_sync(kFull, largest);
+  if (tid == 0) s_total[2] = kStays, s_total[3] = 0u;
+  __syncthreads();
+  if (lane == 0) {
+    atomicMin(&s_total[2], smallest);
+    atomicMax(&s_total[3], largest);
+  }
+  cluster_sync(C);
+  smallest = s_total[2], largest = s_total[3];
+  for (int r = 0; C > 1 && r < C; ++r) {
+    smallest = min(smallest, load_cluster(at_rank(&s_total[2], r)));
+    largest = max(largest, load_cluster(at_rank(&s_total[3], r)));
   }
 
-  // the lightest weight that stays, digit by digit from the top
-  unsigned prefix = 0, need = static_cast<unsigned>(n), equal = 0;
-  int shift = 21;
-  for (int digit = 0;; ++digit) {
+  // The lightest weight that stays: of the keys' distances to the smallest, digit by digit from the top. All whose upper
+  // bits are above `prefix` stay, of the `equal` ones that share it `need`.
+  const int range = 32 - __clz(largest - smallest);  // bits; n < len, so some keys are no kStays
+  unsigned prefix = 0, need = static_cast<unsigned>(n - first - last), equal = static_cast<unsigned>(len - first - last);
+  int shift = range;
+  for (int digit = 0; need > 0 && need < equal && shift > 0; ++digit) {
     unsigned* hist = s_hist + digit * kBins;
+    const int next = max(0, shift - kBinBits);
+    const unsigned mask = (1u << (shift - next)) - 1u;
+    for (int i = tid; i < count; i += kThreads) {
+      const unsigned key = s_key[i], d = key - smallest;
+      if (key != kStays && (shift == 32 || d >> shift == prefix)) atomicAdd(&hist[(d >> next) & mask], 1u);
+    }
     cluster_sync(C);
+    if (C > 1) {  // a CTA adds up its share of the bins for all
+      const int from = kBins / C * rank;
+      for (int i = tid; i < kBins / C; i += kThreads) {
+        unsigned some[kMaxCluster], total = 0;
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; ++r) some[r] = r < C ? load_cluster(at_rank(hist + from + i, r)) : 0u;
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; ++r) total += some[r];
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; ++r)
+          if (r < C) store_cluster(at_rank(hist + from + i, r), total);
+      }
+      cluster_sync(C);
+    }
     constexpr int kEach = kBins / kThreads;
     unsigned mine[kEach], sum = 0;
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
-      const int bin = kBins - 1 - (tid * kEach + k);
-      mine[k] = 0;
-      if (C == 1) {
-        mine[k] = hist[bin];
-      } else {
-        for (int r = 0; r < C; ++r) mine[k] += load_cluster(at_rank(hist + bin, r));
-      }
+      mine[k] = hist[kBins - 1 - (tid * kEach + k)];
       sum += mine[k];
     }
     unsigned all;
-    unsigned before = block_scan(sum, s_warp, &all);
+    unsigned before = block_scan<kWarps>(sum, s_warp, &all);
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
       if (before < need && before + mine[k] >= need) {
@@ -186,75 +226,71 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
       before += mine[k];
     }
     __syncthreads();
-    const int bits = digit == 2 ? 10 : 11;
-    prefix = digit == 0 ? s_found[0] : (prefix << bits) | s_found[0];
+    prefix = (prefix << (shift - next)) | s_found[0];
     need = s_found[1];
     equal = s_found[2];
-    if (digit == 2 || need == equal) break;  // all of the digit's slots stay: no need to look closer
-    const int next = digit == 0 ? 10 : 0;
-    for (int i = tid; i < count; i += kThreads) {
-      const unsigned key = s_key[i];
-      if (key >> shift == prefix) atomicAdd(&s_hist[(digit + 1) * kBins + ((key >> next) & (digit == 0 ? 2047u : 1023u))], 1u);
-    }
     shift = next;
   }
+  const bool some = need > 0 && need < equal;  // of equal ones the lowest slots stay
 
-  // the slots that stay: all above, of the equal ones the lowest
   const int words = (count + 31) / 32;
   for (int i = warp; i < words; i += kWarps) {
     const int at = 32 * i + lane;
-    const unsigned key = at < count ? s_key[at] >> shift : 0u;
-    const unsigned above = __ballot_sync(kFull, at < count && key > prefix);
-    const unsigned same = __ballot_sync(kFull, at < count && key == prefix);
+    const unsigned key = at < count ? s_key[at] : 0u, d = key - smallest;
+    const unsigned top = shift == 32 ? 0u : d >> shift;
+    const unsigned above = __ballot_sync(kFull, at < count && (key == kStays || top > prefix));
+    const unsigned same = __ballot_sync(kFull, at < count && key != kStays && top == prefix);
     if (lane == 0) s_above[i] = above, s_equal[i] = same;
   }
   __syncthreads();
   const int each = (words + kThreads - 1) / kThreads;  // consecutive words of a thread
   const int w0 = min(tid * each, words), w1 = min(w0 + each, words);
-  unsigned before = 0, all;
-  if (need < equal) {
+  unsigned all = 0;
+  if (some) {
     unsigned sum = 0;
     for (int i = w0; i < w1; ++i) sum += __popc(s_equal[i]);
-    before = block_scan(sum, s_warp, &all);
+    unsigned before = block_scan<kWarps>(sum, s_warp, &all);
     if (C > 1) {
       if (tid == 0) s_total[0] = all;
       cluster_sync(C);
       for (int r = 0; r < rank; ++r) before += load_cluster(at_rank(&s_total[0], r));
       cluster_sync(C);  // read by all before it is written again
     }
-  }
-  unsigned places = 0, sources = 0;
-  for (int i = w0; i < w1; ++i) {
-    unsigned same = s_equal[i];
-    if (need < equal) {
-      unsigned take = before < need ? need - before : 0u;  // how many of these stay
-      before += __popc(same);
-      for (unsigned left = same; left; left &= left - 1) {
-        if (take > 0)
-          --take;
-        else
-          same &= ~(left & (0u - left));
-      }
+    for (int i = w0; i < w1; ++i) {
+      s_base[i] = before;
+      before += __popc(s_equal[i]);
     }
-    const unsigned stays = s_above[i] | same;
-    const int at = s0 + 32 * i, low_bits = n - at;
+    __syncthreads();
+    for (int i = warp; i < words; i += kWarps) {
+      const unsigned same = s_equal[i];
+      const bool stays = ((same >> lane) & 1u) && s_base[i] + __popc(same & ((1u << lane) - 1u)) < need;
+      const unsigned keeps = __ballot_sync(kFull, stays);
+      if (lane == 0) s_equal[i] = keeps;
+    }
+    __syncthreads();
+  }
+  unsigned counts = 0;  // of this thread's words: free places above, moves below
+  for (int i = w0; i < w1; ++i) {
+    const unsigned stays = s_above[i] | (need > 0 ? s_equal[i] : 0u);
+    const int low_bits = n - (s0 + 32 * i);
     const unsigned low = low_bits >= 32 ? kFull : low_bits <= 0 ? 0u : (1u << low_bits) - 1u;
     const unsigned free = ~stays & low, moves = stays & ~low;
     s_above[i] = moves, s_equal[i] = free;
-    places += __popc(free), sources += __popc(moves);
+    s_base[i] = counts;
+    counts += (static_cast<unsigned>(__popc(free)) << 16) + static_cast<unsigned>(__popc(moves));
   }
-  unsigned place_all, source_all;
-  unsigned place = block_scan(places, s_warp, &place_all);
-  unsigned source = block_scan(sources, s_warp, &source_all);
-  unsigned total = source_all;
+  static_assert(kMaxPart < 65536, "a CTA's counts have 16 bits");
+  const unsigned before = block_scan<kWarps>(counts, s_warp, &all);
+  for (int i = w0; i < w1; ++i) s_base[i] += before;
+  unsigned place = 0, source = 0, total = all & 0xffffu;  // in the CTAs before; in all
   if (C > 1) {
-    if (tid == 0) s_total[0] = place_all, s_total[1] = source_all;
+    if (tid == 0) s_total[0] = all;
     cluster_sync(C);
     total = 0;
     for (int r = 0; r < C; ++r) {
-      const unsigned other = load_cluster(at_rank(&s_total[1], r));
-      total += other;
-      if (r < rank) source += other, place += load_cluster(at_rank(&s_total[0], r));
+      const unsigned other = load_cluster(at_rank(&s_total[0], r));
+      total += other & 0xffffu;
+      if (r < rank) place += other >> 16, source += other & 0xffffu;
     }
   } else {
     __syncthreads();
@@ -262,18 +298,19 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
   // The moves' list, a share a CTA, where the weights were: every CTA of the cluster is done with its own.
   const unsigned share = (total + C - 1) / C;
   auto put = [&](unsigned number, unsigned offset, unsigned slot) {
-    const unsigned to = share ? number / share : 0u;
-    unsigned* const where = s_key + offset + (number - to * share);
-    if (C == 1)
-      *where = slot;
-    else
-      store_cluster(at_rank(where, static_cast<int>(to)), slot);
+    if (C == 1) {
+      s_key[offset + number] = slot;
+    } else {
+      const unsigned to = number / share;
+      store_cluster(at_rank(s_key + offset + (number - to * share), static_cast<int>(to)), slot);
+    }
   };
-  for (int i = w0; i < w1; ++i) {
-    for (unsigned left = s_above[i]; left; left &= left - 1)
-      put(source++, 0u, static_cast<unsigned>(s0 + 32 * i + __ffs(left) - 1));
-    for (unsigned left = s_equal[i]; left; left &= left - 1)
-      put(place++, share, static_cast<unsigned>(s0 + 32 * i + __ffs(left) - 1));
+  const unsigned below = (1u << lane) - 1u;
+  for (int i = warp; i < words; i += kWarps) {
+    const unsigned moves = s_above[i], free = s_equal[i], base = s_base[i];
+    const unsigned slot = static_cast<unsigned>(s0 + 32 * i + lane);
+    if ((moves >> lane) & 1u) put(source + (base & 0xffffu) + __popc(moves & below), 0u, slot);
+    if ((free >> lane) & 1u) put(place + (base >> 16) + __popc(free & below), share, slot);
   }
   cluster_sync(C);
 
@@ -283,46 +320,55 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
   char* const v = p.cache.v + layer * p.layer_bytes;
   const int per_row = 1 << p.lane_bits, rows = 32 >> p.lane_bits;
   const int sub = lane >> p.lane_bits, word0 = lane & (per_row - 1);
-  for (int m0 = warp * kBatch; m0 < moves; m0 += kWarps * kBatch) {
-    const int many = min(kBatch, moves - m0);
-    long long from = -1, to = -1;
-    if (lane < many) {
-      const int src = static_cast<int>(s_key[m0 + lane]), dst = static_cast<int>(s_key[share + m0 + lane]);
-      from = slot_offset(p.cache, b, src);
-      to = slot_offset(p.cache, b, dst);
-      if (from < 0 || to < 0) {
-        if (p.status) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_PAGE));
-        from = to = -1;
-      } else {
-        from = (from + h * p.cache.head_stride) * p.element;
-        to = (to + h * p.cache.head_stride) * p.element;
-      }
-      weight_out[dst] = __ldcg(weight + src);
+  // A warp's moves: as many as a lane each are looked up at once, the next ones while these are copied. Few moves are
+  // spread over the warps.
+  const int batch = min(32, max(kAtOnce * rows, (moves + kWarps - 1) / kWarps));
+  long long from = -1, to = -1;
+  auto look_up = [&](int m) {
+    from = to = -1;
+    if (lane >= batch || m + lane >= moves) return;
+    const int src = static_cast<int>(s_key[m + lane]), dst = static_cast<int>(s_key[share + m + lane]);
+    const long long f = slot_offset(p.cache, b, src), t = slot_offset(p.cache, b, dst);
+    weight_out[dst] = __ldcg(weight + src);
+    if (f >= 0 && t >= 0) {
+      from = (f + h * p.cache.head_stride) * p.element;
+      to = (t + h * p.cache.head_stride) * p.element;
+    } else if (p.status) {
+      atomicOr(p.status + b, static_cast<int>(ASD_STATUS_PAGE));
     }
-    for (int r0 = 0; r0 < many; r0 += 4 * rows) {
-      long long src[4], dst[4];
+  };
+  look_up(warp * batch);
+  for (int m0 = warp * batch; m0 < moves; m0 += kWarps * batch) {
+    const int many = min(batch, moves - m0);
+    const long long f = from, t = to;
+    bool next = true;
+    for (int r0 = 0; r0 < many; r0 += kAtOnce * rows) {
+      long long src[kAtOnce], dst[kAtOnce];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < kAtOnce; ++i) {
         const int r = r0 + i * rows + sub;
-        src[i] = __shfl_sync(kFull, from, r & 31);
-        dst[i] = __shfl_sync(kFull, to, r & 31);
+        src[i] = __shfl_sync(kFull, f, r & 31);
+        dst[i] = __shfl_sync(kFull, t, r & 31);
         if (r >= many) src[i] = -1;
       }
       for (int w = word0; w < p.words; w += per_row) {
-        Word kw[4], vw[4];
+        Word kw[kAtOnce], vw[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < kAtOnce; ++i)
           if (src[i] >= 0) {
             kw[i] = __ldcg(reinterpret_cast<const Word*>(k + src[i]) + w);
             vw[i] = __ldcg(reinterpret_cast<const Word*>(v + src[i]) + w);
           }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < kAtOnce; ++i)
           if (src[i] >= 0) {
             reinterpret_cast<Word*>(k + dst[i])[w] = kw[i];
             reinterpret_cast<Word*>(v + dst[i])[w] = vw[i];
           }
       }
+      if (next) look_up(m0 + kWarps * batch);
+      next = false;
+      __syncwarp();
     }
   }
 }
@@ -331,23 +377,11 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
 
 constexpr int kMaxDevices = 64;
 
-template <typename Word>
-int launch_evict(EvictParams p, int layers, cudaStream_t stream) {
-  static std::atomic<int> sms_of[kMaxDevices];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return ASD_ERR_CUDA;
-  if (dev < 0 || dev >= kMaxDevices) return ASD_ERR_DEVICE;
-  int sms = sms_of[dev].load(std::memory_order_acquire);
-  if (sms == 0) {
-    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-        cudaFuncSetAttribute(evict_kernel<Word>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             static_cast<int>(evict_smem(kMaxPart))) != cudaSuccess)
-      return ASD_ERR_CUDA;
-    sms_of[dev].store(sms, std::memory_order_release);
-  }
-  const long long heads = static_cast<long long>(layers) * p.B * p.H;
+template <typename Word, int kThreads>
+int launch_evict(EvictParams p, long long heads, int sms, cudaStream_t stream) {
+  auto kernel = evict_kernel<Word, kThreads>;
   int ctas = 1;
-  while (ctas < kMaxCluster && (p.width > ctas * kMaxPart || (heads * ctas < 2 * sms && p.width > 2048 * ctas))) ctas *= 2;
+  while (ctas < kMaxCluster && (p.width > ctas * kMaxPart || (heads * ctas < sms && p.width > 1024 * ctas))) ctas *= 2;
   if (heads * ctas > INT32_MAX) return ASD_ERR_SHAPE;
   p.ctas = ctas;
   p.part = ((p.width + ctas - 1) / ctas + 31) / 32 * 32;
@@ -362,8 +396,29 @@ int launch_evict(EvictParams p, int layers, cudaStream_t stream) {
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.numAttrs = 2;
   }
-  if (cudaLaunchKernelEx(&cfg, evict_kernel<Word>, p) != cudaSuccess) return ASD_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) return ASD_ERR_CUDA;
   return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;
+}
+
+template <typename Word>
+int launch_word(const EvictParams& p, int layers, cudaStream_t stream) {
+  static std::atomic<int> sms_of[kMaxDevices];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return ASD_ERR_CUDA;
+  if (dev < 0 || dev >= kMaxDevices) return ASD_ERR_DEVICE;
+  int sms = sms_of[dev].load(std::memory_order_acquire);
+  if (sms == 0) {
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+        cudaFuncSetAttribute(evict_kernel<Word, 256>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(evict_smem(kMaxPart))) != cudaSuccess ||
+        cudaFuncSetAttribute(evict_kernel<Word, 512>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(evict_smem(kMaxPart))) != cudaSuccess)
+      return ASD_ERR_CUDA;
+    sms_of[dev].store(sms, std::memory_order_release);
+  }
+  const long long heads = static_cast<long long>(layers) * p.B * p.H;
+  return heads <= 2 * sms ? launch_evict<Word, 512>(p, heads, sms, stream)
+                          : launch_evict<Word, 256>(p, heads, sms, stream);
 }
 
 }  // namespace
@@ -403,9 +458,9 @@ extern "C" int asd_kv_evict(const asd_kv_cache* cache, const asd_evict* args, as
       rows_aligned(p.cache.k, es, 16, cache->page_stride, cache->token_stride, cache->head_stride) &&
       reinterpret_cast<uintptr_t>(p.cache.v) % 16 == 0) {
     p.words = cache->head_dim / per;
-    return launch_evict<uint4>(p, cache->layers, s);
+    return launch_word<uint4>(p, cache->layers, s);
   }
   p.words = cache->head_dim;
-  if (es == 4) return launch_evict<unsigned>(p, cache->layers, s);
-  return launch_evict<unsigned short>(p, cache->layers, s);
+  if (es == 4) return launch_word<unsigned>(p, cache->layers, s);
+  return launch_word<unsigned short>(p, cache->layers, s);
 }

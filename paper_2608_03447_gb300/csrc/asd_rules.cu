@@ -6,13 +6,17 @@
 //   z <- z + bias                  tokens that have a record
 //   z <- -inf                      tokens that the grammar does not allow
 //
-// Few tokens have a record, so a row is read as the verifier reads it, by 128-bit
-// loads with a running maximum, in which the elements that a bit of the grammar
-// rules out or a mark sets aside count as -infinity; the marked ones, and the
-// block's drafts, are taken one by one from a list: their logit, their record, the
-// operations above in fp32, each rounded. One CTA takes a range of the vocabulary
-// for all rows of a request, one warp a row, so that a range's marks are looked
-// through once.
+// Few tokens have a record, and hardly any of them matter to a maximum: penalties and
+// biases that lower a logit leave it at most what it was. asd_rules_verify streams
+// the rows as asd_verify does, a warp a unit of one row with a running maximum of the
+// logits as they are (only the grammar's bits turn elements into -infinity), and looks
+// at the marks of the unit's best token alone: if it has a record, it is worked out,
+// taken out of the unit, and the next best one is looked for. What may be larger than
+// its logit (a bias above 0, a penalty that rewards) is other warps' work: each looks
+// through the marks of a part of the vocabulary for such tokens and takes their
+// logits in every row. Both kinds merge (value, index) keys into the rows' slots,
+// from which the selection runs as after any other row stage.
+// asd_rules_logits writes what it reads, so there a warp lists its own unit's tokens.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -27,8 +31,8 @@ namespace {
 
 using namespace asd_detail;
 
-constexpr int kMaxWarps = 10;  // rows at once; more take turns
 constexpr uint32_t kTimes = 0x7fffffffu;
+constexpr uint32_t kLowest = 0x007fffffu;  // ordered_bits(-infinity)
 constexpr int kMarked = 0x8000;  // of a list entry: the token has a record (else it is only a draft)
 
 struct RulesParams {
@@ -44,7 +48,7 @@ struct RulesParams {
   long long allow_batch, allow_row;
   int B, R, K, V;
   int words;              // of a row of marks
-  int chunks;             // ranges of the vocabulary
+  int chunks;             // asd_rules_logits: units of a row
   unsigned long long* row_key;  // asd_rules_verify: as in VerifyParams
   float* draft_logit;
   unsigned* flags;
@@ -75,18 +79,26 @@ __device__ __forceinline__ float widest(uint32_t m, __nv_bfloat16) {
   return fmax_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
 }
 
-// Elements whose bit of `keep` is 0 become -infinity.
-__device__ __forceinline__ uint32_t only(uint32_t w, uint32_t keep, float) { return keep & 1u ? w : 0xff800000u; }
-__device__ __forceinline__ uint32_t only(uint32_t w, uint32_t keep, __nv_bfloat16) {
-  if (!(keep & 1u)) w = (w & 0xffff0000u) | 0xff80u;
-  if (!(keep & 2u)) w = (w & 0xffffu) | 0xff800000u;
-  return w;
+// Elements whose bit of `keep` is 0 become -infinity. Four bits at a time are
+// spread over the signs of a word's bytes by a multiplication, and a byte
+// permutation that repeats signs makes masks of them: 13 instructions for 8 elements.
+__device__ __forceinline__ uint32_t sign_masks(uint32_t spread, uint32_t which) {
+  uint32_t m;
+  asm("prmt.b32 %0, %1, 0, %2;" : "=r"(m) : "r"(spread), "r"(which));
+  return m;
 }
-template <typename T>
-__device__ __forceinline__ uint4 only(const uint4& v, uint32_t keep) {
-  constexpr int n = Elem<T>::kVec / 4;  // elements of a word
-  return make_uint4(only(v.x, keep, T()), only(v.y, keep >> n, T()), only(v.z, keep >> 2 * n, T()),
-                    only(v.w, keep >> 3 * n, T()));
+__device__ __forceinline__ uint32_t choose(uint32_t mask, uint32_t w, uint32_t other) { return (w & mask) | (other & ~mask); }
+__device__ __forceinline__ uint4 only(const uint4& v, uint32_t keep, float) {
+  constexpr uint32_t kNone = 0xff800000u;
+  const uint32_t a = (keep & 15u) * 0x10204080u;
+  return make_uint4(choose(sign_masks(a, 0x8888u), v.x, kNone), choose(sign_masks(a, 0x9999u), v.y, kNone),
+                    choose(sign_masks(a, 0xaaaau), v.z, kNone), choose(sign_masks(a, 0xbbbbu), v.w, kNone));
+}
+__device__ __forceinline__ uint4 only(const uint4& v, uint32_t keep, __nv_bfloat16) {
+  constexpr uint32_t kNone = 0xff80ff80u;
+  const uint32_t a = (keep & 15u) * 0x10204080u, b = ((keep >> 4) & 15u) * 0x10204080u;
+  return make_uint4(choose(sign_masks(a, 0x9988u), v.x, kNone), choose(sign_masks(a, 0xbbaau), v.y, kNone),
+                    choose(sign_masks(b, 0x9988u), v.z, kNone), choose(sign_masks(b, 0xbbaau), v.w, kNone));
 }
 
 // The first element of the unit's vectors that equals best; one of them does.
@@ -106,240 +118,508 @@ __device__ __forceinline__ int first_of(const uint4 (&v)[kU], float best) {
 __device__ __forceinline__ float narrow(float v, float) { return v; }
 __device__ __forceinline__ __nv_bfloat16 narrow(float v, __nv_bfloat16) { return __float2bfloat16_rn(v); }
 
-// kU: vectors a lane has of a row's range. kWrite: writes the changed logits,
-// else reduces them to the row's (value, index) key and its draft's logit.
-template <typename T, int kU, bool kWrite>
-__global__ void __launch_bounds__(kMaxWarps * 32, 3) rules_kernel(const __grid_constant__ RulesParams p) {
-  constexpr int VN = Elem<T>::kVec;
-  constexpr int kChunk = 32 * kU * VN, kWords = kChunk / 32, kWordsLane = (kWords + 31) / 32;
-  __shared__ uint32_t s_special[kWords + 1];  // tokens with a record, and drafts
-  __shared__ uint32_t s_allow[kMaxWarps][kWords + 1];
-  __shared__ uint16_t s_list[kChunk];
-  __shared__ int s_count;
+// A request's penalties.
+struct Penalties {
+  float rho, f, pr;
+  __device__ __forceinline__ Penalties(const RulesParams& p, int b) {
+    rho = p.repetition ? __ldcg(p.repetition + b) : 1.0f;
+    f = p.frequency ? __ldcg(p.frequency + b) : 0.0f;
+    pr = p.presence ? __ldcg(p.presence + b) : 0.0f;
+  }
+  // Whether no logit grows, and none turns NaN (infinities less infinities; the products of counts below 2^31 are finite).
+  __device__ __forceinline__ bool lower() const {
+    return rho >= 1.0f && rho <= 1e30f && f >= 0.0f && f <= 1e20f && pr >= 0.0f && pr <= 1e30f;
+  }
+};
 
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  const int b = blockIdx.x / p.chunks;
-  const int t0 = (blockIdx.x - b * p.chunks) * kChunk;
-  const int len = min(kChunk, p.V - t0);
-  const bool grammar = p.allow != nullptr;
+// The logit z of a token that has been said `times` times before the row.
+__device__ __forceinline__ float changed_logit(const RulesParams& p, const Penalties& q, float z, uint32_t times,
+                                               bool marked, uint2 record) {
+  if (p.repetition && (times > 0u || (record.x & ASD_TOKEN_PROMPT)))
+    z = z > 0.0f ? __fdiv_rn(z, q.rho) : __fmul_rn(z, q.rho);
+  if (times > 0u) {
+    z = __fsub_rn(z, __fmul_rn(static_cast<float>(times), q.f));
+    z = __fsub_rn(z, q.pr);
+  }
+  return marked ? __fadd_rn(z, __uint_as_float(record.y)) : z;
+}
+
+// Bit i: whether draft i is this lane's token. `mine`: the lane's draft, `near` the lanes that may match.
+__device__ __forceinline__ unsigned drafts_equal(int tok, int mine, unsigned near) {
+  unsigned equal = 0;
+  for (unsigned left = near; left; left &= left - 1) {
+    const int i = __ffs(left) - 1;
+    if (__shfl_sync(kFull, mine, i) == tok) equal |= 1u << i;
+  }
+  return equal;
+}
+
+// A word of a request's marks; its bits past the vocabulary may be anything and are dropped.
+__device__ __forceinline__ uint32_t load_marks(const RulesParams& p, int b, int w) {
+  if (w >= p.words) return 0u;
+  const uint32_t x = __ldcg(p.marks + static_cast<long long>(b) * p.words + w);
+  const int left = p.V - 32 * w;
+  return left >= 32 ? x : x & ((1u << left) - 1u);
+}
+
+// Appends the tokens of this lane's words to the list, in order of the lanes. Returns how many a warp has.
+template <int kN>
+__device__ __forceinline__ int append_list(uint16_t* list, int at, const int (&word)[kN], const uint32_t (&all)[kN],
+                                           const uint32_t (&mark)[kN]) {
+  const int lane = threadIdx.x & 31;
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) n += __popc(all[i]);
+  int before = n;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int o = __shfl_up_sync(kFull, before, off);
+    if (lane >= off) before += o;
+  }
+  const int total = __shfl_sync(kFull, before, 31);
+  before += at - n;
+#pragma unroll
+  for (int i = 0; i < kN; ++i)
+    for (uint32_t left = all[i]; left; left &= left - 1) {
+      const int bit = __ffs(left) - 1;
+      list[before++] = static_cast<uint16_t>(32 * word[i] + bit + ((mark[i] >> bit) & 1u) * kMarked);
+    }
+  return total;
+}
+
+// A row's share of a CTA or warp: len elements from z on, as loose ones up to a 16-byte boundary, whole vectors, loose.
+template <typename T>
+struct Range {
+  static constexpr int VN = Elem<T>::kVec;
+  const T* z;
+  int len, lead, nvec;
+  __device__ __forceinline__ Range() {}
+  __device__ __forceinline__ Range(const T* from, int n) : z(from), len(n) {
+    lead = static_cast<int>((16u - static_cast<unsigned>(reinterpret_cast<uintptr_t>(z) & 15u)) & 15u) /
+           static_cast<int>(sizeof(T));
+    lead = lead < len ? lead : len;
+    nvec = (len - lead) / VN;
+  }
+  __device__ __forceinline__ const uint4* vectors() const { return reinterpret_cast<const uint4*>(z + lead); }
+  __device__ __forceinline__ bool has_loose() const { return lead > 0 || lead + nvec * VN < len; }
+  // the loose element of this lane, or -1
+  __device__ __forceinline__ int loose(int lane) const {
+    const int at = lane < VN ? lane : lead + nvec * VN + lane - VN;
+    return (lane < VN ? at < lead : lane < 2 * VN && at < len) ? at : -1;
+  }
+};
+
+// ---------------------------------------------------------------- asd_rules_verify's row stage
+
+constexpr int kThreads = 128;
+constexpr int kWarps = kThreads / 32;
+constexpr int kMinBlocks = 8;
+constexpr int kPart = 2048;  // tokens that a warp looks through for those that may grow
+
+struct StreamPlan {
+  int parts;     // units of a row
+  int unit_ctas; // CTAs of a request that have kWarps units each,
+  int part_ctas; // and those that have kWarps parts of the vocabulary each
+};
+
+__device__ __forceinline__ void merge_key(const RulesParams& p, long long row, unsigned long long key) {
+  if (key != 0ull) atomicMax(p.row_key + row, key);
+}
+
+// By a warp: the tokens of a part that may grow, in all rows of the request; and the logits of the drafts that lie in
+// it. A lane has two words of marks, and reads the biases of several tokens at once.
+template <typename T>
+__device__ __forceinline__ void growing_rows(const RulesParams& p, int b, int part, uint16_t* list) {
+  constexpr int kN = kPart / 32 / 32;
+  const int lane = threadIdx.x & 31;
+  if (part > (p.V - 1) / kPart) return;
+  const int t0 = part * kPart, len = min(kPart, p.V - t0);
+  const int mine = lane < p.K ? __ldcg(p.draft + static_cast<long long>(b) * p.K + lane) - t0 : -1;
+  unsigned long long mark = 0ull;  // bit 32 i + k: token 32 (32 i + lane) + k
+#pragma unroll
+  for (int i = 0; i < kN; ++i)
+    mark |= static_cast<unsigned long long>(load_marks(p, b, t0 / 32 + 32 * i + lane)) << (32 * i);
+  const Penalties penalties(p, b);
+  const bool lower = penalties.lower();
+  const unsigned near = __ballot_sync(kFull, mine >= 0 && mine < len);
+  const T* z = static_cast<const T*>(p.logits) + static_cast<long long>(b) * p.R * p.V + t0;
+  const uint32_t* allow = p.allow ? p.allow + b * p.allow_batch + t0 / 32 : nullptr;
+  const asd_token_record* records = p.records + static_cast<long long>(b) * p.V + t0;
+  auto token = [&](int bit) { return 32 * (bit & ~31) + 32 * lane + (bit & 31); };
+  auto bit_of = [&](int tok) { return (tok >> 10) * 32 + (tok & 31); };  // of lane tok / 32 % 32
+
+  unsigned long long grows = 0ull;
+  if (lower) {  // a bias above 0; one that makes -infinity, or NaN of an infinite logit
+    constexpr int kAtOnce = 4;
+    for (unsigned long long left = mark; __any_sync(kFull, left != 0ull);) {
+      float bias[kAtOnce];
+      int bit[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        bit[k] = __ffsll(static_cast<long long>(left)) - 1;
+        bias[k] = 0.0f;
+        if (bit[k] >= 0) bias[k] = records[token(bit[k])].bias;
+        left &= left - 1;
+      }
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k)
+        if (!(bias[k] <= 0.0f && bias[k] > -INFINITY)) grows |= 1ull << bit[k];
+    }
+  } else {  // any; and drafts in the rows behind them
+    grows = mark;
+    for (unsigned left = near; left; left &= left - 1) {
+      const int x = __shfl_sync(kFull, mine, __ffs(left) - 1);
+      if ((x >> 5 & 31) == lane) grows |= 1ull << bit_of(x);
+    }
+  }
+
+  bool nan = false;
+  if (near) {  // a draft's logit in its own row
+    const unsigned equal = drafts_equal(mine, mine, near);
+    const unsigned long long marks = __shfl_sync(kFull, mark, mine >> 5 & 31);
+    if ((near >> lane) & 1u) {
+      const bool marked = (marks >> bit_of(mine)) & 1ull;
+      const bool may = !allow || ((__ldcg(allow + lane * p.allow_row + mine / 32) >> (mine & 31)) & 1u);
+      const float x = Elem<T>::load_cg(z, static_cast<long long>(lane) * p.V + mine);
+      const uint2 record = marked ? *reinterpret_cast<const uint2*>(records + mine) : make_uint2(0u, 0u);
+      const uint32_t times = (record.x & kTimes) + __popc(equal & ((1u << lane) - 1u));
+      p.draft_logit[static_cast<long long>(b) * p.R + lane] =
+          may ? changed_logit(p, penalties, x, times, marked, record) : -INFINITY;
+    }
+  }
+
+  // A token in a row is a lane's: few tokens in all rows are one round of loads. Few of them lead their row, whose units
+  // have mostly been merged by now: a slot is only touched where that shows.
+  int n = __popcll(grows), before = n;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int o = __shfl_up_sync(kFull, before, off);
+    if (lane >= off) before += o;
+  }
+  const int count = __shfl_sync(kFull, before, 31);
+  before -= n;
+  for (unsigned long long left = grows; left; left &= left - 1) {
+    const int bit = __ffsll(static_cast<long long>(left)) - 1;
+    list[before++] = static_cast<uint16_t>(token(bit) + ((mark >> bit) & 1ull) * kMarked);
+  }
+  __syncwarp();
+  const int items = count * p.R;  // at most kPart * (ASD_MAX_K + 1)
+  for (int i0 = 0; i0 < items; i0 += 32) {
+    const int i = i0 + lane;
+    const bool has = i < items;
+    const int e = i / p.R, j = i - e * p.R, x = has ? list[e] : 0, tok = x & (kMarked - 1);
+    const bool marked = (x & kMarked) != 0;
+    const long long row = static_cast<long long>(b) * p.R + j;
+    float value = 0.0f;
+    uint32_t may = kFull;
+    uint2 record = make_uint2(0u, 0u);
+    unsigned long long most = 0ull;
+    if (has) {
+      value = Elem<T>::load_cg(z, static_cast<long long>(j) * p.V + tok);
+      if (allow) may = __ldcg(allow + j * p.allow_row + (tok >> 5));
+      if (marked) record = *reinterpret_cast<const uint2*>(records + tok);
+      most = __ldcg(p.row_key + row);
+    }
+    const unsigned equal = drafts_equal(tok, mine, near);
+    if (has) {
+      const uint32_t times = (record.x & kTimes) + __popc(equal & ((1u << j) - 1u));
+      value = changed_logit(p, penalties, value, times, marked, record);
+      if (!((may >> (tok & 31)) & 1u)) value = -INFINITY;
+      nan = nan || value != value;
+      const unsigned long long key = make_key(value, static_cast<uint32_t>(t0 + tok));
+      if (value == value && key > most) merge_key(p, row, key);
+    }
+  }
+  nan = __any_sync(kFull, nan);
+  if (nan && lane == 0) atomicOr(p.flags + b, ASD_STATUS_NAN_LOGIT);
+}
+
+// Element t of a vector becomes -infinity.
+__device__ __forceinline__ void take_out(uint4& v, int t, float) {
+  constexpr uint32_t kNone = 0xff800000u;
+  if (t == 0) v.x = kNone;
+  if (t == 1) v.y = kNone;
+  if (t == 2) v.z = kNone;
+  if (t == 3) v.w = kNone;
+}
+__device__ __forceinline__ void take_out(uint4& v, int t, __nv_bfloat16) {
+  const uint32_t mask = t & 1 ? 0xffffu : 0xffff0000u, none = 0xff80ff80u & ~mask;
+  if (t >> 1 == 0) v.x = (v.x & mask) | none;
+  if (t >> 1 == 1) v.y = (v.y & mask) | none;
+  if (t >> 1 == 2) v.z = (v.z & mask) | none;
+  if (t >> 1 == 3) v.w = (v.w & mask) | none;
+}
+
+// kU: vectors a lane has of a unit, all in flight at once.
+template <typename T, int kU>
+__global__ void __launch_bounds__(kThreads, kMinBlocks)
+    rules_stream_kernel(const __grid_constant__ RulesParams p, const __grid_constant__ StreamPlan q) {
+  constexpr int VN = Elem<T>::kVec;
+  constexpr int kUnit = 32 * kU * VN, kWords = kUnit / 32, kN = (kWords + 31) / 32;
+  __shared__ uint32_t s_may[kWarps][kWords + 1];
+  __shared__ uint16_t s_list[kWarps][kPart];
+  __shared__ unsigned long long s_key[kWarps];
+  __shared__ unsigned s_row[kWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_signal_dependents();
+  // what may grow comes behind the request's units
+  const int per = q.unit_ctas + q.part_ctas;
+  const int b = static_cast<int>(blockIdx.x) / per, at_cta = static_cast<int>(blockIdx.x) - b * per;
+  if (at_cta >= q.unit_ctas) {
+    pdl_wait_prerequisites();
+    growing_rows<T>(p, b, (at_cta - q.unit_ctas) * kWarps + warp, s_list[warp]);
+    return;
+  }
+  const int unit = at_cta * kWarps + warp, units = p.R * q.parts;
+  const bool exists = unit < units;
+  const int j = exists ? unit / q.parts : 0;
+  const int t0 = exists ? (unit - j * q.parts) * kUnit : 0;
+  const unsigned row = static_cast<unsigned>(b) * static_cast<unsigned>(p.R) + static_cast<unsigned>(j);
+  const Range<T> r(static_cast<const T*>(p.logits) + static_cast<long long>(row) * p.V + t0, min(kUnit, p.V - t0));
+  pdl_wait_prerequisites();
+
+  // one round of loads: the elements, their marks and the grammar's bits, the block's drafts
+  const bool whole = r.lead == 0 && r.nvec == 32 * kU;  // no index to bound, no bits across words
+  uint4 v[kU];
+  if (whole) {
+#pragma unroll
+    for (int u = 0; u < kU; ++u) v[u] = load_row(reinterpret_cast<const uint4*>(r.z) + lane + 32 * u);
+  } else if (r.nvec > 0) {
+    // past its end a unit repeats its last vector, which changes no maximum and no index
+#pragma unroll
+    for (int u = 0; u < kU; ++u) v[u] = load_row(r.vectors() + min(lane + 32 * u, r.nvec - 1));
+  }
+  const int at_loose = r.has_loose() ? r.loose(lane) : -1;
+  float loose = -INFINITY;
+  if (at_loose >= 0) loose = Elem<T>::load_cg(r.z, at_loose);
+  uint32_t special[kN], may[kN];  // a bit an element: whether it is marked or a draft before the row; may come
+  const uint32_t* marks = p.marks + static_cast<long long>(b) * p.words + t0 / 32;
+  const uint32_t* allow = p.allow + b * p.allow_batch + j * p.allow_row + t0 / 32;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    const int w = 32 * i + lane;
+    special[i] = t0 / 32 + w < p.words ? __ldcg(marks + w) : 0u;
+    if (p.allow) may[i] = t0 / 32 + w < p.words ? __ldcg(allow + w) : 0u;
+  }
+  const int mine = lane < p.K ? __ldcg(p.draft + static_cast<long long>(b) * p.K + lane) - t0 : -1;
+  const unsigned said = __ballot_sync(kFull, lane < j && mine >= 0 && mine < r.len);
+  uint32_t* words = s_may[warp];
+  if (p.allow) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+      if (32 * i + lane <= kWords) words[32 * i + lane] = may[i];
+    if (kWords % 32 == 0 && lane == 0) words[kWords] = 0u;
+    __syncwarp();
+    if (whole) {
+      const unsigned char* bits = reinterpret_cast<const unsigned char*>(words) + lane * VN / 8;
+#pragma unroll
+      for (int u = 0; u < kU; ++u) v[u] = only(v[u], static_cast<uint32_t>(bits[32 * u * VN / 8]) >> (lane * VN % 8), T());
+    } else if (r.nvec > 0) {
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int at = r.lead + min(lane + 32 * u, r.nvec - 1) * VN;
+        v[u] = only(v[u], __funnelshift_r(words[at >> 5], words[(at >> 5) + 1], at & 31), T());
+      }
+    }
+    if (at_loose >= 0 && !((words[at_loose >> 5] >> (at_loose & 31)) & 1u)) loose = -INFINITY;
+  }
+
+  // the unit's best token, until it is one without rules or not better than those worked out
+  unsigned long long key = 0ull;
+  bool nan = false;
+  for (bool again = false;; again = true) {
+    uint32_t order = at_loose >= 0 ? ordered_bits(loose) : 0u;
+    const uint32_t loose_order = order;
+    float best = 0.0f;
+    if (r.nvec > 0) {
+      uint32_t m = max_of<T>(v[0]);
+#pragma unroll
+      for (int u = 1; u < kU; ++u) m = max_of(m, max_of<T>(v[u]), T());
+      best = widest(m, T());
+      order = max(order, ordered_bits(best));
+    }
+    if (!again) {
+      nan = __any_sync(kFull, best != best || loose != loose);
+      if (nan) break;
+    }
+    const uint32_t top = __reduce_max_sync(kFull, order);
+    uint32_t low = 0u;
+    if (r.nvec > 0 && ordered_bits(best) == top) {
+      const int at = first_of<T, kU>(v, best);
+      low = 0xffffffffu - static_cast<uint32_t>(t0 + r.lead + min(lane + 32 * (at / VN), r.nvec - 1) * VN + at % VN);
+    }
+    if (at_loose >= 0 && loose_order == top) low = max(low, 0xffffffffu - static_cast<uint32_t>(t0 + at_loose));
+    low = __reduce_max_sync(kFull, low);
+    const unsigned long long found = (static_cast<unsigned long long>(top) << 32) | low;
+    if (found <= key) break;
+    const int at = static_cast<int>(0xffffffffu - low) - t0, w = at >> 5;
+    uint32_t bits = 0u;
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+      if (w / 32 == i) bits = __shfl_sync(kFull, special[i], w & 31);
+    const bool marked = (bits >> (at & 31)) & 1u;
+    unsigned equal = 0u;
+    for (unsigned left = said; left; left &= left - 1) equal += __shfl_sync(kFull, mine, __ffs(left) - 1) == at;
+    // nothing is left but -infinity: that rules leave as it is, or is one that may grow
+    if ((!marked && equal == 0u) || top == kLowest) {
+      key = found;
+      break;
+    }
+    const Penalties penalties(p, b);
+    const uint2 record = marked ? *reinterpret_cast<const uint2*>(p.records + static_cast<long long>(b) * p.V + t0 + at)
+                                : make_uint2(0u, 0u);
+    const float value = changed_logit(p, penalties, ordered_value(top), (record.x & kTimes) + equal, marked, record);
+    if (value == value) {
+      const unsigned long long changed = make_key(value, static_cast<uint32_t>(t0 + at));
+      key = changed > key ? changed : key;
+    } else {
+      nan = true;
+    }
+    // out of the unit, wherever it is (a repeated last vector has it too)
+    const int e = at - r.lead;
+    if (e >= 0 && e < r.nvec * VN) {
+#pragma unroll
+      for (int u = 0; u < kU; ++u)
+        if (min(lane + 32 * u, r.nvec - 1) == e / VN) take_out(v[u], e % VN, T());
+    } else if (at_loose == at) {
+      loose = -INFINITY;
+    }
+  }
+  if (nan && exists && lane == 0) atomicOr(p.flags + b, ASD_STATUS_NAN_LOGIT);
+
+  // one reduction per row and CTA
+  if (lane == 0) {
+    s_key[warp] = exists ? key : 0ull;
+    s_row[warp] = exists ? row : 0xffffffffu;
+  }
+  __syncthreads();
+  if (warp != 0) return;
+  const unsigned of = lane < kWarps ? s_row[lane] : 0xffffffffu;
+  unsigned long long k = lane < kWarps ? s_key[lane] : 0ull;
+#pragma unroll
+  for (int d = 1; d < kWarps; d *= 2) {
+    const unsigned long long o = __shfl_down_sync(kFull, k, d);
+    if (__shfl_down_sync(kFull, of, d) == of && o > k) k = o;
+  }
+  const unsigned before = __shfl_up_sync(kFull, of, 1);
+  if (of != 0xffffffffu && (lane == 0 || before != of)) merge_key(p, of, k);
+}
+
+// ---------------------------------------------------------------- asd_rules_logits
+
+// A warp a unit of one row: the elements pass through shared memory, where the listed ones are changed in between, so
+// that they are written with the rest. kU: vectors a lane has of a unit, all in flight at once.
+template <typename T, int kU>
+__global__ void __launch_bounds__(kThreads, kMinBlocks) rules_write_kernel(const __grid_constant__ RulesParams p) {
+  constexpr int VN = Elem<T>::kVec;
+  constexpr int kUnit = 32 * kU * VN, kWords = kUnit / 32, kN = (kWords + 31) / 32;
+  constexpr int kList = kUnit < 512 ? kUnit : 512;  // tokens changed at once
+  __shared__ __align__(16) T s_z[kWarps][kUnit + VN];
+  __shared__ uint32_t s_allow[kWarps][kWords + 1];
+  __shared__ uint16_t s_list[kWarps][kList];
+
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long unit = static_cast<long long>(blockIdx.x) * kWarps + warp;
+  pdl_signal_dependents();
+  const long long row = unit / p.chunks;
+  if (row >= static_cast<long long>(p.B) * p.R) return;
+  const int t0 = static_cast<int>(unit - row * p.chunks) * kUnit;
+  const int b = static_cast<int>(row / p.R), j = static_cast<int>(row - static_cast<long long>(b) * p.R);
+  const Range<T> r(static_cast<const T*>(p.logits) + row * p.V + t0, min(kUnit, p.V - t0));
+  T* const out = static_cast<T*>(p.out) + row * p.V + t0;
+  const bool grammar = p.allow != nullptr;
   pdl_wait_prerequisites();
 
   uint4 v[kU];
-  uint32_t allowed[kWordsLane];
-  const T* z;
-  int lead, nvec;
-  // a row's range: loose elements up to a 16-byte boundary, whole vectors, loose ones; all loads in flight at once
-  auto load = [&](int j) {
-    z = static_cast<const T*>(p.logits) + (static_cast<long long>(b) * p.R + j) * p.V + t0;
-    lead = min(static_cast<int>((16u - static_cast<unsigned>(reinterpret_cast<uintptr_t>(z) & 15u)) & 15u) /
-                   static_cast<int>(sizeof(T)),
-               len);
-    nvec = (len - lead) / VN;
-    const uint4* vp = reinterpret_cast<const uint4*>(z + lead);
-    if (nvec > 0) {
 #pragma unroll
-      for (int u = 0; u < kU; ++u) v[u] = load_row(vp + min(lane + 32 * u, nvec - 1));
-    }
-    if (grammar) {
-      const uint32_t* row = p.allow + b * p.allow_batch + j * p.allow_row + t0 / 32;
+  for (int u = 0; u < kU; ++u)
+    if (lane + 32 * u < r.nvec) v[u] = load_row(r.vectors() + lane + 32 * u);
+  const int at_loose = r.has_loose() ? r.loose(lane) : -1;
+  T loose = {};
+  if (at_loose >= 0) loose = r.z[at_loose];
+  uint32_t mark[kN], all[kN];
+  int word[kN];
 #pragma unroll
-      for (int i = 0; i < kWordsLane; ++i) {
-        const int w = lane + 32 * i;
-        allowed[i] = w < kWords && t0 / 32 + w < p.words ? __ldcg(row + w) : 0u;
-      }
-    }
-  };
-  load(warp);
-
-  const int mine = lane < p.K ? __ldcg(p.draft + static_cast<long long>(b) * p.K + lane) - t0 : -1;
-  const unsigned near = __ballot_sync(kFull, mine >= 0 && mine < len);  // drafts in the range
-  if (warp == 0) {
-    uint32_t mark[kWordsLane], all[kWordsLane];
-#pragma unroll
-    for (int i = 0; i < kWordsLane; ++i) {
-      const int w = lane + 32 * i;
-      mark[i] = 0u;
-      if (w < kWords && t0 / 32 + w < p.words)
-        mark[i] = __ldcg(p.marks + static_cast<long long>(b) * p.words + t0 / 32 + w);
-      const int left = p.V - t0 - 32 * w;  // bits past the vocabulary may be anything
-      if (left < 32) mark[i] &= left <= 0 ? 0u : (1u << left) - 1u;
-      all[i] = mark[i];
-    }
-    for (unsigned left = near; left; left &= left - 1) {
-      const int x = __shfl_sync(kFull, mine, __ffs(left) - 1);
-#pragma unroll
-      for (int i = 0; i < kWordsLane; ++i)
-        if (x >> 5 == lane + 32 * i) all[i] |= 1u << (x & 31);
-    }
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < kWordsLane; ++i) n += __popc(all[i]);
-    int before = n;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int o = __shfl_up_sync(kFull, before, off);
-      if (lane >= off) before += o;
-    }
-    if (lane == 31) s_count = before;
-    before -= n;
-#pragma unroll
-    for (int i = 0; i < kWordsLane; ++i) {
-      const int w = lane + 32 * i;
-      if (w <= kWords) s_special[w] = all[i];
-      for (uint32_t left = all[i]; left; left &= left - 1) {
-        const int bit = __ffs(left) - 1;
-        s_list[before++] = static_cast<uint16_t>(32 * w + bit + ((mark[i] >> bit) & 1u) * kMarked);
-      }
-    }
-    if (kWords % 32 == 0 && lane == 0) s_special[kWords] = 0u;
+  for (int i = 0; i < kN; ++i) {
+    word[i] = 32 * i + lane;
+    mark[i] = all[i] = word[i] < kWords ? load_marks(p, b, t0 / 32 + word[i]) : 0u;
+    if (grammar && word[i] <= kWords)
+      s_allow[warp][word[i]] = word[i] < kWords && t0 / 32 + word[i] < p.words
+                                   ? __ldcg(p.allow + b * p.allow_batch + j * p.allow_row + t0 / 32 + word[i])
+                                   : 0u;
   }
-  float rho = 1.0f, f = 0.0f, pr = 0.0f;
-  if (p.repetition) rho = __ldcg(p.repetition + b);
-  if (p.frequency) f = __ldcg(p.frequency + b);
-  if (p.presence) pr = __ldcg(p.presence + b);
-  __syncthreads();
-  const int count = s_count;
+  if (kWords % 32 == 0 && lane == 0) s_allow[warp][kWords] = 0u;
+  const int mine = lane < p.K ? __ldcg(p.draft + static_cast<long long>(b) * p.K + lane) - t0 : -1;
+  const unsigned said = __ballot_sync(kFull, lane < j && mine >= 0 && mine < r.len);  // drafts before the row, in the unit
+  for (unsigned left = said; left; left &= left - 1) {
+    const int x = __shfl_sync(kFull, mine, __ffs(left) - 1);
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+      if (x >> 5 == word[i]) all[i] |= 1u << (x & 31);
+  }
+  const Penalties penalties(p, b);
+  T* const z = s_z[warp] + (r.lead > 0 ? VN - r.lead : 0);  // so that vectors lie on 16-byte boundaries here too
+  uint4* const vectors = reinterpret_cast<uint4*>(z + r.lead);
+#pragma unroll
+  for (int u = 0; u < kU; ++u)
+    if (lane + 32 * u < r.nvec) vectors[lane + 32 * u] = v[u];
+  if (at_loose >= 0) z[at_loose] = loose;
 
-  for (int j = warp; j < p.R; j += warps) {
-    if (j != warp) load(j);
-    const long long row = static_cast<long long>(b) * p.R + j;
-    // what the list's entries need is asked for before the vectors are waited for
-    struct Entry {
-      int tok;  // of the range; -1: none
-      bool marked;
-      float z;
-      uint2 record;
-    };
-    auto fetch = [&](int i) {
-      Entry e = {-1, false, 0.0f, make_uint2(0u, 0u)};
-      if (i < count) {
-        const int x = s_list[i];
-        e.tok = x & (kMarked - 1);
-        e.marked = (x & kMarked) != 0;
-        e.z = Elem<T>::load_cg(z, e.tok);
-        if (e.marked)
-          e.record = *reinterpret_cast<const uint2*>(p.records + static_cast<long long>(b) * p.V + t0 + e.tok);
-      }
-      return e;
-    };
-    Entry e0 = fetch(lane), e1 = fetch(lane + 32);
-    if (grammar) {
-      __syncwarp();  // the row before is done with the words
+  // the listed tokens; all at once unless the list is too short for them
+  int n = 0;
 #pragma unroll
-      for (int i = 0; i < kWordsLane; ++i)
-        if (lane + 32 * i <= kWords) s_allow[warp][lane + 32 * i] = allowed[i];
-      if (kWords % 32 == 0 && lane == 0) s_allow[warp][kWords] = 0u;
-      __syncwarp();
+  for (int i = 0; i < kN; ++i) n += __popc(all[i]);
+  n = __reduce_add_sync(kFull, n);
+  const int each = n <= kList ? kWords : kList / 32;  // words at once
+  for (int w0 = 0; w0 < kWords && n > 0; w0 += each) {
+    uint32_t now[kN];
+#pragma unroll
+    for (int i = 0; i < kN; ++i) now[i] = word[i] >= w0 && word[i] < w0 + each ? all[i] : 0u;
+    __syncwarp();
+    const int count = append_list(s_list[warp], 0, word, now, mark);
+    __syncwarp();
+    for (int i0 = 0; i0 < count; i0 += 64) {
+      int tok[2];
+      bool marked[2];
+      uint2 record[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int i = i0 + 32 * k + lane, x = i < count ? s_list[warp][i] : -1;
+        tok[k] = x < 0 ? -1 : x & (kMarked - 1);
+        marked[k] = x >= 0 && (x & kMarked);
+        record[k] = make_uint2(0u, 0u);
+        if (marked[k])
+          record[k] = *reinterpret_cast<const uint2*>(p.records + static_cast<long long>(b) * p.V + t0 + tok[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (i0 + 32 * k >= count) break;
+        const uint32_t times = (record[k].x & kTimes) + __popc(drafts_equal(tok[k], mine, said));
+        if (tok[k] >= 0)
+          z[tok[k]] = narrow(changed_logit(p, penalties, Elem<T>::load(z, tok[k]), times, marked[k], record[k]), T());
+      }
     }
-    auto may = [&](int at) { return !grammar || ((s_allow[warp][at >> 5] >> (at & 31)) & 1u); };
-    auto bits = [&](const uint32_t* words, int at) {  // of the VN elements from `at` on
-      return __funnelshift_r(words[at >> 5], words[(at >> 5) + 1], at & 31);
-    };
+  }
+  __syncwarp();
 
-    unsigned long long key = 0ull;
-    bool nan = false;
-    uint32_t order = 0u;
-    float best = 0.0f;
-    T* out = kWrite ? static_cast<T*>(p.out) + row * p.V + t0 : nullptr;
-    if (nvec > 0) {
-      if (kWrite ? grammar : grammar || count > 0) {
+  // what may not come is -infinity on the way out
+  if (((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(r.z)) & 15u) == 0) {
 #pragma unroll
-        for (int u = 0; u < kU; ++u) {
-          const int at = lead + min(lane + 32 * u, nvec - 1) * VN;
-          uint32_t keep = grammar ? bits(s_allow[warp], at) : 0xffffffffu;
-          if (!kWrite) keep &= ~bits(s_special, at);
-          v[u] = only<T>(v[u], keep);
+    for (int u = 0; u < kU; ++u)
+      if (lane + 32 * u < r.nvec) {
+        uint4 x = vectors[lane + 32 * u];
+        if (grammar) {
+          const int at = r.lead + (lane + 32 * u) * VN;
+          x = only(x, __funnelshift_r(s_allow[warp][at >> 5], s_allow[warp][(at >> 5) + 1], at & 31), T());
         }
+        reinterpret_cast<uint4*>(out + r.lead)[lane + 32 * u] = x;
       }
-      if (kWrite) {
-        if ((reinterpret_cast<uintptr_t>(out + lead) & 15u) == 0) {
-#pragma unroll
-          for (int u = 0; u < kU; ++u)
-            if (lane + 32 * u < nvec) reinterpret_cast<uint4*>(out + lead)[lane + 32 * u] = v[u];
-        } else {
-#pragma unroll
-          for (int u = 0; u < kU; ++u)
-            if (lane + 32 * u < nvec)
-#pragma unroll
-              for (int t = 0; t < VN; ++t)
-                out[lead + (lane + 32 * u) * VN + t] = narrow(Elem<T>::lane(v[u], t), T());
-        }
-      } else {
-        uint32_t m = max_of<T>(v[0]);
-#pragma unroll
-        for (int u = 1; u < kU; ++u) m = max_of(m, max_of<T>(v[u]), T());
-        best = widest(m, T());
-        nan = __any_sync(kFull, best != best);
-        order = nan ? 0u : ordered_bits(best);
-      }
-    }
-    if (lead > 0 || lead + nvec * VN < len) {  // loose elements, one a lane
-      const int at = lane < VN ? lane : lead + nvec * VN + lane - VN;
-      if ((lane < VN ? at < lead : lane < 2 * VN && at < len)) {
-        const bool special = (s_special[at >> 5] >> (at & 31)) & 1u;
-        float x = Elem<T>::load_cg(z, at);
-        if (!may(at)) x = -INFINITY;
-        if (kWrite) {
-          out[at] = narrow(x, T());
-        } else if (!special) {
-          if (x == x)
-            key = make_key(x, static_cast<uint32_t>(t0 + at));
-          else
-            nan = true;
-        }
-      }
-    }
-    if (kWrite) __syncwarp();  // entries are written over what the vectors had
-    const int here = j < p.K ? __shfl_sync(kFull, mine, j) : -1;  // the row's draft
-    const unsigned said = near & ((1u << j) - 1u);                // drafts before the row, in the range
-    auto finish = [&](const Entry& e) {
-      uint32_t times = e.record.x & kTimes;
-      for (unsigned left = said; left; left &= left - 1) times += __shfl_sync(kFull, mine, __ffs(left) - 1) == e.tok;
-      if (e.tok < 0) return;
-      float x = e.z;
-      if (times > 0u || (e.record.x & ASD_TOKEN_PROMPT))
-        if (p.repetition) x = x > 0.0f ? __fdiv_rn(x, rho) : __fmul_rn(x, rho);
-      if (times > 0u) {
-        x = __fsub_rn(x, __fmul_rn(static_cast<float>(times), f));
-        x = __fsub_rn(x, pr);
-      }
-      if (e.marked) x = __fadd_rn(x, __uint_as_float(e.record.y));
-      if (!may(e.tok)) x = -INFINITY;
-      if (kWrite) {
-        out[e.tok] = narrow(x, T());
-        return;
-      }
-      if (e.tok == here) p.draft_logit[row] = x;
-      if (x == x) {
-        const unsigned long long k = make_key(x, static_cast<uint32_t>(t0 + e.tok));
-        key = k > key ? k : key;
-      } else {
-        nan = true;
-      }
-    };
-    if (count > 0) finish(e0);
-    if (count > 32) finish(e1);
-    for (int i = 64; i < count; i += 64) {
-      const Entry a = fetch(i + lane), c = fetch(i + 32 + lane);
-      finish(a);
-      finish(c);
-    }
-    if (kWrite) continue;
-    const uint32_t high = static_cast<uint32_t>(key >> 32);
-    const uint32_t top = __reduce_max_sync(kFull, order > high ? order : high);
-    uint32_t low = 0u;
-    if (order == top && top != 0u) {
-      const int at = first_of<T, kU>(v, best);
-      low = 0xffffffffu - static_cast<uint32_t>(t0 + lead + min(lane + 32 * (at / VN), nvec - 1) * VN + at % VN);
-    }
-    if (high == top && static_cast<uint32_t>(key) > low) low = static_cast<uint32_t>(key);
-    low = __reduce_max_sync(kFull, low);
-    nan = __any_sync(kFull, nan);
-    if (lane == 0) {
-      if (top != 0u) atomicMax(p.row_key + row, (static_cast<unsigned long long>(top) << 32) | low);
-      if (nan) atomicOr(p.flags + b, ASD_STATUS_NAN_LOGIT);
-    }
+    if (at_loose >= 0)
+      out[at_loose] = !grammar || ((s_allow[warp][at_loose >> 5] >> (at_loose & 31)) & 1u) ? z[at_loose]
+                                                                                           : narrow(-INFINITY, T());
+  } else {
+    for (int at = lane; at < r.len; at += 32)
+      out[at] = !grammar || ((s_allow[warp][at >> 5] >> (at & 31)) & 1u) ? z[at] : narrow(-INFINITY, T());
   }
 }
 
@@ -432,25 +712,44 @@ RulesParams rules_params(const asd_token_rules* r) {
   return p;
 }
 
-template <typename T, int kU, bool kWrite>
-int launch_rows(RulesParams p, long long chunks, cudaStream_t stream) {
-  p.chunks = static_cast<int>(chunks);
-  const int turns = (p.R + kMaxWarps - 1) / kMaxWarps;
-  const int warps = (p.R + turns - 1) / turns;
+template <typename T>
+long long parts_of(int V, int vectors) {
+  const long long n = 32ll * vectors * Elem<T>::kVec;
+  return (V + n - 1) / n;
+}
+
+template <typename T, int kU>
+int launch_write(RulesParams p, cudaStream_t stream) {
+  p.chunks = static_cast<int>(parts_of<T>(p.V, kU));
+  const unsigned units = static_cast<unsigned>(p.B) * static_cast<unsigned>(p.R) * static_cast<unsigned>(p.chunks);
   cudaLaunchAttribute attr;
-  const cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(p.B * chunks)),
-                                            dim3(static_cast<unsigned>(32 * warps)), stream, &attr);
-  if (cudaLaunchKernelEx(&cfg, rules_kernel<T, kU, kWrite>, p) != cudaSuccess) return ASD_ERR_CUDA;
+  const cudaLaunchConfig_t cfg = pdl_config(dim3((units + kWarps - 1) / kWarps), dim3(kThreads), stream, &attr);
+  if (cudaLaunchKernelEx(&cfg, rules_write_kernel<T, kU>, p) != cudaSuccess) return ASD_ERR_CUDA;
   return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;
 }
 
+template <typename T, int kU>
+int launch_stream(const RulesParams& p, cudaStream_t stream) {
+  StreamPlan q = {};
+  q.parts = static_cast<int>(parts_of<T>(p.V, kU));
+  q.unit_ctas = (p.R * q.parts + kWarps - 1) / kWarps;
+  q.part_ctas = ((p.V - 1) / kPart + kWarps) / kWarps;
+  const unsigned ctas = static_cast<unsigned>(p.B) * static_cast<unsigned>(q.part_ctas + q.unit_ctas);
+  cudaLaunchAttribute attr;
+  const cudaLaunchConfig_t cfg = pdl_config(dim3(ctas), dim3(kThreads), stream, &attr);
+  if (cudaLaunchKernelEx(&cfg, rules_stream_kernel<T, kU>, p, q) != cudaSuccess) return ASD_ERR_CUDA;
+  return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;
+}
+
+// Units (or a row's share of a CTA) of eight vectors a lane, or of two where those would be few.
+constexpr int kWide = 8, kNarrow = 2;
 template <typename T, bool kWrite>
 int launch_rules(const RulesParams& p, cudaStream_t stream) {
-  constexpr int kWide = 8, kNarrow = 2;
-  auto chunks = [&](int u) { return (static_cast<long long>(p.V) + 32 * u * Elem<T>::kVec - 1) / (32 * u * Elem<T>::kVec); };
-  if (p.B * chunks(kWide) > INT32_MAX) return ASD_ERR_SHAPE;
-  if (p.B * chunks(kWide) * p.R >= 1200) return launch_rows<T, kWide, kWrite>(p, chunks(kWide), stream);
-  return launch_rows<T, kNarrow, kWrite>(p, chunks(kNarrow), stream);
+  const long long wide = parts_of<T>(p.V, kWide) * p.B;
+  if (wide * p.R > INT32_MAX / 8) return ASD_ERR_SHAPE;  // units and CTAs are counted in 32 bits
+  const bool few = wide * p.R < 1200;
+  if (kWrite) return few ? launch_write<T, kNarrow>(p, stream) : launch_write<T, kWide>(p, stream);
+  return few ? launch_stream<T, kNarrow>(p, stream) : launch_stream<T, kWide>(p, stream);
 }
 
 }  // namespace

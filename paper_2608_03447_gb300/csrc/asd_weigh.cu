@@ -32,9 +32,10 @@ constexpr int kMaxDevices = 64;
 // Shared memory, in floats: rows of the head padded to a multiple of four and
 // one more vector, so that a warp's sixteen rows start in different banks.
 __host__ __device__ constexpr int simt_pitch(int dim) { return (dim + 3) / 4 * 4 + 4; }
-// queries, keys twice where that fits, row scales, sums of the warps
+// queries, two tiles of keys, where the rows lie, their scales, the warps' sums
 constexpr size_t simt_smem(int rows, int dim) {
-  return sizeof(float) * static_cast<size_t>(rows + kSimtTile) * simt_pitch(dim) + sizeof(RowScale) * rows +
+  return sizeof(float) * static_cast<size_t>(rows + 2 * kSimtTile) * simt_pitch(dim) +
+         sizeof(long long) * (rows + 2 * kSimtTile) + sizeof(RowScale) * rows +
          sizeof(float) * (kSimtThreads / 32) * kSimtTile;
 }
 
@@ -57,19 +58,35 @@ __device__ __forceinline__ void load4(const T* p, bool vec, int valid, float (&x
   for (int i = 0; i < 4; ++i) x[i] = i < valid ? Store<T>::widen(p[i]) : 0.0f;
 }
 
+__device__ __forceinline__ void copy16(float* dst, const float* src, bool has) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(has ? 16 : 0)
+               : "memory");
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(r)
+      : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)),
+        "l"(*reinterpret_cast<unsigned long long*>(&c)));
+  return *reinterpret_cast<float2*>(&r);
+}
+
 // kI: query rows of a thread.
 template <typename T, int kI>
-__global__ void __launch_bounds__(kSimtThreads)
+__global__ void __launch_bounds__(kSimtThreads, 2)
     weigh_kernel(const __grid_constant__ WeighParams p, bool vec_q, bool vec_k) {
-  constexpr int kRows = 16 * kI;
+  constexpr int kRows = 16 * kI, kWarps = kSimtThreads / 32;
   extern __shared__ __align__(16) float smem[];
   __shared__ AttnDeal deal;
   const AttnParams a = weigh_deal_params(p);
   const int D = a.D, pitch = simt_pitch(D), quads = (D + 3) / 4;
-  float* sq = smem;                                                       // [kRows][pitch]
-  float* sk = sq + kRows * pitch;                                         // [kSimtTile][pitch]
-  RowScale* s_scale = reinterpret_cast<RowScale*>(sk + kSimtTile * pitch);  // [kRows]
-  float* s_sum = reinterpret_cast<float*>(s_scale + kRows);               // [warps][kSimtTile]
+  float* sq = smem;                // [kRows][pitch]
+  float* sk = sq + kRows * pitch;  // [2][kSimtTile][pitch]
+  long long* s_at = reinterpret_cast<long long*>(sk + 2 * kSimtTile * pitch);  // [2][kSimtTile] of a tile's keys
+  long long* s_row = s_at + 2 * kSimtTile;                                     // [kRows] of the queries
+  RowScale* s_scale = reinterpret_cast<RowScale*>(s_row + kRows);              // [kRows]
+  float* s_sum = reinterpret_cast<float*>(s_scale + kRows);                    // [kWarps][kSimtTile]
+  const bool async = sizeof(T) == 4 && vec_k;
 
   const int tid = threadIdx.x, x = tid & 15, y = tid >> 4, lane = tid & 31, warp = tid >> 5;
   pdl_signal_dependents();
@@ -80,79 +97,118 @@ __global__ void __launch_bounds__(kSimtThreads)
 
   AttnWalk<kSimtTile> w(a, deal);
   for (w.start(); w.more(); w.next()) {
-    const int rows = w.rows(), span = w.span(), ctx = w.r.ctx;
+    const int rows = w.rows(), span = w.span(), ctx = w.r.ctx, j0 = w.j0, j1 = w.j1();
     const int tiles = (rows + kRows - 1) / kRows;
-    auto load_rows = [&](int row0) {
-      for (int r = warp; r < kRows; r += kSimtThreads / 32) {
+    // a thread a row says where it lies; then a warp a row copies it
+    auto find_rows = [&](int row0) {
+      for (int r = tid; r < kRows; r += kSimtThreads) {
         const int row = row0 + r, t = row < rows ? a.by_group.quot(row) : 0;
         const int head = w.h * a.group + row - t * a.group;
         const int token = row < rows ? weigh_token(p, w.b, t) : -1;
-        const T* src = reinterpret_cast<const T*>(a.q) + w.b * a.q_batch + token * a.q_token + head * a.q_head;
+        s_row[r] = token < 0 ? -1 : w.b * a.q_batch + token * a.q_token + head * a.q_head;
+        s_scale[r] = row_scale(p, w.b, token, head);
+      }
+    };
+    auto load_rows = [&] {
+#pragma unroll 4
+      for (int r = warp; r < kRows; r += kWarps) {
+        const long long at = s_row[r];
+        const T* src = reinterpret_cast<const T*>(a.q) + at;
         for (int d4 = lane; d4 < quads; d4 += 32) {
           float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-          if (token >= 0) load4(src + 4 * d4, vec_q, D - 4 * d4, f);
+          if (at >= 0) load4(src + 4 * d4, vec_q, D - 4 * d4, f);
           *reinterpret_cast<float4*>(sq + r * pitch + 4 * d4) =
               make_float4(f[0] * a.scale_log2, f[1] * a.scale_log2, f[2] * a.scale_log2, f[3] * a.scale_log2);
         }
-        if (lane == 0) s_scale[r] = row_scale(p, w.b, token, head);
       }
     };
-    bool loaded = false;
-    const int j1 = w.j1();
-    for (int j = w.j0; j < j1; ++j) {
-      const int slot0 = j * kSimtTile;
-      __syncthreads();  // the tile before is done with shared memory
-      for (int s = warp; s < kSimtTile; s += kSimtThreads / 32) {
-        long long at = -1;
-        if (s < span - slot0) {
-          at = slot_offset(a.cache, w.b, slot0 + s);
-          if (at < 0 && lane == 0 && a.status) atomicOr(a.status + w.b, static_cast<int>(ASD_STATUS_PAGE));
-        }
-        const T* src = reinterpret_cast<const T*>(a.cache.k) + w.h * a.cache.head_stride + at;
-        for (int d4 = lane; d4 < quads; d4 += 32) {
-          float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-          if (at >= 0) load4(src + 4 * d4, vec_k, D - 4 * d4, f);
-          *reinterpret_cast<float4*>(sk + s * pitch + 4 * d4) = make_float4(f[0], f[1], f[2], f[3]);
+    auto find_keys = [&](int j) {
+      const int slot = j * kSimtTile + tid;
+      if (tid >= kSimtTile || j >= j1) return;
+      long long at = -1;
+      if (slot < span) {
+        at = slot_offset(a.cache, w.b, slot);
+        if (at >= 0)
+          at += w.h * a.cache.head_stride;
+        else if (a.status)
+          atomicOr(a.status + w.b, static_cast<int>(ASD_STATUS_PAGE));
+      }
+      s_at[(j & 1) * kSimtTile + tid] = at;
+    };
+    auto load_keys = [&](int j) {  // in the background, or (types to widen, odd rows) by way of registers
+      if (j < j1) {
+        const long long* at = s_at + (j & 1) * kSimtTile;
+        float* dst = sk + (j & 1) * kSimtTile * pitch;
+        const T* base = reinterpret_cast<const T*>(a.cache.k);
+#pragma unroll 4
+        for (int s = warp; s < kSimtTile; s += kWarps) {
+          const long long o = at[s];
+          for (int d4 = lane; d4 < quads; d4 += 32) {
+            if constexpr (sizeof(T) == 4) {
+              if (async) {
+                copy16(dst + s * pitch + 4 * d4, o >= 0 ? base + o + 4 * d4 : base, o >= 0);
+                continue;
+              }
+            }
+            float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (o >= 0) load4(base + o + 4 * d4, vec_k, D - 4 * d4, f);
+            *reinterpret_cast<float4*>(dst + s * pitch + 4 * d4) = make_float4(f[0], f[1], f[2], f[3]);
+          }
         }
       }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    __syncthreads();  // the unit before is done with shared memory
+    find_rows(0);
+    find_keys(j0);
+    find_keys(j0 + 1);
+    __syncthreads();
+    load_keys(j0);
+    load_rows();
+    for (int j = j0; j < j1; ++j) {
+      const int slot0 = j * kSimtTile;
+      const float* keys = sk + (j & 1) * kSimtTile * pitch;
+      load_keys(j + 1);  // the other buffer, which the tile before is done with
+      asm volatile("cp.async.wait_group 1;" ::: "memory");
       const bool masked = slot0 > ctx - kSimtTile;  // slot0 + kSimtTile may be 2^31
       float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
       for (int tile = 0; tile < tiles; ++tile) {
-        if (!loaded || tiles > 1) {
-          if (tile > 0) __syncthreads();
-          load_rows(tile * kRows);
-          loaded = true;
+        if (tiles > 1 && (tile > 0 || j > j0)) {
+          __syncthreads();
+          find_rows(tile * kRows);
+          __syncthreads();
+          load_rows();
         }
         __syncthreads();
-        float s[kI][4];
+        float2 s[kI][4];
 #pragma unroll
-        for (int i = 0; i < kI; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.0f;
+        for (int i = 0; i < kI; ++i)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) s[i][c] = make_float2(0.0f, 0.0f);
+#pragma unroll 2
         for (int d4 = 0; d4 < quads; ++d4) {
           float4 q[kI], kk[4];
 #pragma unroll
           for (int i = 0; i < kI; ++i) q[i] = *reinterpret_cast<const float4*>(sq + (y + 16 * i) * pitch + 4 * d4);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) kk[c] = *reinterpret_cast<const float4*>(sk + (x + 16 * c) * pitch + 4 * d4);
+          for (int c = 0; c < 4; ++c) kk[c] = *reinterpret_cast<const float4*>(keys + (x + 16 * c) * pitch + 4 * d4);
 #pragma unroll
           for (int i = 0; i < kI; ++i)
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-              s[i][c] = fmaf(q[i].x, kk[c].x, s[i][c]);
-              s[i][c] = fmaf(q[i].y, kk[c].y, s[i][c]);
-              s[i][c] = fmaf(q[i].z, kk[c].z, s[i][c]);
-              s[i][c] = fmaf(q[i].w, kk[c].w, s[i][c]);
+              s[i][c] = fma2(make_float2(q[i].x, q[i].y), make_float2(kk[c].x, kk[c].y), s[i][c]);
+              s[i][c] = fma2(make_float2(q[i].z, q[i].w), make_float2(kk[c].z, kk[c].w), s[i][c]);
             }
         }
 #pragma unroll
         for (int i = 0; i < kI; ++i) {
           const RowScale scale = s_scale[y + 16 * i];
-          const int row = tile * kRows + y + 16 * i;
           if (scale.y == 0.0f) continue;
-          // the row's last slot
-          const int see = masked ? ctx - slot0 + a.by_group.quot(row) : kSimtTile;
+          // the last slot that the row sees
+          const int see = masked ? ctx - slot0 + a.by_group.quot(tile * kRows + y + 16 * i) : kSimtTile;
 #pragma unroll
           for (int c = 0; c < 4; ++c)
-            if (x + 16 * c <= see) sum[c] = fmaf(exp2f(s[i][c] - scale.x), scale.y, sum[c]);
+            if (x + 16 * c <= see) sum[c] = fmaf(exp2f(s[i][c].x + s[i][c].y - scale.x), scale.y, sum[c]);
         }
       }
 #pragma unroll
@@ -161,16 +217,19 @@ __global__ void __launch_bounds__(kSimtThreads)
         if (lane < 16) s_sum[warp * kSimtTile + x + 16 * c] = sum[c];
       }
       __syncthreads();
+      find_keys(j + 2);
       const int slot = slot0 + tid;
       if (tid < kSimtTile && tid < span - slot0) {
         float total = s_sum[tid];
 #pragma unroll
-        for (int i = 1; i < kSimtThreads / 32; ++i) total += s_sum[i * kSimtTile + tid];
+        for (int i = 1; i < kWarps; ++i) total += s_sum[i * kSimtTile + tid];
         const long long at = (static_cast<long long>(w.b) * a.heads + w.h) * p.width + slot;
         if (slot < ctx && p.decay != 0.0f) total = fmaf(__ldcg(p.weight + at), p.decay, total);
         p.weight_out[at] = total;
       }
+      __syncthreads();
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
   }
 }
 
@@ -203,7 +262,14 @@ int launch_simt(const WeighParams& p, cudaStream_t stream) {
 
 template <typename T>
 int launch_rows(const WeighParams& p, cudaStream_t stream) {
-  return p.a.unit_rows <= 16 ? launch_simt<T, 1>(p, stream) : launch_simt<T, 4>(p, stream);
+  const int tiles = (p.a.unit_rows + 79) / 80;
+  const int i = p.a.unit_rows <= 16 ? 1 : ((p.a.unit_rows + tiles - 1) / tiles + 15) / 16;
+  if constexpr (sizeof(T) == 4) {
+    if (i == 2) return launch_simt<T, 2>(p, stream);
+    if (i == 3) return launch_simt<T, 3>(p, stream);
+    if (i == 5) return launch_simt<T, 5>(p, stream);
+  }
+  return i == 1 ? launch_simt<T, 1>(p, stream) : launch_simt<T, 4>(p, stream);
 }
 
 int check_weigh(const asd_kv_cache* cache, const asd_weigh& a) {
@@ -266,6 +332,8 @@ extern "C" int asd_kv_weigh(const asd_kv_cache* cache, const asd_weigh* args, as
   p.tokens = a.T;
   p.width = a.width;
   p.decay = a.decay;
+  if (scale_log2 != 0.0f)
+    p.scale_lost = static_cast<float>(static_cast<double>(a.scale) * 1.4426950408889634 / scale_log2 - 1.0);
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (weigh_tc_takes(cache, p)) return launch_weigh_tc(cache, p, s);
   if (cache->dtype == ASD_F32) return launch_rows<float>(p, s);

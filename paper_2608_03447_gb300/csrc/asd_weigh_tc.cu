@@ -6,12 +6,13 @@
 // its lane's columns and adds up exp2(scale S - lse) over them, so a slot's weight
 // never leaves a register until it is written, and no threads exchange anything.
 //
-// Two groups of 128 threads take the tiles in turn, each with two accumulators, so
-// that the next product is there when one is added up. With more than 128 rows a
-// pair of tiles, one a group, meets every slab of queries.
+// Four groups of 128 threads take the tiles in turn, each with an accumulator, so
+// that products and exponentials of several tiles are under way. With more than 128
+// rows some tiles, one a group, meet every slab of queries; the slabs stay where
+// they all fit.
 //
-// A CTA per SM: warps 0-3 and 4-7 are the groups, warp 8 walks the units and loads
-// keys, warp 9 issues the MMAs, warps 10 and 11 copy queries and the rows' scales.
+// A CTA per SM: warps 0 to 15 are the groups, warp 16 walks the units and loads keys,
+// warp 17 issues the MMAs, warps 18 and 19 copy queries and the rows' scales.
 // Keys are TMA boxes of as many slots as the page size and the tile have as a common
 // divisor, or 16-byte copies where that is less than the swizzle's eight rows.
 #include <cuda.h>
@@ -35,17 +36,27 @@ using namespace asd_detail;
 
 constexpr int kTile = kSlabRows;  // slots
 constexpr int kCols = 128;        // query rows of a slab
-constexpr int kSumThreads = 256;
-constexpr int kKeyWarp = 8, kMmaWarp = 9, kQueryWarp = 10;
+constexpr int kChunk = 32;        // that are added up at once
+// log2: how far apart the sums of a chunk's rows may be for one offset to serve them all: exp2(scale S - offset) is
+// then above the smallest 32-bit numbers wherever a weight is above 2^-86.
+constexpr float kSpread = 40.0f;
+constexpr int kGroups = 4;        // of 128 threads
+constexpr int kSumThreads = kGroups * 128;
+constexpr int kKeyWarp = 16, kMmaWarp = 17, kQueryWarp = 18;
 constexpr int kQueryThreads = 64;
-constexpr int kThreads = 12 * 32;
+constexpr int kThreads = 20 * 32;  // five warps a scheduler: 96 registers each
 constexpr int kTmemCols = 512;
 constexpr int kMaxStages = 12;
-constexpr int kQueries = 2;  // slabs of queries
+constexpr int kMaxQueries = 4;
 constexpr unsigned long long kLandNs = 10000000;  // longer than any load takes
 constexpr size_t kSmemMax = 232448;
 
 constexpr int slab_bytes(int dim) { return kTile * dim * 2; }  // 128 rows of a padded head
+// Slabs of queries: 64 KB. A unit that needs no more keeps them for all its tiles.
+constexpr int query_slabs(int dim) { return dim <= 64 ? kMaxQueries : kMaxQueries / 2; }
+// Tiles that meet a slab of queries one after the other where a unit has several slabs: their keys stay meanwhile, and
+// at heads of 128 there are four stages.
+constexpr int tiles_at_once(int dim) { return dim <= 64 ? kGroups : kGroups - 1; }
 
 // What the roles know of a unit; the keys' warp walks the CTA's range and publishes its units through a ring.
 struct alignas(16) WeighUnit {
@@ -54,26 +65,28 @@ struct alignas(16) WeighUnit {
   int tiles, cols, pad[2]; // slabs of queries, and the columns of each (a multiple of 16)
 };
 constexpr int kUnits = 4;
-constexpr int kUnitReaders = 11;  // warps
+constexpr int kUnitReaders = kSumThreads / 32 + 3;  // warps
 
 struct WeighShared {
   unsigned long long k_full[kMaxStages], k_empty[kMaxStages];  // loads have landed; the MMAs have read them
   unsigned long long unit_full[kUnits], unit_empty[kUnits];
-  unsigned long long q_full[kQueries], q_empty[kQueries];
-  unsigned long long s_full[4], s_empty[4];  // accumulator 2 g + i of group g: is complete; has been read
+  unsigned long long q_full[kMaxQueries], q_empty[kMaxQueries];
+  unsigned long long s_full[kGroups], s_empty[kGroups];  // a group's accumulator is complete; has been read
   unsigned long long drain;
   uint32_t tmem_base;
   int abort;
   WeighUnit unit[kUnits];
   AttnDeal deal;
-  alignas(16) RowScale scale[kQueries][kCols];  // read two at a time
+  RowScale scale[kMaxQueries][kCols];
+  alignas(16) float factor[kMaxQueries][kCols];   // 2^offset / (sum of exponentials) of each row,
+  float offset[kMaxQueries][kCols / kChunk];      // with one whole offset a chunk of rows, or NaN: too far apart
 };
 constexpr int stages_for(int dim) {
-  const size_t fit = (kSmemMax - 1024 - sizeof(WeighShared) - kQueries * slab_bytes(dim)) / slab_bytes(dim);
+  const size_t fit = (kSmemMax - 1024 - sizeof(WeighShared) - query_slabs(dim) * slab_bytes(dim)) / slab_bytes(dim);
   return fit < static_cast<size_t>(kMaxStages) ? static_cast<int>(fit) : kMaxStages;
 }
 constexpr size_t smem_for(int dim) {
-  return 1024 + static_cast<size_t>(kQueries + stages_for(dim)) * slab_bytes(dim) + sizeof(WeighShared);
+  return 1024 + static_cast<size_t>(query_slabs(dim) + stages_for(dim)) * slab_bytes(dim) + sizeof(WeighShared);
 }
 static_assert(stages_for(128) >= 4, "ring depth at the widest head");
 
@@ -116,11 +129,75 @@ struct Ring {
   }
 };
 
+__device__ __forceinline__ float warp_max(float x) {
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor_sync(kFull, x, off));
+  return x;
+}
+
+// 32 or 16 consecutive columns of this thread's lane, there when it returns.
+__device__ __forceinline__ void tmem_take(uint32_t taddr, float (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
+        "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]),
+        "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]),
+        "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_take(uint32_t taddr, float (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
+        "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
+      : "r"(taddr));
+}
+
+// exp2(scale z - offset) factor summed over kN columns of this thread's lane, even and odd ones apart.
+template <int kN>
+__device__ __forceinline__ float2 sum_columns(uint32_t from, const float* factor, float scale_log2, float offset) {
+  const float2 by = {scale_log2, scale_log2}, less = {-offset, -offset};
+  float z[kN];
+  tmem_take(from, z);
+  float2 sum[2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
+#pragma unroll
+  for (int k = 0; k < kN; k += 4) {
+    const float4 f = *reinterpret_cast<const float4*>(factor + k);
+    const float2 t0 = fma2(make_float2(z[k], z[k + 1]), by, less), t1 = fma2(make_float2(z[k + 2], z[k + 3]), by, less);
+    sum[0] = fma2(make_float2(exp2_fast(t0.x), exp2_fast(t0.y)), make_float2(f.x, f.y), sum[0]);
+    sum[1] = fma2(make_float2(exp2_fast(t1.x), exp2_fast(t1.y)), make_float2(f.z, f.w), sum[1]);
+  }
+  return add2(sum[0], sum[1]);
+}
+// The same row by row, for any sums and any products: neither a row that adds nothing
+// nor one before `first` counts, whatever its product is.
+__device__ __noinline__ float sum_carefully(uint32_t from, int cols, const RowScale* scale, float scale_log2, int first) {
+  float sum = 0.0f;
+#pragma unroll 1
+  for (int c = 0; c < cols; c += 16) {
+    float z[16];
+    tmem_take(from + c, z);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const RowScale s = scale[c + k];
+      const float e = exp2_fast(fmaf(z[k], scale_log2, -s.x));
+      if (s.y != 0.0f && c + k >= first) sum = fmaf(e, s.y, sum);
+    }
+  }
+  return sum;
+}
+
 // kDim: the head, padded. kTma: keys are loaded as TMA boxes.
 template <typename T, int kDim, bool kTma>
 __global__ void __launch_bounds__(kThreads, 1)
     weigh_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ WeighParams p, int box) {
-  constexpr int kSlab = slab_bytes(kDim), kStages = stages_for(kDim);
+  constexpr int kSlab = slab_bytes(kDim), kStages = stages_for(kDim), kQueries = query_slabs(kDim);
+  constexpr int kStep = tiles_at_once(kDim);
   constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
   constexpr int kChunks = kDim / 8;          // 16-byte chunks of a row
   constexpr int kRowsAtOnce = 32 / kChunks;  // rows that a warp copies per instruction
@@ -146,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&sh.q_full[lane - 16], 2 * kQueryThreads);  // each thread's copies, and its scales
       mbar_init(&sh.q_empty[lane - 16], 1 + kSumThreads / 32);
     }
-    if (lane >= 20 && lane < 24) {
+    if (lane >= 20 && lane < 20 + kGroups) {
       mbar_init(&sh.s_full[lane - 20], 1);
       mbar_init(&sh.s_empty[lane - 20], 4);
     }
@@ -203,17 +280,23 @@ __global__ void __launch_bounds__(kThreads, 1)
       u.tiles = (u.rows + kCols - 1) / kCols;
       u.cols = ((u.rows + u.tiles - 1) / u.tiles + 15) & ~15;
       publish(u);
+      // TMA: where this lane's box of the next tile begins; the page table is read a tile ahead
+      int page = 0, at = 0;
+      auto look_up = [&](int j) {
+        const int slot = j * kTile + lane * box;
+        if (lane * box >= kTile || j >= u.j1 || slot >= u.span) return;
+        const int n = a.cache.div.quot(slot);
+        page = __ldcg(a.cache.table + static_cast<long long>(u.b) * a.cache.table_width + n);
+        at = slot - n * a.cache.div.size;
+      };
+      if (kTma) look_up(u.j0);
       for (int j = u.j0; ok && j < u.j1; ++j) {
         const int slot0 = j * kTile, rows = min(kTile, u.span - slot0);
         const uint32_t dst = sk + ring.at * kSlab;
         unsigned long long* const bar = &sh.k_full[ring.at];
         if constexpr (kTma) {
-          int page = 0, at = 0;  // where this lane's box begins
-          if (lane * box < rows) {
-            const int slot = slot0 + lane * box, n = a.cache.div.quot(slot);
-            page = __ldcg(a.cache.table + static_cast<long long>(u.b) * a.cache.table_width + n);
-            at = slot - n * a.cache.div.size;
-          }
+          const int page_of = page, at_of = at;
+          look_up(j + 1);
           ok = warp_wait(&sh.k_empty[ring.at], ring.phase ^ 1u, sh);
           if (!ok) break;
           const int n = uniform((rows + box - 1) / box), head = uniform(u.h);
@@ -222,14 +305,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           // a page out of range lies outside the tensor: the box is filled with zeros
 #pragma unroll 4
           for (int i = 0; i < n; ++i) {
-            const int pg = __shfl_sync(kFull, page, i), first = __shfl_sync(kFull, at, i);
+            const int pg = __shfl_sync(kFull, page_of, i), first = __shfl_sync(kFull, at_of, i);
             if (elected) {
 #pragma unroll
               for (int half = 0; half < kDim / 64; ++half)
                 load_box(dst + half * kHalfSlab + i * box * 128, &map_k, bar, half * 64, first, head, pg);
             }
           }
-          if (lane < n && static_cast<unsigned>(page) >= static_cast<unsigned>(a.cache.pages) && a.status)
+          if (lane < n && static_cast<unsigned>(page_of) >= static_cast<unsigned>(a.cache.pages) && a.status)
             atomicOr(a.status + u.b, static_cast<int>(ASD_STATUS_PAGE));
           __syncwarp();
         } else {
@@ -260,7 +343,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     publish(WeighUnit{});
     if (!kTma) asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp >= kQueryWarp) {
-    // ---------------- queries, in as many slabs as they need; again for every pair of tiles where there are several
+    // ---------------- queries; those that need more slabs than there are come again for every step
     const int part = warp - kQueryWarp;
     UnitFeed feed;
     Ring<kQueries> ring;
@@ -270,7 +353,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!next) break;
       const WeighUnit u = *next;
       feed.done(sh);
-      const int times = u.tiles > 1 ? (u.j1 - u.j0 + 1) / 2 : 1;
+      const int times = u.tiles > kQueries ? (u.j1 - u.j0 + kStep - 1) / kStep : 1;
       for (int i = 0; ok && i < times; ++i) {
         for (int tile = 0; ok && tile < u.tiles; ++tile) {
           ok = warp_wait(&sh.q_empty[ring.at], ring.phase ^ 1u, sh);
@@ -281,7 +364,17 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int token = r < u.cols && row < u.rows ? weigh_token(p, u.b, t) : -1;
             const int head = u.h * p.a.group + row - t * p.a.group;
             const long long off = token < 0 ? -1 : u.b * p.a.q_batch + token * p.a.q_token + head * p.a.q_head;
-            if (r < u.cols) sh.scale[ring.at][r] = row_scale(p, u.b, token, head);
+            // exp2(z - x) y as exp2(z - m) f with one whole m for the chunk: no number but f that differs from row to row
+            const RowScale scale = row_scale(p, u.b, token, head);
+            const float most = warp_max(scale.y == 0.0f ? -INFINITY : scale.x);
+            const float least = -warp_max(scale.y == 0.0f ? -INFINITY : -scale.x);
+            const float m = most == -INFINITY ? 0.0f : ceilf(most);
+            if (r < u.cols) {
+              sh.scale[ring.at][r] = scale;
+              sh.factor[ring.at][r] = scale.y == 0.0f ? 0.0f : exp2f(m - scale.x) * scale.y;
+            }
+            if (lane == 0)
+              sh.offset[ring.at][r0 / kChunk] = most - least > kSpread || !(m - m == 0.0f) ? NAN : m;
 #pragma unroll 4
             for (int k = 0; k < 32 / kRowsAtOnce; ++k) {
               const int to = k * kRowsAtOnce + sub;
@@ -304,17 +397,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     UnitFeed feed;
     Ring<kStages> keys;
     Ring<kQueries> queries;
-    uint32_t empty = 0xfu;  // per accumulator the parity to wait for
-    int turn = 0;           // of the groups
-    uint32_t which = 0;     // a bit a group: its next accumulator
+    uint32_t empty = (1u << kGroups) - 1u;  // per accumulator the parity to wait for
+    int turn = 0;                           // of the groups: the next tile's
     bool ok = true;
-    auto product = [&](int g, int stage) {  // of a tile's keys with the slab of queries, for group g
-      const int acc = 2 * g + static_cast<int>((which >> g) & 1u);
-      ok = ok && warp_wait(&sh.s_empty[acc], (empty >> acc) & 1u, sh);
-      empty ^= 1u << acc;
-      which ^= 1u << g;
-      return acc;
-    };
     while (ok) {
       const WeighUnit* u = feed.wait(sh);
       if (!u) break;
@@ -322,56 +407,55 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t desc = uniform(instr_desc(kBf16, u->cols, false));
       int left = uniform(u->j1 - u->j0);
       feed.done(sh);
-      if (tiles == 1) {
-        ok = warp_wait(&sh.q_full[queries.at], queries.phase, sh);
-        fence_for_mma();
-      }
+      const bool stays = tiles <= kQueries;
+      bool first = true;  // of the unit's steps
       while (ok && left > 0) {
-        const int pair = tiles == 1 ? 1 : min(left, 2);
-        int stage[2] = {keys.at, keys.at + 1 == kStages ? 0 : keys.at + 1};
+        const int count = tiles == 1 ? 1 : min(left, kStep);
+        const bool ends = left == count;
+        const int stage0 = keys.at;
+        Ring<kQueries> slab = queries;
 #pragma unroll 1
         for (int tile = 0; ok && tile < tiles; ++tile) {
-          if (tiles > 1) {
-            ok = warp_wait(&sh.q_full[queries.at], queries.phase, sh);
-            fence_for_mma();
+          if (first || !stays) {
+            ok = warp_wait(&sh.q_full[slab.at], slab.phase, sh);
+            fence_for_mma();  // threads copied them
           }
 #pragma unroll 1
-          for (int i = 0; ok && i < pair; ++i) {
+          for (int i = 0; ok && i < count; ++i) {
             if (tile == 0) {
               ok = warp_wait(&sh.k_full[keys.at], keys.phase, sh);
               if (!kTma) fence_for_mma();
               keys.next();
             }
-            const int s = uniform(i == 0 ? stage[0] : stage[1]);
-            const int acc = uniform(product(tiles == 1 ? turn : i, s));
+            const int s = stage0 + i < kStages ? stage0 + i : stage0 + i - kStages;
+            const int g = (turn + i) & (kGroups - 1);
+            ok = ok && warp_wait(&sh.s_empty[g], (empty >> g) & 1u, sh);
+            empty ^= 1u << g;
             if (!ok) break;
             tc_fence_after();
-            const uint32_t ka = uniform((sk + s * kSlab) >> 4), qb = uniform((sq + queries.at * kSlab) >> 4);
-            const uint32_t d = uniform(tmem + static_cast<uint32_t>(acc * kCols));
+            const uint32_t ka = (sk + s * kSlab) >> 4, qb = (sq + slab.at * kSlab) >> 4;
+            const uint32_t d = tmem + static_cast<uint32_t>(g * kCols);
             if (elected) {
 #pragma unroll
               for (int k = 0; k < kDim / 16; ++k) {
                 const uint32_t at = ((k >> 2) * kHalfSlab + (k & 3) * 32) >> 4;
                 mma_smem(d, tile_desc(ka + at, false), tile_desc(qb + at, false), desc, k > 0 ? 1u : 0u);
               }
-              mma_commit(&sh.s_full[acc]);
+              mma_commit(&sh.s_full[g]);
               if (tile == tiles - 1) mma_commit(&sh.k_empty[s]);
             }
             __syncwarp();
           }
-          if (tiles > 1) {
-            if (elected) mma_commit(&sh.q_empty[queries.at]);
+          if (ends || !stays) {
+            if (elected) mma_commit(&sh.q_empty[slab.at]);
             __syncwarp();
-            queries.next();
           }
+          slab.next();
         }
-        turn ^= 1;
-        left -= pair;
-      }
-      if (tiles == 1) {
-        if (elected) mma_commit(&sh.q_empty[queries.at]);
-        __syncwarp();
-        queries.next();
+        if (ends || !stays) queries = slab;
+        turn = (turn + count) & (kGroups - 1);
+        first = false;
+        left -= count;
       }
     }
     drain(&sh.drain, elected);
@@ -382,8 +466,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     UnitFeed feed;
     Ring<kQueries> queries;
-    uint32_t full = 0;  // per accumulator the parity to wait for
-    uint32_t which = 0;
+    uint32_t full = 0;  // the parity to wait for
     int turn = 0;
     bool ok = true;
     while (ok) {
@@ -391,67 +474,62 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!next) break;
       const WeighUnit u = *next;
       feed.done(sh);
-      const bool pairs = u.tiles > 1;
-      if (!pairs) ok = warp_wait(&sh.q_full[queries.at], queries.phase, sh);
-      for (int j = u.j0; ok && j < u.j1; j += pairs ? 2 : 1) {
-        const int mine = pairs ? j + g : j;
-        const bool has = pairs ? mine < u.j1 : turn == g;  // whether this group has a tile
-        turn ^= 1;
-        if (!has && !pairs) continue;
+      const bool stays = u.tiles <= kQueries;
+      for (int j = u.j0; ok && j < u.j1;) {
+        const int count = u.tiles == 1 ? 1 : min(u.j1 - j, kStep);
+        const int i = (g - turn) & (kGroups - 1), mine = j + i;
+        const bool has = i < count;  // whether this group has one of the tiles
+        turn = (turn + count) & (kGroups - 1);
+        j += count;
+        const bool ends = j == u.j1;
+        if (!has && !ends && stays) continue;
         const int slot = mine * kTile + slot_of;
         const bool exists = has && slot < u.span;
         const long long at = (static_cast<long long>(u.b) * p.a.heads + u.h) * p.width + slot;
         float before = 0.0f;
         if (exists && slot < u.ctx && p.decay != 0.0f) before = __ldcg(p.weight + at);
         const bool masked = mine * kTile > u.ctx - kTile;  // some slot is not seen by all rows
-        float2 sum = {0.0f, 0.0f};
+        float sum = 0.0f;
+        Ring<kQueries> slab = queries;
         for (int tile = 0; ok && tile < u.tiles; ++tile) {
-          if (pairs) ok = warp_wait(&sh.q_full[queries.at], queries.phase, sh);
-          if (ok && has) {
-            const int acc = 2 * g + static_cast<int>(which);
-            ok = warp_wait(&sh.s_full[acc], (full >> which) & 1u, sh);
-            full ^= 1u << which;
-            which ^= 1u;
+          // the rows' scales; and no slab is given back before it is there, by a group without a tile either
+          if (has || ends || !stays) ok = warp_wait(&sh.q_full[slab.at], slab.phase, sh);
+          if (has) {
+            ok = ok && warp_wait(&sh.s_full[g], full, sh);
+            full ^= 1u;
             if (ok) {
               tc_fence_after();
-              const uint32_t from = tmem + static_cast<uint32_t>(acc * kCols) + lanes;
-              const float4* scale = reinterpret_cast<const float4*>(sh.scale[queries.at]);
-              // the slab's first row that sees the slot
-              const int first = masked && slot > u.ctx ? min((slot - u.ctx) * p.a.group - tile * u.cols, kCols) : 0;
-#pragma unroll 1
-              for (int c = 0; c < u.cols; c += 16) {
-                float z[16];
-                tmem_ld16(from + c, z);
-                tmem_ld_wait();
-#pragma unroll
-                for (int k = 0; k < 16; k += 2) {
-                  const float4 s = scale[(c + k) / 2];
-                  float e0 = exp2_fast(fmaf(z[k], p.a.scale_log2, -s.x));
-                  float e1 = exp2_fast(fmaf(z[k + 1], p.a.scale_log2, -s.z));
-                  // neither a row that adds nothing nor one that does not see the slot, whatever its product is
-                  if (s.y == 0.0f || c + k < first) e0 = 0.0f;
-                  if (s.w == 0.0f || c + k + 1 < first) e1 = 0.0f;
-                  sum.x = fmaf(e0, s.y, sum.x);
-                  sum.y = fmaf(e1, s.w, sum.y);
-                }
+              const uint32_t from = tmem + static_cast<uint32_t>(g * kCols) + lanes;
+              float add = 0.0f;
+              bool careful = masked;
+              for (int c = 0; c < u.cols && !careful; c += kChunk) {
+                const float* factor = sh.factor[slab.at] + c;
+                const float offset = sh.offset[slab.at][c / kChunk];
+                const float2 some = u.cols - c >= kChunk ? sum_columns<kChunk>(from + c, factor, p.a.scale_log2, offset)
+                                                         : sum_columns<16>(from + c, factor, p.a.scale_log2, offset);
+                add += some.x + some.y;
               }
+              // a key that is not finite makes the product with a row that adds nothing NaN too
+              careful = __any_sync(kFull, careful || add != add);
+              if (careful) {
+                // the slab's first row that sees the slot
+                const int first = slot > u.ctx ? min((slot - u.ctx) * p.a.group - tile * u.cols, kCols) : 0;
+                add = sum_carefully(from, u.cols, sh.scale[slab.at], p.a.scale_log2, first);
+              }
+              sum += add;
               tc_fence_before();
               __syncwarp();
-              if (lane == 0) mbar_arrive(&sh.s_empty[acc]);
+              if (lane == 0) mbar_arrive(&sh.s_empty[g]);
             }
           }
-          if (pairs) {
+          if (ends || !stays) {
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.q_empty[queries.at]);
-            queries.next();
+            if (lane == 0) mbar_arrive(&sh.q_empty[slab.at]);
           }
+          slab.next();
         }
-        if (ok && exists) p.weight_out[at] = fmaf(before, p.decay, sum.x + sum.y);
-      }
-      if (!pairs) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.q_empty[queries.at]);
-        queries.next();
+        if (ends || !stays) queries = slab;
+        if (ok && exists) p.weight_out[at] = fmaf(before, p.decay, sum);
       }
     }
   }
