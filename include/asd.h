@@ -624,10 +624,24 @@ typedef struct {
  * fp32: a draft that is not allowed has an infinite one, NaN where no token is
  * allowed (then y* = 0). ASD_RESIDENT_INPUTS is not taken.
  */
-int asd_rules_verify(const asd_token_rules* rules, const void* logits, int dtype, int K, const int32_t* draft,
-                     asd_ledger* ledger, float gate, int cap, int32_t* accepted_len, int32_t* committed,
-                     int32_t* recovery, int32_t* row_argmax, float* row_regret, int32_t* status, void* workspace,
-                     size_t workspace_bytes, asd_stream_t stream);
+typedef struct {
+  const void* logits;     /* [B, K+1, V] */
+  const int32_t* draft;   /* [B, K] */
+  asd_ledger* ledger;     /* [B], or NULL: strict */
+  int32_t* accepted_len;
+  int32_t* committed;
+  int32_t* recovery;
+  int32_t* row_argmax;    /* may be NULL, as row_regret and status may */
+  float* row_regret;
+  int32_t* status;
+  void* workspace;
+  size_t workspace_bytes; /* >= asd_workspace_size(B, K, V, dtype) */
+  int dtype;              /* ASD_F32 or ASD_BF16 */
+  int K;
+  float gate;
+  int cap;
+} asd_rules_block;
+int asd_rules_verify(const asd_token_rules* rules, const asd_rules_block* block, asd_stream_t stream);
 
 /*
  * The changed logits themselves, for callers that sample: logits and out [B, rows,

@@ -120,7 +120,7 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.asd_kv_weigh.restype = i32
     lib.asd_kv_evict.argtypes = [vp, vp, vp]
     lib.asd_kv_evict.restype = i32
-    lib.asd_rules_verify.argtypes = [vp, vp, i32, i32, vp, vp, f32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.asd_rules_verify.argtypes = [vp, vp, vp]
     lib.asd_rules_verify.restype = i32
     lib.asd_rules_logits.argtypes = [vp, vp, i32, i32, vp, vp, vp]
     lib.asd_rules_logits.restype = i32
@@ -884,7 +884,8 @@ def kv_evict(cache: KVCache, kv_len: torch.Tensor, weight: torch.Tensor, keep: t
 
 # ---------------------------------------------------------------- logits under rules
 
-_RULES = struct.Struct("6P 2q 2i")  # asd_token_rules
+_RULES = struct.Struct("6P 2q 2i")           # asd_token_rules
+_RULES_BLOCK = struct.Struct("10P N 2i f i")  # asd_rules_block
 
 
 class TokenRules:
@@ -957,19 +958,23 @@ def rules_verify(logits: torch.Tensor, draft: torch.Tensor, ledger: torch.Tensor
     logits [B, K+1, V] float32 or bfloat16; row j counts the drafts before it. ``allow`` int32 [B, K+1, ceil(V / 32)]:
     a bit a token that the grammar lets come (strides of 0 for masks that several rows share). Workspaces are verify's.
     """
-    B, K, V = _shape(logits, draft)
-    if (B, V) != (rules.B, rules.V):
-        raise ValueError(f"logits must be [{rules.B}, K+1, {rules.V}] like the rules")
+    shape, index = logits.shape, rules.index
+    if len(shape) != 3 or shape[0] != rules.B or shape[2] != rules.V or logits.get_device() != index or \
+            not logits.is_contiguous():
+        raise ValueError(f"logits must be a contiguous [{rules.B}, K+1, {rules.V}] tensor on the rules' device")
+    B, K = shape[0], shape[1] - 1
     code = _dtype_code(logits)
-    zp = _check_rules(rules, "logits", logits, (B, K + 1, V), logits.dtype)
     xp = _check_rules(rules, "draft", draft, (B, K))
-    lp = None if ledger is None else _check_rules(rules, "ledger", ledger, (B, 2), torch.float32)
-    packed = rules._pack(allow, K + 1)
-    ws = workspace or Workspace(B, K, V, code, logits.device, stream)
+    lp = 0 if ledger is None else _check_rules(rules, "ledger", ledger, (B, 2), torch.float32)
+    packed = rules._plain if allow is None else rules._pack(allow, K + 1)
+    ws = workspace or Workspace(B, K, rules.V, code, logits.device, stream)
     o = out or alloc_outputs(B, K, logits.device, stream=stream)
-    rc = load().asd_rules_verify(packed, zp, code, K, xp, lp, float(gate), int(cap), _ptr(o["accepted_len"]),
-                                 _ptr(o["committed"]), _ptr(o["recovery"]), _ptr(o.get("row_argmax")),
-                                 _ptr(o.get("row_regret")), _ptr(o.get("status")), ws.ptr, ws.nbytes, _stream(stream))
+    argmax, regret, status = o.get("row_argmax"), o.get("row_regret"), o.get("status")
+    block = _RULES_BLOCK.pack(
+        logits.data_ptr(), xp, lp, o["accepted_len"].data_ptr(), o["committed"].data_ptr(), o["recovery"].data_ptr(),
+        0 if argmax is None else argmax.data_ptr(), 0 if regret is None else regret.data_ptr(),
+        0 if status is None else status.data_ptr(), ws.buffer.data_ptr(), ws.nbytes, code, K, gate, cap)
+    rc = load().asd_rules_verify(packed, block, _stream(stream))
     if rc:
         raise AsdError("asd_rules_verify", rc)
     return o
@@ -986,7 +991,7 @@ def rules_logits(logits: torch.Tensor, draft: torch.Tensor | None, rules: TokenR
     shape = tuple(logits.shape)
     rows = shape[1]
     code = _dtype_code(logits)
-    zp = _check_rules(rules, "logits", logits, shape, logits.dtype)
+    zp = _check_rules(rules, "logits", logits, logits.shape, logits.dtype)
     xp = None if draft is None else _check_rules(rules, "draft", draft, (rules.B, rows - 1))
     packed = rules._pack(allow, rows)
     if out is None:

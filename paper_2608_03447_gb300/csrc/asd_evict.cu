@@ -33,7 +33,7 @@ constexpr int kBinBits = 11, kBins = 1 << kBinBits;
 constexpr int kDigits = 3;  // that 32 bits have
 constexpr int kMaxCluster = 8;
 constexpr int kMaxPart = ASD_MAX_EVICT_SLOTS / kMaxCluster;  // slots of a CTA
-constexpr int kAtOnce = 4;  // rows of keys and of values that a lane has in flight
+constexpr int kAtOnce = 2;  // rows of keys and of values that a lane has in flight
 static_assert(kMaxPart % 32 == 0, "parts are whole words of bits");
 
 // Dynamic shared memory: histograms; weights (then moves); per 32 slots two words of bits and the counts before them.
@@ -150,19 +150,25 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_kernel(const 
   // keys; those that stay in any case are above every weight and in no histogram
   constexpr unsigned kStays = 0xffffffffu;
   unsigned smallest = kStays, largest = 0u;
-#pragma unroll 8
-  for (int i = tid; i < count; i += kThreads) {
-    const int s = s0 + i;
-    const float w = __ldcg(weight + s);
-    if (copies && s < n) weight_out[s] = w;
-    unsigned key = w == w ? ordered_bits(w) : ordered_bits(-INFINITY);
-    if (s < first || s >= len - last) {
-      key = kStays;
-    } else {
-      smallest = min(smallest, key);
-      largest = max(largest, key);
+  constexpr int kLoads = 16;  // in flight at once: no store between them, which a load might not pass
+  for (int i0 = tid; i0 < count; i0 += kLoads * kThreads) {
+    float w[kLoads];
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) w[k] = i0 + k * kThreads < count ? __ldcg(weight + s0 + i0 + k * kThreads) : 0.0f;
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const int i = i0 + k * kThreads, s = s0 + i;
+      if (i >= count) break;
+      if (copies && s < n) weight_out[s] = w[k];
+      unsigned key = w[k] == w[k] ? ordered_bits(w[k]) : ordered_bits(-INFINITY);
+      if (s < first || s >= len - last) {
+        key = kStays;
+      } else {
+        smallest = min(smallest, key);
+        largest = max(largest, key);
+      }
+      s_key[i] = key;
     }
-    s_key[i] = key;
   }
   smallest = __reduce_min_sync(kFull, smallest);
   largest = __reduce_max_sync(kFull, largest);
@@ -188,6 +194,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_kernel(const 
     unsigned* hist = s_hist + digit * kBins;
     const int next = max(0, shift - kBinBits);
     const unsigned mask = (1u << (shift - next)) - 1u;
+#pragma unroll 4
     for (int i = tid; i < count; i += kThreads) {
       const unsigned key = s_key[i], d = key - smallest;
       if (key != kStays && (shift == 32 || d >> shift == prefix)) atomicAdd(&hist[(d >> next) & mask], 1u);
@@ -234,6 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_kernel(const 
   const bool some = need > 0 && need < equal;  // of equal ones the lowest slots stay
 
   const int words = (count + 31) / 32;
+#pragma unroll 4
   for (int i = warp; i < words; i += kWarps) {
     const int at = 32 * i + lane;
     const unsigned key = at < count ? s_key[at] : 0u, d = key - smallest;
@@ -306,6 +314,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_kernel(const 
     }
   };
   const unsigned below = (1u << lane) - 1u;
+#pragma unroll 4
   for (int i = warp; i < words; i += kWarps) {
     const unsigned moves = s_above[i], free = s_equal[i], base = s_base[i];
     const unsigned slot = static_cast<unsigned>(s0 + 32 * i + lane);

@@ -22,6 +22,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "asd.h"
 #include "asd_device.cuh"
 #include "asd_launch.cuh"
@@ -216,7 +218,23 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kMinBlocks = 8;
 constexpr int kPart = 2048;  // tokens that a warp looks through for those that may grow
 
+// n / d for n < 2^31 by a product.
+struct Divide {
+  unsigned mul, shift, by;
+  void set(unsigned d) {
+    unsigned l = 0;
+    while ((1ull << l) < d) ++l;
+    mul = static_cast<unsigned>((1ull << (31 + l)) / d + 1);
+    shift = 31 + l;
+    by = d;
+  }
+  __device__ __forceinline__ int quot(int n) const {
+    return static_cast<int>((static_cast<unsigned long long>(static_cast<unsigned>(n)) * mul) >> shift);
+  }
+};
+
 struct StreamPlan {
+  Divide by_parts, by_ctas;
   int parts;     // units of a row
   int unit_ctas; // CTAs of a request that have kWarps units each,
   int part_ctas; // and those that have kWarps parts of the vocabulary each
@@ -363,8 +381,8 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_signal_dependents();
   // what may grow comes behind the request's units
-  const int per = q.unit_ctas + q.part_ctas;
-  const int b = static_cast<int>(blockIdx.x) / per, at_cta = static_cast<int>(blockIdx.x) - b * per;
+  const int b = q.by_ctas.quot(static_cast<int>(blockIdx.x));
+  const int at_cta = static_cast<int>(blockIdx.x) - b * static_cast<int>(q.by_ctas.by);
   if (at_cta >= q.unit_ctas) {
     pdl_wait_prerequisites();
     growing_rows<T>(p, b, (at_cta - q.unit_ctas) * kWarps + warp, s_list[warp]);
@@ -372,7 +390,7 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks)
   }
   const int unit = at_cta * kWarps + warp, units = p.R * q.parts;
   const bool exists = unit < units;
-  const int j = exists ? unit / q.parts : 0;
+  const int j = exists ? q.by_parts.quot(unit) : 0;
   const int t0 = exists ? (unit - j * q.parts) * kUnit : 0;
   const unsigned row = static_cast<unsigned>(b) * static_cast<unsigned>(p.R) + static_cast<unsigned>(j);
   const Range<T> r(static_cast<const T*>(p.logits) + static_cast<long long>(row) * p.V + t0, min(kUnit, p.V - t0));
@@ -652,6 +670,52 @@ __global__ void __launch_bounds__(256)
   atomicOr(const_cast<uint32_t*>(p.marks) + static_cast<long long>(b) * p.words + (x >> 5), 1u << (x & 31));
 }
 
+// Many tokens of a request: a CTA has some thousand of them and sees by a bitmap of its own which it has met before.
+// A mark is then one addition a word, and of a prompt's tokens the record is touched once each (64 prompts of up to
+// 8000 tokens, half of them repeated).
+constexpr int kBulkThreads = 512, kBulkTokens = 4096;
+constexpr int kBulkWords = 50000;  // of a bitmap that fits shared memory
+__global__ void __launch_bounds__(kBulkThreads)
+    record_many_kernel(const __grid_constant__ RulesParams p, const int32_t* tokens, int n, int parts,
+                       const int32_t* token_len, int prompt, int32_t* status) {
+  extern __shared__ uint32_t s_seen[];  // [words]
+  pdl_signal_dependents();
+  for (int w = threadIdx.x; w < p.words; w += kBulkThreads) s_seen[w] = 0u;
+  __syncthreads();
+  pdl_wait_prerequisites();
+  const int b = static_cast<int>(blockIdx.x) / parts, from = (static_cast<int>(blockIdx.x) - b * parts) * kBulkTokens;
+  const int length = token_len ? __ldcg(token_len + b) : n;
+  if (length < 0 || length > n) {
+    if (from == 0 && threadIdx.x == 0 && status) atomicOr(status + b, static_cast<int>(ASD_STATUS_LENGTH));
+    return;
+  }
+  constexpr int kEach = kBulkTokens / kBulkThreads;
+  int x[kEach];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int i = from + k * kBulkThreads + static_cast<int>(threadIdx.x);
+    x[k] = i < length ? __ldcg(tokens + static_cast<long long>(b) * n + i) : -1;
+  }
+  asd_token_record* records = const_cast<asd_token_record*>(p.records) + static_cast<long long>(b) * p.V;
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    if (x[k] < 0) continue;
+    if (x[k] >= p.V) {
+      if (status) atomicOr(status + b, static_cast<int>(ASD_STATUS_TOKEN));
+      continue;
+    }
+    const uint32_t bit = 1u << (x[k] & 31), before = atomicOr(&s_seen[x[k] >> 5], bit);
+    if (!prompt)
+      atomicAdd(&records[x[k]].seen, 1u);
+    else if (!(before & bit))
+      atomicOr(&records[x[k]].seen, ASD_TOKEN_PROMPT);
+  }
+  __syncthreads();
+  uint32_t* marks = const_cast<uint32_t*>(p.marks) + static_cast<long long>(b) * p.words;
+  for (int w = threadIdx.x; w < p.words; w += kBulkThreads)
+    if (s_seen[w]) atomicOr(marks + w, s_seen[w]);
+}
+
 // A request a CTA, an entry a thread: it counts unless the same id comes again behind it.
 __global__ void __launch_bounds__(ASD_MAX_BIAS)
     bias_kernel(const __grid_constant__ RulesParams p, const int32_t* ids, const float* bias, int n,
@@ -685,6 +749,8 @@ __global__ void __launch_bounds__(ASD_MAX_BIAS)
 
 // ---------------------------------------------------------------- host side
 
+constexpr int kMaxDevices = 64;
+
 int check_rules(const asd_token_rules* r) {
   if (!r) return ASD_ERR_NULL;
   if (r->B < 0 || r->V < 1 || r->allow_batch < 0 || r->allow_row < 0) return ASD_ERR_SHAPE;
@@ -712,6 +778,29 @@ RulesParams rules_params(const asd_token_rules* r) {
   return p;
 }
 
+int launch_many(const RulesParams& p, const int32_t* tokens, int n, const int32_t* token_len, int prompt,
+                int32_t* status, asd_stream_t stream) {
+  static std::atomic<bool> ready[kMaxDevices];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return ASD_ERR_CUDA;
+  if (dev < 0 || dev >= kMaxDevices) return ASD_ERR_DEVICE;
+  if (!ready[dev].load(std::memory_order_acquire)) {
+    if (cudaFuncSetAttribute(record_many_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * kBulkWords) !=
+        cudaSuccess)
+      return ASD_ERR_CUDA;
+    ready[dev].store(true, std::memory_order_release);
+  }
+  const int parts = (n - 1) / kBulkTokens + 1;
+  cudaLaunchAttribute attr;
+  cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(p.B) * static_cast<unsigned>(parts)),
+                                      dim3(kBulkThreads), reinterpret_cast<cudaStream_t>(stream), &attr);
+  cfg.dynamicSmemBytes = 4 * static_cast<size_t>(p.words);
+  if (cudaLaunchKernelEx(&cfg, record_many_kernel, p, tokens, n, parts, token_len, prompt ? 1 : 0, status) !=
+      cudaSuccess)
+    return ASD_ERR_CUDA;
+  return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;
+}
+
 template <typename T>
 long long parts_of(int V, int vectors) {
   const long long n = 32ll * vectors * Elem<T>::kVec;
@@ -734,6 +823,8 @@ int launch_stream(const RulesParams& p, cudaStream_t stream) {
   q.parts = static_cast<int>(parts_of<T>(p.V, kU));
   q.unit_ctas = (p.R * q.parts + kWarps - 1) / kWarps;
   q.part_ctas = ((p.V - 1) / kPart + kWarps) / kWarps;
+  q.by_parts.set(static_cast<unsigned>(q.parts));
+  q.by_ctas.set(static_cast<unsigned>(q.unit_ctas + q.part_ctas));
   const unsigned ctas = static_cast<unsigned>(p.B) * static_cast<unsigned>(q.part_ctas + q.unit_ctas);
   cudaLaunchAttribute attr;
   const cudaLaunchConfig_t cfg = pdl_config(dim3(ctas), dim3(kThreads), stream, &attr);
@@ -756,34 +847,35 @@ int launch_rules(const RulesParams& p, cudaStream_t stream) {
 
 extern "C" {
 
-int asd_rules_verify(const asd_token_rules* rules, const void* logits, int dtype, int K, const int32_t* draft,
-                     asd_ledger* ledger, float gate, int cap, int32_t* accepted_len, int32_t* committed,
-                     int32_t* recovery, int32_t* row_argmax, float* row_regret, int32_t* status, void* workspace,
-                     size_t workspace_bytes, asd_stream_t stream) {
+int asd_rules_verify(const asd_token_rules* rules, const asd_rules_block* block, asd_stream_t stream) {
   int rc = check_rules(rules);
   if (rc != ASD_OK) return rc;
-  if (dtype != ASD_F32 && dtype != ASD_BF16) return ASD_ERR_DTYPE;
-  rc = check_shape(rules->B, K, rules->V, dtype);
+  if (!block) return ASD_ERR_NULL;
+  const asd_rules_block& a = *block;
+  const int K = a.K;
+  if (a.dtype != ASD_F32 && a.dtype != ASD_BF16) return ASD_ERR_DTYPE;
+  rc = check_shape(rules->B, K, rules->V, a.dtype);
   if (rc != ASD_OK) return rc;
   if (rules->B == 0) return ASD_OK;
-  if (!logits || !workspace || !accepted_len || !committed || !recovery || (K > 0 && !draft)) return ASD_ERR_NULL;
-  if (ledger && (gate != gate || gate < 0.0f || cap < 0)) return ASD_ERR_CONTROL;
+  if (!a.logits || !a.workspace || !a.accepted_len || !a.committed || !a.recovery || (K > 0 && !a.draft))
+    return ASD_ERR_NULL;
+  if (a.ledger && (a.gate != a.gate || a.gate < 0.0f || a.cap < 0)) return ASD_ERR_CONTROL;
   const WorkspaceLayout l = layout_for(rules->B, K);
-  if (workspace_bytes < l.total) return ASD_ERR_WORKSPACE;
-  if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0 ||
-      reinterpret_cast<uintptr_t>(logits) % (dtype == ASD_F32 ? 4 : 2) != 0)
+  if (a.workspace_bytes < l.total) return ASD_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(a.workspace) % 16 != 0 ||
+      reinterpret_cast<uintptr_t>(a.logits) % (a.dtype == ASD_F32 ? 4 : 2) != 0)
     return ASD_ERR_ALIGN;
-  char* ws = static_cast<char*>(workspace);
+  char* ws = static_cast<char*>(a.workspace);
   RulesParams p = rules_params(rules);
-  p.logits = logits;
-  p.draft = draft;
+  p.logits = a.logits;
+  p.draft = a.draft;
   p.R = K + 1;
   p.K = K;
   p.row_key = reinterpret_cast<unsigned long long*>(ws + l.row_key);
   p.draft_logit = reinterpret_cast<float*>(ws + l.draft_logit);
   p.flags = reinterpret_cast<unsigned*>(ws + l.flags);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  rc = dtype == ASD_F32 ? launch_rules<float, false>(p, s) : launch_rules<__nv_bfloat16, false>(p, s);
+  rc = a.dtype == ASD_F32 ? launch_rules<float, false>(p, s) : launch_rules<__nv_bfloat16, false>(p, s);
   if (rc != ASD_OK) return rc;
 
   VerifyParams q = {};  // without logits: the selection takes a zero maximum as it is
@@ -791,22 +883,22 @@ int asd_rules_verify(const asd_token_rules* rules, const void* logits, int dtype
   q.K = K;
   q.V = q.v_total = rules->V;
   q.nblk = 1;
-  q.draft = draft;
-  q.ledger = ledger;
-  q.gate = gate;
-  q.cap = cap;
-  q.accepted_len = accepted_len;
-  q.committed = committed;
-  q.recovery = recovery;
-  q.row_argmax = row_argmax;
-  q.row_regret = row_regret;
-  q.status = status;
+  q.draft = a.draft;
+  q.ledger = a.ledger;
+  q.gate = a.gate;
+  q.cap = a.cap;
+  q.accepted_len = a.accepted_len;
+  q.committed = a.committed;
+  q.recovery = a.recovery;
+  q.row_argmax = a.row_argmax;
+  q.row_regret = a.row_regret;
+  q.status = a.status;
   q.row_key = p.row_key;
   q.draft_logit = p.draft_logit;
   q.done = reinterpret_cast<unsigned long long*>(ws + l.done);
   q.flags = p.flags;
   q.error = reinterpret_cast<unsigned*>(ws + l.error);
-  return ledger ? launch_select<float, false>(q, true, s) : launch_select<float, true>(q, true, s);
+  return a.ledger ? launch_select<float, false>(q, true, s) : launch_select<float, true>(q, true, s);
 }
 
 int asd_rules_logits(const asd_token_rules* rules, const void* logits, int dtype, int rows, const int32_t* draft,
@@ -843,10 +935,12 @@ int asd_tokens_record(const asd_token_rules* rules, const int32_t* tokens, int n
   for (const void* x : words)
     if (reinterpret_cast<uintptr_t>(x) % 4 != 0) return ASD_ERR_ALIGN;
   cudaLaunchAttribute attr;
+  const RulesParams p = rules_params(rules);
+  if (n >= kBulkTokens / 2 && p.words <= kBulkWords) return launch_many(p, tokens, n, token_len, prompt, status, stream);
   const cudaLaunchConfig_t cfg =
       pdl_config(dim3(static_cast<unsigned>((total + kThreads - 1) / kThreads)), dim3(kThreads),
                  reinterpret_cast<cudaStream_t>(stream), &attr);
-  if (cudaLaunchKernelEx(&cfg, record_kernel, rules_params(rules), tokens, n, token_len, prompt ? 1 : 0, status) !=
+  if (cudaLaunchKernelEx(&cfg, record_kernel, p, tokens, n, token_len, prompt ? 1 : 0, status) !=
       cudaSuccess)
     return ASD_ERR_CUDA;
   return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;

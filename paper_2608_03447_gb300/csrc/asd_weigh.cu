@@ -62,6 +62,11 @@ __device__ __forceinline__ void copy16(float* dst, const float* src, bool has) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(has ? 16 : 0)
                : "memory");
 }
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   unsigned long long r;
   asm("fma.rn.f32x2 %0, %1, %2, %3;"
@@ -86,8 +91,6 @@ __global__ void __launch_bounds__(kSimtThreads, 2)
   long long* s_row = s_at + 2 * kSimtTile;                                     // [kRows] of the queries
   RowScale* s_scale = reinterpret_cast<RowScale*>(s_row + kRows);              // [kRows]
   float* s_sum = reinterpret_cast<float*>(s_scale + kRows);                    // [kWarps][kSimtTile]
-  const bool async = sizeof(T) == 4 && vec_k;
-
   const int tid = threadIdx.x, x = tid & 15, y = tid >> 4, lane = tid & 31, warp = tid >> 5;
   pdl_signal_dependents();
   pdl_wait_prerequisites();
@@ -109,16 +112,22 @@ __global__ void __launch_bounds__(kSimtThreads, 2)
         s_scale[r] = row_scale(p, w.b, token, head);
       }
     };
-    auto load_rows = [&] {
+    // in the background, or (types to widen, odd rows) by way of registers
+    auto load_tile = [&](float* dst, const long long* offsets, const char* from, int n, bool vec) {
+      const T* base = reinterpret_cast<const T*>(from);
 #pragma unroll 4
-      for (int r = warp; r < kRows; r += kWarps) {
-        const long long at = s_row[r];
-        const T* src = reinterpret_cast<const T*>(a.q) + at;
+      for (int r = warp; r < n; r += kWarps) {
+        const long long o = offsets[r];
         for (int d4 = lane; d4 < quads; d4 += 32) {
+          if constexpr (sizeof(T) == 4) {
+            if (vec) {
+              copy16(dst + r * pitch + 4 * d4, o >= 0 ? base + o + 4 * d4 : base, o >= 0);
+              continue;
+            }
+          }
           float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-          if (at >= 0) load4(src + 4 * d4, vec_q, D - 4 * d4, f);
-          *reinterpret_cast<float4*>(sq + r * pitch + 4 * d4) =
-              make_float4(f[0] * a.scale_log2, f[1] * a.scale_log2, f[2] * a.scale_log2, f[3] * a.scale_log2);
+          if (o >= 0) load4(base + o + 4 * d4, vec, D - 4 * d4, f);
+          *reinterpret_cast<float4*>(dst + r * pitch + 4 * d4) = make_float4(f[0], f[1], f[2], f[3]);
         }
       }
     };
@@ -135,27 +144,8 @@ __global__ void __launch_bounds__(kSimtThreads, 2)
       }
       s_at[(j & 1) * kSimtTile + tid] = at;
     };
-    auto load_keys = [&](int j) {  // in the background, or (types to widen, odd rows) by way of registers
-      if (j < j1) {
-        const long long* at = s_at + (j & 1) * kSimtTile;
-        float* dst = sk + (j & 1) * kSimtTile * pitch;
-        const T* base = reinterpret_cast<const T*>(a.cache.k);
-#pragma unroll 4
-        for (int s = warp; s < kSimtTile; s += kWarps) {
-          const long long o = at[s];
-          for (int d4 = lane; d4 < quads; d4 += 32) {
-            if constexpr (sizeof(T) == 4) {
-              if (async) {
-                copy16(dst + s * pitch + 4 * d4, o >= 0 ? base + o + 4 * d4 : base, o >= 0);
-                continue;
-              }
-            }
-            float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (o >= 0) load4(base + o + 4 * d4, vec_k, D - 4 * d4, f);
-            *reinterpret_cast<float4*>(dst + s * pitch + 4 * d4) = make_float4(f[0], f[1], f[2], f[3]);
-          }
-        }
-      }
+    auto load_keys = [&](int j) {
+      if (j < j1) load_tile(sk + (j & 1) * kSimtTile * pitch, s_at + (j & 1) * kSimtTile, a.cache.k, kSimtTile, vec_k);
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
     __syncthreads();  // the unit before is done with shared memory
@@ -163,8 +153,8 @@ __global__ void __launch_bounds__(kSimtThreads, 2)
     find_keys(j0);
     find_keys(j0 + 1);
     __syncthreads();
+    load_tile(sq, s_row, a.q, kRows, vec_q);
     load_keys(j0);
-    load_rows();
     for (int j = j0; j < j1; ++j) {
       const int slot0 = j * kSimtTile;
       const float* keys = sk + (j & 1) * kSimtTile * pitch;
@@ -177,7 +167,8 @@ __global__ void __launch_bounds__(kSimtThreads, 2)
           __syncthreads();
           find_rows(tile * kRows);
           __syncthreads();
-          load_rows();
+          load_tile(sq, s_row, a.q, kRows, vec_q);
+          asm volatile("cp.async.wait_all;" ::: "memory");
         }
         __syncthreads();
         float2 s[kI][4];
@@ -208,7 +199,7 @@ __global__ void __launch_bounds__(kSimtThreads, 2)
           const int see = masked ? ctx - slot0 + a.by_group.quot(tile * kRows + y + 16 * i) : kSimtTile;
 #pragma unroll
           for (int c = 0; c < 4; ++c)
-            if (x + 16 * c <= see) sum[c] = fmaf(exp2f(s[i][c].x + s[i][c].y - scale.x), scale.y, sum[c]);
+            if (x + 16 * c <= see) sum[c] = fmaf(exp2_fast(fmaf(s[i][c].x + s[i][c].y, a.scale_log2, -scale.x)), scale.y, sum[c]);
         }
       }
 #pragma unroll

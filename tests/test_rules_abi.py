@@ -34,10 +34,10 @@ def rules(**kw):
 
 
 def verify(lib, r, **kw):
-    a = dict(logits=0x4000, dtype=asd.BF16, K=3, draft=0x5000, ledger=0x6000, gate=1.0, cap=2, a=0x7000, c=0x7100,
-             rec=0x7200, arg=None, reg=None, status=None, ws=0x10000, wsb=1 << 30)
-    a.update(kw)
-    return lib.asd_rules_verify(r, *a.values(), None)
+    a = dict(logits=0x4000, draft=0x5000, ledger=0x6000, a=0x7000, c=0x7100, rec=0x7200, arg=0, reg=0, status=0,
+             ws=0x10000, wsb=1 << 30, dtype=asd.BF16, K=3, gate=1.0, cap=2)
+    a.update({n: 0 if x is None else x for n, x in kw.items()})
+    return lib.asd_rules_verify(r, asd._RULES_BLOCK.pack(*a.values()), None)
 
 
 BAD_RULES = [(dict(marks=0), NULL), (dict(records=0), NULL), (dict(B=-1), SHAPE), (dict(V=0), SHAPE),
@@ -56,7 +56,7 @@ def test_bad_rules(lib, kw, code):
 
 
 def test_no_rules(lib):
-    assert verify(lib, None) == NULL
+    assert verify(lib, None) == NULL and lib.asd_rules_verify(rules(), None, None) == NULL
     assert lib.asd_rules_logits(None, 0x4000, asd.F32, 4, None, 0x8000, None) == NULL
     assert lib.asd_tokens_record(None, 0x4000, 5, None, 0, None, None) == NULL
     assert lib.asd_tokens_bias(None, 0x4000, 0x5000, 5, None, None, None) == NULL
