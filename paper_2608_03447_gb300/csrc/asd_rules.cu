@@ -368,6 +368,54 @@ __device__ __forceinline__ void take_out(uint4& v, int t, __nv_bfloat16) {
   if (t >> 1 == 3) v.w = (v.w & mask) | none;
 }
 
+// The key of len tokens from t0 on of request b's row j, every one by the rules. By a warp; out of line: a unit comes
+// here when several of its best tokens have turned out to be lowered (most of the vocabulary is banned, say).
+template <typename T>
+__device__ __noinline__ unsigned long long work_out_all(const RulesParams& p, int b, int j, int t0, int len, bool& nan) {
+  const int lane = threadIdx.x & 31;
+  const T* z = static_cast<const T*>(p.logits) + (static_cast<long long>(b) * p.R + j) * p.V + t0;
+  const uint32_t* marks = p.marks + static_cast<long long>(b) * p.words + t0 / 32;
+  const uint32_t* allow = p.allow ? p.allow + b * p.allow_batch + j * p.allow_row + t0 / 32 : nullptr;
+  const asd_token_record* records = p.records + static_cast<long long>(b) * p.V + t0;
+  const Penalties penalties(p, b);
+  const int mine = lane < j ? __ldcg(p.draft + static_cast<long long>(b) * p.K + lane) - t0 : -1;
+  const unsigned said = __ballot_sync(kFull, mine >= 0 && mine < len);
+  unsigned long long key = 0ull;
+  bool bad = false;
+  constexpr int kAtOnce = 4;
+#pragma unroll 1
+  for (int w0 = 0; 32 * w0 < len; w0 += kAtOnce) {  // a word of bits, a token a lane
+    float x[kAtOnce];
+    uint32_t mark[kAtOnce], may[kAtOnce];
+    uint2 record[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int at = 32 * (w0 + k) + lane;
+      x[k] = -INFINITY, mark[k] = 0u, may[k] = 0u, record[k] = make_uint2(0u, 0u);
+      if (at >= len) continue;
+      x[k] = Elem<T>::load_cg(z, at);
+      mark[k] = __ldcg(marks + w0 + k);
+      may[k] = allow ? __ldcg(allow + w0 + k) : kFull;
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if ((mark[k] >> lane) & 1u) record[k] = *reinterpret_cast<const uint2*>(records + 32 * (w0 + k) + lane);
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int at = 32 * (w0 + k) + lane;
+      const uint32_t times = (record[k].x & kTimes) + __popc(drafts_equal(at, mine, said));
+      if (at >= len) continue;
+      float value = changed_logit(p, penalties, x[k], times, (mark[k] >> lane) & 1u, record[k]);
+      if (!((may[k] >> lane) & 1u)) value = -INFINITY;
+      bad = bad || value != value;
+      const unsigned long long other = make_key(value, static_cast<uint32_t>(t0 + at));
+      if (value == value && other > key) key = other;
+    }
+  }
+  nan = __any_sync(kFull, bad);
+  return warp_max_key(key);
+}
+
 // kU: vectors a lane has of a unit, all in flight at once.
 template <typename T, int kU>
 __global__ void __launch_bounds__(kThreads, kMinBlocks)
@@ -442,7 +490,10 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks)
     if (at_loose >= 0 && !((words[at_loose >> 5] >> (at_loose & 31)) & 1u)) loose = -INFINITY;
   }
 
-  // the unit's best token, until it is one without rules or not better than those worked out
+  // The unit's best token, until it is one without rules or not better than those worked out; all together where several
+  // have to be.
+  constexpr int kOneByOne = 3;
+  int worked = 0;
   unsigned long long key = 0ull;
   bool nan = false;
   for (bool again = false;; again = true) {
@@ -484,8 +535,12 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks)
       break;
     }
     const Penalties penalties(p, b);
-    const uint2 record = marked ? *reinterpret_cast<const uint2*>(p.records + static_cast<long long>(b) * p.V + t0 + at)
-                                : make_uint2(0u, 0u);
+    const asd_token_record* records = p.records + static_cast<long long>(b) * p.V + t0;
+    if (worked++ == kOneByOne) {
+      key = work_out_all<T>(p, b, j, t0, r.len, nan);
+      break;
+    }
+    const uint2 record = marked ? *reinterpret_cast<const uint2*>(records + at) : make_uint2(0u, 0u);
     const float value = changed_logit(p, penalties, ordered_value(top), (record.x & kTimes) + equal, marked, record);
     if (value == value) {
       const unsigned long long changed = make_key(value, static_cast<uint32_t>(t0 + at));

@@ -158,6 +158,24 @@ def test_kinds_of_rules(asd, dtype, case):
     check_logits(asd, p, in_place=True)
 
 
+@pytest.mark.parametrize("dtype", (BF16, F32), ids=("bf16", "f32"))
+@pytest.mark.parametrize("V,off", ((5000, 0), (3001, 3), (700, 0)))
+@pytest.mark.parametrize("grammar", (None, "third"))
+def test_most_of_the_vocabulary_is_lowered(asd, dtype, V, off, grammar):
+    """Bans and large penalties on nearly every token: the best one that is left may be far down."""
+    p = Problem(dtype, 4, 5, V, said=3 * V, biased=0, grammar=grammar, seed=V)
+    p.repetition, p.frequency, p.presence = p.repetition.clamp(min=1.0), p.frequency.abs() + 3, p.presence + 9
+    p.marked = torch.rand(4, V, generator=torch.Generator().manual_seed(3)) < torch.tensor([0.97, 0.5, 1.0, 1.0])[:, None]
+    p.seen[2:] = torch.where(p.seen[2:] == 0, torch.tensor(1, dtype=torch.int32), p.seen[2:])
+    p.bias[0] = -80.0
+    p.bias[3] = -math.inf
+    p.z[1, 2, 20:40] = math.inf  # infinite logits, some lowered, some not
+    if p.allow is not None:
+        p.allow[1, 2, 20:40] = True
+    check_verify(asd, p, off=off)
+    check_verify(asd, p, off=off, strict=True)
+
+
 def test_strict_equals_zero_budget(asd):
     p = Problem(BF16, 4, 8, 5000, seed=8)
     strict = asd.rules_verify(p.logits(), p.draft.cuda(), None, 1.0, 2, p.rules(asd), allow=p.mask())
