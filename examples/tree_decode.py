@@ -6,7 +6,11 @@ lets every node see the context and its own ancestors); strict verification of a
 the ledger's verification of that path accepts a prefix; kv_compact moves the accepted nodes' keys and values next to
 the context; commit appends the emitted tokens and advances the cache's length.
 
-    python examples/tree_decode.py [--dtype bf16|f32] [--budget 2.0] [--rounds 24]
+With a presence penalty the verification runs under rules (rules_verify), which tokens_record keeps up to date. With a
+limit on the cache, kv_weigh adds up what every cached slot is worth to the accepted path's attention, and kv_evict cuts
+each request back to its limit after every round.
+
+    python examples/tree_decode.py [--dtype bf16|f32] [--budget 2.0] [--rounds 24] [--presence 1.5] [--keep 48]
 """
 from __future__ import annotations
 
@@ -54,16 +58,21 @@ class Decoder:
         table = torch.randperm(B * width).to(torch.int32).view(B, width).to(k.device)  # pages lie anywhere
         return asd.KVCache(k, torch.zeros_like(k), table)
 
-    def forward(self, tokens, cache, kv_len, workspace, status, positions=None, mask=None, new_len=None):
-        """tokens [B, T] -> final hidden rows [B, T, H]; the tokens' keys and values enter the cache."""
+    def forward(self, tokens, cache, kv_len, workspace, status, positions=None, mask=None, new_len=None, kept=None):
+        """tokens [B, T] -> final hidden rows [B, T, H]; the tokens' keys and values enter the cache.
+
+        ``kept``: a list that gets each layer's queries and log-sum-exps, for kv_weigh."""
         B, T = tokens.shape
         x = self.embed[tokens.long()]
         for i in range(self.layers):
             q, k, v = (rms(x) @ self.qkv[i].T).view(B, T, -1, self.D).split((self.q_heads, self.heads, self.heads), 2)
             q = asd.kv_append(k, v, cache, kv_len, layer=i, q=q, positions=positions, new_len=new_len, cos=self.cos,
                               sin=self.sin, q_norm=self.q_norm[i], k_norm=self.k_norm[i], status=status)
-            a = asd.tree_attention(q, cache, kv_len, layer=i, tree_mask=mask, new_len=new_len, workspace=workspace,
-                                   status=status)["out"]
+            o = asd.tree_attention(q, cache, kv_len, layer=i, tree_mask=mask, new_len=new_len, workspace=workspace,
+                                   status=status)
+            if kept is not None:
+                kept.append((q, o["lse"]))
+            a = o["out"]
             x = x + a.view(B, T, -1) @ self.out[i].T
             x = x + torch.relu(rms(x) @ self.up[i].T) @ self.down[i].T
         return rms(x)
@@ -111,8 +120,11 @@ def draft(model: Decoder, tree: Tree, pending: torch.Tensor) -> torch.Tensor:
 
 
 def decode(model: Decoder, prompts: list, rounds: int, budget: float = 0.0, gate: float = 1.0, cap: int = 2,
-           tree: Tree | None = None):
-    """-> the emitted tokens of every request (a list of lists), accepted drafts per round (a float)."""
+           tree: Tree | None = None, presence: float | None = None, keep: int | None = None, lengths_seen=None):
+    """-> the emitted tokens of every request (a list of lists), accepted drafts per round (a float).
+
+    ``presence``: a penalty on tokens that a request has emitted. ``keep``: slots of the cache that a request keeps after
+    a round, the newest K + 1 always. ``lengths_seen``: a list that gets the cache's lengths after every round."""
     tree = tree or Tree()
     dev = model.embed.device
     B, T, K = len(prompts), len(tree.parents), tree.depth
@@ -125,6 +137,18 @@ def decode(model: Decoder, prompts: list, rounds: int, budget: float = 0.0, gate
     ledger = asd.make_ledger(B, budget, device=dev)
     history = torch.zeros(B, rounds * (K + 1), dtype=torch.int32, device=dev)
     emitted = torch.zeros(B, dtype=torch.int32, device=dev)
+    rules = None
+    if presence is not None:
+        rules = asd.TokenRules.empty(B, model.V, presence=torch.full((B,), presence, device=dev), device=dev)
+    weight, kept = None, None
+    if keep is not None:  # what every slot of every layer's heads is worth; how many each request keeps
+        slots = cache.table_width * cache.page_size
+        weight = torch.zeros(model.layers, B, model.heads, slots, device=dev)
+        limit = torch.full((B,), keep, dtype=torch.int32, device=dev)
+
+    def weigh(before, **rows):
+        for i, (q, lse) in enumerate(kept):
+            asd.kv_weigh(q, lse, cache, before, weight[i], layer=i, status=status, **rows)
 
     # the prompts, all but their last token, which is the first round's pending one
     if longest > 1:
@@ -132,8 +156,12 @@ def decode(model: Decoder, prompts: list, rounds: int, budget: float = 0.0, gate
         for b, p in enumerate(prompts):
             padded[b, :len(p) - 1] = torch.tensor(p[:-1], dtype=torch.int32)
         new = (lengths - 1).to(dev)
-        model.forward(padded.to(dev), cache, kv_len, workspace, status, new_len=new)
+        kept = None if weight is None else []
+        model.forward(padded.to(dev), cache, kv_len, workspace, status, new_len=new, kept=kept)
+        if weight is not None:
+            weigh(kv_len, new_len=new)
         kv_len += new
+    seen = kv_len.clone()  # tokens behind each request, which an evicted cache no longer counts
     pending = torch.tensor([p[-1] for p in prompts], dtype=torch.int32, device=dev)
 
     mask = asd.tree_mask(torch.tensor([tree.parents] * B, dtype=torch.int32, device=dev))
@@ -142,14 +170,32 @@ def decode(model: Decoder, prompts: list, rounds: int, budget: float = 0.0, gate
     drafts = 0
     for _ in range(rounds):
         tokens = draft(model, tree, pending)
-        z = model.logits(model.forward(tokens, cache, kv_len, workspace, status, positions=kv_len[:, None] + levels,
-                                       mask=mask))
-        exact = asd.verify_strict(z[:, paths].flatten(0, 1), tokens[:, paths[:, 1:]].flatten(0, 1).contiguous())
-        path = paths[exact["accepted_len"].view(B, -1).argmax(1)]  # [B, K + 1]
+        kept = None if weight is None else []
+        z = model.logits(model.forward(tokens, cache, kv_len, workspace, status, positions=seen[:, None] + levels,
+                                       mask=mask, kept=kept))
+        if rules is None:
+            exact = asd.verify_strict(z[:, paths].flatten(0, 1), tokens[:, paths[:, 1:]].flatten(0, 1).contiguous())
+            best = exact["accepted_len"].view(B, -1)
+        else:  # every path by itself: its rows know its own drafts
+            best = torch.stack([asd.rules_verify(z[:, p].contiguous(), tokens[:, p[1:]].contiguous(), None, gate, cap,
+                                                 rules)["accepted_len"] for p in paths], 1)
+        path = paths[best.argmax(1)]  # [B, K + 1]
         rows = z.gather(1, path[:, :, None].expand(-1, -1, model.V))
-        got = asd.verify(rows, tokens.gather(1, path[:, 1:]), ledger, gate, cap)
-        asd.kv_compact(cache, kv_len, path.int(), got["accepted_len"] + 1, status=status)
+        block = tokens.gather(1, path[:, 1:])
+        got = asd.verify(rows, block, ledger, gate, cap) if rules is None else \
+            asd.rules_verify(rows, block, ledger, gate, cap, rules)
+        if rules is not None:
+            asd.tokens_record(got["committed"], rules, status=status)
+        on = got["accepted_len"] + 1
+        asd.kv_compact(cache, kv_len, path.int(), on, status=status)
+        if weight is not None:
+            weigh(kv_len, path=path.int(), new_len=on)
+        seen += on
         asd.commit(got["accepted_len"], got["committed"], kv_len=kv_len, tokens=history, token_len=emitted)
+        if weight is not None:
+            kv_len = asd.kv_evict(cache, kv_len, weight, limit, first=1, last=K + 1, status=status)
+        if lengths_seen is not None:
+            lengths_seen.append(kv_len.tolist())
         pending = got["recovery"]
         drafts += int(got["accepted_len"].sum())
     if workspace.error() or bool(status.any()):
@@ -163,11 +209,13 @@ def main() -> None:
     a.add_argument("--dtype", choices=("bf16", "f32"), default="bf16")
     a.add_argument("--budget", type=float, default=2.0)
     a.add_argument("--rounds", type=int, default=24)
+    a.add_argument("--presence", type=float)
+    a.add_argument("--keep", type=int)
     a = a.parse_args()
     model = Decoder(torch.bfloat16 if a.dtype == "bf16" else torch.float32)
     prompts = [[1, 2, 3, 4, 5], [7], [11, 13, 17, 19, 23, 29, 31, 37, 41]]
     for budget in (0.0, a.budget):
-        out, rate = decode(model, prompts, a.rounds, budget=budget)
+        out, rate = decode(model, prompts, a.rounds, budget=budget, presence=a.presence, keep=a.keep)
         print(f"budget {budget}: {rate:.2f} drafts accepted a round, {sum(map(len, out))} tokens in {a.rounds} rounds")
         for tokens in out:
             print("  ", tokens[:16])
