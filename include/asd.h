@@ -531,14 +531,13 @@ typedef struct {
   const int32_t* new_len;  /* [B] (0..rows), or NULL: rows */
   const int32_t* path;     /* [B, rows] or NULL: row i is token i, and rows = T */
   int32_t* status;         /* as in asd_append */
+  double scale;            /* |scale| <= 2e38; a rounding of it would be in every weight */
+  float decay;             /* finite, >= 0 */
   int layer;
   int T;                   /* tokens of q and lse */
   int rows;                /* rows of a request, >= 0 */
   int q_heads;
   int width;               /* slots that a head's weights have room for, >= kv_len + new_len of every request */
-  float scale;             /* finite */
-  float decay;             /* finite, >= 0 */
-  int reserved;            /* 0 */
 } asd_weigh;
 int asd_kv_weigh(const asd_kv_cache* cache, const asd_weigh* args, asd_stream_t stream);
 
@@ -559,7 +558,8 @@ int asd_kv_weigh(const asd_kv_cache* cache, const asd_weigh* args, asd_stream_t 
  *
  * weight        [layers, B, heads, width]; weight_out the same or weight itself. Slots
  *               of weight_out from n on are left as they were.
- * kv_len_out    [B] = n; not kv_len itself (every head reads that while the call runs)
+ * kv_len_out    [B] = n; neither kv_len nor keep itself (every head reads them while the
+ *               call runs)
  * keep          [B] >= 0
  * status        ASD_STATUS_LENGTH (kv_len < 0 or past the table or the width, keep <
  *               0): such a request moves nothing and keeps its length.

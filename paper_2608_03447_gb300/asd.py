@@ -209,6 +209,15 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _stream_at(stream, index: int) -> int:
+    """The handle of a call's stream. Kernels run on the current device: tensors of another one are refused."""
+    if stream is not None:
+        return _stream(stream)
+    if torch.cuda.current_device() != index:
+        raise ValueError(f"the call's tensors are on cuda:{index}, the current device is cuda:{torch.cuda.current_device()}")
+    return _stream(None)
+
+
 def _torch_on(stream):
     """A context in which torch allocates and launches on a call's stream, as the call's own kernels do.
 
@@ -812,7 +821,7 @@ def kv_compact(cache: KVCache, kv_len: torch.Tensor, path: torch.Tensor, path_le
 
 
 # asd_weigh and asd_evict as they lie in memory
-_WEIGH = struct.Struct("2P 3q 2P 3P P 5i 2f i")
+_WEIGH = struct.Struct("2P 3q 2P 3P P d f 5i")
 _EVICT = struct.Struct("6P 4i")
 
 
@@ -845,9 +854,9 @@ def kv_weigh(q: torch.Tensor, lse: torch.Tensor, cache: KVCache, kv_len: torch.T
         _check_vector("out", out, cache, shape, torch.float32), _check_vector("kv_len", kv_len, cache, (B,)),
         0 if new_len is None else _check_vector("new_len", new_len, cache, (B,)),
         0 if path is None else _check_vector("path", path, cache, (B, rows)),
-        0 if status is None else _check_vector("status", status, cache, (B,)), layer, T, rows, q_heads, width,
-        D ** -0.5 if scale is None else scale, decay, 0)
-    rc = load().asd_kv_weigh(cache._ref, args, _stream(stream))
+        0 if status is None else _check_vector("status", status, cache, (B,)), D ** -0.5 if scale is None else scale,
+        decay, layer, T, rows, q_heads, width)
+    rc = load().asd_kv_weigh(cache._ref, args, _stream_at(stream, cache.index))
     if rc:
         raise AsdError("asd_kv_weigh", rc)
     return out
@@ -876,7 +885,7 @@ def kv_evict(cache: KVCache, kv_len: torch.Tensor, weight: torch.Tensor, keep: t
                        _check_vector("kv_len", kv_len, cache, one), _check_vector("new_len", new_len, cache, one),
                        _check_vector("keep", keep, cache, one),
                        0 if status is None else _check_vector("status", status, cache, one), first, last, shape[-1], 0)
-    rc = load().asd_kv_evict(cache._ref, args, _stream(stream))
+    rc = load().asd_kv_evict(cache._ref, args, _stream_at(stream, cache.index))
     if rc:
         raise AsdError("asd_kv_evict", rc)
     return new_len
@@ -974,7 +983,7 @@ def rules_verify(logits: torch.Tensor, draft: torch.Tensor, ledger: torch.Tensor
         logits.data_ptr(), xp, lp, o["accepted_len"].data_ptr(), o["committed"].data_ptr(), o["recovery"].data_ptr(),
         0 if argmax is None else argmax.data_ptr(), 0 if regret is None else regret.data_ptr(),
         0 if status is None else status.data_ptr(), ws.buffer.data_ptr(), ws.nbytes, code, K, gate, cap)
-    rc = load().asd_rules_verify(packed, block, _stream(stream))
+    rc = load().asd_rules_verify(packed, block, _stream_at(stream, index))
     if rc:
         raise AsdError("asd_rules_verify", rc)
     return o
@@ -998,7 +1007,7 @@ def rules_logits(logits: torch.Tensor, draft: torch.Tensor | None, rules: TokenR
         with _torch_on(stream):
             out = torch.empty(shape, dtype=logits.dtype, device=logits.device)
     rc = load().asd_rules_logits(packed, zp, code, rows, xp, _check_rules(rules, "out", out, shape, logits.dtype),
-                                 _stream(stream))
+                                 _stream_at(stream, rules.index))
     if rc:
         raise AsdError("asd_rules_logits", rc)
     return out
@@ -1016,7 +1025,7 @@ def tokens_record(tokens: torch.Tensor, rules: TokenRules, prompt: bool = False,
                                   None if token_len is None else _check_rules(rules, "token_len", token_len, one),
                                   int(bool(prompt)),
                                   None if status is None else _check_rules(rules, "status", status, one),
-                                  _stream(stream))
+                                  _stream_at(stream, rules.index))
     if rc:
         raise AsdError("asd_tokens_record", rc)
 
@@ -1030,6 +1039,6 @@ def tokens_bias(ids: torch.Tensor, bias: torch.Tensor, rules: TokenRules, length
                                 _check_rules(rules, "bias", bias, (rules.B, n), torch.float32), n,
                                 None if length is None else _check_rules(rules, "length", length, one),
                                 None if status is None else _check_rules(rules, "status", status, one),
-                                _stream(stream))
+                                _stream_at(stream, rules.index))
     if rc:
         raise AsdError("asd_tokens_bias", rc)

@@ -440,7 +440,7 @@ extern "C" int asd_kv_evict(const asd_kv_cache* cache, const asd_evict* args, as
   if (a.first < 0 || a.last < 0 || a.width < 0 || a.width > ASD_MAX_EVICT_SLOTS || a.reserved != 0) return ASD_ERR_SHAPE;
   if (cache->B == 0) return ASD_OK;
   if (!a.kv_len || !a.kv_len_out || !a.keep || (a.width > 0 && (!a.weight || !a.weight_out))) return ASD_ERR_NULL;
-  if (a.kv_len == a.kv_len_out) return ASD_ERR_SHAPE;
+  if (a.kv_len_out == a.kv_len || a.kv_len_out == a.keep) return ASD_ERR_SHAPE;
   const void* const words[] = {a.weight, a.weight_out, a.kv_len, a.kv_len_out, a.keep, a.status};
   for (const void* x : words)
     if (reinterpret_cast<uintptr_t>(x) % 4 != 0) return ASD_ERR_ALIGN;

@@ -199,7 +199,10 @@ __global__ void __launch_bounds__(kSimtThreads, 2)
           const int see = masked ? ctx - slot0 + a.by_group.quot(tile * kRows + y + 16 * i) : kSimtTile;
 #pragma unroll
           for (int c = 0; c < 4; ++c)
-            if (x + 16 * c <= see) sum[c] = fmaf(exp2_fast(fmaf(s[i][c].x + s[i][c].y, a.scale_log2, -scale.x)), scale.y, sum[c]);
+            if (x + 16 * c <= see) {
+              const float z = s[i][c].x + s[i][c].y;
+              sum[c] = fmaf(exp2_fast(fmaf(z, a.scale_log2, fmaf(z, p.scale_rest, -scale.x))), scale.y, sum[c]);
+            }
         }
       }
 #pragma unroll
@@ -267,7 +270,7 @@ int check_weigh(const asd_kv_cache* cache, const asd_weigh& a) {
   const int rc = check_cache(cache);
   if (rc != ASD_OK) return rc;
   if (a.layer < 0 || a.layer >= cache->layers || a.T < 0 || a.rows < 0 || a.q_heads < 1 ||
-      a.q_heads % cache->heads != 0 || a.width < 0 || a.reserved != 0 || (!a.path && a.rows != a.T))
+      a.q_heads % cache->heads != 0 || a.width < 0 || (!a.path && a.rows != a.T))
     return ASD_ERR_SHAPE;
   // rows and tiles are counted in 32 bits
   const long long group = a.q_heads / cache->heads;
@@ -286,7 +289,8 @@ extern "C" int asd_kv_weigh(const asd_kv_cache* cache, const asd_weigh* args, as
   const asd_weigh& a = *args;
   const int rc = check_weigh(cache, a);
   if (rc != ASD_OK) return rc;
-  const float scale_log2 = a.scale * 1.4426950408889634f;
+  const double scale = a.scale * 1.4426950408889634;
+  const float scale_log2 = static_cast<float>(scale);
   if (!(scale_log2 - scale_log2 == 0.0f) || !(a.decay - a.decay == 0.0f) || a.decay < 0.0f) return ASD_ERR_CONTROL;
   if (cache->B == 0 || a.rows == 0) return ASD_OK;
   if (!a.q || !a.lse || !a.kv_len || !a.weight_out || (!a.weight && a.decay != 0.0f)) return ASD_ERR_NULL;
@@ -323,8 +327,7 @@ extern "C" int asd_kv_weigh(const asd_kv_cache* cache, const asd_weigh* args, as
   p.tokens = a.T;
   p.width = a.width;
   p.decay = a.decay;
-  if (scale_log2 != 0.0f)
-    p.scale_lost = static_cast<float>(static_cast<double>(a.scale) * 1.4426950408889634 / scale_log2 - 1.0);
+  p.scale_rest = static_cast<float>(scale - scale_log2);
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (weigh_tc_takes(cache, p)) return launch_weigh_tc(cache, p, s);
   if (cache->dtype == ASD_F32) return launch_rows<float>(p, s);

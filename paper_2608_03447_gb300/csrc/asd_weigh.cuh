@@ -20,7 +20,7 @@ struct WeighParams {
   int tokens;  // of q and lse
   int width;
   float decay;
-  float scale_lost;  // what a.scale_log2 is short of scale * log2(e), relatively
+  float scale_rest;  // what a.scale_log2 is short of scale * log2(e)
 };
 
 // No kernel of this entry point has a workspace: its error word for the deal, always 0.
@@ -42,9 +42,9 @@ __device__ __forceinline__ int weigh_token(const WeighParams& p, int b, int row)
 }
 
 // What a row's exponentials are taken with: exp(z - lse) = exp2(z' - x) * y with z' in
-// log2 units, x the rounded lse and y what that rounding lost, and the scale's for a
-// score as large as the lse (near 1; 0: the row adds nothing). Without y both would
-// be in every weight of the row alike, up to 2^-20 where the lse is 16.
+// log2 units, x the rounded lse and y what that rounding lost (near 1; 0: the row adds
+// nothing). Without y it would be in every weight of the row alike, up to 2^-20 where
+// the lse is 16; likewise the scale has two parts.
 struct RowScale {
   float x, y;
 };
@@ -55,7 +55,7 @@ __device__ __forceinline__ RowScale row_scale(const WeighParams& p, int b, int t
   if (fabsf(lse) == INFINITY) return r;
   const float lost = fmaf(lse, 1.4426950408889634f, -(lse * 1.4426950408889634f)) + lse * 1.9259629911266175e-8f;
   r.x = lse * 1.4426950408889634f;
-  r.y = exp2f(fmaf(p.scale_lost, r.x, -lost));
+  r.y = exp2f(-lost);
   return r;
 }
 

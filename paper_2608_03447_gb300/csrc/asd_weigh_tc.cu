@@ -160,15 +160,16 @@ __device__ __forceinline__ void tmem_take(uint32_t taddr, float (&r)[16]) {
 
 // exp2(scale z - offset) factor summed over kN columns of this thread's lane, even and odd ones apart.
 template <int kN>
-__device__ __forceinline__ float2 sum_columns(uint32_t from, const float* factor, float scale_log2, float offset) {
-  const float2 by = {scale_log2, scale_log2}, less = {-offset, -offset};
+__device__ __forceinline__ float2 sum_columns(uint32_t from, const float* factor, float2 scale, float offset) {
+  const float2 by = {scale.x, scale.x}, rest = {scale.y, scale.y}, less = {-offset, -offset};
   float z[kN];
   tmem_take(from, z);
   float2 sum[2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
 #pragma unroll
   for (int k = 0; k < kN; k += 4) {
     const float4 f = *reinterpret_cast<const float4*>(factor + k);
-    const float2 t0 = fma2(make_float2(z[k], z[k + 1]), by, less), t1 = fma2(make_float2(z[k + 2], z[k + 3]), by, less);
+    const float2 z0 = {z[k], z[k + 1]}, z1 = {z[k + 2], z[k + 3]};
+    const float2 t0 = fma2(z0, by, fma2(z0, rest, less)), t1 = fma2(z1, by, fma2(z1, rest, less));
     sum[0] = fma2(make_float2(exp2_fast(t0.x), exp2_fast(t0.y)), make_float2(f.x, f.y), sum[0]);
     sum[1] = fma2(make_float2(exp2_fast(t1.x), exp2_fast(t1.y)), make_float2(f.z, f.w), sum[1]);
   }
@@ -176,7 +177,7 @@ __device__ __forceinline__ float2 sum_columns(uint32_t from, const float* factor
 }
 // The same row by row, for any sums and any products: neither a row that adds nothing
 // nor one before `first` counts, whatever its product is.
-__device__ __noinline__ float sum_carefully(uint32_t from, int cols, const RowScale* scale, float scale_log2, int first) {
+__device__ __noinline__ float sum_carefully(uint32_t from, int cols, const RowScale* rows, float2 scale, int first) {
   float sum = 0.0f;
 #pragma unroll 1
   for (int c = 0; c < cols; c += 16) {
@@ -184,8 +185,8 @@ __device__ __noinline__ float sum_carefully(uint32_t from, int cols, const RowSc
     tmem_take(from + c, z);
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
-      const RowScale s = scale[c + k];
-      const float e = exp2_fast(fmaf(z[k], scale_log2, -s.x));
+      const RowScale s = rows[c + k];
+      const float e = exp2_fast(fmaf(z[k], scale.x, fmaf(z[k], scale.y, -s.x)));
       if (s.y != 0.0f && c + k >= first) sum = fmaf(e, s.y, sum);
     }
   }
@@ -466,6 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     UnitFeed feed;
     Ring<kQueries> queries;
+    const float2 scale = {p.a.scale_log2, p.scale_rest};
     uint32_t full = 0;  // the parity to wait for
     int turn = 0;
     bool ok = true;
@@ -505,8 +507,8 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int c = 0; c < u.cols && !careful; c += kChunk) {
                 const float* factor = sh.factor[slab.at] + c;
                 const float offset = sh.offset[slab.at][c / kChunk];
-                const float2 some = u.cols - c >= kChunk ? sum_columns<kChunk>(from + c, factor, p.a.scale_log2, offset)
-                                                         : sum_columns<16>(from + c, factor, p.a.scale_log2, offset);
+                const float2 some = u.cols - c >= kChunk ? sum_columns<kChunk>(from + c, factor, scale, offset)
+                                                         : sum_columns<16>(from + c, factor, scale, offset);
                 add += some.x + some.y;
               }
               // a key that is not finite makes the product with a row that adds nothing NaN too
@@ -514,7 +516,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (careful) {
                 // the slab's first row that sees the slot
                 const int first = slot > u.ctx ? min((slot - u.ctx) * p.a.group - tile * u.cols, kCols) : 0;
-                add = sum_carefully(from, u.cols, sh.scale[slab.at], p.a.scale_log2, first);
+                add = sum_carefully(from, u.cols, sh.scale[slab.at], scale, first);
               }
               sum += add;
               tc_fence_before();

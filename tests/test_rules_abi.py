@@ -104,15 +104,15 @@ def test_bad_token_arguments(lib):
 
 def weigh(lib, c, **kw):
     a = dict(q=0x1000, lse=0x2000, s0=768, s1=256, s2=64, w=0x3000, out=0x3000, kv_len=0x4000, new_len=0, path=0,
-             status=0, layer=0, T=3, rows=3, q_heads=4, width=32, scale=0.1, decay=1.0, reserved=0)
+             status=0, scale=0.1, decay=1.0, layer=0, T=3, rows=3, q_heads=4, width=32)
     a.update(kw)
     return lib.asd_kv_weigh(None if c is None else ctypes.addressof(c), asd._WEIGH.pack(*a.values()), None)
 
 
 BAD_WEIGH = [(dict(layer=-1), SHAPE), (dict(layer=2), SHAPE), (dict(T=-1, rows=-1), SHAPE), (dict(rows=4), SHAPE),
              (dict(rows=-1, path=0x5000), SHAPE), (dict(q_heads=0), SHAPE), (dict(q_heads=3), SHAPE),
-             (dict(width=-1), SHAPE), (dict(reserved=1), SHAPE), (dict(T=2 ** 28, rows=2 ** 28), SHAPE),
-             (dict(scale=math.inf), CONTROL), (dict(scale=math.nan), CONTROL), (dict(decay=-0.5), CONTROL),
+             (dict(width=-1), SHAPE), (dict(T=2 ** 28, rows=2 ** 28), SHAPE),
+             (dict(scale=math.inf), CONTROL), (dict(scale=math.nan), CONTROL), (dict(scale=3e38), CONTROL), (dict(decay=-0.5), CONTROL),
              (dict(decay=math.inf), CONTROL), (dict(decay=math.nan), CONTROL), (dict(q=0), NULL), (dict(lse=0), NULL),
              (dict(w=0), NULL), (dict(out=0), NULL), (dict(kv_len=0), NULL), (dict(q=0x1001), ALIGN),
              (dict(lse=0x2002), ALIGN), (dict(w=0x3001), ALIGN), (dict(out=0x3002), ALIGN), (dict(kv_len=0x4001), ALIGN),
@@ -138,7 +138,7 @@ def evict(lib, c, **kw):
 
 
 BAD_EVICT = [(dict(first=-1), SHAPE), (dict(last=-1), SHAPE), (dict(width=-1), SHAPE),
-             (dict(width=asd.MAX_EVICT_SLOTS + 1), SHAPE), (dict(reserved=1), SHAPE), (dict(new=0x2000), SHAPE),
+             (dict(width=asd.MAX_EVICT_SLOTS + 1), SHAPE), (dict(reserved=1), SHAPE), (dict(new=0x2000), SHAPE), (dict(new=0x4000), SHAPE),
              (dict(w=0), NULL), (dict(out=0), NULL), (dict(kv_len=0), NULL), (dict(new=0), NULL), (dict(keep=0), NULL),
              (dict(w=0x1001), ALIGN), (dict(out=0x1002), ALIGN), (dict(kv_len=0x2001), ALIGN), (dict(new=0x3002), ALIGN),
              (dict(keep=0x4001), ALIGN), (dict(status=0x5002), ALIGN)]
@@ -268,3 +268,20 @@ def test_rules_need_tensors_alike():
     for args in ((m, rec[:, :, :1]), (m[:, :3], rec), (m.float(), rec), (m, rec.float()), (m, rec)):  # the last: on the CPU
         with pytest.raises(ValueError):
             asd.TokenRules(*args)
+
+
+def test_tensors_of_another_device_are_refused(fake, monkeypatch):
+    """Without a stream of their own, calls run on the current device."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    r, c, z, q = host_rules(), host_cache(), torch.ones(2, 4, 100), torch.ones(2, 3, 4, 8)
+    ws = types.SimpleNamespace(buffer=torch.ones(8), nbytes=1 << 20)
+    out = {n: i32(2, 4) for n in ("accepted_len", "committed", "recovery")}
+    calls = [lambda: asd.rules_verify(z, i32(2, 3), None, 1.0, 2, r, workspace=ws, out=out),
+             lambda: asd.rules_logits(z, None, r, out=z), lambda: asd.tokens_record(i32(2, 5), r),
+             lambda: asd.tokens_bias(i32(2, 5), torch.ones(2, 5), r),
+             lambda: asd.kv_weigh(q, torch.ones(2, 3, 4), c, i32(2), torch.ones(2, 2, 30)),
+             lambda: asd.kv_evict(c, i32(2), torch.ones(2, 2, 30), i32(2), new_len=i32(2))]
+    for call in calls:
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    assert fake.calls == []

@@ -251,9 +251,10 @@ def test_without_drafts_rows_see_the_text_only(asd):
 
 # ---------------------------------------------------------------- token records
 
-def test_tokens_record(asd):
-    B, n, V = 5, 300, 1001
-    g = torch.Generator().manual_seed(1)
+@pytest.mark.parametrize("n,V", ((300, 1001), (2048, 1001), (4097, 40000), (9000, 64)))
+def test_tokens_record(asd, n, V):
+    B = 5
+    g = torch.Generator().manual_seed(n)
     rules = asd.TokenRules.empty(B, V)
     seen = torch.zeros(B, V, dtype=torch.int32)
     for call in range(3):
@@ -270,6 +271,23 @@ def test_tokens_record(asd):
     rules.clear(3)
     assert int(rules.records[3].count_nonzero()) == 0 and int(rules.marks[3].count_nonzero()) == 0
     assert torch.equal(rules.records[4, :, 0].cpu(), seen[4])
+
+
+@pytest.mark.parametrize("n", (7, 5000))
+def test_tokens_record_skips_what_is_out_of_range(asd, n):
+    rules = asd.TokenRules.empty(3, 100)
+    tokens = torch.arange(3 * n).view(3, n).to(torch.int32) % 130 - 10
+    status = torch.zeros(3, dtype=torch.int32, device="cuda")
+    length = torch.tensor([n, n + 1, n - 3], dtype=torch.int32)
+    asd.tokens_record(tokens.cuda(), rules, token_len=length.cuda(), status=status)
+    seen = torch.zeros(3, 100, dtype=torch.int32)
+    want = [0, asd.STATUS_LENGTH, 0]
+    for b in (0, 2):
+        mine = tokens[b, :int(length[b])]
+        want[b] = asd.STATUS_TOKEN if bool((mine >= 100).any()) else 0
+        seen[b] = torch.bincount(mine[(mine >= 0) & (mine < 100)], minlength=100).int()
+    assert status.tolist() == want and torch.equal(rules.records[:, :, 0].cpu(), seen)
+    assert torch.equal(rules.marks.cpu(), ref.words_of(seen != 0))
 
 
 def test_tokens_record_flags(asd):

@@ -88,6 +88,36 @@ def test_weigh(asd, case, decay):
     p.check(p.run(asd))
 
 
+@pytest.mark.parametrize("dtype", (BF16, F16, F32), ids=("bf16", "f16", "f32"))
+@pytest.mark.parametrize("case", [(150, 10, 2, 64, 16, [140, 300]), (150, 10, 2, 64, 5, [140]), (70, 5, 1, 128, 64, [400, 1]),
+                                  (90, 4, 1, 128, 7, [130])], ids=str)
+def test_more_rows_than_stay(asd, dtype, case):
+    """Queries that are read again and again while the keys of several tiles wait."""
+    p = Problem(dtype, *case, seed=13)
+    p.check(p.run(asd))
+
+
+@pytest.mark.parametrize("dtype", (BF16, F32), ids=("bf16", "f32"))
+@pytest.mark.parametrize("spread", (30.0, 60.0, 200.0))
+def test_rows_whose_sums_are_far_apart(asd, dtype, spread):
+    """Weights of 2^-80 beside weights of 2^80: neither loses its bits to the other's scale."""
+    p = Problem(dtype, 20, 4, 1, 64, 16, [200], seed=14, decay=0.0)
+    sign = torch.where(torch.arange(20 * 4) % 3 == 0, 1.0, -0.25).view(20, 4)
+    p.lse += spread * sign
+    p.check(p.run(asd))
+    p.lse = torch.where(sign > 0, p.lse, torch.tensor(math.inf))  # only the small ones
+    p.check(p.run(asd))
+
+
+@pytest.mark.parametrize("dtype", (BF16, F32), ids=("bf16", "f32"))
+@pytest.mark.parametrize("scale", (0.0, -0.07, 0.5, 1e-20))
+def test_any_scale(asd, dtype, scale):
+    p = Problem(dtype, 5, 4, 2, 64, 16, [150, 20], seed=15)
+    p.scale = scale
+    p.lse = p.lse + 40 * abs(scale)
+    p.check(p.run(asd))
+
+
 @pytest.mark.parametrize("dtype", (BF16, F32), ids=("bf16", "f32"))
 @pytest.mark.parametrize("layout", ("tokens", "heads", "loose"))
 def test_layouts_and_strided_queries(asd, dtype, layout):
