@@ -103,18 +103,17 @@ __device__ __forceinline__ uint4 only(const uint4& v, uint32_t keep, __nv_bfloat
                     choose(sign_masks(b, 0x9988u), v.z, kNone), choose(sign_masks(b, 0xbbaau), v.w, kNone));
 }
 
-// The first element of the unit's vectors that equals best; one of them does.
-template <typename T, int kU>
+// VN u + t: element t of v[u] is the first that equals best, one of them does. One lane looks, so it stops at its vector.
+template <typename T, int u, int kU>
 __device__ __forceinline__ int first_of(const uint4 (&v)[kU], float best) {
+  if constexpr (u + 1 < kU) {
+    if (widest(max_of<T>(v[u]), T()) != best) return first_of<T, u + 1>(v, best);
+  }
   int at = 0;
 #pragma unroll
-  for (int u = kU - 1; u >= 0; --u)
-    if (widest(max_of<T>(v[u]), T()) == best) {
-#pragma unroll
-      for (int t = Elem<T>::kVec - 1; t >= 0; --t)
-        if (Elem<T>::lane(v[u], t) == best) at = u * Elem<T>::kVec + t;
-    }
-  return at;
+  for (int t = Elem<T>::kVec - 1; t >= 0; --t)
+    if (Elem<T>::lane(v[u], t) == best) at = t;
+  return Elem<T>::kVec * u + at;
 }
 
 __device__ __forceinline__ float narrow(float v, float) { return v; }
@@ -497,24 +496,24 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks)
   unsigned long long key = 0ull;
   bool nan = false;
   for (bool again = false;; again = true) {
-    uint32_t order = at_loose >= 0 ? ordered_bits(loose) : 0u;
-    const uint32_t loose_order = order;
+    const uint32_t loose_order = at_loose >= 0 ? ordered_bits(loose) : 0u;
+    uint32_t order = 0u;
     float best = 0.0f;
     if (r.nvec > 0) {
       uint32_t m = max_of<T>(v[0]);
 #pragma unroll
       for (int u = 1; u < kU; ++u) m = max_of(m, max_of<T>(v[u]), T());
       best = widest(m, T());
-      order = max(order, ordered_bits(best));
+      order = ordered_bits(best);
     }
     if (!again) {
       nan = __any_sync(kFull, best != best || loose != loose);
       if (nan) break;
     }
-    const uint32_t top = __reduce_max_sync(kFull, order);
+    const uint32_t top = __reduce_max_sync(kFull, max(order, loose_order));
     uint32_t low = 0u;
-    if (r.nvec > 0 && ordered_bits(best) == top) {
-      const int at = first_of<T, kU>(v, best);
+    if (r.nvec > 0 && order == top) {
+      const int at = first_of<T, 0>(v, best);
       low = 0xffffffffu - static_cast<uint32_t>(t0 + r.lead + min(lane + 32 * (at / VN), r.nvec - 1) * VN + at % VN);
     }
     if (at_loose >= 0 && loose_order == top) low = max(low, 0xffffffffu - static_cast<uint32_t>(t0 + at_loose));
