@@ -48,10 +48,12 @@ __device__ __forceinline__ int weigh_token(const WeighParams& p, int b, int row)
 struct RowScale {
   float x, y;
 };
-__device__ __forceinline__ RowScale row_scale(const WeighParams& p, int b, int token, int head) {
+__device__ __forceinline__ float row_lse(const WeighParams& p, int b, int token, int head) {
+  if (token < 0) return INFINITY;
+  return __ldcg(p.lse + (static_cast<long long>(b) * p.tokens + token) * p.a.q_heads + head);
+}
+__device__ __forceinline__ RowScale row_scale(float lse) {
   RowScale r = {0.0f, 0.0f};
-  if (token < 0) return r;
-  const float lse = __ldcg(p.lse + (static_cast<long long>(b) * p.tokens + token) * p.a.q_heads + head);
   if (fabsf(lse) == INFINITY) return r;
   const float lost = fmaf(lse, 1.4426950408889634f, -(lse * 1.4426950408889634f)) + lse * 1.9259629911266175e-8f;
   r.x = lse * 1.4426950408889634f;

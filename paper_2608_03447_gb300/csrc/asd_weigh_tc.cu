@@ -15,6 +15,23 @@
 // warp 17 issues the MMAs, warps 18 and 19 copy queries and the rows' scales.
 // Keys are TMA boxes of as many slots as the page size and the tile have as a common
 // divisor, or 16-byte copies where that is less than the swizzle's eight rows.
+//
+// What bounds it: few rows, memory: 32 paths of up to 9 on 8000 slots, 40 heads on 8 of
+// 128 in bf16, 79 to 81 us (471 MB read, 6.0 TB/s). Many rows, the exponentials (32 a
+// clock and SM) and the issue of the products (some 80 cycles a tcgen05.mma, four a
+// tile and slab at heads of 64): 64 rows of 16 prompts of up to 12000 slots, 32 heads on
+// 4 of 64 in f16, 80 us, of which the 393 million exponentials need 42. One token on
+// 4200 slots takes 6.9 us, a chain of latencies. A prompt of 4093 on itself (40 heads on
+// 8 of 128) takes 321 us: the CTAs that have the first slots meet all 160 slabs of rows
+// one after the other, 2 us each. 775 us with every row's place compared with every slot,
+// 697 where only a slab that crosses a tile's causal edge does that, 321 since slabs that
+// see nothing of a step are neither copied nor multiplied and a row's sum is read while
+// its slab is waited for. What else was measured for the 64 rows:
+// two groups with two accumulators each 113 us; row scales read as pairs, both numbers
+// for every column, 132 us; one part of the scale only 75 us (its rounding was then in
+// every weight); two warps that issue MMAs 79 us against 75, by their registers.
+// Truncation in the tensor cores' sums makes products smaller by about 2^-22: weights
+// are 2 to 5e-7 too small, the largest error against 64 bits.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -128,6 +145,15 @@ struct Ring {
     }
   }
 };
+
+// Where slabs come again for every step of tiles: the first that has a row which sees tile j.
+__device__ __forceinline__ int first_slab(int ctx, int cols, int j, int group) {
+  const int after = j * kTile - ctx;  // the tokens before this one see nothing of it
+  return after <= 0 ? 0 : after * group / cols;
+}
+__device__ __forceinline__ int first_slab(const WeighUnit& u, int j, int group) {
+  return first_slab(u.ctx, u.cols, j, group);
+}
 
 __device__ __forceinline__ float warp_max(float x) {
 #pragma unroll
@@ -354,19 +380,30 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!next) break;
       const WeighUnit u = *next;
       feed.done(sh);
-      const int times = u.tiles > kQueries ? (u.j1 - u.j0 + kStep - 1) / kStep : 1;
-      for (int i = 0; ok && i < times; ++i) {
-        for (int tile = 0; ok && tile < u.tiles; ++tile) {
+      const bool stays = u.tiles <= kQueries;
+      for (int j = u.j0; ok && j < u.j1; j = stays ? u.j1 : j + kStep) {
+        for (int tile = stays ? 0 : first_slab(u, j, p.a.group); ok && tile < u.tiles; ++tile) {
+          // 32 rows at a time, a lane a row: where it lies and its sum are read while the slab is waited for
+          constexpr int kParts = kCols / kQueryThreads;
+          long long offs[kParts];
+          float lse[kParts];
+#pragma unroll
+          for (int n = 0; n < kParts; ++n) {
+            const int at = part * 32 + n * kQueryThreads + lane, row = tile * u.cols + at, t = p.a.by_group.quot(row);
+            const int token = at < u.cols && row < u.rows ? weigh_token(p, u.b, t) : -1;
+            const int head = u.h * p.a.group + row - t * p.a.group;
+            offs[n] = token < 0 ? -1 : u.b * p.a.q_batch + token * p.a.q_token + head * p.a.q_head;
+            lse[n] = row_lse(p, u.b, token, head);
+          }
           ok = warp_wait(&sh.q_empty[ring.at], ring.phase ^ 1u, sh);
           if (!ok) break;
-          // 32 rows at a time, a lane their tokens
-          for (int r0 = part * 32; r0 < u.cols; r0 += 64) {
-            const int r = r0 + lane, row = tile * u.cols + r, t = p.a.by_group.quot(row);
-            const int token = r < u.cols && row < u.rows ? weigh_token(p, u.b, t) : -1;
-            const int head = u.h * p.a.group + row - t * p.a.group;
-            const long long off = token < 0 ? -1 : u.b * p.a.q_batch + token * p.a.q_token + head * p.a.q_head;
+#pragma unroll
+          for (int n = 0; n < kParts; ++n) {
+            const int r0 = part * 32 + n * kQueryThreads, r = r0 + lane;
+            if (r0 >= u.cols) break;
+            const long long off = offs[n];
             // exp2(z - x) y as exp2(z - m) f with one whole m for the chunk: no number but f that differs from row to row
-            const RowScale scale = row_scale(p, u.b, token, head);
+            const RowScale scale = row_scale(lse[n]);
             const float most = warp_max(scale.y == 0.0f ? -INFINITY : scale.x);
             const float least = -warp_max(scale.y == 0.0f ? -INFINITY : -scale.x);
             const float m = most == -INFINITY ? 0.0f : ceilf(most);
@@ -404,9 +441,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     while (ok) {
       const WeighUnit* u = feed.wait(sh);
       if (!u) break;
-      const int tiles = uniform(u->tiles);
-      const uint32_t desc = uniform(instr_desc(kBf16, u->cols, false));
-      int left = uniform(u->j1 - u->j0);
+      const int tiles = uniform(u->tiles), cols = uniform(u->cols), ctx = uniform(u->ctx);
+      const uint32_t desc = instr_desc(kBf16, cols, false);
+      int j = uniform(u->j0), left = uniform(u->j1) - j;
       feed.done(sh);
       const bool stays = tiles <= kQueries;
       bool first = true;  // of the unit's steps
@@ -414,16 +451,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int count = tiles == 1 ? 1 : min(left, kStep);
         const bool ends = left == count;
         const int stage0 = keys.at;
+        const int begin = stays ? 0 : first_slab(ctx, cols, j, p.a.group);
         Ring<kQueries> slab = queries;
 #pragma unroll 1
-        for (int tile = 0; ok && tile < tiles; ++tile) {
+        for (int tile = begin; ok && tile < tiles; ++tile) {
           if (first || !stays) {
             ok = warp_wait(&sh.q_full[slab.at], slab.phase, sh);
             fence_for_mma();  // threads copied them
           }
 #pragma unroll 1
           for (int i = 0; ok && i < count; ++i) {
-            if (tile == 0) {
+            if (tile == begin) {
               ok = warp_wait(&sh.k_full[keys.at], keys.phase, sh);
               if (!kTma) fence_for_mma();
               keys.next();
@@ -457,6 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         turn = (turn + count) & (kGroups - 1);
         first = false;
         left -= count;
+        j += count;
       }
     }
     drain(&sh.drain, elected);
@@ -482,6 +521,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int i = (g - turn) & (kGroups - 1), mine = j + i;
         const bool has = i < count;  // whether this group has one of the tiles
         turn = (turn + count) & (kGroups - 1);
+        const int begin = stays ? 0 : first_slab(u, j, p.a.group);
         j += count;
         const bool ends = j == u.j1;
         if (!has && !ends && stays) continue;
@@ -490,10 +530,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         const long long at = (static_cast<long long>(u.b) * p.a.heads + u.h) * p.width + slot;
         float before = 0.0f;
         if (exists && slot < u.ctx && p.decay != 0.0f) before = __ldcg(p.weight + at);
-        const bool masked = mine * kTile > u.ctx - kTile;  // some slot is not seen by all rows
+        const int slot0 = mine * kTile, last_slot = min(slot0 + (kTile - 1), u.span - 1);
         float sum = 0.0f;
         Ring<kQueries> slab = queries;
-        for (int tile = 0; ok && tile < u.tiles; ++tile) {
+        for (int tile = begin; ok && tile < u.tiles; ++tile) {
           // the rows' scales; and no slab is given back before it is there, by a group without a tile either
           if (has || ends || !stays) ok = warp_wait(&sh.q_full[slab.at], slab.phase, sh);
           if (has) {
@@ -502,9 +542,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (ok) {
               tc_fence_after();
               const uint32_t from = tmem + static_cast<uint32_t>(g * kCols) + lanes;
+              // whether all of the slab's rows see all of the tile, or none sees any of it
+              const int first_row = tile * u.cols, last_row = min(first_row + u.cols, u.rows) - 1;
+              const bool none = u.ctx + p.a.by_group.quot(last_row) < slot0;
               float add = 0.0f;
-              bool careful = masked;
-              for (int c = 0; c < u.cols && !careful; c += kChunk) {
+              bool careful = !none && u.ctx + p.a.by_group.quot(first_row) < last_slot;
+              for (int c = 0; c < u.cols && !careful && !none; c += kChunk) {
                 const float* factor = sh.factor[slab.at] + c;
                 const float offset = sh.offset[slab.at][c / kChunk];
                 const float2 some = u.cols - c >= kChunk ? sum_columns<kChunk>(from + c, factor, scale, offset)
@@ -515,7 +558,8 @@ __global__ void __launch_bounds__(kThreads, 1)
               careful = __any_sync(kFull, careful || add != add);
               if (careful) {
                 // the slab's first row that sees the slot
-                const int first = slot > u.ctx ? min((slot - u.ctx) * p.a.group - tile * u.cols, kCols) : 0;
+                const long long sees = static_cast<long long>(slot - u.ctx) * p.a.group - first_row;
+                const int first = slot > u.ctx ? static_cast<int>(min(sees, static_cast<long long>(kCols))) : 0;
                 add = sum_carefully(from, u.cols, sh.scale[slab.at], scale, first);
               }
               sum += add;
