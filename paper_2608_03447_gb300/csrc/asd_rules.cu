@@ -17,6 +17,18 @@
 // logits in every row. Both kinds merge (value, index) keys into the rows' slots,
 // from which the selection runs as after any other row stage.
 // asd_rules_logits writes what it reads, so there a warp lists its own unit's tokens.
+//
+// What bounds it: 32 requests of 9 rows of 151936 (bf16, 4000 tokens said, 300 biases,
+// grammars) take 24 to 25 us, selection included, for 95 MB (3.9 TB/s): instructions,
+// 660 a unit of 4 KB where asd_verify has 244 (the grammar's masks 127, the marks and
+// what is worked out 118, the tokens that may grow 76, the search for the index 63).
+// Without grammars and biases the same rows take 20.6 us, with biases 21.5, with
+// grammars 23.1; 256 requests of 5 rows of 129280 in fp32 119 us (5.6 TB/s). 64 x 5
+// rows of 129280 written in fp32 take 59 us for 331 MB (5.6 TB/s): memory. What else
+// was measured for the 32 requests: all rows of a part by one CTA, its marked tokens
+// excluded from the maximum and taken one by one in every row, 50 us; the same by CTAs
+// of their own 33 to 48 us (1.3 million gathers of a logit); only those that may grow, a
+// lane's token in one row after the other, 33 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -725,8 +737,9 @@ __global__ void __launch_bounds__(256)
 }
 
 // Many tokens of a request: a CTA has some thousand of them and sees by a bitmap of its own which it has met before.
-// A mark is then one addition a word, and of a prompt's tokens the record is touched once each (64 prompts of up to
-// 8000 tokens, half of them repeated).
+// A mark is then one addition a word, and of a prompt's tokens the record is touched once each: 64 prompts of up to
+// 8000 tokens, half of them repeated, 8.0 to 8.5 us, by a thread a token 9.8. Bound by what each record costs, 64 bytes
+// of memory for four (25 MB read).
 constexpr int kBulkThreads = 512, kBulkTokens = 4096;
 constexpr int kBulkWords = 50000;  // of a bitmap that fits shared memory
 __global__ void __launch_bounds__(kBulkThreads)
@@ -886,13 +899,17 @@ int launch_stream(const RulesParams& p, cudaStream_t stream) {
   return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;
 }
 
-// Units (or a row's share of a CTA) of eight vectors a lane, or of two where those would be few.
-constexpr int kWide = 8, kNarrow = 2;
+// Units of eight vectors a lane, or of four where those would be fewer than fill the GPU several times over: 1350 of the
+// wide ones (two requests of 9 rows of 151936, bf16) 6.3 us against 5.7 of twice as many, 2700 7.0 against 6.2, 5400
+// the same 9.9, 10800 13.9 against 15.2, 21600 24.2 against 28.7; written in fp32, 1200 5.2 against 4.8 us, 10200 16.9
+// against 18.4. Units of two vectors are never the fastest (675 wide ones' rows: 5.3 us, as wide; of four 5.0).
+constexpr int kWide = 8, kNarrow = 4;
+constexpr long long kWideUnits = 5000;
 template <typename T, bool kWrite>
 int launch_rules(const RulesParams& p, cudaStream_t stream) {
   const long long wide = parts_of<T>(p.V, kWide) * p.B;
   if (wide * p.R > INT32_MAX / 8) return ASD_ERR_SHAPE;  // units and CTAs are counted in 32 bits
-  const bool few = wide * p.R < 1200;
+  const bool few = wide * p.R < kWideUnits;
   if (kWrite) return few ? launch_write<T, kNarrow>(p, stream) : launch_write<T, kWide>(p, stream);
   return few ? launch_stream<T, kNarrow>(p, stream) : launch_stream<T, kWide>(p, stream);
 }
