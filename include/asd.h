@@ -554,7 +554,8 @@ int asd_kv_weigh(const asd_kv_cache* cache, const asd_weigh* args, asd_stream_t 
  * (keys are rotated by their positions when they are appended), so nothing else
  * moves. Where at least `last` tokens are appended between two evictions, no token
  * with fewer than `last` behind it ever goes. Later tokens take positions of their
- * own (asd_append.positions): kv_len is no longer a token's number.
+ * own (asd_append.positions): kv_len is no longer a token's number. A request's pages
+ * are its own: of a page that two requests' tables share, both move slots.
  *
  * weight        [layers, B, heads, width]; weight_out the same or weight itself. Slots
  *               of weight_out from n on are left as they were.

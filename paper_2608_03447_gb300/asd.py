@@ -210,12 +210,17 @@ def _stream(stream) -> int:
 
 
 def _stream_at(stream, index: int) -> int:
-    """The handle of a call's stream. Kernels run on the current device: tensors of another one are refused."""
-    if stream is not None:
-        return _stream(stream)
-    if torch.cuda.current_device() != index:
-        raise ValueError(f"the call's tensors are on cuda:{index}, the current device is cuda:{torch.cuda.current_device()}")
-    return _stream(None)
+    """The handle of a call's stream. Kernels run on the current device, in a stream of its own: tensors of another one
+    are refused (a raw handle does not show its device)."""
+    if stream is None:
+        if torch.cuda.current_device() != index:
+            raise ValueError(
+                f"the call's tensors are on cuda:{index}, the current device is cuda:{torch.cuda.current_device()}")
+    else:
+        device = getattr(stream, "device", None)
+        if device is not None and device.index != index:
+            raise ValueError(f"the call's tensors are on cuda:{index}, its stream is on {device}")
+    return _stream(stream)
 
 
 def _torch_on(stream):
@@ -868,8 +873,9 @@ def kv_evict(cache: KVCache, kv_len: torch.Tensor, weight: torch.Tensor, keep: t
     """asd_kv_evict: cut every request's cache to ``keep[b]`` slots, in every layer and in place.
 
     weight float32 [layers, B, heads, width] (or without the first dimension for one layer), moved with the slots in
-    place or to ``out``. The first ``first`` and the last ``last`` slots stay. Returns the new lengths, int32 [B]
-    (``new_len``, allocated on ``stream`` if not given; not ``kv_len`` itself).
+    place or to ``out``. The first ``first`` and the last ``last`` slots stay. Pages that two requests' tables share are
+    not for this: each would move the other's slots. Returns the new lengths, int32 [B] (``new_len``, allocated on
+    ``stream`` if not given; not ``kv_len`` itself).
     """
     B = cache.B
     one = (B,)
@@ -904,8 +910,9 @@ class TokenRules:
     records     int32 [B, V, 2]: (TOKEN_PROMPT if in the prompt | times said, the bits of a float32 bias)
     repetition, frequency, presence  float32 [B] or None (no such penalty)
 
-    The tensors stay the caller's; tokens_record and tokens_bias write the first two. ``TokenRules.empty(B, V)`` makes
-    them, ``clear(b)`` empties a request's row for its next user.
+    The tensors stay the caller's, who writes new values into them (calls keep to the tensors given here); tokens_record
+    and tokens_bias write the first two. ``TokenRules.empty(B, V)`` makes them, ``clear(b)`` empties a request's row for
+    its next user.
     """
 
     def __init__(self, marks: torch.Tensor, records: torch.Tensor, repetition: torch.Tensor | None = None,
@@ -947,7 +954,8 @@ class TokenRules:
     def _pack(self, allow: torch.Tensor | None, rows: int) -> bytes:
         if allow is None:
             return self._plain
-        if allow.shape != (self.B, rows, self.words) or allow.dtype is not _I32 or allow.get_device() != self.index or                 (allow.stride(2) != 1 and self.words > 1):
+        if allow.shape != (self.B, rows, self.words) or allow.dtype is not _I32 or allow.get_device() != self.index or \
+                (allow.stride(2) != 1 and self.words > 1):
             raise ValueError(f"allow must be an int32 tensor {[self.B, rows, self.words]} on the rules' device, its "
                              "last dimension contiguous")
         return _RULES.pack(*self._head, allow.data_ptr(), allow.stride(0), allow.stride(1), self.B, self.V)

@@ -285,3 +285,22 @@ def test_tensors_of_another_device_are_refused(fake, monkeypatch):
         with pytest.raises(ValueError, match="current device"):
             call()
     assert fake.calls == []
+
+
+def test_streams_of_another_device_are_refused(fake):
+    r, c, z, q = host_rules(), host_cache(), torch.ones(2, 4, 100), torch.ones(2, 3, 4, 8)
+    other = types.SimpleNamespace(cuda_stream=0x5eed, device=torch.device("cuda", 3))
+    ws = types.SimpleNamespace(buffer=torch.ones(8), nbytes=1 << 20)
+    out = {n: i32(2, 4) for n in ("accepted_len", "committed", "recovery")}
+    calls = [lambda s: asd.rules_verify(z, i32(2, 3), None, 1.0, 2, r, workspace=ws, out=out, stream=s),
+             lambda s: asd.rules_logits(z, None, r, out=z, stream=s), lambda s: asd.tokens_record(i32(2, 5), r, stream=s),
+             lambda s: asd.tokens_bias(i32(2, 5), torch.ones(2, 5), r, stream=s),
+             lambda s: asd.kv_weigh(q, torch.ones(2, 3, 4), c, i32(2), torch.ones(2, 2, 30), stream=s),
+             lambda s: asd.kv_evict(c, i32(2), torch.ones(2, 2, 30), i32(2), new_len=i32(2), stream=s)]
+    for call in calls:
+        with pytest.raises(ValueError, match="its stream is on cuda:3"):
+            call(other)
+    assert fake.calls == []
+    for call in calls:
+        call(STREAM)
+    assert len(fake.calls) == len(calls)
