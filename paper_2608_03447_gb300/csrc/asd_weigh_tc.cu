@@ -18,16 +18,17 @@
 //
 // What bounds it: few rows, memory: 32 paths of up to 9 on 8000 slots, 40 heads on 8 of
 // 128 in bf16, 79 to 81 us (471 MB read, 6.0 TB/s). Many rows, the exponentials (32 a
-// clock and SM) and the issue of the products (some 80 cycles a tcgen05.mma, four a
-// tile and slab at heads of 64): 64 rows of 16 prompts of up to 12000 slots, 32 heads on
-// 4 of 64 in f16, 80 us, of which the 393 million exponentials need 42. One token on
-// 4200 slots takes 6.9 us, a chain of latencies. A prompt of 4093 on itself (40 heads on
+// clock and SM), what goes with them, and the products behind them: 64 rows of 16 prompts
+// of up to 12000 slots, 32 heads on 4 of 64 in f16, 73 us, of which the 393 million
+// exponentials need 42; without any sums the same takes 49, with sums but no exponentials
+// 67, and a group waits 15 % of its time for a product. One token on 4200 slots takes 7.2 us, a chain of latencies. A prompt of 4093 on itself (40 heads on
 // 8 of 128) takes 321 us: the CTAs that have the first slots meet all 160 slabs of rows
 // one after the other, 2 us each. 775 us with every row's place compared with every slot,
 // 697 where only a slab that crosses a tile's causal edge does that, 321 since slabs that
 // see nothing of a step are neither copied nor multiplied and a row's sum is read while
 // its slab is waited for. What else was measured for the 64 rows:
-// two groups with two accumulators each 113 us; row scales read as pairs, both numbers
+// two groups with two accumulators each 113 us; halves of 64 rows, one multiplied while
+// the other is added up, 97 us; the next columns read while some are added up 77 us; row scales read as pairs, both numbers
 // for every column, 132 us; one part of the scale only 75 us (its rounding was then in
 // every weight); two warps that issue MMAs 79 us against 75, by their registers.
 // Truncation in the tensor cores' sums makes products smaller by about 2^-22: weights
@@ -184,9 +185,9 @@ __device__ __forceinline__ void tmem_take(uint32_t taddr, float (&r)[16]) {
       : "r"(taddr));
 }
 
-// exp2(scale z - offset) factor summed over kN columns of this thread's lane, even and odd ones apart.
+// exp2(scale z - offset) factor summed over kN columns of this thread's lane.
 template <int kN>
-__device__ __forceinline__ float2 sum_columns(uint32_t from, const float* factor, float2 scale, float offset) {
+__device__ __forceinline__ float sum_columns(uint32_t from, const float* factor, float2 scale, float offset) {
   const float2 by = {scale.x, scale.x}, rest = {scale.y, scale.y}, less = {-offset, -offset};
   float z[kN];
   tmem_take(from, z);
@@ -199,7 +200,8 @@ __device__ __forceinline__ float2 sum_columns(uint32_t from, const float* factor
     sum[0] = fma2(make_float2(exp2_fast(t0.x), exp2_fast(t0.y)), make_float2(f.x, f.y), sum[0]);
     sum[1] = fma2(make_float2(exp2_fast(t1.x), exp2_fast(t1.y)), make_float2(f.z, f.w), sum[1]);
   }
-  return add2(sum[0], sum[1]);
+  const float2 both = add2(sum[0], sum[1]);
+  return both.x + both.y;
 }
 // The same row by row, for any sums and any products: neither a row that adds nothing
 // nor one before `first` counts, whatever its product is.
@@ -547,12 +549,17 @@ __global__ void __launch_bounds__(kThreads, 1)
               const bool none = u.ctx + p.a.by_group.quot(last_row) < slot0;
               float add = 0.0f;
               bool careful = !none && u.ctx + p.a.by_group.quot(first_row) < last_slot;
-              for (int c = 0; c < u.cols && !careful && !none; c += kChunk) {
-                const float* factor = sh.factor[slab.at] + c;
-                const float offset = sh.offset[slab.at][c / kChunk];
-                const float2 some = u.cols - c >= kChunk ? sum_columns<kChunk>(from + c, factor, scale, offset)
-                                                         : sum_columns<16>(from + c, factor, scale, offset);
-                add += some.x + some.y;
+              const float* factor = sh.factor[slab.at];
+              const float* offset = sh.offset[slab.at];
+              if (careful || none) {
+              } else if (u.cols == kCols) {  // unrolled: the 64 rows of 16 prompts 73 us, in a loop 78
+#pragma unroll
+                for (int c = 0; c < kCols; c += kChunk)
+                  add += sum_columns<kChunk>(from + c, factor + c, scale, offset[c / kChunk]);
+              } else {
+                for (int c = 0; c < u.cols; c += kChunk)
+                  add += u.cols - c >= kChunk ? sum_columns<kChunk>(from + c, factor + c, scale, offset[c / kChunk])
+                                              : sum_columns<16>(from + c, factor + c, scale, offset[c / kChunk]);
               }
               // a key that is not finite makes the product with a row that adds nothing NaN too
               careful = __any_sync(kFull, careful || add != add);
