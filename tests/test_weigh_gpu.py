@@ -231,6 +231,42 @@ def test_long_contexts_whose_every_slot_is_checked(asd, dtype):
         assert bool((w[b, :, n + 2:] == -1).all()) and bool((w[b, :, n:n + 2] >= 0).all())
 
 
+@pytest.mark.parametrize("dtype,D,page", ((BF16, 128, 16), (F16, 64, 48), (BF16, 64, 5), (F32, 32, 24)), ids=str)
+def test_prompts_that_see_themselves(asd, dtype, D, page):
+    """Many tiles a CTA, of which the later ones are seen by ever fewer rows; every weight, with the bound of
+    rules_reference.weighed."""
+    B, T, Hkv, G, u = 16, 1300, 8, 3, 2.0 ** -24
+    g = torch.Generator(device="cuda").manual_seed(D)
+    kv = torch.tensor([0, 0, 1, 127, 200, 0, 511, 512, 0, 64, 3, 0, 900, 0, 0, 31], dtype=torch.int32, device="cuda")
+    new = torch.tensor([T, T - 1, T, 700, T, 1, T, 129, 1024, T, 1153, 43, T, T, 1280, T], dtype=torch.int32, device="cuda")
+    width = -(-(900 + T) // page)
+    k = torch.randn(B * width, page, Hkv, D, generator=g, device="cuda").to(dtype)
+    table = torch.randperm(k.shape[0], generator=g, device="cuda").to(torch.int32).view(B, -1).contiguous()
+    q = torch.randn(B, T, Hkv * G, D, generator=g, device="cuda").to(dtype)
+    lse = torch.empty(B, T, Hkv * G, device="cuda")
+    want, tol = [], []
+    for b in range(B):
+        ctx, n = int(kv[b]), int(new[b])
+        keys = k[table[b].long()].view(-1, Hkv, D)[:ctx + n].double()
+        rows = q[b, :n].view(n, Hkv, G, D).double()
+        z = torch.einsum("thgd,shd->hstg", rows, keys) * D ** -0.5
+        sees = torch.arange(ctx + n, device="cuda")[:, None] <= ctx + torch.arange(n, device="cuda")
+        z.masked_fill_(~sees[None, :, :, None], -math.inf)
+        lse[b, :n] = torch.logsumexp(z, 1).permute(1, 0, 2).reshape(n, Hkv * G).float()
+        ref_lse = lse[b, :n].view(n, Hkv, G).permute(1, 0, 2)[:, None].double()
+        weight = torch.exp(z - ref_lse)
+        reach = torch.einsum("thgd,shd->hstg", rows.abs(), keys.abs()) * D ** -0.5
+        off = weight * ((D + 2) * u * reach + 4 * u * (z.masked_fill(z.isinf(), 0.0).abs() + ref_lse.abs()) + 2.0 ** -22)
+        want.append(weight.sum((2, 3)))
+        tol.append(1.01 * off.sum((2, 3)) + (n * G + 2) * u * want[b] + 1e-37)
+    out = asd.kv_weigh(q, lse, asd.KVCache(k, k, table), kv, None, decay=0.0, new_len=new,
+                       out=torch.full((B, Hkv, 900 + T + 3), -1.0, device="cuda"))
+    for b in range(B):
+        n = want[b].shape[1]
+        assert float(((out[b, :, :n].double() - want[b]).abs() / tol[b]).max()) <= 1.0, b
+        assert bool((out[b, :, n:] == -1).all())
+
+
 def test_results_do_not_depend_on_the_batch(asd):
     """Other requests cut the work differently; a request's weights stay the same bit for bit."""
     p = Problem(BF16, 5, 8, 2, 128, 64, [3000, 700, 1500, 2500, 1], seed=11)
