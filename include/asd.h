@@ -515,7 +515,7 @@ int asd_kv_compact(const asd_kv_cache* cache, int P, const int32_t* kv_len, cons
  * nothing; a row whose path entry is outside [0, T) (ASD_STATUS_PATH) adds nothing,
  * and a slot on a page out of range (ASD_STATUS_PAGE) counts as a key of zeros.
  * Arithmetic: scores, exponentials and sums in fp32, rows added in a fixed order.
- * 16-bit types with head_dim <= 128 and a multiple of 8 and rows on 16-byte
+ * 16-bit types with a head_dim that is a multiple of 8 and rows on 16-byte
  * boundaries run on the tensor cores; a call that gives up waiting on its own
  * pipeline flags all its requests ASD_STATUS_INCOMPLETE (pass a status array to
  * see it). No workspace. Values of the cache are not read. The limits on sizes are

@@ -1,6 +1,6 @@
 // libasd: the attention weight that each cached slot receives (asd_kv_weigh): the
-// entry point, and the kernel on the CUDA cores, for 32-bit caches, wide heads and
-// layouts that the tensor-core kernel does not take.
+// entry point, and the kernel on the CUDA cores, for 32-bit caches and layouts that the
+// tensor-core kernel does not take.
 //
 // w[s] = sum over rows of exp(scale q k_s - lse): the rows' softmax is known by its
 // log-sum-exp, so one pass over the keys does, and every slot's sum stands alone.

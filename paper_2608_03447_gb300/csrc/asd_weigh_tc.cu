@@ -26,7 +26,9 @@
 // one after the other, 2 us each. 775 us with every row's place compared with every slot,
 // 697 where only a slab that crosses a tile's causal edge does that, 321 since slabs that
 // see nothing of a step are neither copied nor multiplied and a row's sum is read while
-// its slab is waited for. What else was measured for the 64 rows:
+// its slab is waited for. Heads beyond 128 have room for one slab and two tiles of 64 KB:
+// four rows of 8 requests on 4000 slots, 16 heads on 4 of 256, 15.4 us (floor 8.6; on the
+// CUDA cores 171). What else was measured for the 64 rows:
 // two groups with two accumulators each 113 us; halves of 64 rows, one multiplied while
 // the other is added up, 97 us; the next columns read while some are added up 77 us; row scales read as pairs, both numbers
 // for every column, 132 us; one part of the scale only 75 us (its rounding was then in
@@ -71,10 +73,10 @@ constexpr size_t kSmemMax = 232448;
 
 constexpr int slab_bytes(int dim) { return kTile * dim * 2; }  // 128 rows of a padded head
 // Slabs of queries: 64 KB. A unit that needs no more keeps them for all its tiles.
-constexpr int query_slabs(int dim) { return dim <= 64 ? kMaxQueries : kMaxQueries / 2; }
+constexpr int query_slabs(int dim) { return dim <= 64 ? kMaxQueries : dim <= 128 ? kMaxQueries / 2 : 1; }
 // Tiles that meet a slab of queries one after the other where a unit has several slabs: their keys stay meanwhile, and
-// at heads of 128 there are four stages.
-constexpr int tiles_at_once(int dim) { return dim <= 64 ? kGroups : kGroups - 1; }
+// at heads of 128 there are four stages, at 256 two.
+constexpr int tiles_at_once(int dim) { return dim <= 64 ? kGroups : dim <= 128 ? kGroups - 1 : 1; }
 
 // What the roles know of a unit; the keys' warp walks the CTA's range and publishes its units through a ring.
 struct alignas(16) WeighUnit {
@@ -106,7 +108,7 @@ constexpr int stages_for(int dim) {
 constexpr size_t smem_for(int dim) {
   return 1024 + static_cast<size_t>(query_slabs(dim) + stages_for(dim)) * slab_bytes(dim) + sizeof(WeighShared);
 }
-static_assert(stages_for(128) >= 4, "ring depth at the widest head");
+static_assert(stages_for(128) >= 4 && stages_for(256) >= 2, "ring depth: more than the tiles of a step");
 
 __device__ __forceinline__ bool warp_wait(unsigned long long* bar, uint32_t parity, WeighShared& sh) {
   if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
@@ -646,18 +648,20 @@ int launch_dim(const asd_kv_cache* cache, const WeighParams& p, cudaStream_t str
 
 namespace asd_detail {
 
-// 16-bit types, heads of at most 128 whose rows are whole 16-byte words on 16-byte boundaries.
+// 16-bit types, heads whose rows are whole 16-byte words on 16-byte boundaries.
 bool weigh_tc_takes(const asd_kv_cache* cache, const WeighParams& p) {
-  return cache->dtype != ASD_F32 && p.a.D <= 128 && p.a.D % 8 == 0 &&
+  return cache->dtype != ASD_F32 && p.a.D % 8 == 0 &&
          rows_aligned(p.a.cache.k, 2, 16, p.a.cache.page_stride, p.a.cache.token_stride, p.a.cache.head_stride) &&
          rows_aligned(p.a.q, 2, 16, p.a.q_batch, p.a.q_token, p.a.q_head);
 }
 
 int launch_weigh_tc(const asd_kv_cache* cache, const WeighParams& p, cudaStream_t stream) {
-  if (cache->dtype == ASD_BF16)
-    return p.a.D <= 64 ? launch_dim<__nv_bfloat16, 64>(cache, p, stream)
-                       : launch_dim<__nv_bfloat16, 128>(cache, p, stream);
-  return p.a.D <= 64 ? launch_dim<__half, 64>(cache, p, stream) : launch_dim<__half, 128>(cache, p, stream);
+  const bool bf16 = cache->dtype == ASD_BF16;
+  if (p.a.D <= 64)
+    return bf16 ? launch_dim<__nv_bfloat16, 64>(cache, p, stream) : launch_dim<__half, 64>(cache, p, stream);
+  if (p.a.D <= 128)
+    return bf16 ? launch_dim<__nv_bfloat16, 128>(cache, p, stream) : launch_dim<__half, 128>(cache, p, stream);
+  return bf16 ? launch_dim<__nv_bfloat16, 256>(cache, p, stream) : launch_dim<__half, 256>(cache, p, stream);
 }
 
 }  // namespace asd_detail

@@ -231,7 +231,17 @@ def test_long_contexts_whose_every_slot_is_checked(asd, dtype):
         assert bool((w[b, :, n + 2:] == -1).all()) and bool((w[b, :, n:n + 2] >= 0).all())
 
 
-@pytest.mark.parametrize("dtype,D,page", ((BF16, 128, 16), (F16, 64, 48), (BF16, 64, 5), (F32, 32, 24)), ids=str)
+@pytest.mark.parametrize("dtype", (BF16, F16), ids=("bf16", "f16"))
+@pytest.mark.parametrize("case", [(1, 4, 1, 256, 64, [700, 1]), (9, 16, 2, 256, 16, [300, 0, 129]), (40, 8, 2, 192, 32, [400, 60]),
+                                  (5, 6, 3, 136, 12, [150, 33]), (100, 4, 1, 256, 48, [0, 300]), (3, 8, 4, 200, 5, [90]),
+                                  (64, 16, 4, 248, 24, [640, 513])], ids=str)
+def test_wide_heads(asd, dtype, case):
+    p = Problem(dtype, *case, seed=21)
+    p.check(p.run(asd))
+    p.check(p.run(asd, layout="heads"))
+
+
+@pytest.mark.parametrize("dtype,D,page", ((BF16, 128, 16), (F16, 64, 48), (BF16, 64, 5), (BF16, 256, 16), (F32, 32, 24)), ids=str)
 def test_prompts_that_see_themselves(asd, dtype, D, page):
     """Many tiles a CTA, of which the later ones are seen by ever fewer rows; every weight, with the bound of
     rules_reference.weighed."""
