@@ -18,23 +18,24 @@
 //
 // What bounds it: few rows, memory: 32 paths of up to 9 on 8000 slots, 40 heads on 8 of
 // 128 in bf16, 79 to 81 us (471 MB read, 6.0 TB/s). Many rows, the exponentials (32 a
-// clock and SM), what goes with them, and the products behind them: 64 rows of 16 prompts
-// of up to 12000 slots, 32 heads on 4 of 64 in f16, 73 us, of which the 393 million
-// exponentials need 42; without any sums the same takes 49, with sums but no exponentials
-// 67, and a group waits 15 % of its time for a product. One token on 4200 slots takes 7.2 us, a chain of latencies. A prompt of 4093 on itself (40 heads on
-// 8 of 128) takes 321 us: the CTAs that have the first slots meet all 160 slabs of rows
-// one after the other, 2 us each. 775 us with every row's place compared with every slot,
-// 697 where only a slab that crosses a tile's causal edge does that, 321 since slabs that
-// see nothing of a step are neither copied nor multiplied and a row's sum is read while
-// its slab is waited for. Heads beyond 128 have room for one slab and two tiles of 64 KB:
-// four rows of 8 requests on 4000 slots, 16 heads on 4 of 256, 15.4 us (floor 8.6; on the
-// CUDA cores 171). What else was measured for the 64 rows:
-// two groups with two accumulators each 113 us; halves of 64 rows, one multiplied while
-// the other is added up, 97 us; the next columns read while some are added up 77 us; row scales read as pairs, both numbers
-// for every column, 132 us; one part of the scale only 75 us (its rounding was then in
-// every weight); two warps that issue MMAs 79 us against 75, by their registers.
-// Truncation in the tensor cores' sums makes products smaller by about 2^-22: weights
-// are 2 to 5e-7 too small, the largest error against 64 bits.
+// clock and SM), what goes with them, and the products behind them: 64 rows of 16
+// prompts of up to 12000 slots, 32 heads on 4 of 64 in f16, 73 us, of which the 393
+// million exponentials need 42; without any sums the same takes 49, with sums but no
+// exponentials 67, and a group waits 15 % of its time for a product. One token on 4200
+// slots takes 7.2 us, a chain of latencies. A prompt of 4093 on itself (40 heads on 8 of
+// 128) takes 321 us: the CTAs that have the first slots meet all 160 slabs of rows one
+// after the other, 2 us each. 775 us with every row's place compared with every slot,
+// 697 where only a slab that crosses a tile's causal edge does that, 321 since slabs
+// that see nothing of a step are neither copied nor multiplied and a row's sum is read
+// while its slab is waited for. Heads beyond 128 have room for one slab and two tiles of
+// 64 KB: four rows of 8 requests on 4000 slots, 16 heads on 4 of 256, 15.4 us (floor
+// 8.6; on the CUDA cores 171). What else was measured for the 64 rows: two groups with
+// two accumulators each 113 us; halves of 64 rows, one multiplied while the other is
+// added up, 97 us; the next columns read while some are added up 77 us; row scales read
+// as pairs, both numbers for every column, 132 us; one part of the scale only 75 us (its
+// rounding was then in every weight); two warps that issue MMAs 79 us against 75, by
+// their registers. Truncation in the tensor cores' sums makes products smaller by about
+// 2^-22: weights are 2 to 5e-7 too small, the largest error against 64 bits.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
