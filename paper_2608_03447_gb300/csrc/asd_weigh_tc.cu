@@ -321,7 +321,20 @@ __global__ void __launch_bounds__(kThreads, 1)
         page = __ldcg(a.cache.table + static_cast<long long>(u.b) * a.cache.table_width + n);
         at = slot - n * a.cache.div.size;
       };
-      if (kTma) look_up(u.j0);
+      // copies: the pages of the next tile's rows, 32 at a time a row a lane
+      int pages[kTile / 32];
+      auto look_up_rows = [&](int j) {
+#pragma unroll
+        for (int i = 0; i < kTile / 32; ++i) {
+          const int slot = j * kTile + 32 * i + lane;
+          if (j < u.j1 && slot < u.span)
+            pages[i] = __ldcg(a.cache.table + static_cast<long long>(u.b) * a.cache.table_width + a.cache.div.quot(slot));
+        }
+      };
+      if (kTma)
+        look_up(u.j0);
+      else
+        look_up_rows(u.j0);
       for (int j = u.j0; ok && j < u.j1; ++j) {
         const int slot0 = j * kTile, rows = min(kTile, u.span - slot0);
         const uint32_t dst = sk + ring.at * kSlab;
@@ -348,23 +361,31 @@ __global__ void __launch_bounds__(kThreads, 1)
             atomicOr(a.status + u.b, static_cast<int>(ASD_STATUS_PAGE));
           __syncwarp();
         } else {
+          long long offs[kTile / 32];
+#pragma unroll
+          for (int i = 0; i < kTile / 32; ++i) {
+            const int slot = slot0 + 32 * i + lane;
+            offs[i] = -1;
+            if (32 * i + lane >= rows) continue;
+            if (static_cast<unsigned>(pages[i]) < static_cast<unsigned>(a.cache.pages))
+              offs[i] = pages[i] * a.cache.page_stride +
+                        static_cast<long long>(slot - a.cache.div.quot(slot) * a.cache.div.size) * a.cache.token_stride +
+                        u.h * a.cache.head_stride;
+            else if (a.status)
+              atomicOr(a.status + u.b, static_cast<int>(ASD_STATUS_PAGE));
+          }
+          look_up_rows(j + 1);
           ok = warp_wait(&sh.k_empty[ring.at], ring.phase ^ 1u, sh);
           if (!ok) break;
-          for (int r0 = 0; r0 < rows; r0 += 32) {
-            long long off = -1;  // of row r0 + lane
-            if (r0 + lane < rows) {
-              off = slot_offset(a.cache, u.b, slot0 + r0 + lane);
-              if (off >= 0)
-                off += u.h * a.cache.head_stride;
-              else if (a.status)
-                atomicOr(a.status + u.b, static_cast<int>(ASD_STATUS_PAGE));
-            }
+#pragma unroll
+          for (int n = 0; n < kTile / 32; ++n) {
+            if (32 * n >= rows) break;
 #pragma unroll 4
             for (int i = 0; i < 32 / kRowsAtOnce; ++i) {
               const int r = i * kRowsAtOnce + sub;
-              const long long o = __shfl_sync(kFull, off, r);
+              const long long o = __shfl_sync(kFull, offs[n], r);
               const bool has = o >= 0 && has_chunk;
-              if (r0 + r < rows) copy16(dst + place(r0 + r), has ? a.cache.k + 2 * (o + chunk * 8) : a.q, has);
+              if (32 * n + r < rows) copy16(dst + place(32 * n + r), has ? a.cache.k + 2 * (o + chunk * 8) : a.q, has);
             }
           }
           copies_arrive(bar);
