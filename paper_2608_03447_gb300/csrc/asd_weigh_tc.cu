@@ -14,7 +14,9 @@
 // A CTA per SM: warps 0 to 15 are the groups, warp 16 walks the units and loads keys,
 // warp 17 issues the MMAs, warps 18 and 19 copy queries and the rows' scales.
 // Keys are TMA boxes of as many slots as the page size and the tile have as a common
-// divisor, or 16-byte copies where that is less than the swizzle's eight rows.
+// divisor, or 16-byte copies by four warps, 32 rows each, where that is less than the
+// swizzle's eight rows (the chains below in pages of five slots 117 us; one warp 389, and
+// 464 if it looks up a tile's pages when it needs them).
 //
 // What bounds it: few rows, memory: 32 paths of up to 9 on 8000 slots, 40 heads on 8 of
 // 128 in bf16, 79 to 81 us (471 MB read, 6.0 TB/s). Many rows, the exponentials (32 a
@@ -65,7 +67,9 @@ constexpr int kGroups = 4;        // of 128 threads
 constexpr int kSumThreads = kGroups * 128;
 constexpr int kKeyWarp = 16, kMmaWarp = 17, kQueryWarp = 18;
 constexpr int kQueryThreads = 64;
-constexpr int kThreads = 20 * 32;  // five warps a scheduler: 96 registers each
+// Twenty warps, five a scheduler: 96 registers each. Where keys are copied by threads, three more share that.
+constexpr int kCopyWarp = 20;
+constexpr int threads_for(bool tma) { return (tma ? kCopyWarp : kCopyWarp + 3) * 32; }
 constexpr int kTmemCols = 512;
 constexpr int kMaxStages = 12;
 constexpr int kMaxQueries = 4;
@@ -86,7 +90,7 @@ struct alignas(16) WeighUnit {
   int tiles, cols, pad[2]; // slabs of queries, and the columns of each (a multiple of 16)
 };
 constexpr int kUnits = 4;
-constexpr int kUnitReaders = kSumThreads / 32 + 3;  // warps
+constexpr int kUnitReaders = kSumThreads / 32 + 3;  // warps, without those that copy keys
 
 struct WeighShared {
   unsigned long long k_full[kMaxStages], k_empty[kMaxStages];  // loads have landed; the MMAs have read them
@@ -226,10 +230,10 @@ __device__ __noinline__ float sum_carefully(uint32_t from, int cols, const RowSc
 
 // kDim: the head, padded. kTma: keys are loaded as TMA boxes.
 template <typename T, int kDim, bool kTma>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(threads_for(kTma), 1)
     weigh_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ WeighParams p, int box) {
   constexpr int kSlab = slab_bytes(kDim), kStages = stages_for(kDim), kQueries = query_slabs(kDim);
-  constexpr int kStep = tiles_at_once(kDim);
+  constexpr int kStep = tiles_at_once(kDim), kThreads = threads_for(kTma);
   constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
   constexpr int kChunks = kDim / 8;          // 16-byte chunks of a row
   constexpr int kRowsAtOnce = 32 / kChunks;  // rows that a warp copies per instruction
@@ -244,12 +248,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   pdl_signal_dependents();
   if (warp == kQueryWarp) {  // a barrier or two a lane
     if (lane < kMaxStages) {
-      mbar_init(&sh.k_full[lane], kTma ? 1 : 32);
+      mbar_init(&sh.k_full[lane], kTma ? 1 : kTile);  // a thread a row
       mbar_init(&sh.k_empty[lane], 1);
     }
     if (lane < kUnits) {
       mbar_init(&sh.unit_full[lane], 1);
-      mbar_init(&sh.unit_empty[lane], kUnitReaders);
+      mbar_init(&sh.unit_empty[lane], kUnitReaders + kThreads / 32 - kCopyWarp);
     }
     if (lane >= 16 && lane < 16 + kQueries) {
       mbar_init(&sh.q_full[lane - 16], 2 * kQueryThreads);  // each thread's copies, and its scales
@@ -286,6 +290,41 @@ __global__ void __launch_bounds__(kThreads, 1)
     return static_cast<uint32_t>((chunk >> 3) * kHalfSlab + r * 128 + (((chunk & 7) ^ (r & 7)) << 4));
   };
   const bool has_chunk = chunk * 8 < p.a.D;
+  // A unit's keys by 16-byte copies: rows 32 n to 32 n + 31 of every tile, whose pages are looked up a tile ahead.
+  auto copy_keys = [&](const WeighUnit& u, int n, Ring<kStages>& ring, bool& ok) {
+    const CacheView& c = p.a.cache;
+    int page = 0;
+    auto look_up = [&](int j) {
+      if (j >= u.j1 || 32 * n + lane >= min(kTile, u.span - j * kTile)) return;
+      page = __ldcg(c.table + static_cast<long long>(u.b) * c.table_width + c.div.quot(j * kTile + 32 * n + lane));
+    };
+    look_up(u.j0);
+    for (int j = u.j0; ok && j < u.j1; ++j) {
+      const int rows = min(32, u.span - j * kTile - 32 * n);  // below 1: none
+      long long off = -1;  // of this lane's row
+      if (lane < rows) {
+        const int slot = j * kTile + 32 * n + lane;
+        if (static_cast<unsigned>(page) < static_cast<unsigned>(c.pages))
+          off = page * c.page_stride + static_cast<long long>(slot - c.div.quot(slot) * c.div.size) * c.token_stride +
+                u.h * c.head_stride;
+        else if (p.a.status)
+          atomicOr(p.a.status + u.b, static_cast<int>(ASD_STATUS_PAGE));
+      }
+      look_up(j + 1);
+      ok = warp_wait(&sh.k_empty[ring.at], ring.phase ^ 1u, sh);
+      if (!ok) break;
+      const uint32_t dst = sk + ring.at * kSlab;
+#pragma unroll 4
+      for (int i = 0; i < 32 / kRowsAtOnce; ++i) {
+        const int r = i * kRowsAtOnce + sub;
+        const long long o = __shfl_sync(kFull, off, r);
+        const bool has = o >= 0 && has_chunk;
+        if (r < rows) copy16(dst + place(32 * n + r), has ? c.k + 2 * (o + chunk * 8) : p.a.q, has);
+      }
+      copies_arrive(&sh.k_full[ring.at]);
+      ring.next();
+    }
+  };
 
   if (warp == kKeyWarp) {
     // ---------------- units and keys
@@ -312,35 +351,20 @@ __global__ void __launch_bounds__(kThreads, 1)
       u.tiles = (u.rows + kCols - 1) / kCols;
       u.cols = ((u.rows + u.tiles - 1) / u.tiles + 15) & ~15;
       publish(u);
-      // TMA: where this lane's box of the next tile begins; the page table is read a tile ahead
-      int page = 0, at = 0;
-      auto look_up = [&](int j) {
-        const int slot = j * kTile + lane * box;
-        if (lane * box >= kTile || j >= u.j1 || slot >= u.span) return;
-        const int n = a.cache.div.quot(slot);
-        page = __ldcg(a.cache.table + static_cast<long long>(u.b) * a.cache.table_width + n);
-        at = slot - n * a.cache.div.size;
-      };
-      // copies: the pages of the next tile's rows, 32 at a time a row a lane
-      int pages[kTile / 32];
-      auto look_up_rows = [&](int j) {
-#pragma unroll
-        for (int i = 0; i < kTile / 32; ++i) {
-          const int slot = j * kTile + 32 * i + lane;
-          if (j < u.j1 && slot < u.span)
-            pages[i] = __ldcg(a.cache.table + static_cast<long long>(u.b) * a.cache.table_width + a.cache.div.quot(slot));
-        }
-      };
-      if (kTma)
+      if constexpr (kTma) {
+        // where this lane's box of the next tile begins; the page table is read a tile ahead
+        int page = 0, at = 0;
+        auto look_up = [&](int j) {
+          if (j >= u.j1 || lane * box >= min(kTile, u.span - j * kTile)) return;
+          const int slot = j * kTile + lane * box, n = a.cache.div.quot(slot);
+          page = __ldcg(a.cache.table + static_cast<long long>(u.b) * a.cache.table_width + n);
+          at = slot - n * a.cache.div.size;
+        };
         look_up(u.j0);
-      else
-        look_up_rows(u.j0);
-      for (int j = u.j0; ok && j < u.j1; ++j) {
-        const int slot0 = j * kTile, rows = min(kTile, u.span - slot0);
-        const uint32_t dst = sk + ring.at * kSlab;
-        unsigned long long* const bar = &sh.k_full[ring.at];
-        if constexpr (kTma) {
-          const int page_of = page, at_of = at;
+        for (int j = u.j0; ok && j < u.j1; ++j) {
+          const int rows = min(kTile, u.span - j * kTile), page_of = page, at_of = at;
+          const uint32_t dst = sk + ring.at * kSlab;
+          unsigned long long* const bar = &sh.k_full[ring.at];
           look_up(j + 1);
           ok = warp_wait(&sh.k_empty[ring.at], ring.phase ^ 1u, sh);
           if (!ok) break;
@@ -360,41 +384,27 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (lane < n && static_cast<unsigned>(page_of) >= static_cast<unsigned>(a.cache.pages) && a.status)
             atomicOr(a.status + u.b, static_cast<int>(ASD_STATUS_PAGE));
           __syncwarp();
-        } else {
-          long long offs[kTile / 32];
-#pragma unroll
-          for (int i = 0; i < kTile / 32; ++i) {
-            const int slot = slot0 + 32 * i + lane;
-            offs[i] = -1;
-            if (32 * i + lane >= rows) continue;
-            if (static_cast<unsigned>(pages[i]) < static_cast<unsigned>(a.cache.pages))
-              offs[i] = pages[i] * a.cache.page_stride +
-                        static_cast<long long>(slot - a.cache.div.quot(slot) * a.cache.div.size) * a.cache.token_stride +
-                        u.h * a.cache.head_stride;
-            else if (a.status)
-              atomicOr(a.status + u.b, static_cast<int>(ASD_STATUS_PAGE));
-          }
-          look_up_rows(j + 1);
-          ok = warp_wait(&sh.k_empty[ring.at], ring.phase ^ 1u, sh);
-          if (!ok) break;
-#pragma unroll
-          for (int n = 0; n < kTile / 32; ++n) {
-            if (32 * n >= rows) break;
-#pragma unroll 4
-            for (int i = 0; i < 32 / kRowsAtOnce; ++i) {
-              const int r = i * kRowsAtOnce + sub;
-              const long long o = __shfl_sync(kFull, offs[n], r);
-              const bool has = o >= 0 && has_chunk;
-              if (32 * n + r < rows) copy16(dst + place(32 * n + r), has ? a.cache.k + 2 * (o + chunk * 8) : a.q, has);
-            }
-          }
-          copies_arrive(bar);
+          ring.next();
         }
-        ring.next();
+      } else {
+        copy_keys(u, 0, ring, ok);
       }
     }
     publish(WeighUnit{});
     if (!kTma) asm volatile("cp.async.wait_all;" ::: "memory");
+  } else if (warp >= kCopyWarp) {
+    // ---------------- keys that threads copy: the other rows of each tile
+    UnitFeed feed;
+    Ring<kStages> ring;
+    bool ok = true;
+    while (ok) {
+      const WeighUnit* next = feed.wait(sh);
+      if (!next) break;
+      const WeighUnit u = *next;
+      feed.done(sh);
+      copy_keys(u, warp - kCopyWarp + 1, ring, ok);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp >= kQueryWarp) {
     // ---------------- queries; those that need more slabs than there are come again for every step
     const int part = warp - kQueryWarp;
@@ -651,7 +661,8 @@ int launch(const CUtensorMap& map, const WeighParams& p, int box, cudaStream_t s
     grid_of[dev].store(grid, std::memory_order_release);
   }
   cudaLaunchAttribute attr;
-  cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(kThreads), stream, &attr);
+  cudaLaunchConfig_t cfg =
+      pdl_config(dim3(static_cast<unsigned>(grid)), dim3(threads_for(kTma)), stream, &attr);
   cfg.dynamicSmemBytes = smem_for(kDim);
   if (cudaLaunchKernelEx(&cfg, kernel, map, p, box) != cudaSuccess) return ASD_ERR_CUDA;
   return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;
