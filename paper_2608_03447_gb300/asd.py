@@ -213,9 +213,11 @@ def _stream_at(stream, index: int) -> int:
     """The handle of a call's stream. Kernels run on the current device, in a stream of its own: tensors of another one
     are refused (a raw handle does not show its device)."""
     if stream is None:
-        if torch.cuda.current_device() != index:
-            raise ValueError(
-                f"the call's tensors are on cuda:{index}, the current device is cuda:{torch.cuda.current_device()}")
+        current = torch.cuda.current_device()
+        if current != index:
+            raise ValueError(f"the call's tensors are on cuda:{index}, the current device is cuda:{current}")
+        if _raw_stream is not None:
+            return _raw_stream(current)
     else:
         device = getattr(stream, "device", None)
         if device is not None and device.index != index:
@@ -954,11 +956,12 @@ class TokenRules:
     def _pack(self, allow: torch.Tensor | None, rows: int) -> bytes:
         if allow is None:
             return self._plain
+        strides = allow.stride()
         if allow.shape != (self.B, rows, self.words) or allow.dtype is not _I32 or allow.get_device() != self.index or \
-                (allow.stride(2) != 1 and self.words > 1):
+                (strides[2] != 1 and self.words > 1):
             raise ValueError(f"allow must be an int32 tensor {[self.B, rows, self.words]} on the rules' device, its "
                              "last dimension contiguous")
-        return _RULES.pack(*self._head, allow.data_ptr(), allow.stride(0), allow.stride(1), self.B, self.V)
+        return _RULES.pack(*self._head, allow.data_ptr(), strides[0], strides[1], self.B, self.V)
 
 
 def _check_rules(rules: TokenRules, name: str, t: torch.Tensor, shape: tuple, dtype: torch.dtype = _I32) -> int:
