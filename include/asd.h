@@ -107,6 +107,8 @@ enum {
 #define ASD_STATUS_PATH 256u      /* asd_kv_compact: path[i] < i or not ascending; asd_kv_weigh: path[i] outside
                                    * [0, T) */
 #define ASD_STATUS_TOKEN 512u     /* asd_tokens_record, asd_tokens_bias: a token id >= V */
+#define ASD_STATUS_EMPTY_ROW 1024u /* asd_rules_verify with ASD_FLAG_EMPTY_ROWS: no token may come where the recovery
+                                   * token does. The accepted drafts and the ledger stand. */
 
 /* Largest draft length: one warp lane per target row of a block. */
 #define ASD_MAX_K 31
@@ -624,7 +626,13 @@ typedef struct {
  * grammar allows its token. Regrets are differences of changed logits, which stay
  * fp32: a draft that is not allowed has an infinite one, NaN where no token is
  * allowed (then y* = 0). ASD_RESIDENT_INPUTS is not taken.
+ *
+ * A draft whose changed logit is -INFINITY (not allowed by the grammar, or banned by its
+ * bias) is never accepted, whatever gate, budget and cap are, not even where it equals
+ * y* = 0 because no token is allowed. The recovery token of a row without any is y* = 0
+ * all the same; with ASD_FLAG_EMPTY_ROWS in dtype such a request's status tells.
  */
+#define ASD_FLAG_EMPTY_ROWS 0x200
 typedef struct {
   const void* logits;     /* [B, K+1, V] */
   const int32_t* draft;   /* [B, K] */
@@ -637,7 +645,7 @@ typedef struct {
   int32_t* status;
   void* workspace;
   size_t workspace_bytes; /* >= asd_workspace_size(B, K, V, dtype) */
-  int dtype;              /* ASD_F32 or ASD_BF16 */
+  int dtype;              /* ASD_F32 or ASD_BF16, ASD_FLAG_EMPTY_ROWS ORed in if wanted */
   int K;
   float gate;
   int cap;

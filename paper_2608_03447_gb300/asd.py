@@ -44,6 +44,7 @@ STATUS_PAGE = 64
 STATUS_POSITION = 128
 STATUS_PATH = 256
 STATUS_TOKEN = 512
+STATUS_EMPTY_ROW = 1024
 MAX_K = 31
 MAX_HEAD_DIM = 256
 MAX_PATH = 256
@@ -51,6 +52,7 @@ MAX_BIAS = 1024
 MAX_EVICT_SLOTS = 360448
 TOKEN_PROMPT = -2**31  # ASD_TOKEN_PROMPT as an int32, of a record's first word
 RESIDENT_INPUTS = 0x100  # ASD_RESIDENT_INPUTS, ORed into the dtype code
+FLAG_EMPTY_ROWS = 0x200  # ASD_FLAG_EMPTY_ROWS, ORed into rules_verify's dtype code
 INT32_MAX = 2**31 - 1
 
 _lock = threading.Lock()
@@ -972,11 +974,13 @@ def _check_rules(rules: TokenRules, name: str, t: torch.Tensor, shape: tuple, dt
 
 def rules_verify(logits: torch.Tensor, draft: torch.Tensor, ledger: torch.Tensor | None, gate: float, cap: int,
                  rules: TokenRules, allow: torch.Tensor | None = None, workspace: Workspace | None = None,
-                 out: dict | None = None, stream=None) -> dict:
+                 out: dict | None = None, stream=None, flag_empty: bool = False) -> dict:
     """asd_rules_verify: ``verify`` of the logits under the rules (``verify_strict`` with ``ledger=None``).
 
     logits [B, K+1, V] float32 or bfloat16; row j counts the drafts before it. ``allow`` int32 [B, K+1, ceil(V / 32)]:
     a bit a token that the grammar lets come (strides of 0 for masks that several rows share). Workspaces are verify's.
+    A draft that may not come (changed logit -inf) is never accepted. ``flag_empty``: a request whose recovery token
+    stands for a row in which no token may come (its 0 means nothing then) has STATUS_EMPTY_ROW in its status.
     """
     shape, index = logits.shape, rules.index
     if len(shape) != 3 or shape[0] != rules.B or shape[2] != rules.V or logits.get_device() != index or \
@@ -993,7 +997,8 @@ def rules_verify(logits: torch.Tensor, draft: torch.Tensor, ledger: torch.Tensor
     block = _RULES_BLOCK.pack(
         logits.data_ptr(), xp, lp, o["accepted_len"].data_ptr(), o["committed"].data_ptr(), o["recovery"].data_ptr(),
         0 if argmax is None else argmax.data_ptr(), 0 if regret is None else regret.data_ptr(),
-        0 if status is None else status.data_ptr(), ws.buffer.data_ptr(), ws.nbytes, code, K, gate, cap)
+        0 if status is None else status.data_ptr(), ws.buffer.data_ptr(), ws.nbytes,
+        code | FLAG_EMPTY_ROWS if flag_empty else code, K, gate, cap)
     rc = load().asd_rules_verify(packed, block, _stream_at(stream, index))
     if rc:
         raise AsdError("asd_rules_verify", rc)

@@ -42,6 +42,7 @@ struct VerifyParams {
   asd_partial* partials;        // vocabulary shard: [B*(K+1)] outputs instead of the selection
   int resident;                 // ASD_RESIDENT_INPUTS: logits and drafts may be read before the
                                 // previous launch on the stream has completed
+  int flag_empty;               // rules: ASD_FLAG_EMPTY_ROWS
 };
 
 // ---------------------------------------------------------------- element access
@@ -170,7 +171,10 @@ __device__ __forceinline__ BlockInputs load_block(const VerifyParams& p, long lo
 // Alg. 1 for block vb of one request, given the request's ledger (budget,
 // spent): writes the block's outputs and advances `spent` (Eq. 13) unless the
 // block is strict, zero-budget or flagged.
-template <typename T, bool kStrict>
+// kRules: the logits are under rules, and a draft whose logit is -infinity may not come. It
+// is a mismatch that nothing accepts: under an infinite gate and budget its infinite regret
+// would pass Eq. 9 and 11, and in a row without any token that may come it is y* where it is 0.
+template <typename T, bool kStrict, bool kRules = false>
 __device__ __forceinline__ void select_block(const VerifyParams& p, long long vb, const BlockInputs& in,
                                              float budget, float& spent, bool& wrote, int lane) {
   const int K = p.K, K1 = p.K + 1;
@@ -198,7 +202,9 @@ __device__ __forceinline__ void select_block(const VerifyParams& p, long long vb
       r = __int_as_float(0x7fc00000);
     }
   }
-  const bool d = lane < K && x != y;  // Eq. 5
+  const bool barred = kRules && valid_x && in.zx == -INFINITY;
+  const unsigned never = kRules ? __ballot_sync(kFull, barred) : 0u;
+  const bool d = lane < K && (x != y || barred);  // Eq. 5
   const unsigned dmask = __ballot_sync(kFull, d);
   if (!kStrict && ledger_invalid(budget, spent)) flags |= ASD_STATUS_BAD_LEDGER;
 
@@ -220,7 +226,8 @@ __device__ __forceinline__ void select_block(const VerifyParams& p, long long vb
       const int N_next = N + 1;
       const bool ok = __fdiv_rn(rj, q) <= p.gate            // Eq. 7 / 11
                       && __fadd_rn(spent, C_next) <= budget  // Eq. 9 as fl(s + C) <= B
-                      && N_next <= p.cap;                    // Eq. 10
+                      && N_next <= p.cap                     // Eq. 10
+                      && !(kRules && ((never >> j) & 1u));
       if (!ok) {
         a = j;
         break;
@@ -232,6 +239,7 @@ __device__ __forceinline__ void select_block(const VerifyParams& p, long long vb
     wrote = true;
   }
   const int ya = __shfl_sync(kFull, y, a);
+  if (kRules && p.flag_empty && __shfl_sync(kFull, top, a) == -INFINITY) flags |= ASD_STATUS_EMPTY_ROW;
 
   if (lane < K1) {
     if (p.row_argmax) p.row_argmax[row] = y;
@@ -285,7 +293,7 @@ __device__ void emit_partials(const VerifyParams& p, int b, int lane) {
 // The selection of request b over its p.nblk blocks in order (block i is the
 // virtual request i * B + b): the ledger is read once, carried in registers
 // from block to block, and written once. Runs in one warp.
-template <typename T, bool kStrict>
+template <typename T, bool kStrict, bool kRules = false>
 __device__ void select_request(const VerifyParams& p, int b, int lane) {
   if (p.partials) {
     emit_partials<T>(p, b, lane);
@@ -307,7 +315,7 @@ __device__ void select_request(const VerifyParams& p, int b, int lane) {
     BlockInputs next = cur;
     if (i + 1 < p.nblk) next = load_block(p, vb + p.B, lane);  // in flight while this block is selected
     cur.flags |= incomplete;
-    select_block<T, kStrict>(p, vb, cur, budget, spent, wrote, lane);
+    select_block<T, kStrict, kRules>(p, vb, cur, budget, spent, wrote, lane);
     cur = next;
   }
   if (lane == 0) {

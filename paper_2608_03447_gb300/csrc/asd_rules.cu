@@ -927,8 +927,9 @@ int asd_rules_verify(const asd_token_rules* rules, const asd_rules_block* block,
   if (!block) return ASD_ERR_NULL;
   const asd_rules_block& a = *block;
   const int K = a.K;
-  if (a.dtype != ASD_F32 && a.dtype != ASD_BF16) return ASD_ERR_DTYPE;
-  rc = check_shape(rules->B, K, rules->V, a.dtype);
+  const int dtype = a.dtype & ~ASD_FLAG_EMPTY_ROWS;
+  if (dtype != ASD_F32 && dtype != ASD_BF16) return ASD_ERR_DTYPE;
+  rc = check_shape(rules->B, K, rules->V, dtype);
   if (rc != ASD_OK) return rc;
   if (rules->B == 0) return ASD_OK;
   if (!a.logits || !a.workspace || !a.accepted_len || !a.committed || !a.recovery || (K > 0 && !a.draft))
@@ -937,7 +938,7 @@ int asd_rules_verify(const asd_token_rules* rules, const asd_rules_block* block,
   const WorkspaceLayout l = layout_for(rules->B, K);
   if (a.workspace_bytes < l.total) return ASD_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(a.workspace) % 16 != 0 ||
-      reinterpret_cast<uintptr_t>(a.logits) % (a.dtype == ASD_F32 ? 4 : 2) != 0)
+      reinterpret_cast<uintptr_t>(a.logits) % (dtype == ASD_F32 ? 4 : 2) != 0)
     return ASD_ERR_ALIGN;
   char* ws = static_cast<char*>(a.workspace);
   RulesParams p = rules_params(rules);
@@ -949,7 +950,7 @@ int asd_rules_verify(const asd_token_rules* rules, const asd_rules_block* block,
   p.draft_logit = reinterpret_cast<float*>(ws + l.draft_logit);
   p.flags = reinterpret_cast<unsigned*>(ws + l.flags);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  rc = a.dtype == ASD_F32 ? launch_rules<float, false>(p, s) : launch_rules<__nv_bfloat16, false>(p, s);
+  rc = dtype == ASD_F32 ? launch_rules<float, false>(p, s) : launch_rules<__nv_bfloat16, false>(p, s);
   if (rc != ASD_OK) return rc;
 
   VerifyParams q = {};  // without logits: the selection takes a zero maximum as it is
@@ -972,7 +973,8 @@ int asd_rules_verify(const asd_token_rules* rules, const asd_rules_block* block,
   q.done = reinterpret_cast<unsigned long long*>(ws + l.done);
   q.flags = p.flags;
   q.error = reinterpret_cast<unsigned*>(ws + l.error);
-  return a.ledger ? launch_select<float, false>(q, true, s) : launch_select<float, true>(q, true, s);
+  q.flag_empty = dtype != a.dtype;
+  return a.ledger ? launch_select<float, false, true>(q, true, s) : launch_select<float, true, true>(q, true, s);
 }
 
 int asd_rules_logits(const asd_token_rules* rules, const void* logits, int dtype, int rows, const int32_t* draft,

@@ -18,14 +18,14 @@ namespace asd_detail {
 
 constexpr int kSelectThreads = 128;
 
-template <typename T, bool kStrict>
+template <typename T, bool kStrict, bool kRules>
 static __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_constant__ VerifyParams p) {
   pdl_signal_dependents();
   pdl_wait_prerequisites();
   const int lane = threadIdx.x & 31;
   const int warps = kSelectThreads / 32;
   for (int b = blockIdx.x * warps + (threadIdx.x >> 5); b < p.B; b += gridDim.x * warps)
-    select_request<T, kStrict>(p, b, lane);
+    select_request<T, kStrict, kRules>(p, b, lane);
 }
 
 // Several blocks of the same requests: one CTA per request, whose warps load as
@@ -73,7 +73,7 @@ static __global__ void __launch_bounds__(kSelectBlocksThreads)
   if (threadIdx.x == 0 && s_wrote) p.ledger[b].spent = s_spent;
 }
 
-template <typename T, bool kStrict>
+template <typename T, bool kStrict, bool kRules = false>
 int launch_select(const VerifyParams& p, bool pdl, cudaStream_t stream) {
   const bool blocks = !kStrict && p.nblk > 1 && !p.partials;
   constexpr int kWarps = kSelectThreads / 32;
@@ -88,7 +88,7 @@ int launch_select(const VerifyParams& p, bool pdl, cudaStream_t stream) {
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
   }
-  auto kernel = blocks ? select_blocks_kernel<T> : select_kernel<T, kStrict>;
+  auto kernel = blocks ? select_blocks_kernel<T> : select_kernel<T, kStrict, kRules>;
   if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) return ASD_ERR_CUDA;
   return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;
 }
