@@ -144,6 +144,7 @@ def decode(model: Decoder, prompts: list, rounds: int, budget: float = 0.0, gate
     if keep is not None:  # what every slot of every layer's heads is worth; how many each request keeps
         slots = cache.table_width * cache.page_size
         weight = torch.zeros(model.layers, B, model.heads, slots, device=dev)
+        numbers = torch.full(weight.shape, -1, dtype=torch.int32, device=dev)  # each slot's token, once slots have moved
         limit = torch.full((B,), keep, dtype=torch.int32, device=dev)
 
     def weigh(before, **rows):
@@ -193,7 +194,8 @@ def decode(model: Decoder, prompts: list, rounds: int, budget: float = 0.0, gate
         seen += on
         asd.commit(got["accepted_len"], got["committed"], kv_len=kv_len, tokens=history, token_len=emitted)
         if weight is not None:
-            kv_len = asd.kv_evict(cache, kv_len, weight, limit, first=1, last=K + 1, status=status)
+            kv_len = asd.kv_evict(cache, kv_len, weight, limit, first=1, last=K + 1, status=status, numbers=numbers,
+                                  tokens=seen)
         if lengths_seen is not None:
             lengths_seen.append(kv_len.tolist())
         pending = got["recovery"]

@@ -103,7 +103,8 @@ enum {
 #define ASD_STATUS_LENGTH 32u     /* cache entry points: kv_len < 0, a token count outside its range, or
                                    * more slots than the request's row of the page table covers */
 #define ASD_STATUS_PAGE 64u       /* cache entry points: a page id outside [0, pages) */
-#define ASD_STATUS_POSITION 128u  /* asd_kv_append: a position outside the rotation's table */
+#define ASD_STATUS_POSITION 128u  /* asd_kv_append: a position outside the rotation's table;
+                                   * asd_kv_evict_numbered: numbers that are not a sequence's */
 #define ASD_STATUS_PATH 256u      /* asd_kv_compact: path[i] < i or not ascending; asd_kv_weigh: path[i] outside
                                    * [0, T) */
 #define ASD_STATUS_TOKEN 512u     /* asd_tokens_record, asd_tokens_bias: a token id >= V */
@@ -554,8 +555,10 @@ int asd_kv_weigh(const asd_kv_cache* cache, const asd_weigh* args, asd_stream_t 
  * ascending order, to the places below n that became free, in ascending order,
  * their weights with them. Attention does not depend on the order of the slots
  * (keys are rotated by their positions when they are appended), so nothing else
- * moves. Where at least `last` tokens are appended between two evictions, no token
- * with fewer than `last` behind it ever goes. Later tokens take positions of their
+ * moves. The last slots are the newest tokens as long as tokens lie in their order: at
+ * the first eviction, and at a later one if at least `last` tokens have been appended
+ * since the one before. With fewer in between `last` holds on to slots that are no longer
+ * the newest ones; asd_kv_evict_numbered knows the tokens. Later tokens take positions of their
  * own (asd_append.positions): kv_len is no longer a token's number. A request's pages
  * are its own: of a page that two requests' tables share, both move slots.
  *
@@ -583,6 +586,27 @@ typedef struct {
 } asd_evict;
 #define ASD_MAX_EVICT_SLOTS 360448
 int asd_kv_evict(const asd_kv_cache* cache, const asd_evict* args, asd_stream_t stream);
+
+/*
+ * The same, and the newest tokens stay however many have been appended since the last
+ * eviction: of request b's tokens 0 .. tokens[b] - 1, in the order in which they were
+ * appended, the last r = min(last, n - f), wherever their slots are, instead of the last r
+ * slots. A head keeps fewer of them where an eviction with a smaller `last` or `keep` has
+ * left some out, and more of the heaviest.
+ *
+ * number        [layers, B, heads, width] the token of each slot; negative: the slot has
+ *               been appended since the last eviction (or there was none), and holds token
+ *               tokens[b] - kv_len[b] + s. Filled with -1 before a request's first eviction,
+ *               and only evictions write it: a request that loses slots has the numbers of the
+ *               slots below n, moved with them, and -1 in those from n to kv_len[b] - 1.
+ * tokens        [B] >= kv_len: how many tokens have been appended to the request's cache
+ *               and not taken back, evicted ones included; not kv_len_out
+ * status        ASD_STATUS_LENGTH: also tokens < kv_len. ASD_STATUS_POSITION: a head whose
+ *               numbers are not of one such sequence (more newest tokens than places): it
+ *               moves nothing, its slots below n stay.
+ */
+int asd_kv_evict_numbered(const asd_kv_cache* cache, const asd_evict* args, int32_t* number, const int32_t* tokens,
+                          asd_stream_t stream);
 
 /* ------------------------------------------------------------------------
  * Rules: what a request's own text, its caller and its grammar do to the logits

@@ -122,6 +122,8 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.asd_kv_weigh.restype = i32
     lib.asd_kv_evict.argtypes = [vp, vp, vp]
     lib.asd_kv_evict.restype = i32
+    lib.asd_kv_evict_numbered.argtypes = [vp, vp, vp, vp, vp]
+    lib.asd_kv_evict_numbered.restype = i32
     lib.asd_rules_verify.argtypes = [vp, vp, vp]
     lib.asd_rules_verify.restype = i32
     lib.asd_rules_logits.argtypes = [vp, vp, i32, i32, vp, vp, vp]
@@ -873,13 +875,19 @@ def kv_weigh(q: torch.Tensor, lse: torch.Tensor, cache: KVCache, kv_len: torch.T
 
 def kv_evict(cache: KVCache, kv_len: torch.Tensor, weight: torch.Tensor, keep: torch.Tensor, first: int = 0,
              last: int = 0, out: torch.Tensor | None = None, new_len: torch.Tensor | None = None,
-             status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+             status: torch.Tensor | None = None, stream=None, numbers: torch.Tensor | None = None,
+             tokens: torch.Tensor | None = None) -> torch.Tensor:
     """asd_kv_evict: cut every request's cache to ``keep[b]`` slots, in every layer and in place.
 
     weight float32 [layers, B, heads, width] (or without the first dimension for one layer), moved with the slots in
     place or to ``out``. The first ``first`` and the last ``last`` slots stay. Pages that two requests' tables share are
     not for this: each would move the other's slots. Returns the new lengths, int32 [B] (``new_len``, allocated on
     ``stream`` if not given; not ``kv_len`` itself).
+
+    The last slots are the newest tokens only where at least ``last`` tokens were appended since the last eviction. A
+    loop that evicts more often passes ``numbers`` int32, of weight's shape, filled with -1 for each new request, and
+    ``tokens`` int32 [B], how many the request's cache has been given in all (asd_kv_evict_numbered): the newest
+    ``last`` tokens stay wherever they lie, and ``numbers`` says afterwards which token a slot holds.
     """
     B = cache.B
     one = (B,)
@@ -895,7 +903,14 @@ def kv_evict(cache: KVCache, kv_len: torch.Tensor, weight: torch.Tensor, keep: t
                        _check_vector("kv_len", kv_len, cache, one), _check_vector("new_len", new_len, cache, one),
                        _check_vector("keep", keep, cache, one),
                        0 if status is None else _check_vector("status", status, cache, one), first, last, shape[-1], 0)
-    rc = load().asd_kv_evict(cache._ref, args, _stream_at(stream, cache.index))
+    if numbers is None and tokens is None:
+        rc = load().asd_kv_evict(cache._ref, args, _stream_at(stream, cache.index))
+    elif numbers is None or tokens is None:
+        raise ValueError("numbers and tokens go together")
+    else:
+        rc = load().asd_kv_evict_numbered(cache._ref, args, _check_vector("numbers", numbers, cache, shape),
+                                          _check_vector("tokens", tokens, cache, one),
+                                          _stream_at(stream, cache.index))
     if rc:
         raise AsdError("asd_kv_evict", rc)
     return new_len

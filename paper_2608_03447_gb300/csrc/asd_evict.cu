@@ -14,6 +14,12 @@
 // cluster, give every move its number, and the moves are dealt in equal shares to the
 // cluster's CTAs, into the memory the weights were in.
 //
+// What is newest: the last slots, as long as tokens lie in their order. Moves fill places
+// anywhere, so a token that one eviction kept as new may lie anywhere at the next. With
+// numbers (asd_kv_evict_numbered) every slot's token is known and the newest tokens stay
+// wherever they are; a number moves with its weight. Without them (kNumbered = false)
+// nothing of this is compiled in.
+//
 // What bounds it: moves, rows of 256 bytes anywhere: 8 prompts of up to 16000 slots cut
 // to 4000, four layers of 8 heads of 128, 145 us for 765 MB (5.3 TB/s). A conversation of
 // 4224 slots cut by 128 in 40 layers of 8 heads: 21.5 us, a third of it the moves, the
@@ -60,6 +66,8 @@ struct EvictParams {
   int32_t* kv_len_out;
   const int32_t* keep;
   int32_t* status;
+  int32_t* number;       // kNumbered: [layers, B, heads, width]
+  const int32_t* tokens;  // kNumbered: [B] appended in all
   int B, H;
   int width, first, last;
   int ctas;       // of a cluster
@@ -117,13 +125,14 @@ __device__ __forceinline__ unsigned block_scan(unsigned x, unsigned* warp_sums, 
 // Word: what a row is copied in. Up to four CTAs an SM of 256 threads, two of 512: the
 // larger ones where no more than two heads come on an SM (8 prompts 145 us, with 256
 // threads 165; the conversation, two to three heads an SM, 21.5 us against 24.4).
-template <typename Word, int kThreads>
+template <typename Word, int kThreads, bool kNumbered>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_kernel(const __grid_constant__ EvictParams p) {
   constexpr int kWarps = kThreads / 32;
   extern __shared__ __align__(16) unsigned s_mem[];
   __shared__ unsigned s_warp[kWarps];
   __shared__ unsigned s_found[3];  // the digit, how many of its slots stay, how many there are
-  __shared__ unsigned s_total[4];  // this CTA's counts, its smallest and largest key, for the cluster
+  // this CTA's counts, its smallest and largest key, how many slots stay in any case, for the cluster
+  __shared__ unsigned s_total[5];
   unsigned* s_hist = s_mem;                   // [kDigits][kBins], cleared by 16-byte words
   unsigned* s_key = s_hist + kDigits * kBins; // [part]
   unsigned* s_above = s_key + p.part;         // [part / 32] bits: heavier than the lightest that stays; then moves
@@ -139,41 +148,60 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_kernel(const 
   pdl_wait_prerequisites();
 
   const int len = __ldcg(p.kv_len + b), keep = __ldcg(p.keep + b);
-  const bool bad = len < 0 || len > p.cache.slots || len > p.width || keep < 0;
+  const int tokens = kNumbered ? __ldcg(p.tokens + b) : 0;
+  const bool bad = len < 0 || len > p.cache.slots || len > p.width || keep < 0 || (kNumbered && tokens < len);
   const int n = bad ? 0 : min(keep, len);
   if (layer == 0 && h == 0 && rank == 0 && tid == 0) {
     if (bad && p.status) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_LENGTH));
     p.kv_len_out[b] = bad ? len : n;
   }
-  if (bad || n == 0) return;
+  if (bad || (n == 0 && !kNumbered)) return;
   const float* weight = p.weight + static_cast<long long>(head_id) * p.width;
   float* weight_out = p.weight_out + static_cast<long long>(head_id) * p.width;
+  int32_t* number = kNumbered ? p.number + static_cast<long long>(head_id) * p.width : nullptr;
   const bool copies = p.weight != p.weight_out;
   const int per = ((len + C - 1) / C + 31) & ~31;
   const int s0 = min(rank * per, len), count = min(per, len - s0);
+  if (kNumbered && n == 0) {
+    for (int i = tid; i < count; i += kThreads) number[s0 + i] = -1;
+    return;
+  }
   if (n == len) {
     if (copies)
       for (int i = tid; i < count; i += kThreads) weight_out[s0 + i] = __ldcg(weight + s0 + i);
     return;
   }
   const int first = min(p.first, n), last = min(p.last, n - first);
+  // a slot without a number has been appended since the last eviction, in order
+  auto token_of = [&](int given, int s) { return given >= 0 ? given : tokens - len + s; };
 
   // keys; those that stay in any case are above every weight and in no histogram
   constexpr unsigned kStays = 0xffffffffu;
-  unsigned smallest = kStays, largest = 0u;
-  constexpr int kLoads = 16;  // in flight at once: no store between them, which a load might not pass
+  unsigned smallest = kStays, largest = 0u, always = 0u;
+  constexpr int kLoads = kNumbered ? 8 : 16;  // in flight at once: no store between them, which a load might not pass
   for (int i0 = tid; i0 < count; i0 += kLoads * kThreads) {
     float w[kLoads];
+    int given[kLoads];
 #pragma unroll
-    for (int k = 0; k < kLoads; ++k) w[k] = i0 + k * kThreads < count ? __ldcg(weight + s0 + i0 + k * kThreads) : 0.0f;
+    for (int k = 0; k < kLoads; ++k) {
+      w[k] = i0 + k * kThreads < count ? __ldcg(weight + s0 + i0 + k * kThreads) : 0.0f;
+      if (kNumbered) given[k] = i0 + k * kThreads < count ? __ldcg(number + s0 + i0 + k * kThreads) : 0;
+    }
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
       const int i = i0 + k * kThreads, s = s0 + i;
       if (i >= count) break;
       if (copies && s < n) weight_out[s] = w[k];
       unsigned key = w[k] == w[k] ? ordered_bits(w[k]) : ordered_bits(-INFINITY);
-      if (s < first || s >= len - last) {
+      bool newest = s >= len - last;
+      if (kNumbered) {
+        const int token = token_of(given[k], s);
+        if (given[k] < 0 && s < n) number[s] = token;
+        newest = token >= tokens - last;
+      }
+      if (s < first || newest) {
         key = kStays;
+        ++always;
       } else {
         smallest = min(smallest, key);
         largest = max(largest, key);
@@ -183,23 +211,33 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_kernel(const 
   }
   smallest = __reduce_min_sync(kFull, smallest);
   largest = __reduce_max_sync(kFull, largest);
-  if (tid == 0) s_total[2] = kStays, s_total[3] = 0u;
+  if (kNumbered) always = __reduce_add_sync(kFull, always);
+  if (tid == 0) s_total[2] = kStays, s_total[3] = 0u, s_total[4] = 0u;
   __syncthreads();
   if (lane == 0) {
     atomicMin(&s_total[2], smallest);
     atomicMax(&s_total[3], largest);
+    if (kNumbered) atomicAdd(&s_total[4], always);
   }
   cluster_sync(C);
   smallest = s_total[2], largest = s_total[3];
+  always = kNumbered ? s_total[4] : static_cast<unsigned>(first + last);
   for (int r = 0; C > 1 && r < C; ++r) {
     smallest = min(smallest, load_cluster(at_rank(&s_total[2], r)));
     largest = max(largest, load_cluster(at_rank(&s_total[3], r)));
+    if (kNumbered && r != rank) always += load_cluster(at_rank(&s_total[4], r));
+  }
+  if (kNumbered && always > static_cast<unsigned>(n)) {  // numbers that no call wrote: twice the same, or too large
+    if (rank == 0 && tid == 0 && p.status) atomicOr(p.status + b, static_cast<int>(ASD_STATUS_POSITION));
+    for (int i = max(n - s0, 0) + tid; i < count; i += kThreads) number[s0 + i] = -1;
+    if (C > 1) cluster_sync(C);  // this CTA's counts have been read
+    return;
   }
 
   // The lightest weight that stays: of the keys' distances to the smallest, digit by digit from the top. All whose upper
   // bits are above `prefix` stay, of the `equal` ones that share it `need`.
-  const int range = 32 - __clz(largest - smallest);  // bits; n < len, so some keys are no kStays
-  unsigned prefix = 0, need = static_cast<unsigned>(n - first - last), equal = static_cast<unsigned>(len - first - last);
+  const int range = 32 - __clz(largest - smallest);  // bits; n < len, so some keys are no kStays (always <= n)
+  unsigned prefix = 0, need = static_cast<unsigned>(n) - always, equal = static_cast<unsigned>(len) - always;
   int shift = range;
   for (int digit = 0; need > 0 && need < equal && shift > 0; ++digit) {
     unsigned* hist = s_hist + digit * kBins;
@@ -330,6 +368,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_kernel(const 
     const unsigned moves = s_above[i], free = s_equal[i], base = s_base[i];
     const unsigned slot = static_cast<unsigned>(s0 + 32 * i + lane);
     if ((moves >> lane) & 1u) put(source + (base & 0xffffu) + __popc(moves & below), 0u, slot);
+    if (kNumbered && !((moves >> lane) & 1u) && slot >= static_cast<unsigned>(n) && slot < static_cast<unsigned>(len))
+      number[slot] = -1;
     if ((free >> lane) & 1u) put(place + (base >> 16) + __popc(free & below), share, slot);
   }
   cluster_sync(C);
@@ -350,6 +390,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_kernel(const 
     const int src = static_cast<int>(s_key[m + lane]), dst = static_cast<int>(s_key[share + m + lane]);
     const long long f = slot_offset(p.cache, b, src), t = slot_offset(p.cache, b, dst);
     weight_out[dst] = __ldcg(weight + src);
+    if (kNumbered) {
+      number[dst] = token_of(__ldcg(number + src), src);
+      number[src] = -1;
+    }
     if (f >= 0 && t >= 0) {
       from = (f + h * p.cache.head_stride) * p.element;
       to = (t + h * p.cache.head_stride) * p.element;
@@ -397,9 +441,9 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_kernel(const 
 
 constexpr int kMaxDevices = 64;
 
-template <typename Word, int kThreads>
+template <typename Word, int kThreads, bool kNumbered>
 int launch_evict(EvictParams p, long long heads, int sms, cudaStream_t stream) {
-  auto kernel = evict_kernel<Word, kThreads>;
+  auto kernel = evict_kernel<Word, kThreads, kNumbered>;
   int ctas = 1;
   while (ctas < kMaxCluster && (p.width > ctas * kMaxPart || (heads * ctas < sms && p.width > 1024 * ctas))) ctas *= 2;
   if (heads * ctas > INT32_MAX) return ASD_ERR_SHAPE;
@@ -420,7 +464,7 @@ int launch_evict(EvictParams p, long long heads, int sms, cudaStream_t stream) {
   return cudaGetLastError() == cudaSuccess ? ASD_OK : ASD_ERR_CUDA;
 }
 
-template <typename Word>
+template <typename Word, bool kNumbered>
 int launch_word(const EvictParams& p, int layers, cudaStream_t stream) {
   static std::atomic<int> sms_of[kMaxDevices];
   int dev = 0;
@@ -429,21 +473,21 @@ int launch_word(const EvictParams& p, int layers, cudaStream_t stream) {
   int sms = sms_of[dev].load(std::memory_order_acquire);
   if (sms == 0) {
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-        cudaFuncSetAttribute(evict_kernel<Word, 256>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        cudaFuncSetAttribute(evict_kernel<Word, 256, kNumbered>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              static_cast<int>(evict_smem(kMaxPart))) != cudaSuccess ||
-        cudaFuncSetAttribute(evict_kernel<Word, 512>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        cudaFuncSetAttribute(evict_kernel<Word, 512, kNumbered>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              static_cast<int>(evict_smem(kMaxPart))) != cudaSuccess)
       return ASD_ERR_CUDA;
     sms_of[dev].store(sms, std::memory_order_release);
   }
   const long long heads = static_cast<long long>(layers) * p.B * p.H;
-  return heads <= 2 * sms ? launch_evict<Word, 512>(p, heads, sms, stream)
-                          : launch_evict<Word, 256>(p, heads, sms, stream);
+  return heads <= 2 * sms ? launch_evict<Word, 512, kNumbered>(p, heads, sms, stream)
+                          : launch_evict<Word, 256, kNumbered>(p, heads, sms, stream);
 }
 
-}  // namespace
-
-extern "C" int asd_kv_evict(const asd_kv_cache* cache, const asd_evict* args, asd_stream_t stream) {
+template <bool kNumbered>
+int evict(const asd_kv_cache* cache, const asd_evict* args, int32_t* number, const int32_t* tokens,
+          asd_stream_t stream) {
   const int rc = check_cache(cache);
   if (rc != ASD_OK) return rc;
   if (!args) return ASD_ERR_NULL;
@@ -451,8 +495,9 @@ extern "C" int asd_kv_evict(const asd_kv_cache* cache, const asd_evict* args, as
   if (a.first < 0 || a.last < 0 || a.width < 0 || a.width > ASD_MAX_EVICT_SLOTS || a.reserved != 0) return ASD_ERR_SHAPE;
   if (cache->B == 0) return ASD_OK;
   if (!a.kv_len || !a.kv_len_out || !a.keep || (a.width > 0 && (!a.weight || !a.weight_out))) return ASD_ERR_NULL;
-  if (a.kv_len_out == a.kv_len || a.kv_len_out == a.keep) return ASD_ERR_SHAPE;
-  const void* const words[] = {a.weight, a.weight_out, a.kv_len, a.kv_len_out, a.keep, a.status};
+  if (kNumbered && (!tokens || (a.width > 0 && !number))) return ASD_ERR_NULL;
+  if (a.kv_len_out == a.kv_len || a.kv_len_out == a.keep || (kNumbered && a.kv_len_out == tokens)) return ASD_ERR_SHAPE;
+  const void* const words[] = {a.weight, a.weight_out, a.kv_len, a.kv_len_out, a.keep, a.status, number, tokens};
   for (const void* x : words)
     if (reinterpret_cast<uintptr_t>(x) % 4 != 0) return ASD_ERR_ALIGN;
   const size_t es = store_bytes(cache->dtype);
@@ -465,6 +510,8 @@ extern "C" int asd_kv_evict(const asd_kv_cache* cache, const asd_evict* args, as
   p.kv_len_out = a.kv_len_out;
   p.keep = a.keep;
   p.status = a.status;
+  p.number = number;
+  p.tokens = tokens;
   p.B = cache->B;
   p.H = cache->heads;
   p.element = static_cast<int>(es);
@@ -478,9 +525,24 @@ extern "C" int asd_kv_evict(const asd_kv_cache* cache, const asd_evict* args, as
       rows_aligned(p.cache.k, es, 16, cache->page_stride, cache->token_stride, cache->head_stride) &&
       reinterpret_cast<uintptr_t>(p.cache.v) % 16 == 0) {
     p.words = cache->head_dim / per;
-    return launch_word<uint4>(p, cache->layers, s);
+    return launch_word<uint4, kNumbered>(p, cache->layers, s);
   }
   p.words = cache->head_dim;
-  if (es == 4) return launch_word<unsigned>(p, cache->layers, s);
-  return launch_word<unsigned short>(p, cache->layers, s);
+  if (es == 4) return launch_word<unsigned, kNumbered>(p, cache->layers, s);
+  return launch_word<unsigned short, kNumbered>(p, cache->layers, s);
 }
+
+}  // namespace
+
+extern "C" {
+
+int asd_kv_evict(const asd_kv_cache* cache, const asd_evict* args, asd_stream_t stream) {
+  return evict<false>(cache, args, nullptr, nullptr, stream);
+}
+
+int asd_kv_evict_numbered(const asd_kv_cache* cache, const asd_evict* args, int32_t* number, const int32_t* tokens,
+                          asd_stream_t stream) {
+  return evict<true>(cache, args, number, tokens, stream);
+}
+
+}  // extern "C"
