@@ -940,6 +940,10 @@ int asd_rules_verify(const asd_token_rules* rules, const asd_rules_block* block,
   if (reinterpret_cast<uintptr_t>(a.workspace) % 16 != 0 ||
       reinterpret_cast<uintptr_t>(a.logits) % (dtype == ASD_F32 ? 4 : 2) != 0)
     return ASD_ERR_ALIGN;
+  const void* const words[] = {a.draft, a.ledger, a.accepted_len, a.committed, a.recovery, a.row_argmax, a.row_regret,
+                               a.status};
+  for (const void* x : words)
+    if (reinterpret_cast<uintptr_t>(x) % 4 != 0) return ASD_ERR_ALIGN;
   char* ws = static_cast<char*>(a.workspace);
   RulesParams p = rules_params(rules);
   p.logits = a.logits;
@@ -987,7 +991,9 @@ int asd_rules_logits(const asd_token_rules* rules, const void* logits, int dtype
   if (rules->B == 0) return ASD_OK;
   if (!logits || !out) return ASD_ERR_NULL;
   const uintptr_t es = dtype == ASD_F32 ? 4 : 2;
-  if (reinterpret_cast<uintptr_t>(logits) % es != 0 || reinterpret_cast<uintptr_t>(out) % es != 0) return ASD_ERR_ALIGN;
+  if (reinterpret_cast<uintptr_t>(logits) % es != 0 || reinterpret_cast<uintptr_t>(out) % es != 0 ||
+      reinterpret_cast<uintptr_t>(draft) % 4 != 0)
+    return ASD_ERR_ALIGN;
   RulesParams p = rules_params(rules);
   p.logits = logits;
   p.out = out;
