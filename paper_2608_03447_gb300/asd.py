@@ -215,17 +215,18 @@ def _stream(stream) -> int:
 
 def _stream_at(stream, index: int) -> int:
     """The handle of a call's stream. Kernels run on the current device, in a stream of its own: tensors of another one
-    are refused (a raw handle does not show its device)."""
-    if stream is None:
-        current = torch.cuda.current_device()
-        if current != index:
-            raise ValueError(f"the call's tensors are on cuda:{index}, the current device is cuda:{current}")
-        if _raw_stream is not None:
-            return _raw_stream(current)
-    else:
+    are refused (a raw handle does not show its device; the current one is compared all the same)."""
+    if stream is not None:
         device = getattr(stream, "device", None)
         if device is not None and device.index != index:
             raise ValueError(f"the call's tensors are on cuda:{index}, its stream is on {device}")
+        if index < 0:  # not of any GPU
+            return _stream(stream)
+    current = torch.cuda.current_device()
+    if current != index:
+        raise ValueError(f"the call's tensors are on cuda:{index}, the current device is cuda:{current}")
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(current)
     return _stream(stream)
 
 
