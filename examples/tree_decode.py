@@ -200,7 +200,7 @@ def decode(model: Decoder, prompts: list, rounds: int, budget: float = 0.0, gate
             lengths_seen.append(kv_len.tolist())
         pending = got["recovery"]
         drafts += int(got["accepted_len"].sum())
-    if workspace.error() or bool(status.any()):
+    if workspace.error() or asd.weigh_error() or bool(status.any()):
         raise RuntimeError(f"a call has reported an error: {workspace.error()}, {status.tolist()}")
     out = [history[b, :int(emitted[b])].tolist() for b in range(B)]
     return out, drafts / (rounds * B)

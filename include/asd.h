@@ -10,7 +10,7 @@
  * Conventions shared by every entry point
  *   - Every array argument is DEVICE memory owned by the caller, contiguous,
  *     row-major unless it comes with strides. The library allocates nothing and keeps no per-call state
- *     outside the caller's workspace.
+ *     outside the caller's workspace (but for the word that asd_weigh_error reads).
  *   - Calls are asynchronous and ordered on `stream` (a cudaStream_t; NULL is
  *     the legacy default stream). Nothing synchronises with the host.
  *   - Indices are 0-based: request b in [0, B), draft position j in [0, K)
@@ -85,7 +85,7 @@ enum {
   ASD_ERR_ALIGN = 6,     /* pointer not aligned as documented */
   ASD_ERR_CUDA = 7,      /* a CUDA call failed (launch or device query) */
   ASD_ERR_DEVICE = 8,    /* the current device cannot run the kernel (not sm_103) */
-  ASD_ERR_TIMEOUT = 9,   /* reported by asd_workspace_error: a kernel gave up waiting */
+  ASD_ERR_TIMEOUT = 9,   /* reported by asd_workspace_error and asd_weigh_error: a kernel gave up waiting */
   ASD_ERR_SCRATCH_LIMIT = 10 /* asd_verify_noalloc: the problem needs more than its scratch */
 };
 
@@ -520,8 +520,8 @@ int asd_kv_compact(const asd_kv_cache* cache, int P, const int32_t* kv_len, cons
  * Arithmetic: scores, exponentials and sums in fp32, rows added in a fixed order.
  * 16-bit types with a head_dim that is a multiple of 8 and rows on 16-byte
  * boundaries run on the tensor cores; a call that gives up waiting on its own
- * pipeline flags all its requests ASD_STATUS_INCOMPLETE (pass a status array to
- * see it). No workspace. Values of the cache are not read. The limits on sizes are
+ * pipeline flags all its requests ASD_STATUS_INCOMPLETE and is remembered until
+ * asd_weigh_error reads it. No workspace. Values of the cache are not read. The limits on sizes are
  * those of asd_tree_attention, with `rows` for T.
  */
 typedef struct {
@@ -543,6 +543,12 @@ typedef struct {
   int width;               /* slots that a head's weights have room for, >= kv_len + new_len of every request */
 } asd_weigh;
 int asd_kv_weigh(const asd_kv_cache* cache, const asd_weigh* args, asd_stream_t stream);
+
+/* Whether an asd_kv_weigh on the current device has given up a wait (about one second; it does
+ * not happen in normal operation) since the last call of this function: 0 or ASD_ERR_TIMEOUT.
+ * Weights that such a call was to write may be missing. Synchronises `stream`, whose calls it
+ * tells of, and clears what it has read. */
+int asd_weigh_error(int* error, asd_stream_t stream);
 
 /*
  * Cuts every request's cache to its budget, in place and in every layer. Of

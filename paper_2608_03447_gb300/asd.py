@@ -120,6 +120,8 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.asd_kv_compact.restype = i32
     lib.asd_kv_weigh.argtypes = [vp, vp, vp]
     lib.asd_kv_weigh.restype = i32
+    lib.asd_weigh_error.argtypes = [ctypes.POINTER(i32), vp]
+    lib.asd_weigh_error.restype = i32
     lib.asd_kv_evict.argtypes = [vp, vp, vp]
     lib.asd_kv_evict.restype = i32
     lib.asd_kv_evict_numbered.argtypes = [vp, vp, vp, vp, vp]
@@ -846,7 +848,7 @@ def kv_weigh(q: torch.Tensor, lse: torch.Tensor, cache: KVCache, kv_len: torch.T
     q [B, T, q_heads, D] and lse [B, T, q_heads] as tree_attention took and left them; weight float32 [B, heads,
     width], one layer's, is written in place or to ``out`` (``None`` with ``decay=0`` and ``out``). Row i of a request
     is token i, or token ``path[b, i]`` of int32 [B, rows], and sees the new slots kv_len .. kv_len + i; ``new_len``
-    int32 [B] counts a request's rows.
+    int32 [B] counts a request's rows. A call that gave up waiting shows in ``status`` and in ``weigh_error()``.
     """
     B, D = cache.B, cache.head_dim
     T, q_heads = q.shape[1:3] if q.dim() == 4 else (-1, -1)
@@ -872,6 +874,18 @@ def kv_weigh(q: torch.Tensor, lse: torch.Tensor, cache: KVCache, kv_len: torch.T
     if rc:
         raise AsdError("asd_kv_weigh", rc)
     return out
+
+
+def weigh_error(stream=None) -> int:
+    """asd_weigh_error: whether a kv_weigh on the current device has given up a wait since the last time.
+
+    0, or 9 (ASD_ERR_TIMEOUT): weights that it was to write may be missing. Synchronises the stream.
+    """
+    word = ctypes.c_int(0)
+    rc = load().asd_weigh_error(ctypes.byref(word), _stream(stream))
+    if rc:
+        raise AsdError("asd_weigh_error", rc)
+    return word.value
 
 
 def kv_evict(cache: KVCache, kv_len: torch.Tensor, weight: torch.Tensor, keep: torch.Tensor, first: int = 0,

@@ -115,9 +115,13 @@ constexpr size_t smem_for(int dim) {
 }
 static_assert(stages_for(128) >= 4 && stages_for(256) >= 2, "ring depth: more than the tiles of a step");
 
+// Set by any call that gives up a wait, until asd_weigh_error reads it: there is no workspace to keep it in, and a call
+// without a status array would lose it.
+__device__ unsigned g_gave_up;
+
 __device__ __forceinline__ bool warp_wait(unsigned long long* bar, uint32_t parity, WeighShared& sh) {
   if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
-  return __all_sync(kFull, warp_wait_on(bar, parity, &sh.abort, nullptr));
+  return __all_sync(kFull, warp_wait_on(bar, parity, &sh.abort, &g_gave_up));
 }
 
 // A place in the ring of units.
@@ -698,3 +702,17 @@ int launch_weigh_tc(const asd_kv_cache* cache, const WeighParams& p, cudaStream_
 }
 
 }  // namespace asd_detail
+
+extern "C" int asd_weigh_error(int* error, asd_stream_t stream) {
+  if (!error) return ASD_ERR_NULL;
+  void* word = nullptr;
+  unsigned value = 0;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (cudaGetSymbolAddress(&word, g_gave_up) != cudaSuccess ||
+      cudaMemcpyAsync(&value, word, sizeof value, cudaMemcpyDeviceToHost, s) != cudaSuccess ||
+      cudaStreamSynchronize(s) != cudaSuccess ||
+      (value != 0 && cudaMemsetAsync(word, 0, sizeof value, s) != cudaSuccess))
+    return ASD_ERR_CUDA;
+  *error = static_cast<int>(value);
+  return ASD_OK;
+}
