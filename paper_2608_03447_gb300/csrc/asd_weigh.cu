@@ -207,7 +207,8 @@ __global__ void __launch_bounds__(kSimtThreads, 2)
           for (int c = 0; c < 4; ++c)
             if (x + 16 * c <= see) {
               const float z = s[i][c].x + s[i][c].y;
-              sum[c] = fmaf(exp2_fast(fmaf(z, a.scale_log2, fmaf(z, p.scale_rest, -scale.x))), scale.y, sum[c]);
+              // the rest comes last: added to the whole of the lse it would be rounded away
+              sum[c] = fmaf(exp2_fast(fmaf(z, p.scale_rest, fmaf(z, a.scale_log2, -scale.x))), scale.y, sum[c]);
             }
         }
       }

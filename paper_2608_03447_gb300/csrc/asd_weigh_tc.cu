@@ -207,7 +207,8 @@ __device__ __forceinline__ float sum_columns(uint32_t from, const float* factor,
   for (int k = 0; k < kN; k += 4) {
     const float4 f = *reinterpret_cast<const float4*>(factor + k);
     const float2 z0 = {z[k], z[k + 1]}, z1 = {z[k + 2], z[k + 3]};
-    const float2 t0 = fma2(z0, by, fma2(z0, rest, less)), t1 = fma2(z1, by, fma2(z1, rest, less));
+    // the rest comes last: added to the whole of the offset it would be rounded away
+    const float2 t0 = fma2(z0, rest, fma2(z0, by, less)), t1 = fma2(z1, rest, fma2(z1, by, less));
     sum[0] = fma2(make_float2(exp2_fast(t0.x), exp2_fast(t0.y)), make_float2(f.x, f.y), sum[0]);
     sum[1] = fma2(make_float2(exp2_fast(t1.x), exp2_fast(t1.y)), make_float2(f.z, f.w), sum[1]);
   }
@@ -225,7 +226,7 @@ __device__ __noinline__ float sum_carefully(uint32_t from, int cols, const RowSc
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
       const RowScale s = rows[c + k];
-      const float e = exp2_fast(fmaf(z[k], scale.x, fmaf(z[k], scale.y, -s.x)));
+      const float e = exp2_fast(fmaf(z[k], scale.y, fmaf(z[k], scale.x, -s.x)));
       if (s.y != 0.0f && c + k >= first) sum = fmaf(e, s.y, sum);
     }
   }
