@@ -55,9 +55,9 @@ __device__ __forceinline__ float row_lse(const WeighParams& p, int b, int token,
 __device__ __forceinline__ RowScale row_scale(float lse) {
   RowScale r = {0.0f, 0.0f};
   if (fabsf(lse) == INFINITY) return r;
-  const float lost = fmaf(lse, 1.4426950408889634f, -(lse * 1.4426950408889634f)) + lse * 1.9259629911266175e-8f;
   r.x = lse * 1.4426950408889634f;
-  r.y = exp2f(-lost);
+  const float lost = fmaf(lse, 1.4426950408889634f, -r.x) + lse * 1.9259629911266175e-8f;
+  r.y = fabsf(r.x) == INFINITY ? 1.0f : exp2f(-lost);  // from 2.4e38 on nothing says what was lost
   return r;
 }
 
