@@ -10,7 +10,7 @@ Entry points mirror the C names: ``verify`` (asd_verify), ``verify_strict``
 Ledgers are float32 tensors of shape [B, 2] holding (budget, spent), the
 memory layout of ``asd_ledger``. The cache side of a block: ``KVCache``
 (asd_kv_cache), ``kv_append``, ``tree_mask``, ``tree_attention``, ``kv_compact``,
-``kv_weigh``, ``kv_evict``. Logits under penalties, biases and grammars:
+``kv_weigh``, ``weigh_error``, ``kv_evict`` (asd_kv_evict, asd_kv_evict_numbered). Logits under penalties, biases and grammars:
 ``TokenRules`` (asd_token_rules), ``rules_verify``, ``rules_logits``,
 ``tokens_record``, ``tokens_bias``.
 """

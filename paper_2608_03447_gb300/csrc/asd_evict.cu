@@ -21,8 +21,9 @@
 // nothing of this is compiled in.
 //
 // What bounds it: moves, rows of 256 bytes anywhere: 8 prompts of up to 16000 slots cut
-// to 4000, four layers of 8 heads of 128, 145 us for 765 MB (5.3 TB/s). A conversation of
-// 4224 slots cut by 128 in 40 layers of 8 heads: 21.5 us, a third of it the moves, the
+// to 4000, four layers of 8 heads of 128, 145 us for 765 MB (5.3 TB/s; 736 of them in the
+// DRAM counters, with numbers 147 us). A conversation of
+// 4224 slots cut by 128 in 40 layers of 8 heads: 21.5 us (with numbers 23), a third of it the moves, the
 // rest a chain of latencies (lengths, weights, three histograms, two sums over the CTA,
 // the list). What else was measured for the two: four rows in flight a lane instead of
 // two 24 and 152 us (spills), one 23.6 and 150; clusters of two and four where there are

@@ -21,8 +21,8 @@
 // What bounds it: few rows, memory: 32 paths of up to 9 on 8000 slots, 40 heads on 8 of
 // 128 in bf16, 79 to 81 us (471 MB read, 6.0 TB/s). Many rows, the exponentials (32 a
 // clock and SM), what goes with them, and the products behind them: 64 rows of 16
-// prompts of up to 12000 slots, 32 heads on 4 of 64 in f16, 73 us, of which the 393
-// million exponentials need 42; without any sums the same takes 49, with sums but no
+// prompts of 9000 to 12000 slots, 32 heads on 4 of 64 in f16, 73 us, of which the 345
+// million exponentials need 37; without any sums the same takes 49, with sums but no
 // exponentials 67, and a group waits 15 % of its time for a product. One token on 4200
 // slots takes 7.2 us, a chain of latencies. A prompt of 4093 on itself (40 heads on 8 of
 // 128) takes 321 us: the CTAs that have the first slots meet all 160 slabs of rows one
