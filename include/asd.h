@@ -606,7 +606,8 @@ int asd_kv_evict(const asd_kv_cache* cache, const asd_evict* args, asd_stream_t 
  *               and only evictions write it: a request that loses slots has the numbers of the
  *               slots below n, moved with them, and -1 in those from n to kv_len[b] - 1.
  * tokens        [B] >= kv_len: how many tokens have been appended to the request's cache
- *               and not taken back, evicted ones included; not kv_len_out
+ *               and not taken back, evicted ones included; not kv_len_out. Tokens can be taken
+ *               back (kv_len and tokens made smaller) that no eviction has seen yet.
  * status        ASD_STATUS_LENGTH: also tokens < kv_len. ASD_STATUS_POSITION: a head whose
  *               numbers are not of one such sequence (more newest tokens than places): it
  *               moves nothing, its slots below n stay.
